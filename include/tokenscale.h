@@ -517,6 +517,93 @@ int ts_gemm_bf16(int32_t device, int32_t M, int32_t N, int32_t K, const void* A,
 int ts_gemm_plan(int32_t device, int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* tile_m, int32_t* split,
                  int32_t* pair_tokens);
 
+/*
+ * Trees of drafted tokens, an 8-bit KV cache, and log probabilities of given tokens. (The paper has no counterpart: its
+ * decoder takes one token per request and step over a bf16 cache. Verifying several drafted tokens per step and
+ * holding twice the tokens are the two usual ways to raise the Decode Velocity of the same decoder.) One iteration:
+ *   ts_tree_attention over every request's drafted nodes -> the model's logits for these nodes
+ *   -> ts_token_logprobs (accept or reject) -> ts_cache_append of the accepted path.
+ *
+ * 8-bit cache (device, owned by the caller), next to or instead of the bf16 pool, addressed by the same page ids:
+ *        values[page][kv][head][slot][d]   e4m3 codes, ts_cache8_value_bytes() bytes
+ *        scales[page][kv][head][slot]      one byte b per row of head_dim codes, ts_cache8_scale_bytes() bytes
+ *   element = code * 2^(b - 127), exact in bf16. A row x is written with E = b - 127 the smallest whole number for which
+ *   max|x| <= 448 * 2^E, clamped to [-62, 62] (0 for a row of zeros), and codes x * 2^-E rounded to nearest even; what is
+ *   larger than 448 * 2^62 saturates, infinities too; a NaN stays one.
+ * ts_cache8_attach: binds such a cache to a context (both pointers 256-byte aligned). The context may then have been
+ *   created without kv_pool (its workspace is still needed): calls on TS_CACHE_E4M3 work, those on the bf16 pool return TS_ERR_CUDA.
+ */
+enum { TS_CACHE_BF16 = 0, TS_CACHE_E4M3 = 1 };
+typedef struct {
+  void* values;
+  size_t values_bytes;
+  void* scales;
+  size_t scales_bytes;
+} ts_cache8;
+size_t ts_cache8_value_bytes(const ts_config* cfg); /* 0 on a bad shape */
+size_t ts_cache8_scale_bytes(const ts_config* cfg);
+int ts_cache8_attach(ts_ctx* ctx, const ts_cache8* cache);
+
+/*
+ * ts_tree_attention: attention of every row's drafted nodes over its cached tokens and over each other. Rows as for
+ * ts_mixed_step, but q_len[r] (1 to 64) are the nodes of row r, which are NOT appended (their K/V are read from
+ * k_new, v_new) and need no room in the row's table; cached lengths and counters do not change, chunk_size does not apply.
+ * Node i of a row attends all ctx_len[r] cached tokens and those nodes j of the row whose bit j of its mask word is
+ * set (bits from q_len[r] on are ignored); a node that sees nothing gets zeros. mask: DEVICE uint64 [N], 8-byte
+ * aligned; NULL = a chain (node i sees the nodes 0..i), so that a row of one node is a decode row. The K and V of a
+ * node that nobody sees may hold anything; a seen node whose V holds an infinity or a NaN makes its viewers' outputs NaN.
+ * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^76).
+ * Arithmetic as for a step: fp32 accumulation and softmax, weights rounded to bf16 (8-bit cache: f16) in front of
+ * the second product, bf16 result. Asynchronous on cuda_stream; uses the context's workspace, as a step does.
+ * ts_tree_masks (host): mask words of one row's nodes from their parents (parents[i] in [-1, i), -1 = attached to the
+ * cached context): a node sees itself and its ancestors.
+ */
+int ts_tree_attention(ts_ctx* ctx, const ts_step* step, int32_t cache, const uint64_t* mask, void* cuda_stream);
+int ts_tree_masks(const int32_t* parents, int32_t n_nodes, uint64_t* masks_out);
+
+/*
+ * ts_cache_append: writes q_len[r] >= 0 tokens of each row at the positions from ctx_len[r] (its cached length) on, as
+ * ts_kv_append does, into either cache. source: DEVICE int32 [N], or NULL; token i of the call is row source[i] of k_new
+ * and v_new, which then hold n_source tokens: the accepted path of a tree goes into the cache by naming its nodes. An
+ * index outside [0, n_source) skips its token and raises TS_DEV_BAD_INDEX. NULL: token i is row i.
+ * Advances the cached lengths unless TS_STEP_KEEP_LEN.
+ * ts_cache_read: the K and V of the q_len[r] >= 0 tokens from position ctx_len[r] on (any position the row's table covers; slots that
+ * hold no token read as whatever they contain), row after row, to k_out and v_out (DEVICE bf16 [N, Hkv, D], 16-byte aligned).
+ */
+int ts_cache_append(ts_ctx* ctx, const ts_step* step, int32_t cache, const int32_t* source, int32_t n_source, void* cuda_stream);
+int ts_cache_read(ts_ctx* ctx, const ts_step* step, int32_t cache, void* k_out, void* v_out, void* cuda_stream);
+
+/*
+ * ts_token_logprobs: for every row x of logits, with y = scale * x:
+ *   logprob of given token t   y_t - log sum_j exp(y_j)                       (natural logarithm, fp32)
+ *   rank of given token t      number of tokens j with x_j > x_t, or x_j = x_t and j < t   (0 = the greedy choice)
+ *   entropy                    -sum_j p_j log p_j
+ *   top                        the n_top tokens that come first by (x descending, index ascending), with their log probabilities
+ * Logits of -inf are tokens with probability 0. A row without any finite logit: log probabilities -inf, entropy 0 (ranks and top
+ * as the order says). A NaN or +inf in a row makes its log probabilities and entropy NaN; a NaN comes behind everything
+ * and is never listed. A given token outside [0, vocab), or whose logit is a NaN, gets logprob NaN and rank -1.
+ * Entries of top beyond the tokens that can be listed: token -1, log probability NaN.
+ * No workspace; asynchronous on cuda_stream; calls on different streams are independent.
+ */
+enum { TS_BF16 = 0, TS_F32 = 1 };
+typedef struct {
+  int32_t device;
+  int32_t n_rows, vocab;     /* vocab >= 1, at most 2^30                                            */
+  int32_t dtype;             /* TS_BF16 or TS_F32                                                   */
+  const void* logits;        /* DEVICE [n_rows], rows row_stride elements apart (>= vocab), aligned to their type only */
+  int64_t row_stride;
+  const float* scale;        /* DEVICE [n_rows], > 0: inverse temperatures; NULL = 1                */
+  const int32_t* tokens;     /* DEVICE [n_rows][n_given]                                            */
+  int32_t n_given;           /* 0 to 8                                                              */
+  int32_t n_top;             /* 0 to 32                                                             */
+  float* logprob;            /* DEVICE [n_rows][n_given]                                            */
+  int32_t* rank;             /* DEVICE [n_rows][n_given], or NULL                                   */
+  float* entropy;            /* DEVICE [n_rows], or NULL                                            */
+  float* top_logprob;        /* DEVICE [n_rows][n_top]                                              */
+  int32_t* top_token;        /* DEVICE [n_rows][n_top]                                              */
+} ts_logprobs;
+int ts_token_logprobs(const ts_logprobs* args, void* cuda_stream);
+
 /* The cudaError_t of the most recent failed CUDA call of this context (0 if none). */
 int ts_last_cuda_error(const ts_ctx* ctx);
 

@@ -29,6 +29,8 @@ TS_DEV_BAD_PAGE = 1
 TS_DEV_TIMEOUT = 2
 TS_DEV_BAD_INDEX = 4
 TS_DEBUG_LOSE_APPEND_ARRIVAL = 1
+TS_CACHE_BF16, TS_CACHE_E4M3 = 0, 1
+TS_BF16, TS_F32 = 0, 1
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 
@@ -75,6 +77,19 @@ class ts_profile(ctypes.Structure):
                 ("mixed_ms", ctypes.c_double), ("mixed_steps", ctypes.c_int64)]
 
 
+class ts_cache8(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("values_bytes", ctypes.c_size_t),
+                ("scales", ctypes.c_void_p), ("scales_bytes", ctypes.c_size_t)]
+
+
+class ts_logprobs(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("scale", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("n_given", ctypes.c_int32), ("n_top", ctypes.c_int32),
+                ("logprob", ctypes.c_void_p), ("rank", ctypes.c_void_p), ("entropy", ctypes.c_void_p),
+                ("top_logprob", ctypes.c_void_p), ("top_token", ctypes.c_void_p)]
+
+
 EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts_request_add",
            "ts_alloc_pages", "ts_block_table", "ts_block_table_set", "ts_request_free",
            "ts_request_set_len", "ts_kv_append", "ts_mixed_step", "ts_mixed_step_host", "ts_host_fence",
@@ -84,7 +99,9 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_convertible_prefill_velocity", "ts_reserved_memory", "ts_reserved_pages",
            "ts_prefiller_instances", "ts_decoder_demand", "ts_regular_decoders", "ts_route_prefill",
            "ts_layer_workspace_bytes", "ts_pack_gate_up", "ts_layer_create", "ts_layer_destroy", "ts_layer_step",
-           "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan"]
+           "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan", "ts_cache8_value_bytes",
+           "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
+           "ts_cache_read", "ts_token_logprobs"]
 
 _lib = None
 
@@ -162,6 +179,14 @@ def lib() -> ctypes.CDLL:
         L.ts_gemm_bf16.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp,
                                    ctypes.c_int32, vp, vp]
         L.ts_gemm_plan.argtypes = [ctypes.c_int32] * 5 + [_i32p] * 3
+        L.ts_cache8_value_bytes.restype = L.ts_cache8_scale_bytes.restype = ctypes.c_size_t
+        L.ts_cache8_value_bytes.argtypes = L.ts_cache8_scale_bytes.argtypes = [cfgp]
+        L.ts_cache8_attach.argtypes = [vp, ctypes.POINTER(ts_cache8)]
+        L.ts_tree_attention.argtypes = [vp, stepp, ctypes.c_int32, vp, vp]
+        L.ts_tree_masks.argtypes = [_i32p, ctypes.c_int32, ctypes.POINTER(ctypes.c_uint64)]
+        L.ts_cache_append.argtypes = [vp, stepp, ctypes.c_int32, vp, ctypes.c_int32, vp]
+        L.ts_cache_read.argtypes = [vp, stepp, ctypes.c_int32, vp, vp, vp]
+        L.ts_token_logprobs.argtypes = [ctypes.POINTER(ts_logprobs), vp]
         L.ts_strerror.restype = ctypes.c_char_p
         L.ts_strerror.argtypes = [ctypes.c_int]
         for name in EXPORTS:
@@ -432,3 +457,41 @@ def ts_gemm_plan(device: int, M: int, N: int, K: int, epilogue: int):
     out = [ctypes.c_int32() for _ in range(3)]
     rc = lib().ts_gemm_plan(device, M, N, K, epilogue, *[ctypes.byref(x) for x in out])
     return rc, tuple(x.value for x in out)
+
+
+# --------------------------------- trees of drafted tokens, the 8-bit cache, log probabilities of given tokens
+def ts_cache8_value_bytes(cfg: ts_config) -> int:
+    return lib().ts_cache8_value_bytes(ctypes.byref(cfg))
+
+
+def ts_cache8_scale_bytes(cfg: ts_config) -> int:
+    return lib().ts_cache8_scale_bytes(ctypes.byref(cfg))
+
+
+def ts_cache8_attach(ctx, cache: ts_cache8) -> int:
+    return lib().ts_cache8_attach(ctx, ctypes.byref(cache))
+
+
+def ts_tree_attention(ctx, step: ts_step, cache: int, mask: int, stream: int) -> int:
+    return lib().ts_tree_attention(ctx, ctypes.byref(step), cache, mask or None, stream)
+
+
+def ts_tree_masks(parents):
+    """Returns (code, mask words of the nodes)."""
+    n = len(parents)
+    a = (ctypes.c_int32 * max(n, 1))(*[int(p) for p in parents])
+    out = (ctypes.c_uint64 * max(n, 1))()
+    rc = lib().ts_tree_masks(a, n, out)
+    return rc, list(out[:n]) if rc == TS_OK else []
+
+
+def ts_cache_append(ctx, step: ts_step, cache: int, source: int, n_source: int, stream: int) -> int:
+    return lib().ts_cache_append(ctx, ctypes.byref(step), cache, source or None, n_source, stream)
+
+
+def ts_cache_read(ctx, step: ts_step, cache: int, k_out: int, v_out: int, stream: int) -> int:
+    return lib().ts_cache_read(ctx, ctypes.byref(step), cache, k_out or None, v_out or None, stream)
+
+
+def ts_token_logprobs(args: ts_logprobs, stream: int) -> int:
+    return lib().ts_token_logprobs(ctypes.byref(args), stream)

@@ -10,6 +10,7 @@
 
 #include "../../include/tokenscale.h"
 #include "ts_internal.h"
+#include "ts_tree.h"
 
 namespace {
 
@@ -143,6 +144,9 @@ struct ts_ctx {
   bool cuda_ready = false;
   CUtensorMap kv_map;               // TMA view of the pool, box = K and V of one (page, head)
   CUtensorMap kv_tile_map;          // box = K or V of 64 columns of one (page, head)
+  ts_cache8 cache8 = {};            // see ts_cache8_attach
+  CUtensorMap cache8_map;           // TMA view of its values, box = K and V of one (page, head)
+  bool kv_maps_ready = false, cache8_map_ready = false;
   void* encode_fn = nullptr;        // cuTensorMapEncodeTiled
   int n_sms = 0;
   int n_prefill_items = 0;          // of the current plan
@@ -206,9 +210,6 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
 // kv_tile_map, for the K and V tiles of the prefill path: head_dim, slot, KV head, K|V, page; box = 64
 // columns of 16 slots of one head of K or V.
 int make_kv_maps(ts_ctx* c) {
-  cudaDriverEntryPointQueryResult qres;
-  TS_CUDA(c, cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &c->encode_fn, cudaEnableDefault, &qres));
-  if (!c->encode_fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorNotSupported);
   const cuuint64_t D = c->cfg.head_dim, P = c->cfg.page_size, H = c->cfg.n_kv_heads, N = c->cfg.n_pages;
   const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   const cuuint64_t dims[2][5] = {{64, H * P, D / 64, 2, N}, {D, P, H, 2, N}};
@@ -258,8 +259,24 @@ int make_new_kv_maps(ts_ctx* c, const ts_step* st, int64_t n_tokens, ts::NewKvMa
   return TS_OK;
 }
 
-int ensure_cuda(ts_ctx* c, cudaStream_t stream) {
-  if (!c->cfg.kv_pool || !c->cfg.workspace) return cuda_fail(c, cudaErrorInvalidDevicePointer);
+// The 8-bit cache viewed as (head_dim, KV head x slot, K|V, page), bytes; swizzled over the width of a row.
+int make_cache8_map(ts_ctx* c) {
+  const cuuint64_t D = c->cfg.head_dim, P = c->cfg.page_size, H = c->cfg.n_kv_heads, N = c->cfg.n_pages;
+  const cuuint64_t dims[4] = {D, H * P, 2, N};
+  const cuuint64_t strides[3] = {D, H * P * D, 2 * H * P * D};
+  const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)P, 2, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  const CUresult r = ((EncodeFn)c->encode_fn)(&c->cache8_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c->cache8.values, dims, strides, box, estr,
+                                              CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return cuda_fail(c, cudaErrorInvalidValue);
+  return TS_OK;
+}
+
+// `cache`: the one the call works on (TS_CACHE_*); a context of an 8-bit cache may have no bf16 pool.
+int ensure_cuda(ts_ctx* c, cudaStream_t stream, int cache = TS_CACHE_BF16) {
+  if (!(cache == TS_CACHE_E4M3 ? c->cache8.values : c->cfg.kv_pool) || !c->cfg.workspace)
+    return cuda_fail(c, cudaErrorInvalidDevicePointer);
   TS_CUDA(c, cudaSetDevice(c->cfg.device));
   if (!c->cuda_ready) {
     c->ring_bytes = c->L.delta_bytes;
@@ -272,9 +289,16 @@ int ensure_cuda(ts_ctx* c, cudaStream_t stream) {
     }
     TS_CUDA(c, cudaStreamCreateWithFlags(&c->copy_stream, cudaStreamNonBlocking));
     TS_CUDA(c, cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, c->cfg.device));
-    int rc = make_kv_maps(c);
-    if (rc != TS_OK) return rc;
+    cudaDriverEntryPointQueryResult qres;
+    TS_CUDA(c, cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &c->encode_fn, cudaEnableDefault, &qres));
+    if (!c->encode_fn || qres != cudaDriverEntryPointSuccess) return cuda_fail(c, cudaErrorNotSupported);
     c->cuda_ready = true;
+  }
+  bool& map_ready = cache == TS_CACHE_E4M3 ? c->cache8_map_ready : c->kv_maps_ready;
+  if (!map_ready) {
+    const int rc = cache == TS_CACHE_E4M3 ? make_cache8_map(c) : make_kv_maps(c);
+    if (rc != TS_OK) return rc;
+    map_ready = true;
   }
   if (!c->status_cleared) {
     TS_CUDA(c, cudaMemsetAsync((char*)c->cfg.workspace + c->L.off_status, 0, c->L.status_bytes, stream));
@@ -580,9 +604,9 @@ void pack_meta(const ts_ctx* c, const ts_step* st, const ts::StepDevice& d, int 
   std::memcpy(dst + d.o_tok0, c->tok0.data(), sizeof(int32_t) * (R + 1));
   if (n_items > 0) {
     std::memcpy(dst + d.o_items, c->items.data(), sizeof(WorkItem) * n_items);
-    // a split row's items name its merge (the list holds the rows in the order of their partial slots)
+    // a split row's items name its merge (the list holds the rows in the order of their partial slots); a tree's do not
     WorkItem* items = (WorkItem*)(dst + d.o_items);
-    for (int i = c->n_prefill_items; n_combines > 0 && i < n_items; ++i)
+    for (int i = c->n_prefill_items; !c->combine_of.empty() && i < n_items; ++i)
       if (items[i].partial_slot >= 0) items[i].combine = c->combine_of[items[i].partial_slot];
   }
   if (n_combines > 0) std::memcpy(dst + d.o_combines, c->combines.data(), sizeof(CombineItem) * n_combines);
@@ -594,11 +618,10 @@ void pack_meta(const ts_ctx* c, const ts_step* st, const ts::StepDevice& d, int 
 // context's copy stream: that copy only has to wait for the step that last read the slot (kRing steps
 // ago), so it runs while the previous step's kernels are still busy, and the caller's stream just
 // waits for its event.
-int send_meta(ts_ctx* c, const ts_step* st, int n_items, int n_combines, int n_slot_deltas, cudaStream_t stream, ts::StepDevice* d) {
+// `inline_words`: as many as the step's kernels take as parameters.
+int send_meta(ts_ctx* c, const ts_step* st, int n_items, int n_combines, int n_slot_deltas, int inline_words, cudaStream_t stream, ts::StepDevice* d) {
   const size_t used = meta_offsets(st->n_rows, n_items, n_combines, d);
-  // the decode and mixed kernels are there for larger parameters
-  const bool large = n_items > 0 && c->cfg.head_dim == 128 && c->G <= 8;
-  const bool inline_meta = used <= (size_t)(large ? ts::kInlineWordsMax : ts::kInlineWords);
+  const bool inline_meta = used <= (size_t)inline_words;
   const bool inline_deltas = n_slot_deltas <= ts::kInlineDeltas;
   char* ws = (char*)c->cfg.workspace;
   c->meta_cur = -1;
@@ -779,7 +802,9 @@ int enqueue_step(ts_ctx* c, const ts_step* st, int64_t n_tokens, int64_t n_prefi
   const int n_combines = attention ? (int)c->combines.size() : 0;
   ts::StepDevice d;
   fill_device(c, st, n_tokens, &d);
-  rc = send_meta(c, st, n_items, n_combines, n_slot_deltas, stream, &d);
+  // the decode and mixed kernels are there for larger parameters
+  const bool large = n_items > 0 && c->cfg.head_dim == 128 && c->G <= 8;
+  rc = send_meta(c, st, n_items, n_combines, n_slot_deltas, large ? ts::kInlineWordsMax : ts::kInlineWords, stream, &d);
   if (rc != TS_OK) return rc;
   commit_table_sync(c);
   d.n_items = n_items;
@@ -960,6 +985,89 @@ int run_step(ts_ctx* c, const ts_step* st, void* cuda_stream, bool attention) {
   if (rc != TS_OK) return rc;
   finish_step(c, st, n_decode, n_prefill, attention);
   return TS_OK;
+}
+
+// ------------------------------------------------- trees of drafted tokens; the cache written and read back
+// Checks the rows of ts_tree_attention, ts_cache_append and ts_cache_read and fills tok0. A row's ctx_len is the slot's cached
+// length, but for reads, where it is the first token. `cover`: the row's table must reach ctx_len + q_len tokens.
+int check_rows(ts_ctx* c, const ts_step* st, int min_len, int max_len, bool any_start, bool cover, int64_t* n_tokens_out) {
+  if (!c || !st) return TS_ERR_INVALID;
+  if (st->n_rows < 0 || st->n_rows > c->cfg.max_requests) return TS_ERR_INVALID;
+  if (st->n_rows > 0 && (!st->slot || !st->q_len || !st->ctx_len)) return TS_ERR_INVALID;
+  c->tok0.assign((size_t)st->n_rows + 1, 0);
+  if (++c->stamp == 0) {
+    for (auto& s : c->slots) s.stamp = 0;
+    c->stamp = 1;
+  }
+  int64_t n = 0;
+  for (int r = 0; r < st->n_rows; ++r) {
+    const int32_t slot = st->slot[r], len = st->q_len[r], ctx = st->ctx_len[r];
+    if (!slot_ok(c, slot)) return TS_ERR_INVALID;
+    Slot& s = c->slots[slot];
+    if (s.stamp == c->stamp) return TS_ERR_INVALID;  // slot listed twice
+    s.stamp = c->stamp;
+    if (len < min_len || len > max_len || ctx < 0) return TS_ERR_INVALID;
+    if (!any_start && ctx != s.n_tokens) return TS_ERR_INVALID;
+    if ((int64_t)ctx + (cover ? len : 0) > (int64_t)s.n_pages * c->cfg.page_size) return TS_ERR_TABLE_SHORT;
+    n += len;
+    if (n > INT32_MAX / 2) return TS_ERR_INVALID;
+    c->tok0[r + 1] = (int32_t)n;
+  }
+  *n_tokens_out = n;
+  return TS_OK;
+}
+
+bool cache_ok(const ts_ctx* c, int32_t cache) { return cache == TS_CACHE_BF16 || (cache == TS_CACHE_E4M3 && c->cache8.values); }
+
+// Tables and row arrays of a checked call of these go to the device; fills d.
+int begin_rows(ts_ctx* c, const ts_step* st, int64_t n_tokens, int32_t cache, cudaStream_t stream, ts::StepDevice* d) {
+  int rc = ensure_cuda(c, stream, cache);
+  if (rc != TS_OK) return rc;
+  int n_slot_deltas = 0;
+  rc = sync_tables(c, st, stream, &n_slot_deltas);
+  if (rc != TS_OK) return rc;
+  const int n_items = (int)c->items.size(), n_combines = (int)c->combines.size();
+  fill_device(c, st, n_tokens, d);
+  rc = send_meta(c, st, n_items, n_combines, n_slot_deltas, ts::kInlineWords, stream, d);
+  if (rc != TS_OK) return rc;
+  commit_table_sync(c);
+  d->n_items = n_items;
+  d->n_combines = n_combines;
+  return TS_OK;
+}
+
+// Work items of a tree step: see ts_tree.h. Rows are cut so that the units of all rows are about as many as thread blocks run at
+// a time, none shorter than kMinTreePages pages.
+constexpr int kMinTreePages = 16, kTreeBlocksPerSm = 2;
+void plan_tree(ts_ctx* c, const ts_step* st, int tile_tokens) {
+  c->items.clear();
+  c->combines.clear();
+  c->combine_of.clear();
+  c->n_prefill_items = 0;
+  const int P = c->cfg.page_size;
+  auto pages_of = [&](int r) { return ceil_div(st->ctx_len[r], P) + ceil_div(st->q_len[r], P); };
+  int64_t work = 0;
+  for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tile_tokens) * c->cfg.n_kv_heads;
+  const int blocks = kTreeBlocksPerSm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
+  int64_t per = std::max<int64_t>(kMinTreePages, (work + blocks - 1) / blocks);
+  for (;; per *= 2) {                                        // the partial results have to fit
+    int64_t partials = 0;
+    for (int r = 0; r < st->n_rows; ++r)
+      if (pages_of(r) > per) partials += (int64_t)st->q_len[r] * ((pages_of(r) + per - 1) / per);
+    if (partials <= c->L.max_partials) break;
+  }
+  int partial = 0;
+  for (int r = 0; r < st->n_rows; ++r) {
+    const int pages = pages_of(r), T = st->q_len[r], pieces = (int)((pages + per - 1) / per), len = ceil_div(pages, pieces);
+    if (pieces == 1) {
+      c->items.push_back(WorkItem{r, 0, 0, T, 0, pages, -1, 0});
+      continue;
+    }
+    const int n = ceil_div(pages, len);
+    c->combines.push_back(CombineItem{c->tok0[r], partial, n, T});
+    for (int i = 0; i < n; ++i, partial += T) c->items.push_back(WorkItem{r, 0, 0, T, i * len, std::min(pages, (i + 1) * len), partial, 0});
+  }
+  std::stable_sort(c->items.begin(), c->items.end(), [](const WorkItem& a, const WorkItem& b) { return a.k_end - a.k_begin > b.k_end - b.k_begin; });
 }
 
 }  // namespace
@@ -1288,6 +1396,101 @@ int ts_mixed_step_host(ts_ctx* c, const ts_step* st, void* cuda_stream) {
     TS_CUDA(c, cudaStreamSynchronize(stream));
   }
   return TS_OK;
+}
+
+size_t ts_cache8_value_bytes(const ts_config* cfg) { return ts_pool_bytes(cfg) / 2; }
+size_t ts_cache8_scale_bytes(const ts_config* cfg) { return cfg && ts_pool_bytes(cfg) ? ts_pool_bytes(cfg) / 2 / cfg->head_dim : 0; }
+
+int ts_cache8_attach(ts_ctx* c, const ts_cache8* cache) {
+  if (!c || !cache || !cache->values || !cache->scales) return TS_ERR_INVALID;
+  if (((uintptr_t)cache->values | (uintptr_t)cache->scales) & (kAlign - 1)) return TS_ERR_INVALID;
+  if (cache->values_bytes < ts_cache8_value_bytes(&c->cfg) || cache->scales_bytes < ts_cache8_scale_bytes(&c->cfg)) return TS_ERR_WORKSPACE;
+  c->cache8 = *cache;
+  c->cache8_map_ready = false;
+  return TS_OK;
+}
+
+int ts_tree_attention(ts_ctx* c, const ts_step* st, int32_t cache, const uint64_t* mask, void* cuda_stream) {
+  int64_t n_tokens = 0;
+  int rc = check_rows(c, st, 1, ts::kTreeNodes, false, false, &n_tokens);
+  if (rc != TS_OK) return rc;
+  if (!cache_ok(c, cache)) return TS_ERR_INVALID;
+  if (st->n_rows == 0) return TS_OK;
+  if (!st->q || !st->k_new || !st->v_new || !st->out || ((uintptr_t)mask & 7u)) return TS_ERR_INVALID;
+  if (!aligned16(st->q) || !aligned16(st->k_new) || !aligned16(st->v_new) || !aligned16(st->out)) return TS_ERR_INVALID;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  ts::TreeArgs a = {};
+  int nodes = 0;
+  for (int r = 0; r < st->n_rows; ++r) nodes = std::max(nodes, st->q_len[r]);
+  a.mask = mask;
+  if (cache == TS_CACHE_E4M3) a.cache = ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales};
+  a.tile_tokens = ts::tree_tile_tokens(c->G, nodes);
+  a.n_tiles = ceil_div(nodes, a.tile_tokens);
+  plan_tree(c, st, a.tile_tokens);
+  ts::StepDevice d;
+  rc = begin_rows(c, st, n_tokens, cache, stream, &d);
+  if (rc != TS_OK) return rc;
+  TS_CUDA(c, ts::launch_tree(d, a, cache == TS_CACHE_E4M3 ? c->cache8_map : c->kv_map, stream));
+  ++c->cnt.kernel_launches;
+  if (d.n_combines > 0) {
+    TS_CUDA(c, ts::launch_tree_combine(d, nodes, stream));
+    ++c->cnt.kernel_launches;
+  }
+  return release_meta(c, stream);
+}
+
+int ts_tree_masks(const int32_t* parents, int32_t n_nodes, uint64_t* masks_out) {
+  if (n_nodes < 0 || n_nodes > ts::kTreeNodes || (n_nodes > 0 && (!parents || !masks_out))) return TS_ERR_INVALID;
+  for (int i = 0; i < n_nodes; ++i)
+    if (parents[i] < -1 || parents[i] >= i) return TS_ERR_INVALID;
+  for (int i = 0; i < n_nodes; ++i) masks_out[i] = (parents[i] >= 0 ? masks_out[parents[i]] : 0) | (uint64_t)1 << i;
+  return TS_OK;
+}
+
+int ts_cache_append(ts_ctx* c, const ts_step* st, int32_t cache, const int32_t* source, int32_t n_source, void* cuda_stream) {
+  int64_t n_tokens = 0;
+  int rc = check_rows(c, st, 0, INT32_MAX, false, true, &n_tokens);
+  if (rc != TS_OK) return rc;
+  if (!cache_ok(c, cache) || n_source < 0 || ((uintptr_t)source & 3u)) return TS_ERR_INVALID;
+  if (n_tokens > 0) {
+    if (!st->k_new || !st->v_new || !aligned16(st->k_new) || !aligned16(st->v_new)) return TS_ERR_INVALID;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    ts::StepDevice d;
+    c->items.clear();
+    c->combines.clear();
+    rc = begin_rows(c, st, n_tokens, cache, stream, &d);
+    if (rc != TS_OK) return rc;
+    const ts::Cache8 c8 = cache == TS_CACHE_E4M3 ? ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales} : ts::Cache8{};
+    TS_CUDA(c, ts::launch_cache_append(d, c8, source, n_source, stream));
+    ++c->cnt.kernel_launches;
+    rc = release_meta(c, stream);
+    if (rc != TS_OK) return rc;
+  }
+  if (!(st->flags & TS_STEP_KEEP_LEN))
+    for (int r = 0; r < st->n_rows; ++r) c->slots[st->slot[r]].n_tokens += st->q_len[r];
+  return TS_OK;
+}
+
+int ts_cache_read(ts_ctx* c, const ts_step* st, int32_t cache, void* k_out, void* v_out, void* cuda_stream) {
+  int64_t n_tokens = 0;
+  int rc = check_rows(c, st, 0, INT32_MAX, true, true, &n_tokens);
+  if (rc != TS_OK) return rc;
+  if (!cache_ok(c, cache)) return TS_ERR_INVALID;
+  if (n_tokens == 0) return TS_OK;
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return TS_ERR_INVALID;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  ts_step out = *st;
+  out.k_new = k_out;
+  out.v_new = v_out;
+  ts::StepDevice d;
+  c->items.clear();
+  c->combines.clear();
+  rc = begin_rows(c, &out, n_tokens, cache, stream, &d);
+  if (rc != TS_OK) return rc;
+  const ts::Cache8 c8 = cache == TS_CACHE_E4M3 ? ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales} : ts::Cache8{};
+  TS_CUDA(c, ts::launch_cache_read(d, c8, stream));
+  ++c->cnt.kernel_launches;
+  return release_meta(c, stream);
 }
 
 int ts_host_fence(ts_ctx* c, void* cuda_stream) {

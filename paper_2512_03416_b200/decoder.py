@@ -14,6 +14,9 @@ from . import binding as B
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+CACHES = {"bf16": B.TS_CACHE_BF16, "e4m3": B.TS_CACHE_E4M3}
+
+
 class TsError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {B.ts_strerror(code)} ({code})")
@@ -41,7 +44,11 @@ class Decoder:
                  max_pages_per_req: int, chunk_size: int = 0, reserved_pages: int = 0,
                  decode_split_tokens: int = 0, softmax_scale: float = 0.0, device: int = 0,
                  alloc_shuffle_seed: int = 0, page_size: int = 16, nan_fill: bool = False,
-                 mixed_prefill_ctas: int = 0, wait_limit_cycles: int = 0, debug_flags: int = 0):
+                 mixed_prefill_ctas: int = 0, wait_limit_cycles: int = 0, debug_flags: int = 0, cache: str = "bf16"):
+        """cache: "bf16" (self.pool), or "e4m3" for the 8-bit cache (self.cache8_values, self.cache8_scales) and no
+        pool: tree_attention, cache_append and cache_read then work on that, mixed steps are refused."""
+        if cache not in CACHES:
+            raise ValueError(f"cache must be one of {sorted(CACHES)}")
         if not torch.cuda.is_available():
             raise RuntimeError("a CUDA device is required; there is no CPU implementation")
         self.device = torch.device("cuda", device)
@@ -52,15 +59,29 @@ class Decoder:
         pool_bytes, ws_bytes = B.ts_pool_bytes(cfg), B.ts_workspace_bytes(cfg)
         if pool_bytes == 0:
             raise TsError(B.TS_ERR_UNSUPPORTED, "ts_pool_bytes")
-        self.pool = torch.empty(pool_bytes // 2, dtype=torch.int16, device=self.device)
-        if nan_fill:
-            self.pool.fill_(0x7FC0)
+        self.cache = CACHES[cache]
+        self.pool = self.cache8_values = self.cache8_scales = None
+        if cache == "bf16":
+            self.pool = torch.empty(pool_bytes // 2, dtype=torch.int16, device=self.device)
+            if nan_fill:
+                self.pool.fill_(0x7FC0)
+        else:
+            self.cache8_values = torch.empty(B.ts_cache8_value_bytes(cfg), dtype=torch.uint8, device=self.device)
+            self.cache8_scales = torch.empty(B.ts_cache8_scale_bytes(cfg), dtype=torch.uint8, device=self.device)
+            if nan_fill:
+                self.cache8_values.fill_(0x7F)
+                self.cache8_scales.fill_(0xFF)
         self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
-        cfg.kv_pool, cfg.kv_pool_bytes = self.pool.data_ptr(), pool_bytes
+        if self.pool is not None:
+            cfg.kv_pool, cfg.kv_pool_bytes = self.pool.data_ptr(), pool_bytes
         cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), ws_bytes
         self.cfg = cfg
         rc, self.ctx = B.ts_create(cfg)
         _check(rc, "ts_create")
+        if self.cache8_values is not None:
+            c8 = B.ts_cache8(self.cache8_values.data_ptr(), self.cache8_values.numel(), self.cache8_scales.data_ptr(),
+                             self.cache8_scales.numel())
+            _check(B.ts_cache8_attach(self.ctx, c8), "ts_cache8_attach")
 
     def close(self) -> None:
         if getattr(self, "ctx", None):
@@ -139,6 +160,50 @@ class Decoder:
         if alloc:
             _check(B.ts_alloc_step(self.ctx, st), "ts_alloc_step")
         _check(B.ts_mixed_step(self.ctx, st, self._stream()), "ts_mixed_step")
+
+    # ------------------------------------- trees of drafted tokens; the cache written and read back
+    def _tokens(self, t, heads: int, what: str) -> int:
+        """Address of a contiguous 16-bit tensor [N, heads, head_dim] on this device."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or t.element_size() != 2:
+            raise ValueError(f"{what} must be a bf16 (or int16) tensor [N, {heads}, {self.cfg.head_dim}], not {t.dtype} {tuple(t.shape)}")
+        if t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous and on {self.device}")
+        return t.data_ptr()
+
+    def tree_attention(self, slots, n_nodes, ctx_len, q, k_new, v_new, out, mask=None) -> None:
+        """Attention of every request's drafted nodes over its cached tokens and, as mask says, over each other (see
+        ts_tree_attention). mask: int64 CUDA tensor [N] of bit sets (tree_masks), None for chains of tokens."""
+        hq, hkv, n = self.cfg.n_q_heads, self.cfg.n_kv_heads, sum(n_nodes)
+        if mask is not None and (mask.numel() < n or mask.element_size() != 8 or mask.device != self.device or not mask.is_contiguous()):
+            raise ValueError(f"mask must be a contiguous int64 tensor of {n} words on {self.device}")
+        if min(q.shape[0], k_new.shape[0], v_new.shape[0], out.shape[0]) < n:
+            raise ValueError(f"the tensors hold fewer than {n} tokens")
+        st, _keep = B.make_step(slots, n_nodes, ctx_len, self._tokens(q, hq, "q"), self._tokens(k_new, hkv, "k_new"),
+                                self._tokens(v_new, hkv, "v_new"), self._tokens(out, hq, "out"))
+        _check(B.ts_tree_attention(self.ctx, st, self.cache, 0 if mask is None else mask.data_ptr(), self._stream()), "ts_tree_attention")
+
+    def cache_append(self, slots, q_len, ctx_len, k_new, v_new, source=None, keep_len: bool = False) -> None:
+        """Write q_len[r] tokens per request behind its cached ones, quantised where the cache is 8 bit. source: int32 CUDA
+        tensor naming each token's row of k_new and v_new (the accepted nodes of a tree); None: in order."""
+        n, hkv = sum(q_len), self.cfg.n_kv_heads
+        if source is None:
+            if min(k_new.shape[0], v_new.shape[0]) < n:
+                raise ValueError(f"the tensors hold fewer than {n} tokens")
+        elif source.numel() < n or source.dtype != torch.int32 or source.device != self.device or not source.is_contiguous():
+            raise ValueError(f"source must be a contiguous int32 tensor of {n} indices on {self.device}")
+        st, _keep = B.make_step(slots, q_len, ctx_len, 0, self._tokens(k_new, hkv, "k_new"), self._tokens(v_new, hkv, "v_new"), 0,
+                                B.TS_STEP_KEEP_LEN if keep_len else 0)
+        _check(B.ts_cache_append(self.ctx, st, self.cache, 0 if source is None else source.data_ptr(),
+                                 min(k_new.shape[0], v_new.shape[0]), self._stream()), "ts_cache_append")
+
+    def cache_read(self, slots, first, count, k_out, v_out) -> None:
+        """The K and V of the count[r] tokens from position first[r] on of each request, as bf16."""
+        n, hkv = sum(count), self.cfg.n_kv_heads
+        if min(k_out.shape[0], v_out.shape[0]) < n:
+            raise ValueError(f"the tensors hold fewer than {n} tokens")
+        st, _keep = B.make_step(slots, count, first)
+        _check(B.ts_cache_read(self.ctx, st, self.cache, self._tokens(k_out, hkv, "k_out"), self._tokens(v_out, hkv, "v_out"),
+                               self._stream()), "ts_cache_read")
 
     def plan_step(self, slots, q_len, ctx_len):
         st, _keep = B.make_step(slots, q_len, ctx_len)

@@ -1,0 +1,147 @@
+"""ts_token_logprobs against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_03416_b200.logprobs import token_logprobs
+from tests import tree_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(logits, tokens=None, n_top=0, scale=None):
+    """Whole numbers must be equal. In fp32 y log2(e) carries 2^-23 of its size, the sums of up to 2^17 terms less than
+    2^-20 of theirs, of which the logarithm makes an absolute error; the entropy's terms are as large as the spread of y."""
+    r = token_logprobs(logits, tokens, n_top, scale)
+    torch.cuda.synchronize()
+    x = logits.double().cpu().numpy()
+    given = np.zeros((len(x), 0), int) if tokens is None else tokens.view(len(x), -1).cpu().numpy()
+    for i in range(len(x)):
+        s = 1.0 if scale is None else float(scale[i])
+        lp, rank, ent, top_lp, top = O.token_logprobs(x[i], s, given[i], n_top)
+        fin = np.abs(x[i][np.isfinite(x[i])]) * s
+        tol = 2.0 ** -19 * (1 + (fin.max() if len(fin) else 0))
+        assert np.array_equal(r.rank[i].cpu().numpy(), rank), (i, given[i])
+        assert np.array_equal(r.top_token[i].cpu().numpy(), top), i
+        for got, want, what in ((r.logprob[i], lp, "logprob"), (r.top_logprob[i], top_lp, "top"), (r.entropy[i:i + 1], np.array([ent]), "entropy")):
+            got = got.cpu().numpy().astype(np.float64)
+            same = (got == want) | (np.isnan(got) & np.isnan(want))
+            with np.errstate(invalid="ignore"):
+                assert (same | (np.abs(got - want) <= tol)).all(), (what, i, got, want)
+    return r
+
+
+def _logits(rows, vocab, dtype, seed=0, size=3.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(rows, vocab, generator=g, device="cuda") * size).to(dtype)
+
+
+def _tokens(rows, given, vocab, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed + 100)
+    return torch.randint(0, vocab, (rows, given), generator=g, device="cuda", dtype=torch.int32)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 31, 33, 1000, 4095, 4096, 4097, 8193, 32000, 50001, 131072, 200003])
+@pytest.mark.parametrize("rows,given,n_top", [(1, 1, 20), (3, 8, 32), (40, 2, 1), (2, 0, 5), (5, 3, 0)])
+def test_sizes(rows, vocab, dtype, given, n_top):
+    _check(_logits(rows, vocab, dtype, vocab), _tokens(rows, given, vocab) if given else None, n_top)
+
+
+@pytest.mark.parametrize("rows", [150, 600])
+def test_many_rows(rows):
+    _check(_logits(rows, 3001, torch.bfloat16), _tokens(rows, 1, 3001), 4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [65, 5000, 40000])
+def test_strides_and_alignment(vocab, dtype):
+    """Rows that start anywhere in a 16-byte block, with neighbours that must not be looked at."""
+    wide = torch.full((6, vocab + 37), 1e4, dtype=dtype, device="cuda")
+    for start in (0, 1, 3, 8, 13):
+        wide.fill_(float("nan"))
+        view = wide[:, start:start + vocab]
+        view.copy_(_logits(6, vocab, dtype, start))
+        _check(view, _tokens(6, 2, vocab), 7)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [40, 5000, 70001])
+def test_masked_and_odd_logits(vocab, dtype):
+    inf = float("inf")
+    x = _logits(12, vocab, dtype, 5)
+    x[0] = -inf                                                    # nothing is left
+    x[1, 3:] = -inf                                                # three tokens are left: the next ones go by index
+    x[2] = 1.5                                                     # all alike
+    x[3, vocab // 2] = float("nan")
+    x[4, 7] = inf
+    x[5, ::2] = torch.finfo(dtype).min                             # masked by the type's lowest value
+    x[6] = torch.arange(vocab, device="cuda") * (60.0 / vocab)     # ascending
+    x[7] = -torch.arange(vocab, device="cuda") * (60.0 / vocab)
+    x[8] = float("nan")
+    x[9, 5:] = float("nan")                                        # fewer numbers than alternatives
+    x[10] = torch.where(torch.arange(vocab, device="cuda") % 2 == 0, 0.0, -0.0)
+    x[11] = -inf
+    x[11, vocab - 1] = -3.0
+    tokens = _tokens(12, 5, vocab)
+    tokens[:, 1] = vocab - 1
+    tokens[:, 2] = 0
+    tokens[:, 3] = torch.tensor([vocab, -1, 1 << 30, -(1 << 31)] * 3, dtype=torch.int32, device="cuda")
+    for n_top in (1, 6, 32):
+        _check(x, tokens, n_top)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [1, 400])
+def test_best_tokens_in_one_place(dtype, rows):
+    """The best tokens all in the blocks that one or few threads read, in ascending order: more candidates than the list holds."""
+    n = 8 if dtype == torch.bfloat16 else 4
+    x = _logits(rows, 300000, dtype, 6, 0.5)
+    block = torch.arange(300000, device="cuda") // n
+    for r in range(0, rows, 50):
+        part = block % 512 < 1 + r // 50
+        x[r, part] = (10 + torch.arange(300000, device="cuda")[part] * 1e-4).to(dtype)
+    _check(x[::50].contiguous() if rows > 1 else x, None, 32)
+    if rows > 1:
+        r = token_logprobs(x, None, 32)
+        one = token_logprobs(x[:1], None, 32)
+        assert torch.equal(r.top_token[0], one.top_token[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_scales_and_sizes(dtype):
+    x = _logits(8, 9000, dtype, 7)
+    x[4:] *= 300                                                    # hundreds of nats apart, positive and negative
+    x[6] += 2000
+    x[7] -= 2000
+    _check(x, _tokens(8, 4, 9000), 10, torch.tensor([0.25, 1, 2, 10, 0.01, 1, 1, 1], device="cuda"))
+
+
+def test_single_values_rise():
+    """A reference that has to move again and again: every block's values exceed all earlier ones by more than 2^64."""
+    x = (torch.arange(200000, device="cuda") // 4096 * 70.0)[None].contiguous()
+    _check(x, _tokens(1, 3, 200000), 5)
+
+
+def test_same_bits_again_and_on_another_stream():
+    x, t = _logits(30, 60001, torch.bfloat16, 8), _tokens(30, 3, 60001)
+    a = token_logprobs(x, t, 9)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        b = token_logprobs(x, t, 9)
+    st.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_refusals():
+    x = _logits(2, 100, torch.float32)
+    t = _tokens(2, 1, 100)
+    for f in (lambda: token_logprobs(x.half()), lambda: token_logprobs(x.cpu()), lambda: token_logprobs(x.t()), lambda: token_logprobs(x[0]),
+              lambda: token_logprobs(x, t.long()), lambda: token_logprobs(x, t[:1]), lambda: token_logprobs(x, _tokens(2, 9, 100)),
+              lambda: token_logprobs(x, n_top=33), lambda: token_logprobs(x, n_top=-1), lambda: token_logprobs(x, scale=torch.ones(3, device="cuda")),
+              lambda: token_logprobs(x[:, :0]), lambda: token_logprobs(x[:1].expand(2, 100))):
+        with pytest.raises(ValueError):
+            f()
+    r = token_logprobs(x[:0], t[:0], 3)
+    assert r.logprob.shape == (0, 1) and r.top_token.shape == (0, 3)

@@ -146,6 +146,7 @@ struct ts_ctx {
   CUtensorMap kv_tile_map;          // box = K or V of 64 columns of one (page, head)
   ts_cache8 cache8 = {};            // see ts_cache8_attach
   CUtensorMap cache8_map;           // TMA view of its values, box = K and V of one (page, head)
+  CUtensorMap cache8_tile_map;      // box = K or V of one (page, head)
   bool kv_maps_ready = false, cache8_map_ready = false;
   void* encode_fn = nullptr;        // cuTensorMapEncodeTiled
   int n_sms = 0;
@@ -259,17 +260,21 @@ int make_new_kv_maps(ts_ctx* c, const ts_step* st, int64_t n_tokens, ts::NewKvMa
   return TS_OK;
 }
 
-// The 8-bit cache viewed as (head_dim, KV head x slot, K|V, page), bytes; swizzled over the width of a row.
-int make_cache8_map(ts_ctx* c) {
+// The 8-bit cache's tensor maps, bytes, swizzled over the width of a row. cache8_map: (head_dim, KV head x slot, K|V, page);
+// cache8_tile_map: (head_dim, slot, KV head, K|V, page).
+int make_cache8_maps(ts_ctx* c) {
   const cuuint64_t D = c->cfg.head_dim, P = c->cfg.page_size, H = c->cfg.n_kv_heads, N = c->cfg.n_pages;
-  const cuuint64_t dims[4] = {D, H * P, 2, N};
-  const cuuint64_t strides[3] = {D, H * P * D, 2 * H * P * D};
-  const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)P, 2, 1};
-  const cuuint32_t estr[4] = {1, 1, 1, 1};
-  const CUresult r = ((EncodeFn)c->encode_fn)(&c->cache8_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c->cache8.values, dims, strides, box, estr,
-                                              CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return cuda_fail(c, cudaErrorInvalidValue);
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  const cuuint64_t dims[2][5] = {{D, H * P, 2, N, 0}, {D, P, H, 2, N}};
+  const cuuint64_t strides[2][4] = {{D, H * P * D, 2 * H * P * D, 0}, {D, P * D, H * P * D, 2 * H * P * D}};
+  const cuuint32_t box[2][5] = {{(cuuint32_t)D, (cuuint32_t)P, 2, 1, 0}, {(cuuint32_t)D, (cuuint32_t)P, 1, 1, 1}};
+  for (int i = 0; i < 2; ++i) {
+    const CUresult r = ((EncodeFn)c->encode_fn)(i == 0 ? &c->cache8_map : &c->cache8_tile_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4 + i,
+                                                c->cache8.values, dims[i], strides[i], box[i], estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                                D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return cuda_fail(c, cudaErrorInvalidValue);
+  }
   return TS_OK;
 }
 
@@ -296,7 +301,7 @@ int ensure_cuda(ts_ctx* c, cudaStream_t stream, int cache = TS_CACHE_BF16) {
   }
   bool& map_ready = cache == TS_CACHE_E4M3 ? c->cache8_map_ready : c->kv_maps_ready;
   if (!map_ready) {
-    const int rc = cache == TS_CACHE_E4M3 ? make_cache8_map(c) : make_kv_maps(c);
+    const int rc = cache == TS_CACHE_E4M3 ? make_cache8_maps(c) : make_kv_maps(c);
     if (rc != TS_OK) return rc;
     map_ready = true;
   }
@@ -1036,10 +1041,28 @@ int begin_rows(ts_ctx* c, const ts_step* st, int64_t n_tokens, int32_t cache, cu
   return TS_OK;
 }
 
+// How a tree step runs.
+struct TreePlan {
+  bool tc;                 // on tcgen05
+  int tile_tokens;         // nodes of a query tile
+  int tiles_per_unit;      // query tiles of a work unit (1 but for tcgen05)
+  int n_tiles;             // units of the longest row, per item and KV head
+};
+// Queries per KV head of the row with most nodes above which a step runs on tcgen05 (head_dim 128).
+constexpr int kTreeTcQueries = 32;
+TreePlan choose_tree(const ts_ctx* c, int nodes) {
+  TreePlan p = {};
+  p.tc = c->cfg.head_dim == 128 && nodes * c->G > kTreeTcQueries;
+  p.tile_tokens = p.tc ? 128 / c->G : ts::tree_tile_tokens(c->G, nodes);
+  p.tiles_per_unit = p.tc && nodes > p.tile_tokens ? 2 : 1;
+  p.n_tiles = ceil_div(nodes, p.tile_tokens * p.tiles_per_unit);
+  return p;
+}
+
 // Work items of a tree step: see ts_tree.h. Rows are cut so that the units of all rows are about as many as thread blocks run at
-// a time, none shorter than kMinTreePages pages.
+// a time, none shorter than kMinTreePages pages. A row's own nodes stay together.
 constexpr int kMinTreePages = 16, kTreeBlocksPerSm = 2;
-void plan_tree(ts_ctx* c, const ts_step* st, int tile_tokens) {
+void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   c->items.clear();
   c->combines.clear();
   c->combine_of.clear();
@@ -1047,8 +1070,8 @@ void plan_tree(ts_ctx* c, const ts_step* st, int tile_tokens) {
   const int P = c->cfg.page_size;
   auto pages_of = [&](int r) { return ceil_div(st->ctx_len[r], P) + ceil_div(st->q_len[r], P); };
   int64_t work = 0;
-  for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tile_tokens) * c->cfg.n_kv_heads;
-  const int blocks = kTreeBlocksPerSm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
+  for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tp.tile_tokens * tp.tiles_per_unit) * c->cfg.n_kv_heads;
+  const int blocks = (tp.tc ? 1 : kTreeBlocksPerSm) * (c->n_sms > 0 ? c->n_sms : kSmsB200);
   int64_t per = std::max<int64_t>(kMinTreePages, (work + blocks - 1) / blocks);
   for (;; per *= 2) {                                        // the partial results have to fit
     int64_t partials = 0;
@@ -1058,14 +1081,18 @@ void plan_tree(ts_ctx* c, const ts_step* st, int tile_tokens) {
   }
   int partial = 0;
   for (int r = 0; r < st->n_rows; ++r) {
-    const int pages = pages_of(r), T = st->q_len[r], pieces = (int)((pages + per - 1) / per), len = ceil_div(pages, pieces);
-    if (pieces == 1) {
-      c->items.push_back(WorkItem{r, 0, 0, T, 0, pages, -1, 0});
-      continue;
+    const int cached = ceil_div(st->ctx_len[r], P), pages = pages_of(r), T = st->q_len[r], pieces = (int)((pages + per - 1) / per);
+    const int len = ceil_div(pages, pieces);
+    const size_t first = c->items.size();
+    for (int at = 0; at < pages;) {
+      const int end = at + len >= cached ? pages : at + len;
+      c->items.push_back(WorkItem{r, 0, 0, T, at, end, -1, 0});
+      at = end;
     }
-    const int n = ceil_div(pages, len);
+    const int n = (int)(c->items.size() - first);
+    if (n == 1) continue;
     c->combines.push_back(CombineItem{c->tok0[r], partial, n, T});
-    for (int i = 0; i < n; ++i, partial += T) c->items.push_back(WorkItem{r, 0, 0, T, i * len, std::min(pages, (i + 1) * len), partial, 0});
+    for (int i = 0; i < n; ++i, partial += T) c->items[first + i].partial_slot = partial;
   }
   std::stable_sort(c->items.begin(), c->items.end(), [](const WorkItem& a, const WorkItem& b) { return a.k_end - a.k_begin > b.k_end - b.k_begin; });
 }
@@ -1424,13 +1451,15 @@ int ts_tree_attention(ts_ctx* c, const ts_step* st, int32_t cache, const uint64_
   for (int r = 0; r < st->n_rows; ++r) nodes = std::max(nodes, st->q_len[r]);
   a.mask = mask;
   if (cache == TS_CACHE_E4M3) a.cache = ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales};
-  a.tile_tokens = ts::tree_tile_tokens(c->G, nodes);
-  a.n_tiles = ceil_div(nodes, a.tile_tokens);
-  plan_tree(c, st, a.tile_tokens);
+  const TreePlan tp = choose_tree(c, nodes);
+  a.tile_tokens = tp.tile_tokens;
+  a.n_tiles = tp.n_tiles;
+  plan_tree(c, st, tp);
   ts::StepDevice d;
   rc = begin_rows(c, st, n_tokens, cache, stream, &d);
   if (rc != TS_OK) return rc;
-  TS_CUDA(c, ts::launch_tree(d, a, cache == TS_CACHE_E4M3 ? c->cache8_map : c->kv_map, stream));
+  if (tp.tc) TS_CUDA(c, ts::launch_tree_tc(d, a, tp.tiles_per_unit, cache == TS_CACHE_E4M3 ? c->cache8_tile_map : c->kv_tile_map, c->n_sms, stream));
+  else TS_CUDA(c, ts::launch_tree(d, a, cache == TS_CACHE_E4M3 ? c->cache8_map : c->kv_map, stream));
   ++c->cnt.kernel_launches;
   if (d.n_combines > 0) {
     TS_CUDA(c, ts::launch_tree_combine(d, nodes, stream));

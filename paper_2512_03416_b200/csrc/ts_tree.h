@@ -17,6 +17,9 @@ struct TreeArgs {
 };
 // kv_map: the pool's or the 8-bit cache's pages, box = K and V of one (page, KV head).
 cudaError_t launch_tree(const StepDevice& s, const TreeArgs& a, const CUtensorMap& kv_map, cudaStream_t stream);
+// The same on tcgen05 (head_dim 128): query tiles of up to 128 / G nodes, a.n_tiles units of tiles_per_unit (1 or 2) of them per row and
+// KV head. A row's own nodes are in one item. map: box = 16 slots of K or V of a (page, KV head), 128 bytes of each.
+cudaError_t launch_tree_tc(const StepDevice& s, const TreeArgs& a, int tiles_per_unit, const CUtensorMap& map, int n_sms, cudaStream_t stream);
 cudaError_t launch_tree_combine(const StepDevice& s, int max_nodes, cudaStream_t stream);
 // Nodes of a query tile of the streaming kernel for rows of up to `nodes` nodes.
 int tree_tile_tokens(int G, int nodes);

@@ -529,7 +529,7 @@ int ts_gemm_plan(int32_t device, int32_t M, int32_t N, int32_t K, int32_t epilog
  *        scales[page][kv][head][slot]      one byte b per row of head_dim codes, ts_cache8_scale_bytes() bytes
  *   element = code * 2^(b - 127), exact in bf16. A row x is written with E = b - 127 the smallest whole number for which
  *   max|x| <= 448 * 2^E, clamped to [-62, 62] (0 for a row of zeros), and codes x * 2^-E rounded to nearest even; what is
- *   larger than 448 * 2^62 saturates, infinities too; a NaN stays one.
+ *   larger than 448 * 2^62 saturates, infinities too. A row with a NaN gets b = 255 and counts as one of NaN.
  * ts_cache8_attach: binds such a cache to a context (both pointers 256-byte aligned). The context may then have been
  *   created without kv_pool (its workspace is still needed): calls on TS_CACHE_E4M3 work, those on the bf16 pool return TS_ERR_CUDA.
  */
@@ -552,7 +552,8 @@ int ts_cache8_attach(ts_ctx* ctx, const ts_cache8* cache);
  * set (bits from q_len[r] on are ignored); a node that sees nothing gets zeros. mask: DEVICE uint64 [N], 8-byte
  * aligned; NULL = a chain (node i sees the nodes 0..i), so that a row of one node is a decode row. The K and V of a
  * node that nobody sees may hold anything; a seen node whose V holds an infinity or a NaN makes its viewers' outputs NaN.
- * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^76).
+ * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^70), and V rows
+ * more than 2^22 smaller than the largest of 32 neighbouring keys may lose bits.
  * Arithmetic as for a step: fp32 accumulation and softmax, weights rounded to bf16 (8-bit cache: f16) in front of
  * the second product, bf16 result. Asynchronous on cuda_stream; uses the context's workspace, as a step does.
  * ts_tree_masks (host): mask words of one row's nodes from their parents (parents[i] in [-1, i), -1 = attached to the

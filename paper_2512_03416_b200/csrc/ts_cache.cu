@@ -1,7 +1,7 @@
 // The KV cache written and read back (sm_100a): bf16 pages, or the 8-bit cache.
 //
 // 8-bit cache: the D elements of a (token, KV head, K or V) row are e4m3 codes of x * 2^-E, where E is the smallest
-// whole number with max|x| <= 448 * 2^E (0 for a row of zeros, clamped to [-62, 62]). A power of two costs no precision: e4m3
+// whole number with max|x| <= 448 * 2^E (0 for a row of zeros, clamped to [-62, 62]). A row with a NaN is one of NaN: its scale says so. A power of two costs no precision: e4m3
 // has the same four significant bits in every binade, so it loses nothing against a scale of max|x| / 448, the codes are the
 // bf16 value rounded once, and code * 2^E is exact in bf16. It is one byte per row (E + 127) instead of four.
 //
@@ -49,19 +49,15 @@ __device__ __forceinline__ Place place_of(const StepDevice& s, const int32_t* ro
 // Eight bf16 of one row in a lane, LPR lanes per row -> the row's codes in place and its scale byte.
 template <int LPR>
 __device__ __forceinline__ uint2 quantise(const uint4& v, uint8_t& scale) {
-  // magnitudes as integers are ordered as the numbers are; a NaN does not take part
+  // magnitudes as integers are ordered as the numbers are, NaN behind infinity
   uint32_t most = 0;
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = w[i] & 0x7fff, b = (w[i] >> 16) & 0x7fff;
-    most = max(most, a > 0x7f80u ? 0u : a);
-    most = max(most, b > 0x7f80u ? 0u : b);
-  }
+  for (int i = 0; i < 4; ++i) most = max(most, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
 #pragma unroll
   for (int sh = 1; sh < LPR; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
   const int E = cache8_exponent(most);
-  scale = (uint8_t)(E + 127);
+  scale = most > 0x7f80u ? 255 : (uint8_t)(E + 127);
   const float by = __int_as_float((127 - E) << 23);
   uint32_t out[2];
 #pragma unroll

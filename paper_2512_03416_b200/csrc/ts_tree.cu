@@ -263,8 +263,8 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
       ks0 = cache8_power(exps[g]);
       ks1 = cache8_power(exps[g + 8]);
       const int e0 = cache8_exp_of(exps[16 + g]), e1 = cache8_exp_of(exps[16 + g + 8]);
-      ve0 = (float)e0;
-      ve1 = (float)e1;
+      ve0 = exps[16 + g] == 255 ? CUDART_NAN_F : (float)e0;
+      ve1 = exps[16 + g + 8] == 255 ? CUDART_NAN_F : (float)e1;
       out0 = power(-e0);
       out1 = power(-e1);
     }

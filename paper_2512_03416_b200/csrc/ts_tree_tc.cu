@@ -5,9 +5,9 @@
 // come off a global queue, longest first. A unit's keys pass by in blocks of 128 (eight pages; the row's own nodes are a block
 // of their own, the last one):
 //     S = Q K^T   (tcgen05.mma, fp32 accumulator in TMEM)
-//     online softmax, a thread per query row
+//     online softmax, four lanes per query row
 //     O += P V    (tcgen05.mma, P from TMEM, O accumulates in TMEM)
-// There are two slots, each with its S (128 TMEM columns, P over it), its O (128 columns) and four softmax warps, half a period apart,
+// There are two slots, each with its S (128 TMEM columns, P over it), its O (128 columns) and eight softmax warps, half a period apart,
 // so that the tensor cores work for one while the other is in its softmax. A unit of two query tiles gives each slot a tile; both
 // take every block. A unit of one tile gives the slots its blocks in turn, as two splits, which are added up in the epilogue.
 //
@@ -18,11 +18,14 @@
 // 8-bit cache: K goes to the tensor cores as it is (kind::f8f6f4). The queries are two e4m3 addends each, q = (q1 + q2) 2^e with
 // a power of two per row: bf16's eight significant bits are twice e4m3's four, so the sum is exact down to 2^-9 of the row's
 // largest element (and off by 2^-18 of that below). V is widened to f16 (exact) by four warps between its copy and the MMA, because P in
-// 8 bits would lose what many small weights carry together. Exponents as in ts_tree.cu. The row's own K are two e4m3 addends as well: their 64
-// rows at most are rows 0..63 and 64..127 of one K tile, and the scores are added in pairs; their V are f16 with a power of two.
+// 8 bits would lose what many small weights carry together. A K row's exponent is multiplied to its score. The V rows of 32 keys are
+// brought to the largest of their exponents, E, as they are widened (exact for rows up to 2^15 smaller, to 2^-8 of their largest element up to
+// 2^22), so that the weights of these keys get E alone: 2^(s + E - m), m the running maximum of s + E, and the sum takes it out again. The
+// row's own K are two e4m3 addends as well: their 64 rows at most are rows 0..63 and 64..127 of one K tile, and the scores are added in
+// pairs; their V are f16 with an exponent per 32 nodes.
 //
-// Warps: 0-3 / 4-7 softmax of slot A / B (thread = TMEM lane = query row), 8-11 transform (queries, V, the row's own nodes, the keys'
-// exponents), 12 K loader (also takes the units), 13 V loader, 14 MMA issuer. Every wait is bounded; one that runs out raises
+// Warps: 0-7 / 8-15 softmax of slot A / B (sixteen query rows each, four lanes per row), 16-19 transform (queries, V, the row's own nodes,
+// the keys' exponents), 20 K loader (also takes the units), 21 V loader, 22 MMA issuer. Every wait is bounded; one that runs out raises
 // TS_DEV_TIMEOUT, and the CTA ends: no new copies or MMAs, those in flight are waited for (with a limit).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -38,15 +41,17 @@
 namespace ts {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kRegsSoftmax = 200, kRegsAux = 56, kRegsLaunch = 128;
-static_assert(256 * kRegsSoftmax + 256 * kRegsAux <= kThreads * kRegsLaunch, "register split exceeds the launch's total");
-constexpr int kWarpTransform = 8, kWarpK = 12, kWarpV = 13, kWarpMma = 14;
+constexpr int kThreads = 768;
+// Register split (setmaxnreg works on whole warpgroups): four of softmax warps, one of transform warps, one of loaders and MMA issuer
+constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsTransform = 56, kRegsAux = 40;
+static_assert(512 * kRegsSoftmax + 128 * (kRegsTransform + kRegsAux) <= kThreads * kRegsLaunch, "register split exceeds the launch's total");
+constexpr int kWarpTransform = 16, kWarpK = 20, kWarpV = 21, kWarpMma = 22;
 constexpr int kD = 128, kBlock = 128, kBlockPages = kBlock / kPageSize;
 constexpr int kTile = 128 * kD * 2;              // 128 x 128 16-bit operand: two 64-column halves of 128 rows of 128 bytes
 constexpr int kHalf = kTile / 2;
 constexpr int kTile8 = 128 * kD;                 // 128 x 128 8-bit operand: 128 rows of 128 bytes
-constexpr int kUnitRing = 4, kUnitReaders = 14;  // V loader, MMA issuer, 4 transform and 8 softmax warps
+constexpr int kUnitRing = 4, kUnitReaders = 22;  // V loader, MMA issuer, 4 transform and 16 softmax warps
+constexpr int kTabStages = 4;                    // blocks whose keys' exponents are held
 constexpr float kMoveBy = 8.f;                   // log2: how far a row's maximum may exceed its reference
 constexpr float kShift16 = 7.f;                  // log2 of the factor on f16 weights: 2^(8 + 7) is within f16, 2^-21 a normal number
 constexpr long long kDrainCycles = 20000000;
@@ -61,10 +66,11 @@ struct Map {
   static constexpr int kOffK = kOffQ + NT * kTile;
   static constexpr int kOffV = kOffK + kKStages * kKBytes;
   static constexpr int kOffRaw = kOffV + kVStages * kTile;
-  static constexpr int kOffTab = kOffRaw + kRawStages * kTile8;           // Q8, per V stage: K power, V exponent, its inverse power [3][128]
-  static constexpr int kOffQScale = kOffTab + (Q8 ? kVStages * 3 * kBlock * 4 : 0);   // Q8: [NT][128] power of two of a query
+  static constexpr int kOffTab = kOffRaw + kRawStages * kTile8;           // Q8, of a block: [128] powers of two of the K rows
+  static constexpr int kOffExp = kOffTab + (Q8 ? kTabStages * kBlock * 4 : 0);          // Q8: exponents of the block's four groups of 32 V rows
+  static constexpr int kOffQScale = kOffExp + (Q8 ? kTabStages * 16 : 0);   // Q8: [NT][128] powers of two of the queries
   static constexpr int kOffXchg = kOffQScale + (Q8 ? NT * 128 * 4 : 0);   // [slot][128] (maximum, sum)
-  static constexpr int kOffBad = kOffXchg + 2 * 128 * 8;                  // per V stage: the row's own V rows that are not finite, 64 bits
+  static constexpr int kOffBad = kOffXchg + 2 * 128 * 8;                  // of a block of nodes: those whose V is not finite, 64 bits
   static constexpr int kOffUnits = kOffBad + 32;
   static constexpr int kOffBar = kOffUnits + kUnitRing * 64;
   enum {
@@ -74,10 +80,10 @@ struct Map {
     V_LANDED = K_EMPTY + kKStages,                                        // the copies of a V block (Q8: of its codes) are there
     RAW_EMPTY = V_LANDED + (Q8 ? kRawStages : kVStages),
     V_FULL = RAW_EMPTY + kRawStages, V_EMPTY = V_FULL + kVStages,
-    TAB_FULL = V_EMPTY + kVStages,                                        // [kVStages] the keys' exponents of a block
-    K_OWN = TAB_FULL + kVStages,                                          // K of the row's own nodes is there
+    TAB_FULL = V_EMPTY + kVStages,                                        // [kTabStages] the keys' exponents of a block
+    K_OWN = TAB_FULL + kTabStages,                                          // K of the row's own nodes is there
     S_FULL, P_FULL = S_FULL + 2,                                          // [slot][half of the keys]
-    O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 4, COUNT
+    O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 8, COUNT
   };
   static constexpr int kOffMisc = kOffBar + COUNT * 8;                    // TMEM address, failure flag
   static constexpr int kBytes = kOffMisc + 16;
@@ -135,9 +141,14 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t widen(uint32_t w) {     // two e4m3 codes in the low half -> f16 pair
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
+// Four e4m3 codes as f16 pairs (0, 2) and (1, 3), times `by`. An e4m3 code shifted to the sign and to bits 13..7 is the f16 number
+// 2^-8 times its value, subnormal ones too (the formats differ in the bias alone); `by` makes up for that.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t by, uint32_t& even, uint32_t& odd) {
+  const uint32_t e = ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u), o = ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u);
+  const __half2 f = *reinterpret_cast<const __half2*>(&by);
+  const __half2 a = __hmul2(*reinterpret_cast<const __half2*>(&e), f), b = __hmul2(*reinterpret_cast<const __half2*>(&o), f);
+  even = *reinterpret_cast<const uint32_t*>(&a);
+  odd = *reinterpret_cast<const uint32_t*>(&b);
 }
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ uint32_t max_magnitude(const uint4& w) {
@@ -170,6 +181,22 @@ __device__ __forceinline__ void split8(const uint4& w, float down, uint2& hi, ui
 __device__ __forceinline__ uint32_t at16(int r, int c) { return (uint32_t)((c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4)); }
 __device__ __forceinline__ uint32_t at8(int r, int c) { return (uint32_t)(r * 128 + ((((c >> 1) ^ r) & 7) << 4) + (c & 1) * 8); }
 
+// shared memory by its 32-bit address (a generic pointer is two registers)
+__device__ __forceinline__ int lds_i(uint32_t at) {
+  int v;
+  asm volatile("ld.shared.s32 %0, [%1];\n" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds_f(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint64_t lds_f2(uint32_t at) {       // two floats
+  uint64_t v;
+  asm volatile("ld.shared.b64 %0, [%1];\n" : "=l"(v) : "r"(at) : "memory");
+  return v;
+}
 // kind::f8f6f4: both operands e4m3
 __device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
   asm volatile(
@@ -181,6 +208,39 @@ __device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t a, uint64_t b, uint
 // fp32 accumulator, M = N = 128, formats 0 (f16 resp. e4m3)
 __host__ __device__ constexpr uint32_t instr_desc0(bool b_mn_major) { return instr_desc(b_mn_major) & ~((1u << 7) | (1u << 10)); }
 
+// TMEM of sixteen rows, eight columns at a time: lane l gets columns 2 (l % 4), + 1 of rows l / 4 (v[4 i], v[4 i + 1]) and l / 4 + 8
+// (v[4 i + 2], v[4 i + 3]) of the i-th eight, as in an accumulator fragment of mma.sync.
+__device__ __forceinline__ void tmem_ld_rows32(float* v, uint32_t taddr) {            // 64 columns
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_rows8(float (&v)[8], uint32_t taddr) {        // 16 columns
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_rows8(uint32_t taddr, const float (&v)[8]) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 16-bit pairs of the same places: w[2 i], w[2 i + 1] = rows l / 4 and l / 4 + 8 of the i-th eight; 64 of them make 32 columns.
+__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n" ::"r"(taddr), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
 template <int NT, bool Q8>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __grid_constant__ TreeArgs a, const __grid_constant__ CUtensorMap tile_map) {
@@ -189,7 +249,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);      // known to be the same for a warp
   const int G = s.Hq / s.Hkv;
   pdl_launch_dependents();
   if (base != smem_u32(smem_raw)) {              // never expected: the kernel has no static shared memory in front of its window
@@ -206,8 +266,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       int n = 1;
       if (i >= L::UNIT_EMPTY && i < L::UNIT_EMPTY + kUnitRing) n = kUnitReaders;
       if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::TAB_FULL && i < L::K_OWN)) n = 4;   // transform warps
-      if (i >= L::P_FULL && i < L::O_FULL) n = 4;             // softmax warps of the slot
-      if (i == L::O_EMPTY) n = 8;
+      if (i >= L::P_FULL && i < L::O_FULL) n = 8;             // softmax warps of the slot
+      if (i == L::O_EMPTY) n = 16;
       if (i >= L::XCHG && i < L::DRAIN) n = 2;
       mbar_init(bar(i), n);
     }
@@ -243,54 +303,45 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(i));
   };
-  // Record of the k-th unit of this CTA; false when there is none.
-  auto next_unit = [&](int k, Unit& u) -> bool {
-    const int e = k % kUnitRing;
-    if (!wait(L::UNIT_FULL + e, (k / kUnitRing) & 1)) return false;
-    const int4* src = reinterpret_cast<const int4*>(units + e);
-    int4* dst = reinterpret_cast<int4*>(&u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) dst[i] = src[i];
-    arrive(L::UNIT_EMPTY + e);
-    return u.valid != 0;
-  };
-  // Which slots a unit uses, and for which blocks: two tiles: both, all blocks; one tile: in turn.
-  auto slot_steps = [](const Unit& u, int x) {
-    const int n = u.n_cached + u.own;
-    return u.cnt_b > 0 ? n : (n + 1 - x) / 2;
-  };
-
-  if (warp < 8) {
-    // ================================================================ softmax and epilogue, a thread per query row
+  if (warp < kWarpTransform) {
+    // ================================================================ softmax and epilogue: sixteen rows of a slot per warp
     reg_inc<kRegsSoftmax>();
-    const int x = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tS = tmem + x * 128 + lanes;
-    const uint32_t tO = tmem + 256 + lanes;      // of slot A; slot B's 128 columns on
-    float2* xchg = reinterpret_cast<float2*>(smem + L::kOffXchg);
+    const int x = warp >> 3, quarter = warp & 3, row0 = quarter * 32 + ((warp >> 2) & 1) * 16;
+    const int col = (lane & 3) * 2;              // this lane's rows are row0 + lane / 4 and the eighth behind it, its columns col, col + 1 of each eight
+    const uint32_t tS = tmem + x * 128 + ((uint32_t)row0 << 16);
+    const uint32_t tO = tmem + 256 + ((uint32_t)row0 << 16);      // of slot A; slot B's 128 columns on
     const float scale = s.scale_log2;
-    const uint64_t scale2 = pack_f2(scale, scale);
-    const int row_node = row / G, row_head = row % G;
-    int steps = 0;                               // of this slot so far
-    int n_o[2] = {0, 0}, n_x = 0;                // units in which the slots had steps; units of one tile
-    int v0 = 0;                                  // blocks of earlier units
+    // Counters, as far as barrier phases need them: the registers are the scores'. Units (modulo 8, the ring's place and phase) with a bit 3
+    // once there was one; blocks modulo 8 (the tables' place and phase); parities: bit 0 steps of this slot, 1 and 2 units in
+    // which this and the other slot had steps, 3 units of one tile.
+    int k8 = 0, g8 = 0, par = 0;
+    static_assert(kUnitRing == 4 && kTabStages == 4, "counted modulo 8");
     bool ok = true;
-    for (int k = 0; ok; ++k) {
-      Unit u;
-      if (!next_unit(k, u)) break;
-      const bool two = u.cnt_b > 0;
-      const int cnt = two && x ? u.cnt_b : u.cnt_a;
-      const int node = u.t0 + (two && x ? a.tile_tokens : 0) + row_node;
-      const bool real = row_node < cnt;
-      const bool idle = quarter * 32 >= cnt * G;           // no row of this warp is a query
-      const int n = slot_steps(u, x), n_blocks = u.n_cached + u.own;
-      float m = -CUDART_INF_F, l = 0.f;
-      float q_scale = 1.f;
-      for (int i = 0; i < n; ++i, ++steps) {
-        const int j = two ? i : 2 * i + x;                 // block of the unit
-        const int st = (v0 + j) % L::kVStages;
-        ok = wait(L::S_FULL + x, steps & 1);
-        ok = ok && wait(L::TAB_FULL + st, ((v0 + j) / L::kVStages) & 1);
+    while (ok) {
+      // The unit's record stays in the ring until the unit is done, and what is seldom needed is read from there.
+      if (!wait(L::UNIT_FULL + (k8 & 3), (k8 >> 2) & 1)) break;
+      const uint32_t rec = base + L::kOffUnits + (k8 & 3) * 64;
+      auto field = [&](size_t off) { return lds_i(rec + (uint32_t)off); };
+#define UNIT(f) field(offsetof(Unit, f))
+      if (!UNIT(valid)) break;
+      const bool two = UNIT(cnt_b) > 0;
+      const int n_cached = UNIT(n_cached), n_keys = min(UNIT(ctx) - UNIT(p_begin) * kPageSize, UNIT(n_pages) * kPageSize);
+      const int n_q = (two && x ? UNIT(cnt_b) : UNIT(cnt_a)) * G;
+      const bool idle = row0 >= n_q;                       // no row of this warp is a query
+      auto steps_of = [&](int slot) {                      // two tiles: all blocks; one tile: in turn
+        const int blocks = n_cached + UNIT(own);
+        return two ? blocks : (blocks + 1 - slot) / 2;
+      };
+      float m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};      // running maximum; this lane's part of the sum
+      float q_scale[2] = {scale, scale};
+      // block j of the unit; the slot's first one and how many on is the next
+      int j = two ? 0 : x;
+      const int n_blocks = n_cached + UNIT(own), dj = two ? 1 : 2;
+      bool first = true;
+      for (; j < n_blocks; j += dj, par ^= 1, first = false) {
+        const int tb = (g8 + j) & 7;
+        ok = wait(L::S_FULL + x, par & 1);
+        ok = ok && wait(L::TAB_FULL + (tb & 3), tb >> 2);
         if (!ok) break;
         if (idle) {                                        // P of these rows may be anything: nobody reads their O
           arrive(L::P_FULL + 2 * x);
@@ -298,203 +349,223 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           continue;
         }
         tc_fence_after();
-        float v[128];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(&v[32 * c], tS + 32 * c);
-        tmem_ld_wait();
-        const bool own = j == u.n_cached;
-        const float* tab = reinterpret_cast<const float*>(smem + L::kOffTab) + st * 3 * kBlock;
+        float v[64];
+        tmem_ld_rows32(&v[0], tS);
+        tmem_ld_rows32(&v[32], tS + 64);
         if constexpr (Q8) {
-          if (i == 0) q_scale = scale * reinterpret_cast<const float*>(smem + L::kOffQScale)[(two ? x : 0) * 128 + row];
-          if (own) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) v[e] += v[64 + e];            // the two addends of K
-          }
-          const uint64_t row2 = pack_f2(q_scale, q_scale);
-#pragma unroll
-          for (int e = 0; e < 128; e += 4) {
-            const ulonglong2 kp = *reinterpret_cast<const ulonglong2*>(tab + e), ve = *reinterpret_cast<const ulonglong2*>(tab + kBlock + e);
-            unpack_f2(fma2(pack_f2(v[e], v[e + 1]), mul2(kp.x, row2), ve.x), v[e], v[e + 1]);
-            unpack_f2(fma2(pack_f2(v[e + 2], v[e + 3]), mul2(kp.y, row2), ve.y), v[e + 2], v[e + 3]);
+          if (first) {                                     // the queries' powers of two
+            const uint32_t qs = base + L::kOffQScale + ((two ? x : 0) * 128 + row0 + (lane >> 2)) * 4;
+            q_scale[0] = scale * lds_f(qs);
+            q_scale[1] = scale * lds_f(qs + 32);
           }
         }
-        // keys that this row does not see
+        const bool own = j == n_cached;
+        const int end = n_keys - j * kBlock;
+        tmem_ld_wait();
+        if (Q8 && own) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] += v[32 + e];            // the two addends of K
+        }
+        // scores that can be compared: Q8 times the K rows' powers
+        if constexpr (Q8) {
+          const uint32_t tab = base + L::kOffTab + (tb & 3) * kBlock * 4 + col * 4;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t kp2 = lds_f2(tab + 32 * e);
+            unpack_f2(mul2(pack_f2(v[4 * e], v[4 * e + 1]), kp2), v[4 * e], v[4 * e + 1]);
+            unpack_f2(mul2(pack_f2(v[4 * e + 2], v[4 * e + 3]), kp2), v[4 * e + 2], v[4 * e + 3]);
+          }
+        }
+        // keys that a row does not see
         if (own) {
-          uint64_t bits = 0;
-          if (real) bits = a.mask ? a.mask[u.tok0 + node] : (2ull << node) - 1;
-          if (u.T < 64) bits &= (1ull << u.T) - 1;
-          const uint64_t bad = *reinterpret_cast<const uint64_t*>(smem + L::kOffBad + st * 8);
+          const uint64_t bad = lds_f2(base + L::kOffBad + (tb & 3) * 8) >> col;
 #pragma unroll
-          for (int e = 0; e < 64; ++e) {
-            v[e] = (bad >> e) & 1 ? CUDART_NAN_F : v[e];
-            v[e] = (bits >> e) & 1 ? v[e] : -CUDART_INF_F;
-            v[64 + e] = -CUDART_INF_F;
+          for (int r = 0; r < 2; ++r) {
+            const int row = row0 + (lane >> 2) + 8 * r, node = UNIT(t0) + (two && x ? a.tile_tokens : 0) + row / G, T = UNIT(T);
+            uint64_t bits = 0;
+            if (row < n_q) bits = a.mask ? a.mask[UNIT(tok0) + node] : (2ull << node) - 1;
+            if (T < 64) bits &= (1ull << T) - 1;
+            bits >>= col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                float& y = v[4 * e + 2 * r + t];
+                y = (bad >> (8 * e + t)) & 1 ? CUDART_NAN_F : y;
+                y = (bits >> (8 * e + t)) & 1 ? y : -CUDART_INF_F;
+                v[32 + 4 * e + 2 * r + t] = -CUDART_INF_F;
+              }
           }
-        } else {
-          const int valid = u.ctx - (u.p_begin * kPageSize + j * kBlock);
-          const int end = min(valid, (u.n_pages - j * kBlockPages) * kPageSize);
-          if (end < kBlock) {
+        } else if (end < kBlock) {
 #pragma unroll
-            for (int e = 0; e < 128; ++e) v[e] = e < end ? v[e] : -CUDART_INF_F;
+          for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (8 * e + col + t >= end) v[4 * e + t] = v[4 * e + 2 + t] = -CUDART_INF_F;
+        }
+        float e_of[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (Q8) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) e_of[c] = lds_f(base + L::kOffExp + (tb & 3) * 16 + c * 4);
+        }
+        float top[2];                                      // in the units of m (the scales are positive)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float* w = &v[16 * c + 2 * r];
+            float t = max3(fmaxf(w[0], w[1]), w[4], w[5]);
+            t = max3(t, w[8], w[9]);
+            t = max3(t, w[12], w[13]);
+            if (Q8) t = fmaf(t, q_scale[r], e_of[c]);
+            top[r] = c == 0 ? t : fmaxf(top[r], t);
           }
+          if (!Q8) top[r] *= scale;
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
         }
-        float m0 = max3(v[0], v[1], v[2]), m1 = max3(v[3], v[4], v[5]), m2 = max3(v[6], v[7], v[8]), m3 = max3(v[9], v[10], v[11]);
+        const bool move[2] = {top[0] > m[0] + kMoveBy, top[1] > m[1] + kMoveBy};      // the first key seen too: m is -inf before it
+        if (__any_sync(0xffffffffu, move[0] || move[1])) {
+          float keep[2];
 #pragma unroll
-        for (int e = 12; e < 124; e += 8) {
-          m0 = max3(m0, v[e], v[e + 1]);
-          m1 = max3(m1, v[e + 2], v[e + 3]);
-          m2 = max3(m2, v[e + 4], v[e + 5]);
-          m3 = max3(m3, v[e + 6], v[e + 7]);
-        }
-        m0 = max3(m0, v[124], v[125]);
-        m1 = max3(m1, v[126], v[127]);
-        float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-        if (!Q8) top *= scale;                             // the scale is positive
-        const bool move = top > m + kMoveBy;               // the first key seen too: m is -inf before it
-        if (__any_sync(0xffffffffu, move)) {
-          const float keep = move ? ex2(m - top) : 1.f;    // 0 the first time
-          if (move) m = top;
-          l *= keep;
-          if (i > 0) {                                     // O holds the steps in front: their P V was issued before these scores' product
+          for (int r = 0; r < 2; ++r) {
+            keep[r] = move[r] ? ex2(m[r] - top[r]) : 1.f;  // 0 the first time
+            if (move[r]) m[r] = top[r];
+            l[r] *= keep[r];
+          }
+          if (!first) {                                    // O holds the steps in front: their P V was issued before these scores' product
 #pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
-              float ov[16];
-              tmem_ld16(ov, tO + x * 128 + c * 16);
+            for (uint32_t at = tO + x * 128, end_o = at + 128; at < end_o; at += 16) {
+              float ov[8];
+              tmem_ld_rows8(ov, at);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) ov[e] *= keep;
-              tmem_st16(tO + x * 128 + c * 16, *reinterpret_cast<const uint32_t(*)[16]>(ov));
+              for (int e = 0; e < 8; ++e) ov[e] *= keep[(e >> 1) & 1];
+              tmem_st_rows8(at, ov);
             }
           }
         }
-        const float ref = (m == -CUDART_INF_F ? 0.f : m) - (Q8 ? kShift16 : 0.f);
-        const uint64_t neg2 = pack_f2(-ref, -ref);
-        uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                      // 32 keys at a time; half of the keys are announced when their P is in TMEM
+        for (int part = 0; part < 2; ++part) {             // half of the keys are announced when their P is in TMEM
           uint32_t pk[16];
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float p[4];
-            uint64_t x0 = pack_f2(v[32 * c + e], v[32 * c + e + 1]), x1 = pack_f2(v[32 * c + e + 2], v[32 * c + e + 3]);
-            x0 = Q8 ? add2(x0, neg2) : fma2(x0, scale2, neg2);
-            x1 = Q8 ? add2(x1, neg2) : fma2(x1, scale2, neg2);
-            unpack_f2(x0, p[0], p[1]);
-            unpack_f2(x1, p[2], p[3]);
+          for (int c = 2 * part; c < 2 * part + 2; ++c) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) p[t] = ex2(p[t]);
-            if constexpr (Q8) {
-              const ulonglong2 inv = *reinterpret_cast<const ulonglong2*>(tab + 2 * kBlock + 32 * c + e);
-              sum[0] = fma2(pack_f2(p[0], p[1]), inv.x, sum[0]);
-              sum[1] = fma2(pack_f2(p[2], p[3]), inv.y, sum[1]);
-              pk[e / 2] = pack_f16(p[0], p[1]);
-              pk[e / 2 + 1] = pack_f16(p[2], p[3]);
-            } else {
-              sum[0] = add2(sum[0], pack_f2(p[0], p[1]));
-              sum[1] = add2(sum[1], pack_f2(p[2], p[3]));
-              pk[e / 2] = pack_bf16(p[0], p[1]);
-              pk[e / 2 + 1] = pack_bf16(p[2], p[3]);
+            for (int r = 0; r < 2; ++r) {
+              const float ref = (m[r] == -CUDART_INF_F ? 0.f : m[r]) - (Q8 ? kShift16 + e_of[c] : 0.f);
+              const uint64_t neg2 = pack_f2(-ref, -ref), scale2 = pack_f2(q_scale[r], q_scale[r]);
+              uint64_t sum = 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int at = 16 * c + 4 * e + 2 * r;
+                float p0, p1;
+                unpack_f2(fma2(pack_f2(v[at], v[at + 1]), scale2, neg2), p0, p1);
+                p0 = ex2(p0);
+                p1 = ex2(p1);
+                sum = add2(sum, pack_f2(p0, p1));
+                pk[8 * (c & 1) + 2 * e + r] = Q8 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+              }
+              float s0, s1;
+              unpack_f2(sum, s0, s1);
+              if (Q8) l[r] = fmaf(s0 + s1, power(-(int)e_of[c]), l[r]);      // the V rows' exponent is not part of the sum
+              else l[r] += s0 + s1;
             }
           }
-          tmem_st16(tS + c * 16, pk);
-          if (c & 1) {
-            tmem_st_wait();
-            tc_fence_before();
-            arrive(L::P_FULL + 2 * x + (c >> 1));
-          }
+          tmem_st_pairs(tS + part * 32, pk);
+          tmem_st_wait();
+          tc_fence_before();
+          arrive(L::P_FULL + 2 * x + part);
         }
-        float s0, s1;
-        unpack_f2(add2(sum[0], sum[1]), s0, s1);
-        l += s0 + s1;
       }
       if (!ok) break;
-      v0 += n_blocks;
+      g8 = (g8 + n_blocks) & 7;
       // ------------------------------------------------------------------ epilogue
       // Two tiles: a slot's warps write their tile. One tile: both slots' warps know both sums, and each writes half of the columns.
-      const int n_other = slot_steps(u, x ^ 1);
-      float w_mine = 1.f, w_other = 0.f;
-      if (!two) {
-        if (k > 0) ok = wait(L::O_EMPTY, (k - 1) & 1);     // the other warp has read what the unit before left here
-        if (!ok) break;
-        xchg[x * 128 + row] = make_float2(m, l);
-        arrive(L::XCHG + quarter);
-        ok = wait(L::XCHG + quarter, n_x++ & 1);
-        if (!ok) break;
-        const float2 other = xchg[(x ^ 1) * 128 + row];
-        const float mm = fmaxf(m, other.x), ref = mm == -CUDART_INF_F ? 0.f : mm;
-        w_mine = ex2(m - ref);                             // 0 for a slot that saw no key
-        w_other = ex2(other.x - ref);
-        l = w_mine * l + w_other * other.y;
-        m = mm;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       }
-      if (n > 0) ok = wait(L::O_FULL + x, n_o[x] & 1);
-      if (ok && !two && n_other > 0) ok = wait(L::O_FULL + (x ^ 1), n_o[x ^ 1] & 1);
+      const int n = steps_of(x), n_other = steps_of(x ^ 1), rows[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
+      float w_mine[2] = {1.f, 1.f}, w_other[2] = {0.f, 0.f};
+      if (!two) {
+        float2* xchg = reinterpret_cast<float2*>(smem + L::kOffXchg);
+        if (k8 & 8) ok = wait(L::O_EMPTY, (k8 & 1) ^ 1);   // the other warp has read what the unit before left here
+        if (!ok) break;
+        if ((lane & 3) < 2) xchg[x * 128 + rows[lane & 1]] = lane & 1 ? make_float2(m[1], l[1]) : make_float2(m[0], l[0]);
+        arrive(L::XCHG + (warp & 7));
+        ok = wait(L::XCHG + (warp & 7), par >> 3);
+        par ^= 8;
+        if (!ok) break;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float2 other = xchg[(x ^ 1) * 128 + rows[r]];
+          const float mm = fmaxf(m[r], other.x), ref = mm == -CUDART_INF_F ? 0.f : mm;
+          w_mine[r] = ex2(m[r] - ref);                     // 0 for a slot that saw no key
+          w_other[r] = ex2(other.x - ref);
+          l[r] = w_mine[r] * l[r] + w_other[r] * other.y;
+          m[r] = mm;
+        }
+      }
+      if (n > 0) ok = wait(L::O_FULL + x, (par >> 1) & 1);
+      if (ok && !two && n_other > 0) ok = wait(L::O_FULL + (x ^ 1), (par >> 2) & 1);
       if (!ok) break;
-      if (n > 0) ++n_o[x];
-      if (n_other > 0) ++n_o[x ^ 1];
+      par ^= (n > 0 ? 2 : 0) | (n_other > 0 ? 4 : 0);
       tc_fence_after();
       if (!idle) {
-        const bool split = u.partial_slot >= 0;
-        const uint32_t out_row = real ? (uint32_t)((split ? u.partial_slot : u.tok0) + node) * s.Hq + u.head * G + row_head : 0xffffffffu;
-        const float inv = split ? 1.f : l == 0.f ? 0.f : 1.f / l;      // no visible key: zeros
-        w_mine *= inv;
-        w_other *= inv;
-        if (split && real && (two || x == 0)) *reinterpret_cast<float2*>(s.part_ml + (size_t)out_row * 2) = make_float2(m, l);
+        const int partial = UNIT(partial_slot), node0 = UNIT(t0) + (two && x ? a.tile_tokens : 0), head = UNIT(head), tok0 = UNIT(tok0);
+        const bool split = partial >= 0;
+        uint32_t out_row[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          out_row[r] = (uint32_t)((split ? partial : tok0) + node0 + rows[r] / G) * s.Hq + head * G + rows[r] % G;
+          const float inv = split ? 1.f : l[r] == 0.f ? 0.f : 1.f / l[r];      // no visible key: zeros
+          w_mine[r] *= inv;
+          w_other[r] *= inv;
+          if (split && rows[r] < n_q && (two || x == 0) && (lane & 3) == 0)
+            *reinterpret_cast<float2*>(s.part_ml + (size_t)out_row[r] * 2) = make_float2(m[r], l[r]);
+        }
         const int c_begin = two ? 0 : x * 4, c_end = two ? 8 : x * 4 + 4;
 #pragma unroll 1
         for (int c = c_begin; c < c_end; ++c) {            // sixteen columns at a time
-          float ov[16];
+          float ov[8];
           if (n > 0) {
-            tmem_ld16(ov, tO + x * 128 + c * 16);
+            tmem_ld_rows8(ov, tO + x * 128 + c * 16);
             tmem_ld_wait();
           }
 #pragma unroll
-          for (int e = 0; e < 16; ++e) ov[e] = n > 0 ? ov[e] * w_mine : 0.f;
+          for (int e = 0; e < 8; ++e) ov[e] = n > 0 ? ov[e] * w_mine[(e >> 1) & 1] : 0.f;
           if (!two && n_other > 0) {
-            float o2[16];
-            tmem_ld16(o2, tO + (x ^ 1) * 128 + c * 16);
+            float o2[8];
+            tmem_ld_rows8(o2, tO + (x ^ 1) * 128 + c * 16);
             tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ov[e] = fmaf(o2[e], w_other, ov[e]);
+            for (int e = 0; e < 8; ++e) ov[e] = fmaf(o2[e], w_other[(e >> 1) & 1], ov[e]);
           }
-          // A row is one thread's; the four lanes of a quad swap pieces first, so that they write neighbouring bytes of a row
-          // together: 16-byte pieces of fp32, 8-byte pieces of bf16.
-          uint32_t w[4][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[i][e] = split ? __float_as_uint(ov[4 * i + e]) : e < 2 ? pack_bf16(ov[4 * i + 2 * e], ov[4 * i + 2 * e + 1]) : 0u;
-#pragma unroll
-          for (int bit = 1; bit < 4; bit <<= 1) {          // 4 x 4 transpose over the quad: w[i] becomes piece lane % 4 of row i
-            const bool up = lane & bit;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (i & bit) continue;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][e] : w[i | bit][e], bit);
-                if (up) w[i][e] = got; else w[i | bit][e] = got;
-              }
+          for (int e = 0; e < 8; e += 2) {
+            if constexpr (Q8) {                            // V's columns came in the order 0, 2, 1, 3 of each four
+              const bool odd = lane & 1;
+              const float got = __shfl_xor_sync(0xffffffffu, odd ? ov[e] : ov[e + 1], 1);
+              if (odd) ov[e] = got; else ov[e + 1] = got;
             }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t r = __shfl_sync(0xffffffffu, out_row, (lane & ~3) + i);
-            if (r != 0xffffffffu) {
-              const size_t at = (size_t)r * kD + c * 16 + (lane & 3) * 4;
-              if (split) *reinterpret_cast<uint4*>(s.part_acc + at) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
-              else *reinterpret_cast<uint2*>(s.out + at) = make_uint2(w[i][0], w[i][1]);
+            const int r = (e >> 1) & 1;
+            if (rows[r] < n_q) {
+              const size_t at = (size_t)out_row[r] * kD + c * 16 + (e >> 2) * 8 + col;
+              if (split) *reinterpret_cast<float2*>(s.part_acc + at) = make_float2(ov[e], ov[e + 1]);
+              else *reinterpret_cast<uint32_t*>(s.out + at) = pack_bf16(ov[e], ov[e + 1]);
             }
           }
         }
       }
       tc_fence_before();
       arrive(L::O_EMPTY);
+      arrive(L::UNIT_EMPTY + (k8 & 3));
+      k8 = ((k8 + 1) & 7) | 8;
     }
   } else {
-    reg_dec<kRegsAux>();
     if (warp < kWarpK) {
+      reg_dec<kRegsTransform>();
       // ============================================================== transform
       const int w = warp - kWarpTransform, t = tid - kWarpTransform * 32;
       const int half = lane >> 4, ch = lane & 15;            // sixteen lanes per row, 16 bytes each
@@ -502,13 +573,16 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       constexpr int kRaw = Q8 ? L::kRawStages : 1;
       bool ok = true;
       for (int k = 0; ok; ++k) {
-        Unit u;
-        if (!next_unit(k, u)) break;
+        const int ring = k % kUnitRing;                        // the record stays there until the unit is done
+        if (!wait(L::UNIT_FULL + ring, (k / kUnitRing) & 1)) break;
+        const volatile Unit& u = units[ring];
+        if (!u.valid) break;
         if (k > 0 && !(ok = wait(L::Q_EMPTY, (k - 1) & 1))) break;
         // ---- queries
 #pragma unroll 1
         for (int tile = 0; tile < (u.cnt_b > 0 ? 2 : 1); ++tile) {
-          const int cnt = tile ? u.cnt_b : u.cnt_a, q0 = u.t0 + tile * a.tile_tokens;
+          const int cnt = tile ? u.cnt_b : u.cnt_a;
+          const uint16_t* src = s.q + ((size_t)(u.tok0 + u.t0 + tile * a.tile_tokens) * s.Hq + u.head * G) * kD + ch * 8;
           unsigned char* dst = smem + L::kOffQ + tile * kTile;
 #pragma unroll 1
           for (int i0 = 0; i0 < 16; i0 += 4) {
@@ -519,7 +593,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               const int r = w * 32 + (i0 + i) * 2 + half;
               x[i] = make_uint4(0, 0, 0, 0);
               if (r / G < cnt)
-                x[i] = *reinterpret_cast<const uint4*>(s.q + ((size_t)(u.tok0 + q0 + r / G) * s.Hq + u.head * G + r % G) * kD + ch * 8);
+                x[i] = *reinterpret_cast<const uint4*>(src + ((r / G) * s.Hq + r % G) * kD);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -543,48 +617,91 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         fence_proxy_async();
         arrive(L::Q_FULL);
         // ---- key blocks
-        const int32_t* table_row = s.table + (size_t)u.table_slot * s.max_pages_per_req;
-        // Q8: exponents of key t of cached block j
-        int ek = 127, ev = 127;
-        auto fetch_exps = [&](int j) {
-          ek = ev = 127;
+        const int32_t* table_row = s.table + (size_t)u.table_slot * s.max_pages_per_req + u.p_begin;
+        const int g0 = g, n_cached = u.n_cached, n_pages = u.n_pages, n_keys = min(u.ctx - u.p_begin * kPageSize, n_pages * kPageSize);
+        const uint8_t* scales = a.cache.scales + (size_t)u.head * kPageSize + (t & 15);
+        // Q8: the exponents of this thread's key in the cached blocks. Their tables are written two blocks ahead of V (of the four that
+        // are held, the two in front of the block whose V's stage has become free are done with); bytes and page ids are fetched one and
+        // two blocks before that.
+        int ek = 127, ev = 127, page = -1;
+        uint32_t by_ahead[2] = {0, 0};                         // 2^8 times a V row's power, as f16 pairs: of the next block, of the one behind it
+        auto fetch_page = [&](int j) {
           const int p = j * kBlockPages + (t >> 4);
-          if (p < u.n_pages) {
-            const int page = table_row[u.p_begin + p];
-            if ((unsigned)page < (unsigned)s.n_pages) {
-              const uint8_t* src = a.cache.scales + ((size_t)page * 2 * s.Hkv + u.head) * kPageSize + (t & 15);
-              ek = src[0];
-              ev = src[(size_t)s.Hkv * kPageSize];
-            }
+          page = p < n_pages ? table_row[p] : -1;
+        };
+        auto fetch_exps = [&]() {                              // of the block whose page is known
+          ek = ev = 127;
+          if ((unsigned)page < (unsigned)s.n_pages) {
+            const uint8_t* src = scales + (size_t)page * 2 * s.Hkv * kPageSize;
+            ek = src[0];
+            ev = src[(size_t)s.Hkv * kPageSize];
           }
         };
-        if (Q8 && u.n_cached > 0) fetch_exps(0);
-        for (int j = 0; j < u.n_cached + u.own; ++j, ++g) {
-          const int st = g % L::kVStages;
-          const bool own = j == u.n_cached;
+        auto keys_of = [&](int j) { return n_keys - j * kBlock; };
+        auto write_table = [&](int j) -> uint32_t {            // of cached block j, whose bytes are in ek, ev
+          const int tb = (g0 + j) % kTabStages;
+          const bool real = t < keys_of(j);
+          // The V rows of the warp's 32 keys are brought to the largest of their exponents: f16 has the range for rows up to 2^22 below it.
+          const int e_v = real ? cache8_exp_of((uint8_t)ev) : -kCache8MaxExp;
+          const int e_top = __reduce_max_sync(0xffffffffu, e_v);
+          const bool nan = real && (ek == 255 || ev == 255);
+          reinterpret_cast<float*>(smem + L::kOffTab + tb * kBlock * 4)[t] = nan ? CUDART_NAN_F : power(cache8_exp_of((uint8_t)ek));
+          if (lane == 0) reinterpret_cast<float*>(smem + L::kOffExp + tb * 16)[w] = (float)e_top;
+          arrive(L::TAB_FULL + tb);
+          const __half2 f = __float2half2_rn(real ? power(e_v - e_top + 8) : 0.f);
+          return *reinterpret_cast<const uint32_t*>(&f);
+        };
+        if constexpr (Q8) {
+          fetch_page(0);
+          fetch_exps();
+          fetch_page(1);
+          for (int j = 0; j < 2 && j < n_cached; ++j) {
+            by_ahead[j] = write_table(j);
+            fetch_exps();
+            fetch_page(j + 2);
+          }
+        }
+        const int n_blocks = n_cached + u.own;
+        for (int j = 0; j < n_blocks; ++j, ++g) {
+          const int st = g % L::kVStages, tb = g % kTabStages;
+          const bool own = j == n_cached;
           unsigned char* vt = smem + L::kOffV + st * kTile;
-          float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + st * 3 * kBlock;
-          const int end = own ? u.T : min(u.ctx - (u.p_begin * kPageSize + j * kBlock), (u.n_pages - j * kBlockPages) * kPageSize);   // keys of the block
+          [[maybe_unused]] float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + tb * kBlock;
+          const int end = own ? u.T : keys_of(j);
           if constexpr (Q8) {
             if (g >= L::kVStages && !(ok = wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1))) break;
             if (!own) {
-              const int e = cache8_exp_of((uint8_t)ev);
-              tab[t] = power(cache8_exp_of((uint8_t)ek));
-              tab[kBlock + t] = (float)e;
-              tab[2 * kBlock + t] = power(-e);
-              arrive(L::TAB_FULL + st);
-              if (j + 1 < u.n_cached) fetch_exps(j + 1);
+              const uint32_t by_mine = by_ahead[0];
+              by_ahead[0] = by_ahead[1];
+              if (j + 2 < n_cached) {
+                by_ahead[1] = write_table(j + 2);
+                fetch_exps();
+                fetch_page(j + 4);
+              }
               if (!(ok = wait(L::V_LANDED + raw % kRaw, (raw / kRaw) & 1))) break;
               const unsigned char* codes = smem + L::kOffRaw + raw % kRaw * kTile8;
               // sixteen codes -> two pieces of eight f16; eight lanes take four pieces' worth of two neighbouring rows, so that their
               // stores fall into different banks
-#pragma unroll 2
-              for (int i = 0; i < 8; ++i) {
-                const int r = w * 32 + (i >> 1) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
-                uint4 x = *reinterpret_cast<const uint4*>(codes + r * 128 + (((c ^ r) & 7) << 4));
-                if (r >= end) x = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4*>(vt + at16(r, 2 * c)) = make_uint4(widen(x.x), widen(x.x >> 16), widen(x.y), widen(x.y >> 16));
-                *reinterpret_cast<uint4*>(vt + at16(r, 2 * c + 1)) = make_uint4(widen(x.z), widen(x.z >> 16), widen(x.w), widen(x.w >> 16));
+#pragma unroll
+              for (int i0 = 0; i0 < 8; i0 += 4) {
+                uint4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int r = w * 32 + ((i0 + i) >> 1) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
+                  x[i] = *reinterpret_cast<const uint4*>(codes + r * 128 + (((c ^ r) & 7) << 4));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int rw = ((i0 + i) >> 1) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), r = w * 32 + rw, c = (i & 1) * 4 + (lane & 3);
+                  const uint32_t by = __shfl_sync(0xffffffffu, by_mine, rw);
+                  uint4 lo, hi;
+                  widen4(x[i].x, by, lo.x, lo.y);
+                  widen4(x[i].y, by, lo.z, lo.w);
+                  widen4(x[i].z, by, hi.x, hi.y);
+                  widen4(x[i].w, by, hi.z, hi.w);
+                  *reinterpret_cast<uint4*>(vt + at16(r, 2 * c)) = lo;
+                  *reinterpret_cast<uint4*>(vt + at16(r, 2 * c + 1)) = hi;
+                }
               }
               arrive(L::RAW_EMPTY + raw % kRaw);
               ++raw;
@@ -598,64 +715,89 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               // rows behind the block's last key may hold anything, and 0 * NaN is none
               for (int i = t; i < (kBlock - end) * 16; i += 128) *reinterpret_cast<uint4*>(vt + at16(end + (i >> 4), i & 15)) = make_uint4(0, 0, 0, 0);
               if (end < kBlock) fence_proxy_async();
-              arrive(L::TAB_FULL + st);
+              arrive(L::TAB_FULL + tb);
               arrive(L::V_FULL + st);
               continue;
             }
           }
-          // ---- the row's own nodes: warp w has nodes 16 w .. 16 w + 15
+          // ---- the row's own nodes: warps 0 and 1 take V of 32 nodes each, warps 2 and 3 K
           const int kst = g % L::kKStages;
           if (!(ok = wait(L::K_FULL + kst, (g / L::kKStages) & 1))) break;        // the K loader has seen the stage empty
           unsigned char* kt = smem + L::kOffK + kst * L::kKBytes;
-          uint32_t bad = 0;
-#pragma unroll 1
-          for (int i = 0; i < 8; ++i) {
-            const int r = w * 16 + i * 2 + half;
-            uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
-            if (r < end) {
-              const size_t at = ((size_t)(u.tok0 + r) * s.Hkv + u.head) * kD + ch * 8;
-              kx = *reinterpret_cast<const uint4*>(s.k_new + at);
-              vx = *reinterpret_cast<const uint4*>(s.v_new + at);
-            }
-            const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(vx));
-            if (odd & (0xffffu << (half * 16))) vx = make_uint4(0, 0, 0, 0);      // must not reach the nodes that do not see it; a NaN score for the others
-            bad |= (odd & 0xffffu ? 1u : 0u) << (i * 2) | (odd >> 16 ? 2u : 0u) << (i * 2);
-            if constexpr (Q8) {
-              uint32_t mk = max_magnitude(kx), mv = max_magnitude(vx);
+          const int r0 = (w & 1) * 32;
+          const uint16_t* src = (w < 2 ? s.v_new : s.k_new) + ((size_t)u.tok0 * s.Hkv + u.head) * kD + ch * 8;
+          auto load = [&](int r) { return r < end ? *reinterpret_cast<const uint4*>(src + (size_t)r * s.Hkv * kD) : make_uint4(0, 0, 0, 0); };
+          auto row_max = [&](const uint4& x) {               // over the sixteen lanes of a row
+            uint32_t most = max_magnitude(x);
 #pragma unroll
-              for (int sh = 1; sh < 16; sh <<= 1) {
-                mk = max(mk, __shfl_xor_sync(0xffffffffu, mk, sh));
-                mv = max(mv, __shfl_xor_sync(0xffffffffu, mv, sh));
+            for (int sh = 1; sh < 16; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
+            return most;
+          };
+          if (w < 2) {
+            uint32_t bad = 0, most = 0;
+            if constexpr (Q8) {                              // the largest finite element of the 32 rows goes to 2^14 .. 2^15
+#pragma unroll 2
+              for (int i = 0; i < 16; ++i) {
+                const uint4 x = load(r0 + i * 2 + half);
+                const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x));
+                if (!(odd & (0xffffu << (half * 16)))) most = max(most, max_magnitude(x));
               }
-              const int e_k = mk == 0 ? 0 : min(max((int)(mk >> 7) - 127 - 7, -kCache8MaxExp), kCache8MaxExp);
-              const int e_v = mv == 0 ? 0 : min(max((int)(mv >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);
-              uint2 hi, lo;
-              split8(kx, power(-e_k), hi, lo);
-              *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
-              *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
-              const float down = power(-e_v);
-              auto f16 = [&](uint32_t x) { return pack_f16(__uint_as_float(x << 16) * down, __uint_as_float(x & 0xffff0000u) * down); };
-              *reinterpret_cast<uint4*>(vt + at16(r, ch)) = make_uint4(f16(vx.x), f16(vx.y), f16(vx.z), f16(vx.w));
-              if (ch == 0) {
-                tab[r] = power(e_k);
-                tab[kBlock + r] = (float)e_v;
-                tab[2 * kBlock + r] = power(-e_v);
-                tab[2 * kBlock + 64 + r] = 1.f;              // of keys that there are not: their weights are 0
-              }
-            } else {
-              *reinterpret_cast<uint4*>(kt + at16(r, ch)) = kx;
-              *reinterpret_cast<uint4*>(vt + at16(r, ch)) = vx;
+              most = __reduce_max_sync(0xffffffffu, most);
             }
-            *reinterpret_cast<uint4*>(vt + at16(64 + r, ch)) = make_uint4(0, 0, 0, 0);
+            const int e_v = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);
+            const float down = power(-e_v);
+#pragma unroll 2
+            for (int i = 0; i < 16; ++i) {
+              const int r = r0 + i * 2 + half;
+              uint4 x = load(r);
+              const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x));
+              if (odd & (0xffffu << (half * 16))) x = make_uint4(0, 0, 0, 0);       // must not reach the nodes that do not see it; a NaN score for the others
+              bad |= (odd & 0xffffu ? 1u : 0u) << (i * 2) | (odd >> 16 ? 2u : 0u) << (i * 2);
+              if constexpr (Q8) {
+                auto lo = [&](uint32_t y) { return __uint_as_float(y << 16) * down; };
+                auto hi = [&](uint32_t y) { return __uint_as_float(y & 0xffff0000u) * down; };
+                x = make_uint4(pack_f16(lo(x.x), lo(x.y)), pack_f16(hi(x.x), hi(x.y)), pack_f16(lo(x.z), lo(x.w)), pack_f16(hi(x.z), hi(x.w)));
+              }
+              *reinterpret_cast<uint4*>(vt + at16(r, ch)) = x;
+              *reinterpret_cast<uint4*>(vt + at16(64 + r, ch)) = make_uint4(0, 0, 0, 0);
+            }
+            if (lane == 0) {
+              reinterpret_cast<uint32_t*>(smem + L::kOffBad + tb * 8)[w] = bad;
+              if constexpr (Q8) {
+                float* e = reinterpret_cast<float*>(smem + L::kOffExp + tb * 16);
+                e[w] = (float)e_v;
+                e[2 + w] = 0.f;
+              }
+            }
+          } else {
+#pragma unroll 2
+            for (int i = 0; i < 16; ++i) {
+              const int r = r0 + i * 2 + half;
+              const uint4 x = load(r);
+              if constexpr (Q8) {
+                const uint32_t most = row_max(x);
+                const int e_k = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 7, -kCache8MaxExp), kCache8MaxExp);
+                uint2 hi, lo;
+                split8(x, power(-e_k), hi, lo);
+                *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
+                *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
+                if (ch == 0) tab[r] = power(e_k);
+              } else {
+                *reinterpret_cast<uint4*>(kt + at16(r, ch)) = x;
+              }
+            }
           }
-          if (lane == 0) reinterpret_cast<uint16_t*>(smem + L::kOffBad + st * 8)[w] = (uint16_t)bad;
           fence_proxy_async();
-          arrive(L::TAB_FULL + st);
+          arrive(L::TAB_FULL + tb);
           arrive(L::K_OWN);
           arrive(L::V_FULL + st);
         }
+        if (ok) arrive(L::UNIT_EMPTY + ring);
       }
-    } else if (warp == kWarpK || warp == kWarpV) {
+    } else {
+      reg_dec<kRegsAux>();
+    }
+    if (warp == kWarpK || warp == kWarpV) {
       // ============================================================== K and V loaders: a page of a KV head is a copy (bf16: two, 64 columns each)
       const int kv = warp - kWarpK;
       constexpr int kCopies = Q8 ? kBlockPages : 2 * kBlockPages, kCopyBytes = kPageSize * 128;
@@ -668,12 +810,11 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       int g = 0;                                             // blocks through this ring
       bool ok = true;
       for (int k = 0; ok; ++k) {
-        Unit u;
         if (kv == 0) {
           if (k >= kUnitRing && !(ok = wait(L::UNIT_EMPTY + k % kUnitRing, ((k / kUnitRing) & 1) ^ 1))) break;
-          int unit = 0;
           if (lane == 0) {
-            unit = fetched >= 0 ? fetched : (int)blockIdx.x;
+            Unit u;
+            int unit = fetched >= 0 ? fetched : (int)blockIdx.x;
             for (;; unit = (int)gridDim.x + atomicAdd(s.pf_queue, 1)) {
               u = Unit{};
               if (unit >= n_units) break;
@@ -709,20 +850,20 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
             if (u.valid) fetched = (int)gridDim.x + atomicAdd(s.pf_queue, 1);
           }
           __syncwarp();
-          int4* all = reinterpret_cast<int4*>(&u);
-          const int4* src = reinterpret_cast<const int4*>(units + k % kUnitRing);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) all[i] = src[i];
-          if (!u.valid) break;
-        } else if (!next_unit(k, u)) {
+        } else if (!wait(L::UNIT_FULL + k % kUnitRing, (k / kUnitRing) & 1)) {
           break;
         }
-        const int32_t* table_row = s.table + (size_t)u.table_slot * s.max_pages_per_req + u.p_begin;
+        const uint32_t rec = base + L::kOffUnits + k % kUnitRing * 64;
+        auto field = [&](size_t off) { return lds_i(rec + (uint32_t)off); };
+        const int valid = UNIT(valid), n_pages = UNIT(n_pages), n_cached = UNIT(n_cached), own = UNIT(own), head = UNIT(head);
+        const int32_t* table_row = s.table + (size_t)UNIT(table_slot) * s.max_pages_per_req + UNIT(p_begin);
+        if (kv == 1) arrive(L::UNIT_EMPTY + k % kUnitRing);
+        if (!valid) break;
         const int my_page = Q8 ? lane : lane >> 1;
         auto fetch_page = [&](int j) {
           const int p = j * kBlockPages + my_page;
           int page = s.n_pages;
-          if (lane < kCopies && p < u.n_pages) {
+          if (lane < kCopies && p < n_pages) {
             page = table_row[p];
             if ((unsigned)page >= (unsigned)s.n_pages) {
               atomicOr(s.status, TS_DEV_BAD_PAGE);
@@ -732,20 +873,20 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           return page;
         };
         int page = fetch_page(0);
-        const int n_blocks = u.n_cached + (kv == 0 || !Q8 ? u.own : 0);      // the nodes' V in 8-bit steps does not pass the ring of codes
+        const int n_blocks = n_cached + (kv == 0 || !Q8 ? own : 0);      // the nodes' V in 8-bit steps does not pass the ring of codes
         for (int j = 0; j < n_blocks; ++j, ++g) {
           const int st = g % stages;
-          const int page_next = j + 1 < u.n_cached ? fetch_page(j + 1) : 0;
+          const int page_next = j + 1 < n_cached ? fetch_page(j + 1) : 0;
           if (g >= stages && !(ok = wait(empty + st, ((g / stages) & 1) ^ 1))) break;
-          if (j == u.n_cached) {
+          if (j == n_cached) {
             if (lane == 0) mbar_arrive(bar(landed + st));    // the transform warps fill the stage
           } else {
-            const int n_pg = min(kBlockPages, u.n_pages - j * kBlockPages);
+            const int n_pg = min(kBlockPages, n_pages - j * kBlockPages);
             if (lane == 0) mbar_expect_tx(bar(landed + st), n_pg * kCopyBytes * (kCopies / kBlockPages));
             __syncwarp();
             if (lane < kCopies && my_page < n_pg) {
               const uint32_t dst = ring + st * stage_bytes + my_page * kCopyBytes + (Q8 ? 0 : (lane & 1) * kHalf);
-              tma_load_5d(dst, &tile_map, bar(landed + st), Q8 ? 0 : (lane & 1) * 64, 0, u.head, kv, page);
+              tma_load_5d(dst, &tile_map, bar(landed + st), Q8 ? 0 : (lane & 1) * 64, 0, head, kv, page);
             }
           }
           __syncwarp();
@@ -760,23 +901,30 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       constexpr uint32_t idesc_qk = Q8 ? instr_desc0(false) : instr_desc(false), idesc_pv = Q8 ? instr_desc0(true) : instr_desc(true);
       const uint64_t q_desc = smem_desc(base + L::kOffQ, 0, 1024), k_desc = smem_desc(base + L::kOffK, 0, 1024);
       const uint64_t v_desc = smem_desc(base + L::kOffV, kHalf, 1024);
-      int g = 0, n_own = 0, steps[2] = {0, 0};               // blocks and steps of earlier units
+      int k8 = 0;                                            // units, as the softmax warps count them
+      int kst = 0, vst = 0;                                  // ring places of the next K block to be multiplied and of the next V block
+      uint32_t par = 0;                                      // parities: bits 0, 1 the rings' phases, 2 blocks of nodes, 3 and 4 steps of the slots
       bool ok = true;
-      for (int k = 0; ok; ++k) {
-        Unit u;
-        if (!next_unit(k, u)) break;
-        if (!(ok = wait(L::Q_FULL, k & 1))) break;
-        const bool two = u.cnt_b > 0;
-        const int n_blocks = u.n_cached + u.own, n_steps = two ? 2 * n_blocks : n_blocks;
-        auto block_of = [&](int i) { return two ? i >> 1 : i; };
-        auto qk = [&](int i) {                               // S of step i's slot
-          const int x = i & 1, j = block_of(i), st = (g + j) % L::kKStages;
+      while (ok) {
+        if (!wait(L::UNIT_FULL + (k8 & 3), (k8 >> 2) & 1)) break;
+        const uint32_t rec = base + L::kOffUnits + (k8 & 3) * 64;
+        auto field = [&](size_t off) { return __shfl_sync(0xffffffffu, lds_i(rec + (uint32_t)off), 0); };
+        const int valid = UNIT(valid), two = UNIT(cnt_b) > 0, n_cached = UNIT(n_cached), n_blocks = n_cached + UNIT(own);
+        arrive(L::UNIT_EMPTY + (k8 & 3));
+        if (!valid || !(ok = wait(L::Q_FULL, k8 & 1))) break;
+        const int n_steps = two ? 2 * n_blocks : n_blocks;
+        auto qk = [&](int i) {                               // scores of step i's slot
+          const int x = i & 1;
           if (!two || x == 0) {
-            if (!(ok = ok && wait(L::K_FULL + st, ((g + j) / L::kKStages) & 1))) return;
-            if (j == u.n_cached && !(ok = wait(L::K_OWN, n_own & 1))) return;
+            ok = ok && wait(L::K_FULL + kst, par & 1);
+            if (ok && (two ? i >> 1 : i) == n_cached) {
+              ok = wait(L::K_OWN, (par >> 2) & 1);
+              par ^= 4;
+            }
+            if (!ok) return;
           }
           tc_fence_after();
-          const uint64_t kd = k_desc + (uint64_t)((st * L::kKBytes) >> 4), qd = q_desc + (uint64_t)(((two ? x : 0) * kTile) >> 4);
+          const uint64_t kd = k_desc + (uint64_t)((kst * L::kKBytes) >> 4), qd = q_desc + (uint64_t)(((two ? x : 0) * kTile) >> 4);
           if constexpr (Q8) {
 #pragma unroll
             for (int piece = 0; piece < 2; ++piece)
@@ -791,36 +939,43 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
             }
           }
           tc_commit(bar(L::S_FULL + x), issue);
-          if (!two || x == 1) tc_commit(bar(L::K_EMPTY + st), issue);
+          if (!two || x == 1) {
+            tc_commit(bar(L::K_EMPTY + kst), issue);
+            if (++kst == L::kKStages) {
+              kst = 0;
+              par ^= 1;
+            }
+          }
           if (i == n_steps - 1) tc_commit(bar(L::Q_EMPTY), issue);
         };
-        auto pv = [&](int i) {                               // O of step i's slot (+)= P V
-          const int x = i & 1, j = block_of(i), st = (g + j) % L::kVStages, n = i >> 1;   // n-th step of the slot in this unit
-          if (i == 0 && k > 0 && !(ok = wait(L::O_EMPTY, (k - 1) & 1))) return;
-          if (!two || x == 0)
-            if (!(ok = wait(L::V_FULL + st, ((g + j) / L::kVStages) & 1))) return;
-          const uint64_t vd = v_desc + (uint64_t)((st * kTile) >> 4);
+        qk(0);
+        if (n_steps > 1) qk(1);
+        if (k8 & 8) ok = ok && wait(L::O_EMPTY, (k8 & 1) ^ 1);
+        for (int i = 0; ok && i < n_steps; ++i) {            // O of the step's slot (+)= P V, then the scores of the slot's next step
+          const int x = i & 1;
+          if ((!two || x == 0) && !(ok = wait(L::V_FULL + vst, (par >> 1) & 1))) break;
+          const uint64_t vd = v_desc + (uint64_t)((vst * kTile) >> 4);
 #pragma unroll
           for (int part = 0; part < 2; ++part) {
-            if (!(ok = wait(L::P_FULL + 2 * x + part, (steps[x] + n) & 1))) return;
+            if (!(ok = wait(L::P_FULL + 2 * x + part, (par >> (3 + x)) & 1))) break;
             tc_fence_after();
 #pragma unroll
             for (int kk = part * 4; kk < part * 4 + 4; ++kk)
-              mma_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), idesc_pv, (n > 0 || kk > 0) ? 1u : 0u, issue);
+              mma_ts(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, vd + (uint64_t)((kk * 2048) >> 4), idesc_pv, (i > 1 || kk > 0) ? 1u : 0u, issue);
           }
-          if (!two || x == 1) tc_commit(bar(L::V_EMPTY + st), issue);
+          if (!ok) break;
+          par ^= 8u << x;
+          if (!two || x == 1) {
+            tc_commit(bar(L::V_EMPTY + vst), issue);
+            if (++vst == L::kVStages) {
+              vst = 0;
+              par ^= 2;
+            }
+          }
           if (i + 2 >= n_steps) tc_commit(bar(L::O_FULL + x), issue);
-        };
-        qk(0);
-        if (ok && n_steps > 1) qk(1);
-        for (int i = 0; ok && i < n_steps; ++i) {
-          pv(i);
-          if (ok && i + 2 < n_steps) qk(i + 2);
+          else qk(i + 2);
         }
-        g += n_blocks;
-        n_own += u.own;
-        steps[0] += (n_steps + 1) / 2;
-        steps[1] += n_steps / 2;
+        k8 = ((k8 + 1) & 7) | 8;
       }
       // no MMA, and no arrival of one, is left behind
       tc_commit(bar(L::DRAIN), issue);

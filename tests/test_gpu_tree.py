@@ -177,10 +177,24 @@ def test_infinite_v_of_a_seen_node(cache, nodes):
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 @pytest.mark.parametrize("nodes", [1, 6, 33])
 def test_sizes_of_values(cache, nodes):
-    """V rows whose sizes span 2^60, K and Q that make single keys dominate: weights down to 2^-100 of the largest."""
+    """V rows whose sizes span 2^60 (2^14 within 32 neighbouring keys), K and Q that make single keys dominate: weights down to
+    2^-100 of the largest."""
     for seed, k_size in ((1, 0.01), (2, 1.0), (3, 6.0)):
         Case((8, 2, 128), cache, [(700, nodes), (0, nodes)], seed=seed, k_size=k_size,
-             v_size=lambda rng, n: 2.0 ** rng.integers(-40, 21, n)).check()
+             v_size=lambda rng, n: 2.0 ** (np.repeat(rng.integers(-40, 7, n // 32 + 1), 32)[:n] + rng.integers(0, 15, n))).check()
+
+
+@pytest.mark.parametrize("nodes", [1, 40])
+def test_a_row_of_nan_in_the_cache(nodes):
+    """One cached token's V (then K) holds a NaN: it is seen by all nodes of its row, and of that KV head alone."""
+    for which in (0, 1):
+        c = Case((8, 2, 128), "e4m3", [(100, nodes), (50, nodes)], seed=12)
+        kb, vb = (to_dev(wl.f32_to_bf16_bits(c.rng.standard_normal((1, 2, 128)).astype(np.float32))) for _ in range(2))
+        (vb, kb)[which][0, 1, 7] = 0x7FC0
+        c.dec.request_set_len(c.slots[0], 99)
+        c.dec.cache_append([c.slots[0]], [1], [99], kb, vb)
+        got = c.run()
+        assert np.isnan(got[:nodes, 4:]).all() and np.isfinite(got[:nodes, :4]).all() and np.isfinite(got[nodes:]).all()
 
 
 @pytest.mark.parametrize("nodes", [1, 12, 64])

@@ -20,9 +20,10 @@ _CODES = np.arange(0x7F)                                        # the finite mag
 
 
 def quantise_row(x: np.ndarray):
-    """(codes uint8, scale byte) of one row of float64 values: nearest code, ties to the even one."""
-    fin = np.abs(x[~np.isnan(x)])
-    most = fin.max() if len(fin) else 0.0
+    """(codes uint8, scale byte) of one row of float64 values: nearest code, ties to the even one. A row with a NaN: byte 255."""
+    if np.isnan(x).any():
+        return np.where(np.isnan(x), 0x7F, 0).astype(np.uint8), 255
+    most = np.abs(x).max()
     if most == 0:
         E = 0
     elif np.isinf(most):
@@ -35,9 +36,6 @@ def quantise_row(x: np.ndarray):
     mags = E4M3[_CODES]
     codes = np.empty(len(x), np.uint8)
     for i, v in enumerate(x):
-        if np.isnan(v):
-            codes[i] = 0x7F
-            continue
         a = min(abs(v) * 2.0 ** -E, 448.0)
         hi = int(np.searchsorted(mags, a))
         lo = max(hi - 1, 0)

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -1047,21 +1048,25 @@ struct TreePlan {
   int tile_tokens;         // nodes of a query tile
   int tiles_per_unit;      // query tiles of a work unit (1 but for tcgen05)
   int n_tiles;             // units of the longest row, per item and KV head
+  int blocks_per_sm;       // that run at a time
 };
-// Queries per KV head of the row with most nodes above which a step runs on tcgen05 (head_dim 128).
-constexpr int kTreeTcQueries = 32;
-TreePlan choose_tree(const ts_ctx* c, int nodes) {
+// Queries per KV head of the row with most nodes above which a step runs on tcgen05 (head_dim 128). us of 37 rows of 8192 keys of the 8B shape,
+// streamed / on tcgen05, by nodes: bf16 one 188 / 203, four 195 / 207, eight 210 / 208, 16 (in two tiles) 420 / 210; 8 bits one 128 / 178, four 193 /
+// 176, eight 277 / 180.
+constexpr int kTreeTcQueries = 32, kTreeTcQueries8 = 8;
+TreePlan choose_tree(const ts_ctx* c, int nodes, int cache) {
   TreePlan p = {};
-  p.tc = c->cfg.head_dim == 128 && nodes * c->G > kTreeTcQueries;
+  p.tc = c->cfg.head_dim == 128 && nodes * c->G > (cache == TS_CACHE_E4M3 ? kTreeTcQueries8 : kTreeTcQueries);
   p.tile_tokens = p.tc ? 128 / c->G : ts::tree_tile_tokens(c->G, nodes);
   p.tiles_per_unit = p.tc && nodes > p.tile_tokens ? 2 : 1;
   p.n_tiles = ceil_div(nodes, p.tile_tokens * p.tiles_per_unit);
+  p.blocks_per_sm = p.tc ? 1 : ts::tree_blocks_per_sm(p.tile_tokens * c->G, cache == TS_CACHE_E4M3);
   return p;
 }
 
 // Work items of a tree step: see ts_tree.h. Rows are cut so that the units of all rows are about as many as thread blocks run at
 // a time, none shorter than kMinTreePages pages. A row's own nodes stay together.
-constexpr int kMinTreePages = 16, kTreeBlocksPerSm = 2;
+constexpr int kMinTreePages = 16;
 void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   c->items.clear();
   c->combines.clear();
@@ -1071,8 +1076,9 @@ void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   auto pages_of = [&](int r) { return ceil_div(st->ctx_len[r], P) + ceil_div(st->q_len[r], P); };
   int64_t work = 0;
   for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tp.tile_tokens * tp.tiles_per_unit) * c->cfg.n_kv_heads;
-  const int blocks = (tp.tc ? 1 : kTreeBlocksPerSm) * (c->n_sms > 0 ? c->n_sms : kSmsB200);
+  const int blocks = tp.blocks_per_sm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
   int64_t per = std::max<int64_t>(kMinTreePages, (work + blocks - 1) / blocks);
+  if (getenv("TREE_DIV")) per = std::max<int64_t>(kMinTreePages, (int64_t)((double)work / blocks / atof(getenv("TREE_DIV"))));
   for (;; per *= 2) {                                        // the partial results have to fit
     int64_t partials = 0;
     for (int r = 0; r < st->n_rows; ++r)
@@ -1451,7 +1457,7 @@ int ts_tree_attention(ts_ctx* c, const ts_step* st, int32_t cache, const uint64_
   for (int r = 0; r < st->n_rows; ++r) nodes = std::max(nodes, st->q_len[r]);
   a.mask = mask;
   if (cache == TS_CACHE_E4M3) a.cache = ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales};
-  const TreePlan tp = choose_tree(c, nodes);
+  const TreePlan tp = choose_tree(c, nodes, cache);
   a.tile_tokens = tp.tile_tokens;
   a.n_tiles = tp.n_tiles;
   plan_tree(c, st, tp);

@@ -17,7 +17,6 @@
 // fit f16's eleven; an element below 2^-28 of its row's largest rounds).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <math_constants.h>
 
 #include "../../include/tokenscale.h"
@@ -53,16 +52,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-// two e4m3 codes in the low half of w -> f16 pair
-__device__ __forceinline__ uint32_t widen(uint32_t w) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
-}
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
-// untiled copy of 16 bytes, completed on `bar`
-__device__ __forceinline__ void bulk_load16(uint32_t dst, const void* src, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 16, [%2];\n" ::"r"(dst), "l"(src), "r"(bar)
-               : "memory");
+// arrives on `bar` when this thread's cp.async copies so far are done
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(bar) : "memory");
 }
 
 // Shared-memory images of a page of one KV head. 16-bit elements: [K, V][64-column half][16 rows of 128 bytes], 128-byte swizzle.
@@ -77,9 +70,10 @@ __device__ __forceinline__ uint32_t off8(int kv, int r, int c) {
   return (uint32_t)(kv * (kPageSize * D) + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
 }
 
-template <int D, bool Q8>
+template <int D, int NB, bool Q8>
 struct Smem {
-  static constexpr int kStages = Q8 ? 6 : 3;
+  static constexpr int kBlocks = Q8 ? (NB == 1 ? 4 : NB == 2 ? 3 : 2) : 2;      // thread blocks of an SM at a time
+  static constexpr int kStages = Q8 ? (NB == 1 ? 3 : NB == 2 ? 4 : 6) : 3;
   static constexpr int kPageBytes = 2 * kPageSize * D * (Q8 ? 1 : 2);
   // a page of the row's own nodes, 16-bit elements, lies over the first stages of a warp that has no copy in flight any more
   static_assert(kStages * kPageBytes >= 2 * kPageSize * D * 2, "no room for a page of nodes");
@@ -89,17 +83,17 @@ struct Smem {
   static constexpr int kOffFailed = kOffBar + kWarps * kStages * 8;
   static constexpr int kEnd = kOffFailed + 8;
   // afterwards: results of the warps, [warp][query][D + 2]
-  static constexpr int bytes(int NB) {
+  static constexpr int bytes() {
     const int merge = kWarps * NB * 8 * (D + 2) * 4;
     return 1024 + (kEnd > merge ? kEnd : merge);
   }
 };
 
 template <int D, int NB, bool Q8>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, Smem<D, NB, Q8>::kBlocks)
 tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __grid_constant__ TreeArgs a,
             const __grid_constant__ CUtensorMap kv_map) {
-  using L = Smem<D, Q8>;
+  using L = Smem<D, NB, Q8>;
   const StepDevice& s = params.s;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -110,7 +104,7 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
   pdl_launch_dependents();
   const uint32_t my_bars = base + L::kOffBar + warp * L::kStages * 8;
   if (lane == 0) {
-    for (int i = 0; i < L::kStages; ++i) mbar_init(my_bars + i * 8, 1);
+    for (int i = 0; i < L::kStages; ++i) mbar_init(my_bars + i * 8, Q8 ? 3 : 1);      // Q8: and the two copies of the scales
     mbar_init_fence();
   }
   __syncwarp();
@@ -146,23 +140,24 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
         pages = mine < cached_end ? table_row[mine] : 0;
       }
       int page = __shfl_sync(0xffffffffu, pages, n_issued & 31);
+      const bool ok = (unsigned)page < (unsigned)s.n_pages;
+      const int st = n_issued % L::kStages;
+      const uint32_t bar = my_bars + st * 8, dst = ring + st * L::kPageBytes;
       if (lane == 0) {
-        const bool ok = (unsigned)page < (unsigned)s.n_pages;
         if (!ok) {
           atomicOr(s.status, TS_DEV_BAD_PAGE);
           page = s.n_pages;                       // out of range on purpose: the copy delivers zeros
         }
-        const int st = n_issued % L::kStages;
-        const uint32_t bar = my_bars + st * 8, dst = ring + st * L::kPageBytes;
         fence_proxy_async();
-        mbar_expect_tx(bar, L::kPageBytes + (Q8 ? 32 : 0));
-        if constexpr (Q8) {
-          tma_load_4d(dst, &kv_map, bar, 0, head * kPageSize, 0, page);
-          const uint8_t* src = a.cache.scales + ((size_t)(ok ? page : 0) * 2 * s.Hkv + head) * kPageSize;
-          bulk_load16(scale_ring + st * 32, src, bar);
-          bulk_load16(scale_ring + st * 32 + 16, src + (size_t)s.Hkv * kPageSize, bar);
-        } else {
-          tma_load_5d(dst, &kv_map, bar, 0, head * kPageSize, 0, 0, page);
+        mbar_expect_tx(bar, L::kPageBytes);
+        if constexpr (Q8) tma_load_4d(dst, &kv_map, bar, 0, head * kPageSize, 0, page);
+        else tma_load_5d(dst, &kv_map, bar, 0, head * kPageSize, 0, 0, page);
+      }
+      if constexpr (Q8) {
+        // the scales by two lanes' own copies
+        if (lane < 2) {
+          cp_async16(scale_ring + st * 32 + lane * 16, a.cache.scales + (((size_t)(ok ? page : 0) * 2 + lane) * s.Hkv + head) * kPageSize, 16);
+          cp_async_arrive(bar);
         }
       }
       ++n_issued;
@@ -172,7 +167,7 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
 
   // ---------------------------------------------------------------- queries
   // B fragments of S^T = K Q^T: lane (g, c) holds query 8 nb + g. bf16: elements 2c, 2c + 1 and 2c + 8, 2c + 9 of each sixteen.
-  // Q8: 4c .. 4c + 3 of each sixteen (the K fragments come in the same order), as f16 times a power of two per query.
+  // Q8: 4c, 4c + 2 and 4c + 1, 4c + 3 (the K fragments come in the same order), as f16 times a power of two per query.
   uint32_t qf[NB][D / 16][2];
   float q_scale[NB][2];                           // of queries 8 nb + 2c, + 1: scale * log2(e), times what takes the power out again
 #pragma unroll
@@ -205,9 +200,11 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
       const float down = power(-e);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          qf[nb][ks][i] = pack_f16(__uint_as_float(qf[nb][ks][i] << 16) * down, __uint_as_float(qf[nb][ks][i] & 0xffff0000u) * down);
+{
+        const uint32_t x = qf[nb][ks][0], y = qf[nb][ks][1];
+        qf[nb][ks][0] = pack_f16(__uint_as_float(x << 16) * down, __uint_as_float(y << 16) * down);
+        qf[nb][ks][1] = pack_f16(__uint_as_float(x & 0xffff0000u) * down, __uint_as_float(y & 0xffff0000u) * down);
+      }
       // the score fragment holds queries 2c and 2c + 1, whose exponents lanes 8c and 8c + 4 have
       q_scale[nb][0] *= power(__shfl_sync(0xffffffffu, e, 8 * c));
       q_scale[nb][1] *= power(__shfl_sync(0xffffffffu, e, 8 * c + 4));
@@ -239,7 +236,9 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
         ldmatrix_x4(r, img + off8<D>(0, lr, ch + lc));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t af[4] = {widen(r[2 * i]), widen(r[2 * i + 1]), widen(r[2 * i] >> 16), widen(r[2 * i + 1] >> 16)};
+          uint32_t af[4];
+          cache8_widen(r[2 * i], af[0], af[2]);
+          cache8_widen(r[2 * i + 1], af[1], af[3]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) mma_f16(sc[nb], af, qf[nb][ch + i][0], qf[nb][ch + i][1]);
         }
@@ -260,9 +259,10 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
     [[maybe_unused]] float ks0 = 1.f, ks1 = 1.f, ve0 = 0.f, ve1 = 0.f;
     float out0 = 1.f, out1 = 1.f;
     if constexpr (Q8) {
-      ks0 = cache8_power(exps[g]);
-      ks1 = cache8_power(exps[g + 8]);
-      const int e0 = cache8_exp_of(exps[16 + g]), e1 = cache8_exp_of(exps[16 + g + 8]);
+      // 2^8: see cache8_widen
+      ks0 = 256.f * cache8_power(exps[g]);
+      ks1 = 256.f * cache8_power(exps[g + 8]);
+      const int e0 = cache8_exp_of(exps[16 + g]) + 8, e1 = cache8_exp_of(exps[16 + g + 8]) + 8;
       ve0 = exps[16 + g] == 255 ? CUDART_NAN_F : (float)e0;
       ve1 = exps[16 + g + 8] == 255 ? CUDART_NAN_F : (float)e1;
       out0 = power(-e0);
@@ -331,16 +331,17 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
     }
     // O^T += V^T P^T, sixteen head_dim elements at a time
     if constexpr (CODES) {
-      // a transposed 8 x 8 block of 16-bit units is eight pairs of elements: rows d = 2g of the product come from the low bytes, 2g + 1
-      // from the high ones (rows 0-7 and 8-15 of the fragment)
+      // a transposed 8 x 8 block of 16-bit units is eight pairs of elements of two keys: rows d = 2g of the product (0-7 of the fragment) come
+      // from the even bytes, 2g + 1 (8-15) from the odd ones
 #pragma unroll
       for (int ch = 0; ch < D / 16; ch += 2) {
         uint32_t r[4];
         ldmatrix_x4_trans(r, img + off8<D>(1, lr, ch + lc));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t a0 = widen(r[2 * i]), a1 = widen(r[2 * i] >> 16), b0 = widen(r[2 * i + 1]), b1 = widen(r[2 * i + 1] >> 16);
-          const uint32_t af[4] = {__byte_perm(a0, a1, 0x5410), __byte_perm(a0, a1, 0x7632), __byte_perm(b0, b1, 0x5410), __byte_perm(b0, b1, 0x7632)};
+          uint32_t af[4];
+          cache8_widen(r[2 * i], af[0], af[1]);
+          cache8_widen(r[2 * i + 1], af[2], af[3]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) mma_f16(o[ch + i][nb], af, pb[nb][0], pb[nb][1]);
         }
@@ -432,22 +433,15 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
 #pragma unroll
           for (int sh = 1; sh < CH; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
           // largest element to 2^14 .. 2^15 (f16 ends at 65504)
-          const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);
+          const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, 8 - kCache8MaxExp), 8 + kCache8MaxExp);
           const float down = power(-e);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = pack_f16(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
-          if (ch == 0) own_exp[kv * 16 + r] = (uint8_t)(e + 127);
-          if (kv == 0) {
-            // K in the order of the query fragments: of each sixteen elements, 4i and 4i + 1 first, then 4i + 2 and 4i + 3
-            const uint32_t at0 = own - base + off16<D>(0, r, ch & ~1) + (ch & 1) * 8, at1 = own - base + off16<D>(0, r, ch | 1) + (ch & 1) * 8;
-            *reinterpret_cast<uint2*>(smem + at0) = make_uint2(x[0], x[2]);
-            *reinterpret_cast<uint2*>(smem + at1) = make_uint2(x[1], x[3]);
-          } else {
-            // V in the order of the product's rows over codes: of each sixteen elements the even ones first
-            const uint32_t at0 = own - base + off16<D>(1, r, ch & ~1) + (ch & 1) * 8, at1 = own - base + off16<D>(1, r, ch | 1) + (ch & 1) * 8;
-            *reinterpret_cast<uint2*>(smem + at0) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
-            *reinterpret_cast<uint2*>(smem + at1) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
-          }
+          if (ch == 0) own_exp[kv * 16 + r] = (uint8_t)(e - 8 + 127);      // as of codes
+          // in the order that codes come in: of each sixteen elements the even ones first
+          const uint32_t at0 = own - base + off16<D>(kv, r, ch & ~1) + (ch & 1) * 8, at1 = own - base + off16<D>(kv, r, ch | 1) + (ch & 1) * 8;
+          *reinterpret_cast<uint2*>(smem + at0) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
+          *reinterpret_cast<uint2*>(smem + at1) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
         } else {
           *reinterpret_cast<uint4*>(smem + (own - base) + off16<D>(kv, r, ch)) = w;
         }
@@ -575,7 +569,7 @@ tree_combine_kernel(const __grid_constant__ StepParams<kInlineWords> params) {
 
 template <int D, int NB, bool Q8>
 cudaError_t launch_t(const StepDevice& s, const TreeArgs& a, const CUtensorMap& kv_map, cudaStream_t stream) {
-  constexpr int smem = Smem<D, Q8>::bytes(NB);
+  constexpr int smem = Smem<D, NB, Q8>::bytes();
   cudaError_t e = cudaFuncSetAttribute(tree_kernel<D, NB, Q8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   StepParams<kInlineWords> params;
@@ -595,6 +589,10 @@ cudaError_t launch_d(const StepDevice& s, const TreeArgs& a, const CUtensorMap& 
 int tree_tile_tokens(int G, int nodes) {
   const int most = 32 / G;
   return nodes < most ? nodes : most;
+}
+int tree_blocks_per_sm(int queries, bool q8) {
+  if (!q8) return Smem<128, 1, false>::kBlocks;
+  return queries <= 8 ? Smem<128, 1, true>::kBlocks : queries <= 16 ? Smem<128, 2, true>::kBlocks : Smem<128, 4, true>::kBlocks;
 }
 
 cudaError_t launch_tree(const StepDevice& s, const TreeArgs& a, const CUtensorMap& kv_map, cudaStream_t stream) {

@@ -23,6 +23,8 @@ cudaError_t launch_tree_tc(const StepDevice& s, const TreeArgs& a, int tiles_per
 cudaError_t launch_tree_combine(const StepDevice& s, int max_nodes, cudaStream_t stream);
 // Nodes of a query tile of the streaming kernel for rows of up to `nodes` nodes.
 int tree_tile_tokens(int G, int nodes);
+// Its thread blocks that an SM runs at a time, for tiles of `queries` (node, head) pairs.
+int tree_blocks_per_sm(int queries, bool q8);
 
 // The cache written and read back (ts_cache.cu): s.k_new, s.v_new are the step's tensors; `source`: see ts_cache_append.
 cudaError_t launch_cache_append(const StepDevice& s, const Cache8& cache, const int32_t* source, int n_source, cudaStream_t stream);

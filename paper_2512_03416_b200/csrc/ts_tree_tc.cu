@@ -24,13 +24,14 @@
 // row's own K are two e4m3 addends as well: their 64 rows at most are rows 0..63 and 64..127 of one K tile, and the scores are added in
 // pairs; their V are f16 with an exponent per 32 nodes.
 //
-// Warps: 0-7 / 8-15 softmax of slot A / B (sixteen query rows each, four lanes per row), 16-19 transform (queries, V, the row's own nodes,
-// the keys' exponents), 20 K loader (also takes the units), 21 V loader, 22 MMA issuer. Every wait is bounded; one that runs out raises
+// Warps: 0-7 / 8-15 softmax of slot A / B (sixteen query rows each, four lanes per row), 16-23 transform (queries, V, the row's own nodes,
+// the keys' exponents), 24 K loader (also takes the units), 25 V loader, 26 MMA issuer. Every wait is bounded; one that runs out raises
 // TS_DEV_TIMEOUT, and the CTA ends: no new copies or MMAs, those in flight are waited for (with a limit).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <math_constants.h>
+
+#include <type_traits>
 
 #include "../../include/tokenscale.h"
 #include "ts_ptx.h"
@@ -41,16 +42,16 @@
 namespace ts {
 namespace {
 
-constexpr int kThreads = 768;
-// Register split (setmaxnreg works on whole warpgroups): four of softmax warps, one of transform warps, one of loaders and MMA issuer
-constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsTransform = 56, kRegsAux = 40;
-static_assert(512 * kRegsSoftmax + 128 * (kRegsTransform + kRegsAux) <= kThreads * kRegsLaunch, "register split exceeds the launch's total");
-constexpr int kWarpTransform = 16, kWarpK = 20, kWarpV = 21, kWarpMma = 22;
+constexpr int kThreads = 896;
+// Register split (setmaxnreg works on whole warpgroups): four of softmax warps, two of transform warps, one of loaders and MMA issuer
+constexpr int kRegsLaunch = 72, kRegsSoftmax = 88, kRegsTransform = 48, kRegsAux = 56;
+static_assert(512 * kRegsSoftmax + 256 * kRegsTransform + 128 * kRegsAux <= kThreads * kRegsLaunch, "register split exceeds the launch's total");
+constexpr int kWarpTransform = 16, kTransformWarps = 8, kWarpK = 24, kWarpV = 25, kWarpMma = 26;
 constexpr int kD = 128, kBlock = 128, kBlockPages = kBlock / kPageSize;
 constexpr int kTile = 128 * kD * 2;              // 128 x 128 16-bit operand: two 64-column halves of 128 rows of 128 bytes
 constexpr int kHalf = kTile / 2;
 constexpr int kTile8 = 128 * kD;                 // 128 x 128 8-bit operand: 128 rows of 128 bytes
-constexpr int kUnitRing = 4, kUnitReaders = 22;  // V loader, MMA issuer, 4 transform and 16 softmax warps
+constexpr int kUnitRing = 4, kUnitReaders = 26;  // V loader, MMA issuer, 8 transform and 16 softmax warps
 constexpr int kTabStages = 4;                    // blocks whose keys' exponents are held
 constexpr float kMoveBy = 8.f;                   // log2: how far a row's maximum may exceed its reference
 constexpr float kShift16 = 7.f;                  // log2 of the factor on f16 weights: 2^(8 + 7) is within f16, 2^-21 a normal number
@@ -83,7 +84,7 @@ struct Map {
     TAB_FULL = V_EMPTY + kVStages,                                        // [kTabStages] the keys' exponents of a block
     K_OWN = TAB_FULL + kTabStages,                                          // K of the row's own nodes is there
     S_FULL, P_FULL = S_FULL + 2,                                          // [slot][half of the keys]
-    O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 8, COUNT
+    O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 4, COUNT
   };
   static constexpr int kOffMisc = kOffBar + COUNT * 8;                    // TMEM address, failure flag
   static constexpr int kBytes = kOffMisc + 16;
@@ -141,12 +142,11 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Four e4m3 codes as f16 pairs (0, 2) and (1, 3), times `by`. An e4m3 code shifted to the sign and to bits 13..7 is the f16 number
-// 2^-8 times its value, subnormal ones too (the formats differ in the bias alone); `by` makes up for that.
+// Four e4m3 codes as f16 pairs (0, 2) and (1, 3), times 2^-8 `by`
 __device__ __forceinline__ void widen4(uint32_t w, uint32_t by, uint32_t& even, uint32_t& odd) {
-  const uint32_t e = ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u), o = ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u);
+  cache8_widen(w, even, odd);
   const __half2 f = *reinterpret_cast<const __half2*>(&by);
-  const __half2 a = __hmul2(*reinterpret_cast<const __half2*>(&e), f), b = __hmul2(*reinterpret_cast<const __half2*>(&o), f);
+  const __half2 a = __hmul2(*reinterpret_cast<const __half2*>(&even), f), b = __hmul2(*reinterpret_cast<const __half2*>(&odd), f);
   even = *reinterpret_cast<const uint32_t*>(&a);
   odd = *reinterpret_cast<const uint32_t*>(&b);
 }
@@ -162,21 +162,14 @@ __device__ __forceinline__ bool not_finite(const uint4& w) {
   auto odd = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
   return odd(w.x) || odd(w.y) || odd(w.z) || odd(w.w);
 }
-// x * 2^-e of eight bf16 as two e4m3 addends each: hi + lo
-__device__ __forceinline__ void split8(const uint4& w, float down, uint2& hi, uint2& lo) {
-  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = make_float2(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
-    h[i] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
-    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h[i], __NV_E4M3);
-    const float2 g = __half22float2(__half2(r));
-    l[i] = __nv_cvt_float2_to_fp8x2(make_float2(f.x - g.x, f.y - g.y), __NV_SATFINITE, __NV_E4M3);
-  }
-  hi = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-  lo = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+// eight bf16, times `by`, as two e4m3 addends each: hi + lo
+__device__ __forceinline__ void split8(const uint4& w, float by, uint2& hi, uint2& lo) {
+  cache8_split(w.x, w.y, by, hi.x, lo.x);
+  cache8_split(w.z, w.w, by, hi.y, lo.y);
 }
+// Query q of a tile sits in this row of its operand and TMEM lane: sixteen at a time go to the four lane quarters in turn, each of which is one SM
+// sub-partition's, so that few queries use all four (37 rows of 8192 keys x 16 nodes x 4 heads in 8 bits: see the table of measurements below).
+__device__ __forceinline__ int row_of(int q) { return (q >> 4 & 3) * 32 + (q >> 6) * 16 + (q & 15); }
 // 16-byte chunk c (of eight 16-bit elements) of row r of a 16-bit operand tile; eight codes c of row r of an 8-bit one
 __device__ __forceinline__ uint32_t at16(int r, int c) { return (uint32_t)((c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4)); }
 __device__ __forceinline__ uint32_t at8(int r, int c) { return (uint32_t)(r * 128 + ((((c >> 1) ^ r) & 7) << 4) + (c & 1) * 8); }
@@ -192,6 +185,11 @@ __device__ __forceinline__ float lds_f(uint32_t at) {
   asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ void lds_f4(uint32_t at, uint64_t& lo, uint64_t& hi) {      // four
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];\n" : "=l"(lo), "=l"(hi) : "r"(at) : "memory");
+}
+// Place of key k's power in its table: the columns of a lane in two neighbouring eights lie together.
+__device__ __forceinline__ int tab_at(int k) { return ((k >> 4) * 4 + (k >> 1 & 3)) * 4 + (k >> 3 & 1) * 2 + (k & 1); }
 __device__ __forceinline__ uint64_t lds_f2(uint32_t at) {       // two floats
   uint64_t v;
   asm volatile("ld.shared.b64 %0, [%1];\n" : "=l"(v) : "r"(at) : "memory");
@@ -265,10 +263,10 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     for (int i = 0; i < L::COUNT; ++i) {
       int n = 1;
       if (i >= L::UNIT_EMPTY && i < L::UNIT_EMPTY + kUnitRing) n = kUnitReaders;
-      if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::TAB_FULL && i < L::K_OWN)) n = 4;   // transform warps
+      if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::TAB_FULL && i < L::K_OWN)) n = kTransformWarps;
       if (i >= L::P_FULL && i < L::O_FULL) n = 8;             // softmax warps of the slot
       if (i == L::O_EMPTY) n = 16;
-      if (i >= L::XCHG && i < L::DRAIN) n = 2;
+      if (i >= L::XCHG && i < L::DRAIN) n = 4;                // the warps of a lane quarter, of both slots
       mbar_init(bar(i), n);
     }
     mbar_init_fence();
@@ -299,6 +297,11 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       }
     }
   };
+  auto wait_both = [&](int i, uint32_t pi, int j, uint32_t pj) -> bool {
+    const bool a0 = mbar_try_wait(bar(i), pi), b0 = mbar_try_wait(bar(j), pj);      // both looks are under way together
+    if (__all_sync(0xffffffffu, a0 && b0)) return true;
+    return wait(i, pi) && wait(j, pj);
+  };
   auto arrive = [&](int i) {                     // one arrival of the warp, behind everything its lanes did
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(i));
@@ -306,7 +309,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
   if (warp < kWarpTransform) {
     // ================================================================ softmax and epilogue: sixteen rows of a slot per warp
     reg_inc<kRegsSoftmax>();
-    const int x = warp >> 3, quarter = warp & 3, row0 = quarter * 32 + ((warp >> 2) & 1) * 16;
+    const int x = warp >> 3, quarter = warp & 3, part = (warp >> 2) & 1, row0 = row_of((warp & 7) * 16);
     const int col = (lane & 3) * 2;              // this lane's rows are row0 + lane / 4 and the eighth behind it, its columns col, col + 1 of each eight
     const uint32_t tS = tmem + x * 128 + ((uint32_t)row0 << 16);
     const uint32_t tO = tmem + 256 + ((uint32_t)row0 << 16);      // of slot A; slot B's 128 columns on
@@ -327,7 +330,10 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       const bool two = UNIT(cnt_b) > 0;
       const int n_cached = UNIT(n_cached), n_keys = min(UNIT(ctx) - UNIT(p_begin) * kPageSize, UNIT(n_pages) * kPageSize);
       const int n_q = (two && x ? UNIT(cnt_b) : UNIT(cnt_a)) * G;
-      const bool idle = row0 >= n_q;                       // no row of this warp is a query
+      // A unit of one tile of up to 64 queries has them in its rows twice: the two warps of a lane quarter take 64 of a block's keys each.
+      const bool half = !two && n_q <= 64;
+      const int query0 = half ? quarter * 16 : (warp & 7) * 16;
+      const bool idle = query0 >= n_q;                     // the warp has no query
       auto steps_of = [&](int slot) {                      // two tiles: all blocks; one tile: in turn
         const int blocks = n_cached + UNIT(own);
         return two ? blocks : (blocks + 1 - slot) / 2;
@@ -340,8 +346,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       bool first = true;
       for (; j < n_blocks; j += dj, par ^= 1, first = false) {
         const int tb = (g8 + j) & 7;
-        ok = wait(L::S_FULL + x, par & 1);
-        ok = ok && wait(L::TAB_FULL + (tb & 3), tb >> 2);
+        // the table of a block of cached tokens in bf16 says nothing
+        ok = Q8 || j == n_cached ? wait_both(L::TAB_FULL + (tb & 3), tb >> 2, L::S_FULL + x, par & 1) : wait(L::S_FULL + x, par & 1);
         if (!ok) break;
         if (idle) {                                        // P of these rows may be anything: nobody reads their O
           arrive(L::P_FULL + 2 * x);
@@ -349,161 +355,201 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           continue;
         }
         tc_fence_after();
-        float v[64];
-        tmem_ld_rows32(&v[0], tS);
-        tmem_ld_rows32(&v[32], tS + 64);
         if constexpr (Q8) {
           if (first) {                                     // the queries' powers of two
-            const uint32_t qs = base + L::kOffQScale + ((two ? x : 0) * 128 + row0 + (lane >> 2)) * 4;
+            const uint32_t qs = base + L::kOffQScale + ((two ? x : 0) * 128 + query0 + (lane >> 2)) * 4;
             q_scale[0] = scale * lds_f(qs);
             q_scale[1] = scale * lds_f(qs + 32);
           }
         }
-        const bool own = j == n_cached;
-        const int end = n_keys - j * kBlock;
-        tmem_ld_wait();
-        if (Q8 && own) {
+        auto step = [&](auto halves_tag) {
+          constexpr int H = decltype(halves_tag)::value;   // how many halves of the block's keys the warp takes
+          const int h0 = H == 2 ? 0 : part;                // the first of them
+          float v[32 * H];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] += v[32 + e];            // the two addends of K
-        }
-        // scores that can be compared: Q8 times the K rows' powers
-        if constexpr (Q8) {
-          const uint32_t tab = base + L::kOffTab + (tb & 3) * kBlock * 4 + col * 4;
+          for (int h = 0; h < H; ++h) tmem_ld_rows32(&v[32 * h], tS + 64 * (h0 + h));
+          const bool own = j == n_cached;
+          const int end = n_keys - j * kBlock - 64 * h0;
+          [[maybe_unused]] const uint32_t tab = base + L::kOffTab + (tb & 3) * kBlock * 4 + h0 * 256 + col * 8;
+          [[maybe_unused]] uint64_t kp[4];                 // looked up while the scores come
+          if constexpr (Q8) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t kp2 = lds_f2(tab + 32 * e);
-            unpack_f2(mul2(pack_f2(v[4 * e], v[4 * e + 1]), kp2), v[4 * e], v[4 * e + 1]);
-            unpack_f2(mul2(pack_f2(v[4 * e + 2], v[4 * e + 3]), kp2), v[4 * e + 2], v[4 * e + 3]);
+            for (int e = 0; e < 4; e += 2) lds_f4(tab + 32 * e, kp[e], kp[e + 1]);
           }
-        }
-        // keys that a row does not see
-        if (own) {
-          const uint64_t bad = lds_f2(base + L::kOffBad + (tb & 3) * 8) >> col;
+          tmem_ld_wait();
+          if constexpr (Q8) {
+            if (own) {                                     // the two addends of K
+              if constexpr (H == 2) {
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int row = row0 + (lane >> 2) + 8 * r, node = UNIT(t0) + (two && x ? a.tile_tokens : 0) + row / G, T = UNIT(T);
-            uint64_t bits = 0;
-            if (row < n_q) bits = a.mask ? a.mask[UNIT(tok0) + node] : (2ull << node) - 1;
-            if (T < 64) bits &= (1ull << T) - 1;
-            bits >>= col;
+                for (int e = 0; e < 32; ++e) v[e] += v[32 + e];
+              } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+                for (int c = 0; c < 4; ++c) {
+                  float o2[8];
+                  tmem_ld_rows8(o2, tS + 64 + 16 * c);
+                  tmem_ld_wait();
 #pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                float& y = v[4 * e + 2 * r + t];
-                y = (bad >> (8 * e + t)) & 1 ? CUDART_NAN_F : y;
-                y = (bits >> (8 * e + t)) & 1 ? y : -CUDART_INF_F;
-                v[32 + 4 * e + 2 * r + t] = -CUDART_INF_F;
+                  for (int e = 0; e < 8; ++e) v[8 * c + e] += o2[e];
+                }
               }
-          }
-        } else if (end < kBlock) {
+            }
+            // scores that can be compared: times the K rows' powers
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-              if (8 * e + col + t >= end) v[4 * e + t] = v[4 * e + 2 + t] = -CUDART_INF_F;
-        }
-        float e_of[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (Q8) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) e_of[c] = lds_f(base + L::kOffExp + (tb & 3) * 16 + c * 4);
-        }
-        float top[2];                                      // in the units of m (the scales are positive)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float* w = &v[16 * c + 2 * r];
-            float t = max3(fmaxf(w[0], w[1]), w[4], w[5]);
-            t = max3(t, w[8], w[9]);
-            t = max3(t, w[12], w[13]);
-            if (Q8) t = fmaf(t, q_scale[r], e_of[c]);
-            top[r] = c == 0 ? t : fmaxf(top[r], t);
-          }
-          if (!Q8) top[r] *= scale;
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-        }
-        const bool move[2] = {top[0] > m[0] + kMoveBy, top[1] > m[1] + kMoveBy};      // the first key seen too: m is -inf before it
-        if (__any_sync(0xffffffffu, move[0] || move[1])) {
-          float keep[2];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            keep[r] = move[r] ? ex2(m[r] - top[r]) : 1.f;  // 0 the first time
-            if (move[r]) m[r] = top[r];
-            l[r] *= keep[r];
-          }
-          if (!first) {                                    // O holds the steps in front: their P V was issued before these scores' product
-#pragma unroll 1
-            for (uint32_t at = tO + x * 128, end_o = at + 128; at < end_o; at += 16) {
-              float ov[8];
-              tmem_ld_rows8(ov, at);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 8; ++e) ov[e] *= keep[(e >> 1) & 1];
-              tmem_st_rows8(at, ov);
+            for (int e = 0; e < 8 * H; ++e) {
+              if (e >= 4 && e % 2 == 0) lds_f4(tab + 32 * e, kp[e & 3], kp[(e & 3) + 1]);
+              unpack_f2(mul2(pack_f2(v[4 * e], v[4 * e + 1]), kp[e & 3]), v[4 * e], v[4 * e + 1]);
+              unpack_f2(mul2(pack_f2(v[4 * e + 2], v[4 * e + 3]), kp[e & 3]), v[4 * e + 2], v[4 * e + 3]);
             }
           }
-        }
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {             // half of the keys are announced when their P is in TMEM
-          uint32_t pk[16];
-#pragma unroll
-          for (int c = 2 * part; c < 2 * part + 2; ++c) {
+          // keys that a row does not see
+          if (own) {
+            const uint64_t bad = lds_f2(base + L::kOffBad + (tb & 3) * 8) >> col;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const float ref = (m[r] == -CUDART_INF_F ? 0.f : m[r]) - (Q8 ? kShift16 + e_of[c] : 0.f);
-              const uint64_t neg2 = pack_f2(-ref, -ref), scale2 = pack_f2(q_scale[r], q_scale[r]);
-              uint64_t sum = 0;
+              const int q = query0 + (lane >> 2) + 8 * r, node = UNIT(t0) + (two && x ? a.tile_tokens : 0) + q / G, T = UNIT(T);
+              uint64_t bits = 0;
+              if (q < n_q) bits = a.mask ? a.mask[UNIT(tok0) + node] : (2ull << node) - 1;
+              if (T < 64) bits &= (1ull << T) - 1;
+              bits = h0 == 0 ? bits >> col : 0;            // 64 nodes at most
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int at = 16 * c + 4 * e + 2 * r;
-                float p0, p1;
-                unpack_f2(fma2(pack_f2(v[at], v[at + 1]), scale2, neg2), p0, p1);
-                p0 = ex2(p0);
-                p1 = ex2(p1);
-                sum = add2(sum, pack_f2(p0, p1));
-                pk[8 * (c & 1) + 2 * e + r] = Q8 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+              for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                  float& y = v[4 * e + 2 * r + t];
+                  y = (bad >> (8 * e + t)) & 1 ? CUDART_NAN_F : y;
+                  y = (bits >> (8 * e + t)) & 1 ? y : -CUDART_INF_F;
+                  if (H == 2) v[32 * (H - 1) + 4 * e + 2 * r + t] = -CUDART_INF_F;
+                }
+            }
+          } else if (end < 64 * H) {
+#pragma unroll
+            for (int e = 0; e < 8 * H; ++e)
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                if (8 * e + col + t >= end) v[4 * e + t] = v[4 * e + 2 + t] = -CUDART_INF_F;
+          }
+          float e_of[2 * H] = {};                          // Q8: the exponents of the groups of 32 keys
+          if constexpr (Q8) {
+#pragma unroll
+            for (int c = 0; c < 2 * H; ++c) e_of[c] = lds_f(base + L::kOffExp + (tb & 3) * 16 + (2 * h0 + c) * 4);
+          }
+          float top[2];                                    // in the units of m (the scales are positive)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int c = 0; c < 2 * H; ++c) {
+              const float* w = &v[16 * c + 2 * r];
+              float t = max3(fmaxf(w[0], w[1]), w[4], w[5]);
+              t = max3(t, w[8], w[9]);
+              t = max3(t, w[12], w[13]);
+              if (Q8) t = fmaf(t, q_scale[r], e_of[c]);
+              top[r] = c == 0 ? t : fmaxf(top[r], t);
+            }
+            if (!Q8) top[r] *= scale;
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          }
+          const bool move[2] = {top[0] > m[0] + kMoveBy, top[1] > m[1] + kMoveBy};      // the first key seen too: m is -inf before it
+          if (__any_sync(0xffffffffu, move[0] || move[1])) {
+            float keep[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              keep[r] = move[r] ? ex2(m[r] - top[r]) : 1.f;                            // 0 the first time
+              if (move[r]) m[r] = top[r];
+              l[r] *= keep[r];
+            }
+            if (!first) {                                  // O holds the steps in front: their P V was issued before these scores' product
+#pragma unroll 1
+              for (uint32_t at = tO + x * 128, end_o = at + 128; at < end_o; at += 16) {
+                float ov[8];
+                tmem_ld_rows8(ov, at);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ov[e] *= keep[(e >> 1) & 1];
+                tmem_st_rows8(at, ov);
               }
-              float s0, s1;
-              unpack_f2(sum, s0, s1);
-              if (Q8) l[r] = fmaf(s0 + s1, power(-(int)e_of[c]), l[r]);      // the V rows' exponent is not part of the sum
-              else l[r] += s0 + s1;
             }
           }
-          tmem_st_pairs(tS + part * 32, pk);
-          tmem_st_wait();
-          tc_fence_before();
-          arrive(L::P_FULL + 2 * x + part);
-        }
+#pragma unroll
+          for (int h = 0; h < H; ++h) {                    // half of the keys are announced when their P is in TMEM
+            uint32_t pk[16];
+#pragma unroll
+            for (int c = 2 * h; c < 2 * h + 2; ++c) {
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                const float ref = (m[r] == -CUDART_INF_F ? 0.f : m[r]) - (Q8 ? kShift16 + e_of[c] : 0.f);
+                const uint64_t neg2 = pack_f2(-ref, -ref), scale2 = pack_f2(q_scale[r], q_scale[r]);
+                uint64_t sum = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int at = 16 * c + 4 * e + 2 * r;
+                  float p0, p1;
+                  unpack_f2(fma2(pack_f2(v[at], v[at + 1]), scale2, neg2), p0, p1);
+                  p0 = ex2(p0);
+                  p1 = ex2(p1);
+                  sum = add2(sum, pack_f2(p0, p1));
+                  pk[8 * (c & 1) + 2 * e + r] = Q8 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+                }
+                float s0, s1;
+                unpack_f2(sum, s0, s1);
+                if (Q8) l[r] = fmaf(s0 + s1, power(-(int)e_of[c]), l[r]);              // the V rows' exponent is not part of the sum
+                else l[r] += s0 + s1;
+              }
+            }
+            tmem_st_pairs(tS + (h0 + h) * 32, pk);
+            if (H == 1) {                                  // the other half's weights are the other warp's rows'
+#pragma unroll
+              for (int e = 0; e < 16; ++e) pk[e] = 0;
+              tmem_st_pairs(tS + (1 - h0) * 32, pk);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(L::P_FULL + 2 * x + (h0 + h));
+            if (H == 1) arrive(L::P_FULL + 2 * x + 1 - h0);
+          }
+        };
+        if (half) step(std::integral_constant<int, 1>());
+        else step(std::integral_constant<int, 2>());
       }
       if (!ok) break;
       g8 = (g8 + n_blocks) & 7;
       // ------------------------------------------------------------------ epilogue
-      // Two tiles: a slot's warps write their tile. One tile: both slots' warps know both sums, and each writes half of the columns.
+      // Two tiles: a slot's warps write their tile. One tile: the warps that have keys of the same queries (of both slots; and both of a
+      // lane quarter) know each other's sums, and each writes its share of the columns.
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       }
-      const int n = steps_of(x), n_other = steps_of(x ^ 1), rows[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
-      float w_mine[2] = {1.f, 1.f}, w_other[2] = {0.f, 0.f};
+      const int n = steps_of(x), n_other = steps_of(x ^ 1), q_of[2] = {query0 + (lane >> 2), query0 + (lane >> 2) + 8};
+      // weights of the results: slot A's and B's of this warp's half (or all) of the keys, and, `half`, of the other half
+      float w[4][2] = {{1.f, 1.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
       if (!two) {
-        float2* xchg = reinterpret_cast<float2*>(smem + L::kOffXchg);
-        if (k8 & 8) ok = wait(L::O_EMPTY, (k8 & 1) ^ 1);   // the other warp has read what the unit before left here
+        float2* xchg = reinterpret_cast<float2*>(smem + L::kOffXchg);      // [slot][warp][16]
+        if (k8 & 8) ok = wait(L::O_EMPTY, (k8 & 1) ^ 1);   // what the unit before left here has been read
         if (!ok) break;
-        if ((lane & 3) < 2) xchg[x * 128 + rows[lane & 1]] = lane & 1 ? make_float2(m[1], l[1]) : make_float2(m[0], l[0]);
-        arrive(L::XCHG + (warp & 7));
-        ok = wait(L::XCHG + (warp & 7), par >> 3);
+        if ((lane & 3) < 2)
+          xchg[warp * 16 + (lane >> 2) + 8 * (lane & 1)] = lane & 1 ? make_float2(m[1], l[1]) : make_float2(m[0], l[0]);
+        arrive(L::XCHG + quarter);
+        ok = wait(L::XCHG + quarter, par >> 3);
         par ^= 8;
         if (!ok) break;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float2 other = xchg[(x ^ 1) * 128 + rows[r]];
-          const float mm = fmaxf(m[r], other.x), ref = mm == -CUDART_INF_F ? 0.f : mm;
-          w_mine[r] = ex2(m[r] - ref);                     // 0 for a slot that saw no key
-          w_other[r] = ex2(other.x - ref);
-          l[r] = w_mine[r] * l[r] + w_other[r] * other.y;
+          float2 ml[4];
+          float mm = -CUDART_INF_F;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            ml[i] = i < 2 || half ? xchg[((i & 1) * 8 + ((warp & 7) ^ (i & 2) * 2)) * 16 + (lane >> 2) + 8 * r] : make_float2(-CUDART_INF_F, 0.f);
+            mm = fmaxf(mm, ml[i].x);
+          }
+          const float ref = mm == -CUDART_INF_F ? 0.f : mm;
+          l[r] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            w[i][r] = ex2(ml[i].x - ref);                  // 0 for one that saw no key
+            l[r] = fmaf(w[i][r], ml[i].y, l[r]);
+          }
           m[r] = mm;
         }
       }
@@ -518,29 +564,34 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         uint32_t out_row[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          out_row[r] = (uint32_t)((split ? partial : tok0) + node0 + rows[r] / G) * s.Hq + head * G + rows[r] % G;
+          out_row[r] = (uint32_t)((split ? partial : tok0) + node0 + q_of[r] / G) * s.Hq + head * G + q_of[r] % G;
           const float inv = split ? 1.f : l[r] == 0.f ? 0.f : 1.f / l[r];      // no visible key: zeros
-          w_mine[r] *= inv;
-          w_other[r] *= inv;
-          if (split && rows[r] < n_q && (two || x == 0) && (lane & 3) == 0)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i][r] *= inv;
+          if (split && q_of[r] < n_q && (two || (x == 0 && !(half && part))) && (lane & 3) == 0)
             *reinterpret_cast<float2*>(s.part_ml + (size_t)out_row[r] * 2) = make_float2(m[r], l[r]);
         }
-        const int c_begin = two ? 0 : x * 4, c_end = two ? 8 : x * 4 + 4;
+        const int c_count = two ? 8 : half ? 2 : 4, c_begin = two ? 0 : half ? (x * 2 + part) * 2 : x * 4;
+        const int n_a = two ? n : steps_of(0), n_b = two ? 0 : steps_of(1);
+        const uint32_t tO_a = two ? tO + x * 128 : tO;
 #pragma unroll 1
-        for (int c = c_begin; c < c_end; ++c) {            // sixteen columns at a time
+        for (int c = c_begin; c < c_begin + c_count; ++c) {                            // sixteen columns at a time
           float ov[8];
-          if (n > 0) {
-            tmem_ld_rows8(ov, tO + x * 128 + c * 16);
-            tmem_ld_wait();
-          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ov[e] = n > 0 ? ov[e] * w_mine[(e >> 1) & 1] : 0.f;
-          if (!two && n_other > 0) {
+          for (int e = 0; e < 8; ++e) ov[e] = 0.f;
+          auto add = [&](uint32_t at, const float (&by)[2]) {
             float o2[8];
-            tmem_ld_rows8(o2, tO + (x ^ 1) * 128 + c * 16);
+            tmem_ld_rows8(o2, at + c * 16);
             tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ov[e] = fmaf(o2[e], w_other[(e >> 1) & 1], ov[e]);
+            for (int e = 0; e < 8; ++e) ov[e] = fmaf(o2[e], by[(e >> 1) & 1], ov[e]);
+          };
+          if (n_a > 0) add(tO_a, w[0]);                    // what a slot without a step holds is no result
+          if (n_b > 0) add(tO + 128, w[1]);
+          if (half) {
+            const uint32_t other = (uint32_t)(part ? -16 : 16) << 16;                  // the other warp's lanes of the quarter
+            if (n_a > 0) add(tO + other, w[2]);
+            if (n_b > 0) add(tO + other + 128, w[3]);
           }
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
@@ -550,7 +601,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               if (odd) ov[e] = got; else ov[e + 1] = got;
             }
             const int r = (e >> 1) & 1;
-            if (rows[r] < n_q) {
+            if (q_of[r] < n_q) {
               const size_t at = (size_t)out_row[r] * kD + c * 16 + (e >> 2) * 8 + col;
               if (split) *reinterpret_cast<float2*>(s.part_acc + at) = make_float2(ov[e], ov[e + 1]);
               else *reinterpret_cast<uint32_t*>(s.out + at) = pack_bf16(ov[e], ov[e + 1]);
@@ -567,7 +618,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     if (warp < kWarpK) {
       reg_dec<kRegsTransform>();
       // ============================================================== transform
-      const int w = warp - kWarpTransform, t = tid - kWarpTransform * 32;
+      const int w = warp - kWarpTransform, t = (w & 3) * 32 + lane;      // warps w and w + 4 have the same 32 keys of a block, half of the work on each
       const int half = lane >> 4, ch = lane & 15;            // sixteen lanes per row, 16 bytes each
       int g = 0, raw = 0;                                    // blocks of earlier units; of cached tokens
       constexpr int kRaw = Q8 ? L::kRawStages : 1;
@@ -582,22 +633,23 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
 #pragma unroll 1
         for (int tile = 0; tile < (u.cnt_b > 0 ? 2 : 1); ++tile) {
           const int cnt = tile ? u.cnt_b : u.cnt_a;
+          const bool twice = u.cnt_b == 0 && cnt * G <= 64;      // see the softmax warps
           const uint16_t* src = s.q + ((size_t)(u.tok0 + u.t0 + tile * a.tile_tokens) * s.Hq + u.head * G) * kD + ch * 8;
           unsigned char* dst = smem + L::kOffQ + tile * kTile;
 #pragma unroll 1
-          for (int i0 = 0; i0 < 16; i0 += 4) {
-            if ((w * 32 + i0 * 2) / G >= cnt) break;   // the rest of the warp's rows are no queries: whatever the tile holds there stays
+          for (int i0 = 0; i0 < 8; i0 += 4) {
+            if ((w * 16 + i0 * 2) / G >= cnt) break;   // the rest of the warp's are no queries: whatever the tile holds there stays
             uint4 x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int r = w * 32 + (i0 + i) * 2 + half;
+              const int r = w * 16 + (i0 + i) * 2 + half;
               x[i] = make_uint4(0, 0, 0, 0);
               if (r / G < cnt)
                 x[i] = *reinterpret_cast<const uint4*>(src + ((r / G) * s.Hq + r % G) * kD);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int r = w * 32 + (i0 + i) * 2 + half;
+              const int r = w * 16 + (i0 + i) * 2 + half;
               if constexpr (Q8) {
                 uint32_t most = max_magnitude(x[i]);
 #pragma unroll
@@ -605,11 +657,14 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                 const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 7, -118), 118);      // largest to 2^7 .. 2^8
                 uint2 hi, lo;
                 split8(x[i], power(-e), hi, lo);
-                *reinterpret_cast<uint2*>(dst + at8(r, ch)) = hi;
-                *reinterpret_cast<uint2*>(dst + kTile8 + at8(r, ch)) = lo;
+                for (int copy = 0; copy < (twice ? 2 : 1); ++copy) {
+                  *reinterpret_cast<uint2*>(dst + at8(row_of(r) + 16 * copy, ch)) = hi;
+                  *reinterpret_cast<uint2*>(dst + kTile8 + at8(row_of(r) + 16 * copy, ch)) = lo;
+                }
                 if (ch == 0) reinterpret_cast<float*>(smem + L::kOffQScale)[tile * 128 + r] = power(e);
               } else {
-                *reinterpret_cast<uint4*>(dst + at16(r, ch)) = x[i];
+                *reinterpret_cast<uint4*>(dst + at16(row_of(r), ch)) = x[i];
+                if (twice) *reinterpret_cast<uint4*>(dst + at16(row_of(r) + 16, ch)) = x[i];
               }
             }
           }
@@ -645,8 +700,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           const int e_v = real ? cache8_exp_of((uint8_t)ev) : -kCache8MaxExp;
           const int e_top = __reduce_max_sync(0xffffffffu, e_v);
           const bool nan = real && (ek == 255 || ev == 255);
-          reinterpret_cast<float*>(smem + L::kOffTab + tb * kBlock * 4)[t] = nan ? CUDART_NAN_F : power(cache8_exp_of((uint8_t)ek));
-          if (lane == 0) reinterpret_cast<float*>(smem + L::kOffExp + tb * 16)[w] = (float)e_top;
+          if (w < 4) reinterpret_cast<float*>(smem + L::kOffTab + tb * kBlock * 4)[tab_at(t)] = nan ? CUDART_NAN_F : power(cache8_exp_of((uint8_t)ek));
+          if (w < 4 && lane == 0) reinterpret_cast<float*>(smem + L::kOffExp + tb * 16)[w] = (float)e_top;
           arrive(L::TAB_FULL + tb);
           const __half2 f = __float2half2_rn(real ? power(e_v - e_top + 8) : 0.f);
           return *reinterpret_cast<const uint32_t*>(&f);
@@ -682,26 +737,23 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               const unsigned char* codes = smem + L::kOffRaw + raw % kRaw * kTile8;
               // sixteen codes -> two pieces of eight f16; eight lanes take four pieces' worth of two neighbouring rows, so that their
               // stores fall into different banks
+              uint4 x[4];
 #pragma unroll
-              for (int i0 = 0; i0 < 8; i0 += 4) {
-                uint4 x[4];
+              for (int i = 0; i < 4; ++i) {
+                const int r = (w & 3) * 32 + ((w >> 2) * 2 + (i >> 1)) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
+                x[i] = *reinterpret_cast<const uint4*>(codes + r * 128 + (((c ^ r) & 7) << 4));
+              }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const int r = w * 32 + ((i0 + i) >> 1) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
-                  x[i] = *reinterpret_cast<const uint4*>(codes + r * 128 + (((c ^ r) & 7) << 4));
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const int rw = ((i0 + i) >> 1) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), r = w * 32 + rw, c = (i & 1) * 4 + (lane & 3);
-                  const uint32_t by = __shfl_sync(0xffffffffu, by_mine, rw);
-                  uint4 lo, hi;
-                  widen4(x[i].x, by, lo.x, lo.y);
-                  widen4(x[i].y, by, lo.z, lo.w);
-                  widen4(x[i].z, by, hi.x, hi.y);
-                  widen4(x[i].w, by, hi.z, hi.w);
-                  *reinterpret_cast<uint4*>(vt + at16(r, 2 * c)) = lo;
-                  *reinterpret_cast<uint4*>(vt + at16(r, 2 * c + 1)) = hi;
-                }
+              for (int i = 0; i < 4; ++i) {
+                const int rw = ((w >> 2) * 2 + (i >> 1)) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), r = (w & 3) * 32 + rw, c = (i & 1) * 4 + (lane & 3);
+                const uint32_t by = __shfl_sync(0xffffffffu, by_mine, rw);
+                uint4 lo, hi;
+                widen4(x[i].x, by, lo.x, lo.y);
+                widen4(x[i].y, by, lo.z, lo.w);
+                widen4(x[i].z, by, hi.x, hi.y);
+                widen4(x[i].w, by, hi.z, hi.w);
+                *reinterpret_cast<uint4*>(vt + at16(r, 2 * c)) = lo;
+                *reinterpret_cast<uint4*>(vt + at16(r, 2 * c + 1)) = hi;
               }
               arrive(L::RAW_EMPTY + raw % kRaw);
               ++raw;
@@ -713,7 +765,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
             if (!(ok = wait(L::V_LANDED + st, (g / L::kVStages) & 1))) break;
             if (!own) {
               // rows behind the block's last key may hold anything, and 0 * NaN is none
-              for (int i = t; i < (kBlock - end) * 16; i += 128) *reinterpret_cast<uint4*>(vt + at16(end + (i >> 4), i & 15)) = make_uint4(0, 0, 0, 0);
+              for (int i = w * 32 + lane; i < (kBlock - end) * 16; i += kTransformWarps * 32) *reinterpret_cast<uint4*>(vt + at16(end + (i >> 4), i & 15)) = make_uint4(0, 0, 0, 0);
               if (end < kBlock) fence_proxy_async();
               arrive(L::TAB_FULL + tb);
               arrive(L::V_FULL + st);
@@ -733,7 +785,9 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
             for (int sh = 1; sh < 16; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
             return most;
           };
-          if (w < 2) {
+          if (w >= 4) {
+            // nothing: the nodes are few
+          } else if (w < 2) {
             uint32_t bad = 0, most = 0;
             if constexpr (Q8) {                              // the largest finite element of the 32 rows goes to 2^14 .. 2^15
 #pragma unroll 2
@@ -781,7 +835,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                 split8(x, power(-e_k), hi, lo);
                 *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
                 *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
-                if (ch == 0) tab[r] = power(e_k);
+                if (ch == 0) tab[tab_at(r)] = power(e_k);
               } else {
                 *reinterpret_cast<uint4*>(kt + at16(r, ch)) = x;
               }
@@ -913,17 +967,10 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         arrive(L::UNIT_EMPTY + (k8 & 3));
         if (!valid || !(ok = wait(L::Q_FULL, k8 & 1))) break;
         const int n_steps = two ? 2 * n_blocks : n_blocks;
+        auto takes_block = [&](int i) { return !two || (i & 1) == 0; };      // the first step of its block
+        auto is_own = [&](int i) { return (two ? i >> 1 : i) == n_cached; };
         auto qk = [&](int i) {                               // scores of step i's slot
           const int x = i & 1;
-          if (!two || x == 0) {
-            ok = ok && wait(L::K_FULL + kst, par & 1);
-            if (ok && (two ? i >> 1 : i) == n_cached) {
-              ok = wait(L::K_OWN, (par >> 2) & 1);
-              par ^= 4;
-            }
-            if (!ok) return;
-          }
-          tc_fence_after();
           const uint64_t kd = k_desc + (uint64_t)((kst * L::kKBytes) >> 4), qd = q_desc + (uint64_t)(((two ? x : 0) * kTile) >> 4);
           if constexpr (Q8) {
 #pragma unroll
@@ -948,12 +995,30 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           }
           if (i == n_steps - 1) tc_commit(bar(L::Q_EMPTY), issue);
         };
-        qk(0);
-        if (n_steps > 1) qk(1);
+        auto wait_k = [&](int i) {
+          if (takes_block(i)) ok = ok && wait(L::K_FULL + kst, par & 1);
+        };
+        auto wait_own = [&](int i) {                         // K of the row's own nodes
+          if (takes_block(i) && is_own(i)) {
+            ok = ok && wait(L::K_OWN, (par >> 2) & 1);
+            par ^= 4;
+          }
+        };
+        for (int i = 0; i < 2 && i < n_steps; ++i) {
+          wait_k(i);
+          wait_own(i);
+          tc_fence_after();
+          if (ok) qk(i);
+        }
         if (k8 & 8) ok = ok && wait(L::O_EMPTY, (k8 & 1) ^ 1);
         for (int i = 0; ok && i < n_steps; ++i) {            // O of the step's slot (+)= P V, then the scores of the slot's next step
           const int x = i & 1;
-          if ((!two || x == 0) && !(ok = wait(L::V_FULL + vst, (par >> 1) & 1))) break;
+          // Operands are waited for ahead of P, so that between P and the slot's next scores nothing else is looked at; but for the row's
+          // own nodes, whose K and V the transform warps write together once V's stage is free.
+          const bool more = i + 2 < n_steps;
+          if (takes_block(i)) ok = wait(L::V_FULL + vst, (par >> 1) & 1);
+          if (more) wait_k(i + 2);
+          if (!ok) break;
           const uint64_t vd = v_desc + (uint64_t)((vst * kTile) >> 4);
 #pragma unroll
           for (int part = 0; part < 2; ++part) {
@@ -972,8 +1037,15 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               par ^= 2;
             }
           }
-          if (i + 2 >= n_steps) tc_commit(bar(L::O_FULL + x), issue);
-          else qk(i + 2);
+          if (!more) {
+            tc_commit(bar(L::O_FULL + x), issue);
+          } else {
+            if (is_own(i + 2)) {
+              wait_own(i + 2);
+              tc_fence_after();
+            }
+            if (ok) qk(i + 2);
+          }
         }
         k8 = ((k8 + 1) & 7) | 8;
       }

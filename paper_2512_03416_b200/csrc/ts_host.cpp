@@ -5,7 +5,6 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
-#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -1078,7 +1077,6 @@ void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tp.tile_tokens * tp.tiles_per_unit) * c->cfg.n_kv_heads;
   const int blocks = tp.blocks_per_sm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
   int64_t per = std::max<int64_t>(kMinTreePages, (work + blocks - 1) / blocks);
-  if (getenv("TREE_DIV")) per = std::max<int64_t>(kMinTreePages, (int64_t)((double)work / blocks / atof(getenv("TREE_DIV"))));
   for (;; per *= 2) {                                        // the partial results have to fit
     int64_t partials = 0;
     for (int r = 0; r < st->n_rows; ++r)

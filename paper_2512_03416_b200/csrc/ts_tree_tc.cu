@@ -24,8 +24,8 @@
 // row's own K are two e4m3 addends as well: their 64 rows at most are rows 0..63 and 64..127 of one K tile, and the scores are added in
 // pairs; their V are f16 with an exponent per 32 nodes.
 //
-// Warps: 0-7 / 8-15 softmax of slot A / B (sixteen query rows each, four lanes per row), 16-23 transform (queries, V, the row's own nodes,
-// the keys' exponents), 24 K loader (also takes the units), 25 V loader, 26 MMA issuer. Every wait is bounded; one that runs out raises
+// Warps: 0-7 / 8-15 softmax of slot A / B (sixteen query rows each, four lanes per row), 16-23 transform (queries, V, the row's own nodes),
+// 24 K loader (also takes the units), 25 V loader, 26 MMA issuer, 27 exponents of the cached keys. Every wait is bounded; one that runs out raises
 // TS_DEV_TIMEOUT, and the CTA ends: no new copies or MMAs, those in flight are waited for (with a limit).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -46,13 +46,13 @@ constexpr int kThreads = 896;
 // Register split (setmaxnreg works on whole warpgroups): four of softmax warps, two of transform warps, one of loaders and MMA issuer
 constexpr int kRegsLaunch = 72, kRegsSoftmax = 88, kRegsTransform = 48, kRegsAux = 56;
 static_assert(512 * kRegsSoftmax + 256 * kRegsTransform + 128 * kRegsAux <= kThreads * kRegsLaunch, "register split exceeds the launch's total");
-constexpr int kWarpTransform = 16, kTransformWarps = 8, kWarpK = 24, kWarpV = 25, kWarpMma = 26;
+constexpr int kWarpTransform = 16, kTransformWarps = 8, kWarpK = 24, kWarpV = 25, kWarpMma = 26, kWarpTables = 27;
 constexpr int kD = 128, kBlock = 128, kBlockPages = kBlock / kPageSize;
 constexpr int kTile = 128 * kD * 2;              // 128 x 128 16-bit operand: two 64-column halves of 128 rows of 128 bytes
 constexpr int kHalf = kTile / 2;
 constexpr int kTile8 = 128 * kD;                 // 128 x 128 8-bit operand: 128 rows of 128 bytes
-constexpr int kUnitRing = 4, kUnitReaders = 26;  // V loader, MMA issuer, 8 transform and 16 softmax warps
-constexpr int kTabStages = 4;                    // blocks whose keys' exponents are held
+constexpr int kUnitRing = 4, kUnitReaders = 26;  // V loader, MMA issuer, 8 transform and 16 softmax warps; in 8 bits the tables' warp
+constexpr int kTabStages = 4;                    // blocks of cached tokens whose keys' exponents are held; two of nodes
 constexpr float kMoveBy = 8.f;                   // log2: how far a row's maximum may exceed its reference
 constexpr float kShift16 = 7.f;                  // log2 of the factor on f16 weights: 2^(8 + 7) is within f16, 2^-21 a normal number
 constexpr long long kDrainCycles = 20000000;
@@ -67,11 +67,14 @@ struct Map {
   static constexpr int kOffK = kOffQ + NT * kTile;
   static constexpr int kOffV = kOffK + kKStages * kKBytes;
   static constexpr int kOffRaw = kOffV + kVStages * kTile;
-  static constexpr int kOffTab = kOffRaw + kRawStages * kTile8;           // Q8, of a block: [128] powers of two of the K rows
-  static constexpr int kOffExp = kOffTab + (Q8 ? kTabStages * kBlock * 4 : 0);          // Q8: exponents of the block's four groups of 32 V rows
-  static constexpr int kOffQScale = kOffExp + (Q8 ? kTabStages * 16 : 0);   // Q8: [NT][128] powers of two of the queries
-  static constexpr int kOffXchg = kOffQScale + (Q8 ? NT * 128 * 4 : 0);   // [slot][128] (maximum, sum)
-  static constexpr int kOffBad = kOffXchg + 2 * 128 * 8;                  // of a block of nodes: those whose V is not finite, 64 bits
+  // Q8, of a block (cached ones take the first kTabStages places in turn, blocks of nodes the other two): [128] powers of two of the K rows;
+  // exponents of the four groups of 32 V rows and two to minus these; of cached blocks [128] f16 factors that bring the V rows to them
+  static constexpr int kOffTab = kOffRaw + kRawStages * kTile8;
+  static constexpr int kOffExp = kOffTab + (Q8 ? (kTabStages + 2) * kBlock * 4 : 0);
+  static constexpr int kOffBy = kOffExp + (Q8 ? (kTabStages + 2) * 32 : 0);
+  static constexpr int kOffQScale = kOffBy + (Q8 ? kTabStages * kBlock * 2 : 0);      // Q8: [NT][128] powers of two of the queries
+  static constexpr int kOffXchg = kOffQScale + (Q8 ? NT * 128 * 4 : 0);   // [slot][warp][16] (maximum, sum)
+  static constexpr int kOffBad = kOffXchg + 2 * 128 * 8;                  // two blocks of nodes: those whose V is not finite, 64 bits
   static constexpr int kOffUnits = kOffBad + 32;
   static constexpr int kOffBar = kOffUnits + kUnitRing * 64;
   enum {
@@ -81,8 +84,9 @@ struct Map {
     V_LANDED = K_EMPTY + kKStages,                                        // the copies of a V block (Q8: of its codes) are there
     RAW_EMPTY = V_LANDED + (Q8 ? kRawStages : kVStages),
     V_FULL = RAW_EMPTY + kRawStages, V_EMPTY = V_FULL + kVStages,
-    TAB_FULL = V_EMPTY + kVStages,                                        // [kTabStages] the keys' exponents of a block
-    K_OWN = TAB_FULL + kTabStages,                                          // K of the row's own nodes is there
+    TAB_FULL = V_EMPTY + kVStages, TAB_EMPTY = TAB_FULL + kTabStages,     // Q8: the exponents of a block of cached tokens
+    OWN_TAB = TAB_EMPTY + kTabStages,                                     // [2] what there is to know of a block of nodes
+    K_OWN = OWN_TAB + 2,                                          // K of the row's own nodes is there
     S_FULL, P_FULL = S_FULL + 2,                                          // [slot][half of the keys]
     O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 4, COUNT
   };
@@ -262,8 +266,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     misc[1] = 0;
     for (int i = 0; i < L::COUNT; ++i) {
       int n = 1;
-      if (i >= L::UNIT_EMPTY && i < L::UNIT_EMPTY + kUnitRing) n = kUnitReaders;
-      if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::TAB_FULL && i < L::K_OWN)) n = kTransformWarps;
+      if (i >= L::UNIT_EMPTY && i < L::UNIT_EMPTY + kUnitRing) n = kUnitReaders + (Q8 ? 1 : 0);
+      if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::OWN_TAB && i < L::K_OWN)) n = kTransformWarps;
       if (i >= L::P_FULL && i < L::O_FULL) n = 8;             // softmax warps of the slot
       if (i == L::O_EMPTY) n = 16;
       if (i >= L::XCHG && i < L::DRAIN) n = 4;                // the warps of a lane quarter, of both slots
@@ -315,9 +319,9 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     const uint32_t tO = tmem + 256 + ((uint32_t)row0 << 16);      // of slot A; slot B's 128 columns on
     const float scale = s.scale_log2;
     // Counters, as far as barrier phases need them: the registers are the scores'. Units (modulo 8, the ring's place and phase) with a bit 3
-    // once there was one; blocks modulo 8 (the tables' place and phase); parities: bit 0 steps of this slot, 1 and 2 units in
+    // once there was one; blocks of cached tokens modulo 8 and of nodes modulo 4 (their tables' place and phase); parities: bit 0 steps of this slot, 1 and 2 units in
     // which this and the other slot had steps, 3 units of one tile.
-    int k8 = 0, g8 = 0, par = 0;
+    int k8 = 0, c8 = 0, o4 = 0, par = 0;
     static_assert(kUnitRing == 4 && kTabStages == 4, "counted modulo 8");
     bool ok = true;
     while (ok) {
@@ -345,9 +349,11 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       const int n_blocks = n_cached + UNIT(own), dj = two ? 1 : 2;
       bool first = true;
       for (; j < n_blocks; j += dj, par ^= 1, first = false) {
-        const int tb = (g8 + j) & 7;
-        // the table of a block of cached tokens in bf16 says nothing
-        ok = Q8 || j == n_cached ? wait_both(L::TAB_FULL + (tb & 3), tb >> 2, L::S_FULL + x, par & 1) : wait(L::S_FULL + x, par & 1);
+        const bool own = j == n_cached;
+        const int tb = own ? kTabStages + (o4 & 1) : (c8 + j) & 3;         // place of the block's tables
+        if (own) ok = wait_both(L::OWN_TAB + (o4 & 1), o4 >> 1, L::S_FULL + x, par & 1);
+        else if (Q8) ok = wait_both(L::TAB_FULL + tb, ((c8 + j) >> 2) & 1, L::S_FULL + x, par & 1);
+        else ok = wait(L::S_FULL + x, par & 1);
         if (!ok) break;
         if (idle) {                                        // P of these rows may be anything: nobody reads their O
           arrive(L::P_FULL + 2 * x);
@@ -368,9 +374,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           float v[32 * H];
 #pragma unroll
           for (int h = 0; h < H; ++h) tmem_ld_rows32(&v[32 * h], tS + 64 * (h0 + h));
-          const bool own = j == n_cached;
           const int end = n_keys - j * kBlock - 64 * h0;
-          [[maybe_unused]] const uint32_t tab = base + L::kOffTab + (tb & 3) * kBlock * 4 + h0 * 256 + col * 8;
+          [[maybe_unused]] const uint32_t tab = base + L::kOffTab + tb * kBlock * 4 + h0 * 256 + col * 8;
           [[maybe_unused]] uint64_t kp[4];                 // looked up while the scores come
           if constexpr (Q8) {
 #pragma unroll
@@ -403,7 +408,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           }
           // keys that a row does not see
           if (own) {
-            const uint64_t bad = lds_f2(base + L::kOffBad + (tb & 3) * 8) >> col;
+            const uint64_t bad = lds_f2(base + L::kOffBad + (o4 & 1) * 8) >> col;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               const int q = query0 + (lane >> 2) + 8 * r, node = UNIT(t0) + (two && x ? a.tile_tokens : 0) + q / G, T = UNIT(T);
@@ -429,9 +434,10 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                 if (8 * e + col + t >= end) v[4 * e + t] = v[4 * e + 2 + t] = -CUDART_INF_F;
           }
           float e_of[2 * H] = {};                          // Q8: the exponents of the groups of 32 keys
+          [[maybe_unused]] const uint32_t exps = base + L::kOffExp + tb * 32 + h0 * 8;
           if constexpr (Q8) {
 #pragma unroll
-            for (int c = 0; c < 2 * H; ++c) e_of[c] = lds_f(base + L::kOffExp + (tb & 3) * 16 + (2 * h0 + c) * 4);
+            for (int c = 0; c < 2 * H; ++c) e_of[c] = lds_f(exps + c * 4);
           }
           float top[2];                                    // in the units of m (the scales are positive)
 #pragma unroll
@@ -492,7 +498,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                 }
                 float s0, s1;
                 unpack_f2(sum, s0, s1);
-                if (Q8) l[r] = fmaf(s0 + s1, power(-(int)e_of[c]), l[r]);              // the V rows' exponent is not part of the sum
+                if (Q8) l[r] = fmaf(s0 + s1, lds_f(exps + 16 + c * 4), l[r]);          // the V rows' exponent is not part of the sum
                 else l[r] += s0 + s1;
               }
             }
@@ -512,7 +518,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         else step(std::integral_constant<int, 2>());
       }
       if (!ok) break;
-      g8 = (g8 + n_blocks) & 7;
+      c8 = (c8 + n_cached) & 7;
+      o4 = (o4 + n_blocks - n_cached) & 3;
       // ------------------------------------------------------------------ epilogue
       // Two tiles: a slot's warps write their tile. One tile: the warps that have keys of the same queries (of both slots; and both of a
       // lane quarter) know each other's sums, and each writes its share of the columns.
@@ -618,9 +625,9 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     if (warp < kWarpK) {
       reg_dec<kRegsTransform>();
       // ============================================================== transform
-      const int w = warp - kWarpTransform, t = (w & 3) * 32 + lane;      // warps w and w + 4 have the same 32 keys of a block, half of the work on each
+      const int w = warp - kWarpTransform;
       const int half = lane >> 4, ch = lane & 15;            // sixteen lanes per row, 16 bytes each
-      int g = 0, raw = 0;                                    // blocks of earlier units; of cached tokens
+      int g = 0, raw = 0, n_own = 0;                         // blocks of earlier units; of cached tokens; of nodes
       constexpr int kRaw = Q8 ? L::kRawStages : 1;
       bool ok = true;
       for (int k = 0; ok; ++k) {
@@ -673,70 +680,22 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         arrive(L::Q_FULL);
         // ---- key blocks
         const int32_t* table_row = s.table + (size_t)u.table_slot * s.max_pages_per_req + u.p_begin;
-        const int g0 = g, n_cached = u.n_cached, n_pages = u.n_pages, n_keys = min(u.ctx - u.p_begin * kPageSize, n_pages * kPageSize);
-        const uint8_t* scales = a.cache.scales + (size_t)u.head * kPageSize + (t & 15);
-        // Q8: the exponents of this thread's key in the cached blocks. Their tables are written two blocks ahead of V (of the four that
-        // are held, the two in front of the block whose V's stage has become free are done with); bytes and page ids are fetched one and
-        // two blocks before that.
-        int ek = 127, ev = 127, page = -1;
-        uint32_t by_ahead[2] = {0, 0};                         // 2^8 times a V row's power, as f16 pairs: of the next block, of the one behind it
-        auto fetch_page = [&](int j) {
-          const int p = j * kBlockPages + (t >> 4);
-          page = p < n_pages ? table_row[p] : -1;
-        };
-        auto fetch_exps = [&]() {                              // of the block whose page is known
-          ek = ev = 127;
-          if ((unsigned)page < (unsigned)s.n_pages) {
-            const uint8_t* src = scales + (size_t)page * 2 * s.Hkv * kPageSize;
-            ek = src[0];
-            ev = src[(size_t)s.Hkv * kPageSize];
-          }
-        };
-        auto keys_of = [&](int j) { return n_keys - j * kBlock; };
-        auto write_table = [&](int j) -> uint32_t {            // of cached block j, whose bytes are in ek, ev
-          const int tb = (g0 + j) % kTabStages;
-          const bool real = t < keys_of(j);
-          // The V rows of the warp's 32 keys are brought to the largest of their exponents: f16 has the range for rows up to 2^22 below it.
-          const int e_v = real ? cache8_exp_of((uint8_t)ev) : -kCache8MaxExp;
-          const int e_top = __reduce_max_sync(0xffffffffu, e_v);
-          const bool nan = real && (ek == 255 || ev == 255);
-          if (w < 4) reinterpret_cast<float*>(smem + L::kOffTab + tb * kBlock * 4)[tab_at(t)] = nan ? CUDART_NAN_F : power(cache8_exp_of((uint8_t)ek));
-          if (w < 4 && lane == 0) reinterpret_cast<float*>(smem + L::kOffExp + tb * 16)[w] = (float)e_top;
-          arrive(L::TAB_FULL + tb);
-          const __half2 f = __float2half2_rn(real ? power(e_v - e_top + 8) : 0.f);
-          return *reinterpret_cast<const uint32_t*>(&f);
-        };
-        if constexpr (Q8) {
-          fetch_page(0);
-          fetch_exps();
-          fetch_page(1);
-          for (int j = 0; j < 2 && j < n_cached; ++j) {
-            by_ahead[j] = write_table(j);
-            fetch_exps();
-            fetch_page(j + 2);
-          }
-        }
+        const int n_cached = u.n_cached, n_keys = min(u.ctx - u.p_begin * kPageSize, u.n_pages * kPageSize);
         const int n_blocks = n_cached + u.own;
         for (int j = 0; j < n_blocks; ++j, ++g) {
-          const int st = g % L::kVStages, tb = g % kTabStages;
+          const int st = g % L::kVStages;
           const bool own = j == n_cached;
           unsigned char* vt = smem + L::kOffV + st * kTile;
-          [[maybe_unused]] float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + tb * kBlock;
-          const int end = own ? u.T : keys_of(j);
+          const int end = own ? u.T : n_keys - j * kBlock;
           if constexpr (Q8) {
             if (g >= L::kVStages && !(ok = wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1))) break;
             if (!own) {
-              const uint32_t by_mine = by_ahead[0];
-              by_ahead[0] = by_ahead[1];
-              if (j + 2 < n_cached) {
-                by_ahead[1] = write_table(j + 2);
-                fetch_exps();
-                fetch_page(j + 4);
-              }
-              if (!(ok = wait(L::V_LANDED + raw % kRaw, (raw / kRaw) & 1))) break;
+              const int tb = raw % kTabStages;
+              if (!(ok = wait_both(L::TAB_FULL + tb, (raw / kTabStages) & 1, L::V_LANDED + raw % kRaw, (raw / kRaw) & 1))) break;
               const unsigned char* codes = smem + L::kOffRaw + raw % kRaw * kTile8;
-              // sixteen codes -> two pieces of eight f16; eight lanes take four pieces' worth of two neighbouring rows, so that their
-              // stores fall into different banks
+              const uint16_t* by_row = reinterpret_cast<const uint16_t*>(smem + L::kOffBy) + tb * kBlock;
+              // Sixteen codes -> two pieces of eight f16; eight lanes take four pieces' worth of two neighbouring rows, so that their
+              // stores fall into different banks.
               uint4 x[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -745,8 +704,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               }
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int rw = ((w >> 2) * 2 + (i >> 1)) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), r = (w & 3) * 32 + rw, c = (i & 1) * 4 + (lane & 3);
-                const uint32_t by = __shfl_sync(0xffffffffu, by_mine, rw);
+                const int r = (w & 3) * 32 + ((w >> 2) * 2 + (i >> 1)) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
+                const uint32_t by = by_row[r] * 0x10001u;
                 uint4 lo, hi;
                 widen4(x[i].x, by, lo.x, lo.y);
                 widen4(x[i].y, by, lo.z, lo.w);
@@ -767,13 +726,13 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               // rows behind the block's last key may hold anything, and 0 * NaN is none
               for (int i = w * 32 + lane; i < (kBlock - end) * 16; i += kTransformWarps * 32) *reinterpret_cast<uint4*>(vt + at16(end + (i >> 4), i & 15)) = make_uint4(0, 0, 0, 0);
               if (end < kBlock) fence_proxy_async();
-              arrive(L::TAB_FULL + tb);
               arrive(L::V_FULL + st);
               continue;
             }
           }
           // ---- the row's own nodes: warps 0 and 1 take V of 32 nodes each, warps 2 and 3 K
-          const int kst = g % L::kKStages;
+          const int kst = g % L::kKStages, tb = kTabStages + (n_own & 1);
+          [[maybe_unused]] float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + tb * kBlock;
           if (!(ok = wait(L::K_FULL + kst, (g / L::kKStages) & 1))) break;        // the K loader has seen the stage empty
           unsigned char* kt = smem + L::kOffK + kst * L::kKBytes;
           const int r0 = (w & 1) * 32;
@@ -816,11 +775,13 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               *reinterpret_cast<uint4*>(vt + at16(64 + r, ch)) = make_uint4(0, 0, 0, 0);
             }
             if (lane == 0) {
-              reinterpret_cast<uint32_t*>(smem + L::kOffBad + tb * 8)[w] = bad;
+              reinterpret_cast<uint32_t*>(smem + L::kOffBad + (n_own & 1) * 8)[w] = bad;
               if constexpr (Q8) {
-                float* e = reinterpret_cast<float*>(smem + L::kOffExp + tb * 16);
+                float* e = reinterpret_cast<float*>(smem + L::kOffExp + tb * 32);
                 e[w] = (float)e_v;
+                e[4 + w] = down;
                 e[2 + w] = 0.f;
+                e[6 + w] = 1.f;
               }
             }
           } else {
@@ -842,7 +803,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
             }
           }
           fence_proxy_async();
-          arrive(L::TAB_FULL + tb);
+          arrive(L::OWN_TAB + (n_own & 1));
+          ++n_own;
           arrive(L::K_OWN);
           arrive(L::V_FULL + st);
         }
@@ -956,7 +918,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       const uint64_t q_desc = smem_desc(base + L::kOffQ, 0, 1024), k_desc = smem_desc(base + L::kOffK, 0, 1024);
       const uint64_t v_desc = smem_desc(base + L::kOffV, kHalf, 1024);
       int k8 = 0;                                            // units, as the softmax warps count them
-      int kst = 0, vst = 0;                                  // ring places of the next K block to be multiplied and of the next V block
+      int kst = 0, vst = 0, tst = 0;                         // ring places of the next K block to be multiplied, of the next V block and its tables
       uint32_t par = 0;                                      // parities: bits 0, 1 the rings' phases, 2 blocks of nodes, 3 and 4 steps of the slots
       bool ok = true;
       while (ok) {
@@ -1032,6 +994,10 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           par ^= 8u << x;
           if (!two || x == 1) {
             tc_commit(bar(L::V_EMPTY + vst), issue);
+            if (Q8 && (two ? i >> 1 : i) < n_cached) {
+              tc_commit(bar(L::TAB_EMPTY + tst), issue);
+              tst = (tst + 1) & 3;
+            }
             if (++vst == L::kVStages) {
               vst = 0;
               par ^= 2;
@@ -1052,6 +1018,72 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       // no MMA, and no arrival of one, is left behind
       tc_commit(bar(L::DRAIN), issue);
       if (!mbar_wait(bar(L::DRAIN), 0, kDrainCycles) && lane == 0) atomicOr(s.status, TS_DEV_TIMEOUT);
+    } else if (Q8 && warp == kWarpTables) {
+      // ============================================================== exponents of the cached keys, four of a block's keys per lane
+      int c = 0;                                             // blocks of earlier units
+      bool ok = true;
+      for (int k = 0; ok; ++k) {
+        const int ring = k % kUnitRing;
+        if (!wait(L::UNIT_FULL + ring, (k / kUnitRing) & 1)) break;
+        const uint32_t rec = base + L::kOffUnits + ring * 64;
+        auto field = [&](size_t off) { return lds_i(rec + (uint32_t)off); };
+        const int valid = UNIT(valid), n_pages = UNIT(n_pages), n_cached = UNIT(n_cached);
+        const int n_keys = min(UNIT(ctx) - UNIT(p_begin) * kPageSize, n_pages * kPageSize);
+        const int32_t* table_row = s.table + (size_t)UNIT(table_slot) * s.max_pages_per_req + UNIT(p_begin);
+        const uint8_t* scales = a.cache.scales + (size_t)UNIT(head) * kPageSize + (lane & 3) * 4;
+        arrive(L::UNIT_EMPTY + ring);
+        if (!valid) break;
+        // loads that depend on each other are a block apart
+        int page = -1;
+        uint32_t kb = 0, vb = 0;
+        auto fetch_page = [&](int j) {
+          const int p = j * kBlockPages + (lane >> 2);
+          page = p < n_pages ? table_row[p] : -1;
+        };
+        auto fetch_bytes = [&]() {                           // of the block whose page is known
+          kb = vb = 0;
+          if ((unsigned)page < (unsigned)s.n_pages) {
+            const uint8_t* src = scales + (size_t)page * 2 * s.Hkv * kPageSize;
+            kb = *reinterpret_cast<const uint32_t*>(src);
+            vb = *reinterpret_cast<const uint32_t*>(src + (size_t)s.Hkv * kPageSize);
+          }
+        };
+        fetch_page(0);
+        fetch_bytes();
+        fetch_page(1);
+        for (int j = 0; j < n_cached; ++j, ++c) {
+          const uint32_t bytes_k = kb, bytes_v = vb;
+          fetch_bytes();
+          fetch_page(j + 2);
+          const int st = c % kTabStages, real = n_keys - j * kBlock - lane * 4;        // keys of this lane's four
+          float kp[4];
+          int e_v[4], e_top = -kCache8MaxExp;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint8_t k_byte = (uint8_t)(bytes_k >> (8 * i)), v_byte = (uint8_t)(bytes_v >> (8 * i));
+            kp[i] = v_byte == 255 && i < real ? CUDART_NAN_F : cache8_power(k_byte);   // a row with a NaN
+            e_v[i] = i < real ? cache8_exp_of(v_byte) : -kCache8MaxExp;
+            e_top = max(e_top, e_v[i]);
+          }
+          // The V rows of 32 keys are brought to the largest of their exponents: f16 has the range for rows up to 2^22 below it.
+#pragma unroll
+          for (int sh = 1; sh < 8; sh <<= 1) e_top = max(e_top, __shfl_xor_sync(0xffffffffu, e_top, sh));
+          uint16_t by[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) by[i] = __half_as_ushort(__float2half_rn(i < real ? power(e_v[i] - e_top + 8) : 0.f));      // 2^8: see widen4
+          if (c >= kTabStages && !(ok = wait(L::TAB_EMPTY + st, ((c / kTabStages) & 1) ^ 1))) break;
+          float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + st * kBlock;
+          *reinterpret_cast<float2*>(tab + tab_at(lane * 4)) = make_float2(kp[0], kp[1]);
+          *reinterpret_cast<float2*>(tab + tab_at(lane * 4 + 2)) = make_float2(kp[2], kp[3]);
+          *reinterpret_cast<uint2*>(smem + L::kOffBy + (st * kBlock + lane * 4) * 2) = make_uint2(by[0] | by[1] << 16, by[2] | by[3] << 16);
+          if ((lane & 7) == 0) {
+            float* e = reinterpret_cast<float*>(smem + L::kOffExp + st * 32);
+            e[lane >> 3] = (float)e_top;
+            e[4 + (lane >> 3)] = power(-e_top);
+          }
+          arrive(L::TAB_FULL + st);
+        }
+      }
     }
   }
   tc_fence_before();

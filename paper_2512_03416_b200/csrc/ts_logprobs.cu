@@ -3,30 +3,46 @@
 //     y = scale * x,  lse = log sum_j exp y_j,  logprob(t) = y_t - lse,  H = lse - sum_j p_j y_j,
 //     rank(t) = number of tokens in front of t in the order (x descending, index ascending); the first n of that order.
 //
-// One pass over the logits (they are what has to be read; everything else is a few values a row). A row is a thread block's, or
-// a cluster's of up to eight where there are few rows: the blocks leave their sums in the first one's shared memory. Per element
-// a thread adds up e^d and (x - ref) e^d, d = scale (x - ref), against a logit ref that only moves when one exceeds it by a factor
-// of 2^64 (any reference is exact; fp32 has the range), and counts what lies in front of the given tokens.
+// One pass over the logits (they are what has to be read; everything else is a few values a row). A row is a thread block's, and a
+// block takes row after row; where there are few rows, one is a cluster's of up to eight blocks, which leave their sums in the first one's
+// shared memory. A warp of its own copies the row into a ring of 16 KB stages (cp.async.bulk), across the ends of rows, so
+// that memory is busy while the other sixteen warps choose a row's alternatives. Per element a thread adds up e = exp(scale (x - ref)) and x e
+// against a logit ref that only moves when one exceeds it by a factor of 2^64 (any reference is exact; fp32 has the
+// range), and counts what lies in front of the given tokens: bf16 logits two at a time, as pairs of ones that are added up, and no
+// block of 16 bytes whose largest logit is behind the token.
 //
 // Alternatives cost the pass no more than its maximum: every thread keeps the largest logit of its own part of the row and where
 // that part first has it. The n best tokens lie in the n parts that come first by (that logit, that place), since each of these
 // holds a token at least as far in front as the last part's first one. Only those parts are read again (from L2), and of them only
 // what is not behind the last part's largest is sorted.
+//
+// What bounds it: HBM for fp32 logits and few given tokens. An SM's share of HBM is 11 bf16 logits a cycle, which is 11 instructions for
+// each; the sums take 6 and every given token one more.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "../../include/tokenscale.h"
 #include "ts_internal.h"
+#include "ts_ptx.h"
+#include "ts_tma.h"
 
 namespace ts {
 namespace {
 
 namespace cg = cooperative_groups;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;      // that work on the logits; one more warp copies
+constexpr int kBlocksPerSm = 3;          // so that two stream while one chooses its row's alternatives
+constexpr int kStageBytes = 16384, kStages = 4, kStageBlocks = kStageBytes / 16, kPerThread = kStageBlocks / kThreads;
+constexpr int kCand = 2 * kThreads;      // candidates that are sorted at a time
 constexpr int kMaxTop = 32, kMaxGiven = 8, kMaxCluster = 8;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMove = 64.f;            // log2: how far a value may exceed the reference of its sum
-constexpr float kLowest = -200.f;        // log2 of a weight that is 0 in fp32 anyway (-inf's among them): keeps 0 * inf out of the entropy
+// Stands for -inf, and for what lies below it, in a row's sums (a bf16 number), as long as the reference is no larger.
+constexpr float kLowest = -0x1p126f;
+constexpr float kNothing = -200.f;       // log2 of a weight that is 0 in fp32 anyway: keeps 0 * inf out of the entropy where it is
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -43,6 +59,8 @@ __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_flo
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t place) { return (uint64_t)ordered(x) << 32 | (uint32_t)~place; }
 __device__ __forceinline__ uint32_t place_of(uint64_t key) { return ~(uint32_t)key; }
 
+// Barrier of the working warps (id 1; 0 is the whole block's).
+__device__ __forceinline__ void work_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(kThreads) : "memory"); }
 // The keys of a warp sorted, largest in lane 0.
 __device__ __forceinline__ uint64_t warp_sort(uint64_t k, int lane) {
 #pragma unroll
@@ -70,24 +88,28 @@ __device__ __forceinline__ uint64_t warp_merge(uint64_t a, uint64_t b, int lane)
 }
 // The 32 largest of the warps' sorted lists (one of them each, the first n_lists warps'), left sorted in best[0..31]. All threads call it.
 __device__ __forceinline__ void merge_lists(uint64_t k, uint64_t* best, int n_lists, int warp, int lane) {
-  __syncthreads();
-  for (int half = 8; half > 0; half >>= 1) {
+  work_sync();
+  for (int half = kWarps / 2; half > 0; half >>= 1) {
     if (half >= n_lists) continue;                   // the same for all
     if (warp >= half && warp < 2 * half) best[warp * 32 + lane] = k;
-    __syncthreads();
+    work_sync();
     if (warp < half) k = warp_merge(k, best[(warp + half) * 32 + lane], lane);
-    __syncthreads();
+    work_sync();
   }
   if (warp == 0) best[lane] = k;
-  __syncthreads();
+  work_sync();
 }
-static_assert(kWarps == 16, "the lists of two times eight warps are merged");
-
-struct Stats {                                       // of a part of a row, d = (x - ref) * scale
-  float ref, s, t;                                   // a logit to refer to (any is exact), sum e^d, sum (x - ref) e^d
+// Whether a reference is so large that its product with the scale, or a distance from it, may leave fp32.
+__device__ __forceinline__ bool is_huge(float ref) { return fabsf(ref) > 0x1p126f && ref != -CUDART_INF_F; }
+struct Stats {                                       // of a part of a row, weights e(x) = exp(scale (x - ref))
+  float ref, s, t;                                   // a logit to refer to (any is exact), sum e(x), sum (x - ref) e(x)
 };
+// log2 of the factor between weights against two references. The sums' weights are 2^(x c - fl(ref c)), c = scale log2(e): so are these.
+__device__ __forceinline__ float log2_factor(float from, float to, float to_log2) {
+  return is_huge(from) || is_huge(to) ? (from - to) * to_log2 : __fmul_rn(from, to_log2) - __fmul_rn(to, to_log2);
+}
 __device__ __forceinline__ void move_ref(Stats& a, float ref, float to_log2) {
-  const float by = a.ref - ref, f = ex2(by * to_log2);
+  const float by = a.ref - ref, f = ex2(log2_factor(a.ref, ref, to_log2));
   if (a.s == 0.f || f == 0.f) {                      // nothing yet, or nothing that counts (ref = -inf before the first number)
     a.t = 0.f;
     a.s = a.s == a.s ? 0.f : a.s;                    // a NaN stays
@@ -114,20 +136,63 @@ struct Args {
   int32_t vocab, n_given, n_top;
 };
 
+__device__ __forceinline__ uint64_t pack_f2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack_f2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float one_if_ge(float x, float y) {
+  float d;
+  asm("set.ge.f32.f32 %0, %1, %2;\n" : "=f"(d) : "f"(x), "f"(y));
+  return d;
+}
+// The next number above a finite one or -inf, in the type's bits; above +inf a NaN, which nothing reaches.
 template <typename T>
 struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
   static __device__ __forceinline__ float load(const float* p) { return *p; }
+  static __device__ __forceinline__ float above(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return __uint_as_float(u == 0x80000000u ? 1u : u >> 31 ? u - 1 : u + 1);
+  }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) {      // a NaN only where all are
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  // -inf as the lowest number: its weight is 0 all the same, and 0 times its distance is no NaN. (A NaN stays one.)
+  static __device__ __forceinline__ uint4 not_inf(const uint4& v) {
+    auto f = [](uint32_t x) {
+      float y;
+      asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(__uint_as_float(x)), "f"(kLowest));
+      return __float_as_uint(y);
+    };
+    return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
+  }
+  static __device__ __forceinline__ float count_ge(const uint4& v, float y) {
+    float a, b;
+    unpack_f2(add2(pack_f2(one_if_ge(__uint_as_float(v.x), y), one_if_ge(__uint_as_float(v.y), y)),
+                   pack_f2(one_if_ge(__uint_as_float(v.z), y), one_if_ge(__uint_as_float(v.w), y))), a, b);
+    return a + b;
   }
 };
 template <>
 struct Vec<uint16_t> {                               // bf16 bits
   static constexpr int N = 8;
   static __device__ __forceinline__ float load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+  static __device__ __forceinline__ float above(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f) >> 16;
+    return __uint_as_float((u == 0x8000u ? 1u : u >> 15 ? u - 1 : u + 1) << 16);
+  }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -136,270 +201,421 @@ struct Vec<uint16_t> {                               // bf16 bits
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const __nv_bfloat162 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ uint4 not_inf(const uint4& v) {
+    const __nv_bfloat162 low = __float2bfloat162_rn(kLowest);
+    auto f = [&](uint32_t x) {
+      const __nv_bfloat162 y = __hmax2_nan(pair(x), low);
+      return *reinterpret_cast<const uint32_t*>(&y);
+    };
+    return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
+  }
+  static __device__ __forceinline__ float count_ge(const uint4& v, float y) {      // y is a bf16 number
+    const __nv_bfloat162 t = __float2bfloat162_rn(y);
+    const __nv_bfloat162 n = __hadd2(__hadd2(__hge2(pair(v.x), t), __hge2(pair(v.y), t)), __hadd2(__hge2(pair(v.z), t), __hge2(pair(v.w), t)));
+    return __low2float(n) + __high2float(n);
+  }
 };
 __device__ __forceinline__ uint4 load16(const void* p) {
   uint4 v;
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 
-// GIVEN: how many given tokens the loop counts for (kMaxGiven: any number).
+// GIVEN: how many given tokens the loop counts for (at least a.n_given).
 template <typename T, int GIVEN, bool TOP>
-__global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const Args a) {
-  constexpr int N = Vec<T>::N, kUnroll = 4;
+__global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(const Args a, const int n_rows) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ __align__(128) unsigned char ring[];       // [kStages][kStageBytes]
   __shared__ uint64_t lists[kWarps * 32];
-  __shared__ uint64_t cand[kThreads];
+  __shared__ uint64_t cand[kCand];
   __shared__ Stats warp_stats[kWarps], row_stats[kMaxCluster];
-  __shared__ int32_t warp_count[kWarps][kMaxGiven], row_count[kMaxCluster][kMaxGiven];
+  __shared__ int32_t warp_count[kWarps][kMaxGiven];
+  __shared__ int32_t row_count[kMaxCluster][kMaxGiven];
   __shared__ uint64_t row_lists[kMaxCluster * 32];
+  __shared__ float given_x[kMaxGiven];                         // of the row's given tokens: logit (a NaN for one that is none), index
+  __shared__ int32_t given_tok[kMaxGiven];
   __shared__ int32_t n_cand;
+  __shared__ __align__(8) uint64_t full[kStages], empty[kStages];
   cg::cluster_group cluster = cg::this_cluster();
   const int n_parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
-  const int row = blockIdx.x / n_parts;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int first_row = blockIdx.x / n_parts, row_step = gridDim.x / n_parts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty);
   pdl_launch_dependents();
-  pdl_wait();
-
-  const T* x0 = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.row_stride;
-  const float scale = a.scale ? a.scale[row] : 1.f, to_log2 = scale * 1.4426950408889634f;
-  const float lowest = kLowest / to_log2;
-  // The row as 16-byte blocks of memory: block b holds the tokens b * N - off .. + N - 1, the first and last one maybe fewer.
-  const int off = (int)(((uintptr_t)x0 & 15u) / sizeof(T));
-  const T* blocks = x0 - off;
-  const int n_blocks = (a.vocab + off + N - 1) / N;
-  const int b_begin = (int)((long long)n_blocks * part / n_parts), b_end = (int)((long long)n_blocks * (part + 1) / n_parts);
-
-  constexpr int kCount = GIVEN;
-  const int n_given = GIVEN < kMaxGiven ? GIVEN : a.n_given;
-  float given_x[kCount > 0 ? kCount : 1];            // of a given token: its logit, the next number above, its block
-  int given_block[kCount > 0 ? kCount : 1], count[kCount > 0 ? kCount : 1];
-#pragma unroll
-  for (int j = 0; j < kCount; ++j) {
-    const int tok = j < n_given ? a.tokens[(size_t)row * n_given + j] : -1;
-    const bool real = (unsigned)tok < (unsigned)a.vocab;
-    given_x[j] = real ? Vec<T>::load(x0 + tok) : CUDART_NAN_F;   // nothing is in front of a NaN, see below
-    given_block[j] = real ? (tok + off) / N : -1;
-    count[j] = 0;
-  }
-
-  Stats st = {-CUDART_INF_F, 0.f, 0.f};
-  float best = -CUDART_INF_F;                        // this thread's largest logit and the first block that has it
-  int best_block = -1;
-  auto take = [&](const float (&x)[N], int b) {
-    float mx = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[i]);  // a NaN only where all are
-    if (TOP && (mx > best || (best_block < 0 && mx == mx))) {
-      best = mx;
-      best_block = b;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(full0 + 8 * i, 1);
+      mbar_init(empty0 + 8 * i, kWarps);
     }
-    if ((mx - st.ref) * to_log2 > kMove) move_ref(st, mx, to_log2);       // the first number too: the reference is -inf before it
-    const float ref = st.ref == -CUDART_INF_F ? 0.f : st.ref;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float d = x[i] - ref, e = ex2(d * to_log2);
-      st.s += e;
-      st.t = fmaf(e, fmaxf(d, lowest), st.t);
-    }
-#pragma unroll
-    for (int j = 0; j < kCount; ++j) {
-      if (j >= n_given) break;
-      if (b == given_block[j]) {                     // index by index in the token's own block
-        const int tok = a.tokens[(size_t)row * n_given + j];
-#pragma unroll
-        for (int i = 0; i < N; ++i) count[j] += x[i] > given_x[j] || (x[i] == given_x[j] && b * N - off + i < tok);
-      } else {
-        const bool front = b < given_block[j];       // equal logits count in front of the token
-#pragma unroll
-        for (int i = 0; i < N; ++i) count[j] += front ? x[i] >= given_x[j] : x[i] > given_x[j];
-      }
-    }
-  };
-  // A block that the row fills in part: token by token; what is outside counts as -inf, but for nothing else.
-  auto take_partial = [&](int b) {
-#pragma unroll 1
-    for (int i = 0; i < N; ++i) {
-      const int t = b * N - off + i;
-      if (t < 0 || t >= a.vocab) continue;
-      const float x = Vec<T>::load(blocks + (size_t)b * N + i);
-      if (TOP && (x > best || (best_block < 0 && x == x))) {
-        best = x;
-        best_block = b;
-      }
-      if ((x - st.ref) * to_log2 > kMove) move_ref(st, x, to_log2);
-      const float d = x - (st.ref == -CUDART_INF_F ? 0.f : st.ref), e = ex2(d * to_log2);
-      st.s += e;
-      st.t = fmaf(e, fmaxf(d, lowest), st.t);
-#pragma unroll
-      for (int j = 0; j < kCount; ++j)
-        if (j < n_given) count[j] += x > given_x[j] || (x == given_x[j] && t < a.tokens[(size_t)row * n_given + j]);
-    }
-  };
-  auto whole = [&](int b) { return b * N >= off && (b + 1) * N - off <= a.vocab; };
-  // ------------------------------------------------------------------------ the pass
-#pragma unroll 1
-  for (int b0 = b_begin + tid; b0 < b_end; b0 += kUnroll * kThreads) {
-    uint4 v[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int b = b0 + u * kThreads;
-      if (b < b_end && whole(b)) v[u] = load16(blocks + (size_t)b * N);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int b = b0 + u * kThreads;
-      if (b >= b_end) break;
-      if (whole(b)) {
-        float x[N];
-        Vec<T>::unpack(v[u], x);
-        take(x, b);
-      } else {
-        take_partial(b);
-      }
-    }
-  }
-  // ------------------------------------------------------------------------ sums of the block
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) {
-    Stats o;
-    o.ref = __shfl_xor_sync(0xffffffffu, st.ref, sh);
-    o.s = __shfl_xor_sync(0xffffffffu, st.s, sh);
-    o.t = __shfl_xor_sync(0xffffffffu, st.t, sh);
-    st = join(st, o, to_log2);
-  }
-#pragma unroll
-  for (int j = 0; j < kCount; ++j) {
-    if (j >= n_given) break;
-    const int sum = __reduce_add_sync(0xffffffffu, count[j]);
-    if (lane == 0) warp_count[warp][j] = sum;
-  }
-  if (lane == 0) warp_stats[warp] = st;
-  if (tid == 0) n_cand = 0;
-
-  if constexpr (TOP) {
-    // ---------------------------------------------------------------------- alternatives of the block
-    // the parts of the n threads that come first; a part is known by its first block
-    const uint64_t mine = best_block < 0 ? 0 : key_of(best, (uint32_t)best_block);
-    const uint64_t sorted = warp_sort(mine, lane);
-    merge_lists(sorted, lists, kWarps, warp, lane);
-    const uint64_t last = lists[a.n_top - 1];        // 0: fewer parts than that hold a number
-    const float last_x = last ? from_ordered((uint32_t)(last >> 32)) : -CUDART_INF_F;
-    const int last_block = last ? (int)place_of(last) : INT32_MAX;
-    const int per_part = (b_end - b_begin + kThreads - 1) / kThreads;
-    // token i of the block that is item `it`'s: its key, 0 where it is none or behind the last part's largest
-    auto block_of = [&](int it) {
-      const int p = it / per_part;
-      if (p >= a.n_top || lists[p] == 0) return -1;
-      const int b = b_begin + ((int)place_of(lists[p]) - b_begin) % kThreads + (it % per_part) * kThreads;
-      return b < b_end ? b : -1;
-    };
-    auto key_at = [&](float x, int b, int i) -> uint64_t {
-      const int t = b * N - off + i;
-      if (t < 0 || t >= a.vocab || !(x > last_x || (x == last_x && b <= last_block))) return 0;
-      return key_of(x, (uint32_t)t);
-    };
-    const int n_items = a.n_top * per_part;
-    for (int it = tid; it < n_items; it += kThreads) {
-      const int b = block_of(it);
-      if (b < 0) continue;
-      float x[N];
-      if (whole(b)) {
-        Vec<T>::unpack(load16(blocks + (size_t)b * N), x);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int t = b * N - off + i;
-          x[i] = t >= 0 && t < a.vocab ? Vec<T>::load(blocks + (size_t)b * N + i) : CUDART_NAN_F;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint64_t k = key_at(x[i], b, i);
-        if (k) {
-          const int at = atomicAdd(&n_cand, 1);
-          if (at < kThreads) cand[at] = k;
-        }
-      }
-    }
-    __syncthreads();
-    const int n = n_cand;
-    if (n <= kThreads) {
-      const int n_lists = (n + 31) / 32;
-      uint64_t k = 0;
-      if (warp < n_lists) k = warp_sort(tid < n ? cand[tid] : 0, lane);
-      merge_lists(k, lists, n_lists, warp, lane);
-    } else {
-      // So many only where a part has the larger share of a row's best tokens: all of these parts' tokens, as many at a time as
-      // there are threads, next to the best so far.
-      if (tid < 32) cand[tid] = lists[tid];          // the parts: `lists` is needed
-      __syncthreads();
-      uint64_t top32 = 0;                            // warp 0: the best so far
-      const int n_elems = n_items * N;
-      for (int e0 = 0; e0 < n_elems; e0 += kThreads) {
-        const int e = e0 + tid, it = e / N, i = e % N;
-        uint64_t k = 0;
-        const int p = it / per_part;
-        if (e < n_elems && p < a.n_top && cand[p] != 0) {
-          const int b = b_begin + ((int)place_of(cand[p]) - b_begin) % kThreads + (it % per_part) * kThreads;
-          const int t = b * N - off + i;
-          if (b < b_end && t >= 0 && t < a.vocab) k = key_at(Vec<T>::load(x0 + t), b, i);
-        }
-        merge_lists(warp_sort(k, lane), lists, kWarps, warp, lane);
-        if (warp == 0) top32 = warp_merge(top32, lists[lane], lane);
-      }
-      __syncthreads();
-      if (warp == 0) lists[lane] = top32;
-      __syncthreads();
-    }
+    mbar_init_fence();
   }
   __syncthreads();
-  // ------------------------------------------------------------------------ the blocks of the row meet in the first one
-  if (tid == 0) {
-    Stats all = warp_stats[0];
-    for (int w = 1; w < kWarps; ++w) all = join(all, warp_stats[w], to_log2);
-    *cluster.map_shared_rank(&row_stats[part], 0) = all;
+  pdl_wait();
+
+  // A row as 16-byte blocks of memory: block b holds the tokens b * N - off .. + N - 1, the first and the last one maybe fewer. This thread
+  // block's share of those that the row fills: [begin, end); the part-filled ones are the first and the last thread block's.
+  struct Row {
+    const T* blocks;
+    int off, begin, end;
+  };
+  auto row_of = [&](int row) {
+    const T* x0 = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.row_stride;
+    Row r;
+    r.off = (int)(((uintptr_t)x0 & 15u) / sizeof(T));
+    r.blocks = x0 - r.off;
+    const int lo = r.off > 0, hi = (a.vocab + r.off) / N, n = max(hi - lo, 0);
+    r.begin = lo + (int)((long long)n * part / n_parts);
+    r.end = lo + (int)((long long)n * (part + 1) / n_parts);
+    return r;
+  };
+
+  if (warp == kWarps) {
+    // ---------------------------------------------------------------------- copies
+    int n = 0;                                                 // stages filled so far
+    for (int row = first_row; row < n_rows; row += row_step) {
+      const Row r = row_of(row);
+      for (int b = r.begin; b < r.end; b += kStageBlocks, ++n) {
+        const int st = n % kStages;
+        if (n >= kStages && !__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * st, ((n / kStages) & 1) ^ 1))) {
+          row = n_rows;                                        // a wait that ran out: nobody takes the stages any more
+          break;
+        }
+        if (lane == 0) {
+          const uint32_t bytes = (uint32_t)min(kStageBlocks, r.end - b) * 16;
+          mbar_expect_tx(full0 + 8 * st, bytes);
+          bulk_load(smem_u32(ring) + st * kStageBytes, r.blocks + (size_t)b * N, bytes, full0 + 8 * st);
+        }
+        __syncwarp();
+      }
+    }
+    for (int i = max(0, n - kStages); i < n; ++i) mbar_wait(full0 + 8 * (i % kStages), (i / kStages) & 1);      // none is left in flight
+    if (n_parts > 1) cluster.sync();
+    return;
   }
-  if (tid < n_given) {
-    int sum = 0;
-    for (int w = 0; w < kWarps; ++w) sum += warp_count[w][tid];
-    *cluster.map_shared_rank(&row_count[part][tid], 0) = sum;
+
+  // The given tokens of a row are looked up while the row in front passes: index a row earlier than logit.
+  auto tok_of = [&](int row) { return row < n_rows && tid < a.n_given ? a.tokens[(size_t)row * a.n_given + tid] : -1; };
+  auto x_of = [&](int row, int tok) {
+    return (unsigned)tok < (unsigned)a.vocab ? Vec<T>::load(reinterpret_cast<const T*>(a.logits) + (size_t)row * a.row_stride + tok) : CUDART_NAN_F;
+  };
+  int tok_now = -1, tok_next = -1;
+  float x_now = CUDART_NAN_F;
+  if (GIVEN > 0 && tid < a.n_given) {
+    tok_now = tok_of(first_row);
+    tok_next = tok_of(first_row + row_step);
+    x_now = x_of(first_row, tok_now);
   }
-  if (TOP && n_parts > 1 && warp == 1) *cluster.map_shared_rank(&row_lists[part * 32 + lane], 0) = lists[lane];
-  if (n_parts > 1) cluster.sync(); else __syncthreads();
-  if (part != 0) return;
-  Stats all = row_stats[0];
-  for (int p = 1; p < n_parts; ++p) all = join(all, row_stats[p], to_log2);
-  // a row without a finite logit has no distribution: every log probability is -inf, the entropy 0
-  const bool none = all.s == 0.f;
-  const float log_sum = logf(all.s);
-  auto logprob = [&](float x) { return none ? -CUDART_INF_F : fmaf(x - all.ref, scale, -log_sum); };
-  if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : fmaf(-scale, all.t / all.s, log_sum);
-  if (tid < n_given) {
-    const int tok = a.tokens[(size_t)row * n_given + tid];
-    const bool real = (unsigned)tok < (unsigned)a.vocab;
-    const float x = real ? Vec<T>::load(x0 + tok) : CUDART_NAN_F;
-    a.logprob[(size_t)row * n_given + tid] = x == x ? logprob(x) : CUDART_NAN_F;
-    if (a.rank) {
+  int n = 0;                                                   // stages read so far
+  bool dead = false;
+  for (int row = first_row; row < n_rows; row += row_step) {
+    const Row r = row_of(row);
+    const float scale = a.scale ? a.scale[row] : 1.f, to_log2 = scale * 1.4426950408889634f, lowest = kNothing / to_log2;
+    if (GIVEN > 0 && tid < kMaxGiven) {
+      given_x[tid] = x_now;
+      given_tok[tid] = tok_now;
+    }
+    if (tid == 0) n_cand = 0;
+    work_sync();
+    if (GIVEN > 0 && tid < a.n_given) {                        // these loads fly until the next row
+      tok_now = tok_next;
+      x_now = x_of(row + row_step, tok_now);
+      tok_next = tok_of(row + 2 * row_step);
+    }
+    // Of a given token: its logit, the next number above (equal logits in front of it count, behind it not), its block. Nothing is in
+    // front of a NaN.
+    float gx[GIVEN > 0 ? GIVEN : 1], up[GIVEN > 0 ? GIVEN : 1], count[GIVEN > 0 ? GIVEN : 1];
+    int gb[GIVEN > 0 ? GIVEN : 1];
+#pragma unroll
+    for (int j = 0; j < GIVEN; ++j) {
+      gx[j] = given_x[j];
+      up[j] = Vec<T>::above(gx[j]);
+      gb[j] = (given_tok[j] + r.off) / N;
+      count[j] = 0.f;
+    }
+
+    // The sums against ref: of e(x) and of x e(x), which is one instruction less per logit (huge references: of (x - ref) e(x)).
+    float ref = -CUDART_INF_F, neg_log2 = 0.f;                 // and -fl(ref c)
+    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    float best = CUDART_NAN_F;                                 // this thread's largest logit (a NaN: none yet) and the first block that has it
+    int best_block = -1;
+    auto stats = [&]() {
+      const float sum = s0 + s1, t = t0 + t1;
+      return Stats{ref, sum, is_huge(ref) || ref == -CUDART_INF_F ? t : fmaf(-ref, sum, t)};
+    };
+    auto refer_to = [&](float mx) {                            // the first number too: the reference is -inf before it
+      if ((mx - ref) * to_log2 > kMove) {
+        const float f = ex2(log2_factor(ref, mx, to_log2));    // 0 the first time, and where ref was or becomes a huge one
+        ref = mx;
+        neg_log2 = -__fmul_rn(mx, to_log2);
+        s0 *= f; s1 *= f; t0 *= f; t1 *= f;
+      }
+    };
+    // One logit, whatever its size and the reference's.
+    auto take_exact = [&](float x) {
+      const float from = ref == -CUDART_INF_F ? 0.f : ref, d = x - from;
+      const bool huge = is_huge(ref);
+      const float e = ex2(huge ? d * to_log2 : fmaf(x, to_log2, neg_log2));
+      s0 += e;
+      t0 += huge ? e * fmaxf(d, lowest) : e == 0.f ? 0.f : e * x;
+    };
+    // U blocks, kThreads apart. What seldom happens is asked for once for all of them.
+    auto take = [&](auto count_tag, const uint4* blocks, int b0) {
+      constexpr int U = decltype(count_tag)::value;
+      uint4 v[U];
+      float mx[U], top = -CUDART_INF_F;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u] = blocks[u * kThreads];
+        mx[u] = Vec<T>::largest(v[u]);
+        top = fmaxf(top, mx[u]);
+        if (TOP && !(mx[u] <= best) && mx[u] == mx[u]) {
+          best = mx[u];
+          best_block = b0 + u * kThreads;
+        }
+      }
+      refer_to(top);
+      if (is_huge(ref)) {                                      // rows of the type's lowest value, and the like
+#pragma unroll 1
+        for (int i = 0; i < U * N; ++i) take_exact(Vec<T>::load(reinterpret_cast<const T*>(blocks + i / N * kThreads) + i % N));
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float x[N];
+          Vec<T>::unpack(Vec<T>::not_inf(v[u]), x);
+#pragma unroll
+          for (int i = 0; i < N; i += 2) {
+            const float e0 = ex2(fmaf(x[i], to_log2, neg_log2)), e1 = ex2(fmaf(x[i + 1], to_log2, neg_log2));
+            s0 += e0;
+            s1 += e1;
+            t0 = fmaf(e0, x[i], t0);
+            t1 = fmaf(e1, x[i + 1], t1);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < GIVEN; ++j) {
+        if (!(top >= gx[j])) continue;                         // nothing here is in front of the token: most blocks, if it is a likely one
+        bool mine = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u) mine = mine || b0 + u * kThreads == gb[j];
+        if (mine) {                                            // index by index, the token's own block is among them
+          const int tok = given_tok[j];
+#pragma unroll 1
+          for (int i = 0; i < U * N; ++i) {
+            const float x = Vec<T>::load(reinterpret_cast<const T*>(blocks + i / N * kThreads) + i % N);
+            count[j] += x > gx[j] || (x == gx[j] && (b0 + i / N * kThreads) * N - r.off + i % N < tok) ? 1.f : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < U; ++u) count[j] += Vec<T>::count_ge(v[u], b0 + u * kThreads < gb[j] ? gx[j] : up[j]);
+        }
+      }
+    };
+    // One logit of a block that the row fills in part.
+    auto take_one = [&](int t) {
+      const float x = Vec<T>::load(r.blocks + r.off + t);
+      refer_to(x);
+      take_exact(x);
+#pragma unroll
+      for (int j = 0; j < GIVEN; ++j) count[j] += x > gx[j] || (x == gx[j] && t < given_tok[j]) ? 1.f : 0.f;
+    };
+    // The row's tokens [0, head) and [tail, vocab) lie in such blocks: one thread each.
+    const int head = min(a.vocab, r.off > 0 ? N - r.off : 0), tail = max(head, (a.vocab + r.off) / N * N - r.off);
+    if (part == 0 && tid < head) take_one(tid);
+    if (part == n_parts - 1 && tid >= 32 && tid - 32 < a.vocab - tail) take_one(tail + tid - 32);
+    // ---------------------------------------------------------------------- the pass
+#pragma unroll 1
+    for (int b = r.begin; b < r.end; b += kStageBlocks, ++n) {
+      const int st = n % kStages;
+      dead = dead || !__all_sync(0xffffffffu, mbar_wait(full0 + 8 * st, (n / kStages) & 1));
+      if (!dead) {
+        const uint4* blocks = reinterpret_cast<const uint4*>(ring + st * kStageBytes);
+        if (r.end - b >= kStageBlocks) {
+          take(std::integral_constant<int, kPerThread>(), blocks + tid, b + tid);
+        } else {
+          for (int i = tid; i < r.end - b; i += kThreads) take(std::integral_constant<int, 1>(), blocks + i, b + i);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty0 + 8 * st);
+    }
+    Stats st = stats();
+    if (dead) st.s = CUDART_NAN_F;                             // a copy that never came: no result
+    // ---------------------------------------------------------------------- sums of the block
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) {
+      Stats o;
+      o.ref = __shfl_xor_sync(0xffffffffu, st.ref, sh);
+      o.s = __shfl_xor_sync(0xffffffffu, st.s, sh);
+      o.t = __shfl_xor_sync(0xffffffffu, st.t, sh);
+      st = join(st, o, to_log2);
+    }
+    if (lane == 0) warp_stats[warp] = st;
+#pragma unroll
+    for (int j = 0; j < GIVEN; ++j) {                          // a thread's counts are whole numbers below 2^24
+      const int sum = __reduce_add_sync(0xffffffffu, (int)count[j]);
+      if (lane == 0) warp_count[warp][j] = sum;
+    }
+
+    if constexpr (TOP) {
+      // -------------------------------------------------------------------- alternatives of the block
+      // the parts of the n threads that come first; a part is known by its first block
+      merge_lists(warp_sort(best_block < 0 ? 0 : key_of(best, (uint32_t)best_block), lane), lists, kWarps, warp, lane);
+      const uint64_t last = lists[a.n_top - 1];                // 0: fewer parts than that hold a number
+      const float last_x = last ? from_ordered((uint32_t)(last >> 32)) : -CUDART_INF_F;
+      const int last_block = last ? (int)place_of(last) : INT32_MAX;
+      const int per_part = (r.end - r.begin + kThreads - 1) / kThreads, n_items = a.n_top * per_part;
+      // block `it` of the chosen parts (-1: none)
+      auto block_of = [&](const uint64_t* parts, int it) {
+        const uint64_t k = parts[it / per_part];
+        if (k == 0) return -1;
+        const int b = r.begin + ((int)place_of(k) - r.begin) % kThreads + it % per_part * kThreads;
+        return b < r.end ? b : -1;
+      };
+      // key of token t, whose logit is x and lies in block b; 0 where it is none or behind the last part's largest
+      auto key_at = [&](float x, int b, int t) -> uint64_t { return x > last_x || (x == last_x && b <= last_block) ? key_of(x, (uint32_t)t) : 0; };
+      auto push = [&](uint64_t k) {
+        if (k) {
+          const int at = atomicAdd(&n_cand, 1);
+          if (at < kCand) cand[at] = k;
+        }
+      };
+      if (part == 0 && tid < head) push(key_at(Vec<T>::load(r.blocks + r.off + tid), 0, tid));
+      if (part == n_parts - 1 && tid >= 32 && tid - 32 < a.vocab - tail) {
+        const int t = tail + tid - 32;
+        push(key_at(Vec<T>::load(r.blocks + r.off + t), (t + r.off) / N, t));
+      }
+      for (int it0 = tid; it0 < n_items; it0 += 4 * kThreads) {
+        uint4 v[4];
+        int b[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int it = it0 + u * kThreads;
+          b[u] = it < n_items ? block_of(lists, it) : -1;
+          if (b[u] >= 0) v[u] = load16(r.blocks + (size_t)b[u] * N);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (b[u] < 0 || !(Vec<T>::largest(v[u]) >= last_x)) continue;      // most blocks
+          float x[N];
+          Vec<T>::unpack(v[u], x);
+#pragma unroll 1
+          for (int i = 0; i < N; ++i) {
+            float y = x[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) y = i == j ? x[j] : y;
+            push(key_at(y, b[u], b[u] * N - r.off + i));
+          }
+        }
+      }
+      work_sync();
+      const int n_found = n_cand;
+      if (n_found <= kCand) {
+        const int n_lists = min(kWarps, (n_found + 31) / 32);
+        uint64_t k = 0;
+        if (warp < n_lists) k = warp_sort(tid < n_found ? cand[tid] : 0, lane);
+        if (tid - lane + kThreads < n_found)                   // a second list of the warp's
+          k = warp_merge(k, warp_sort(tid + kThreads < n_found ? cand[tid + kThreads] : 0, lane), lane);
+        merge_lists(k, lists, n_lists, warp, lane);
+      } else {
+        // So many only where few parts have the larger share of a row's best tokens: all of these parts' tokens, as many at a time as
+        // there are threads, next to the best so far. The tokens of part-filled blocks, 2 N - 2 at most, come last.
+        if (tid < 32) cand[tid] = lists[tid];                  // the parts: `lists` is needed
+        work_sync();
+        uint64_t top32 = 0;                                    // warp 0: the best so far
+        const int n_elems = n_items * N;
+        for (int e0 = 0; e0 < n_elems + 64; e0 += kThreads) {
+          const int e = e0 + tid, odd = e - n_elems;
+          uint64_t k = 0;
+          if (e < n_elems) {
+            const int b = block_of(cand, e / N);
+            if (b >= 0) k = key_at(Vec<T>::load(r.blocks + (size_t)b * N + e % N), b, b * N - r.off + e % N);
+          } else if (odd < 32 ? part == 0 && odd < head : part == n_parts - 1 && odd - 32 < a.vocab - tail) {
+            const int t = odd < 32 ? odd : tail + odd - 32;
+            k = key_at(Vec<T>::load(r.blocks + r.off + t), (t + r.off) / N, t);
+          }
+          merge_lists(warp_sort(k, lane), lists, kWarps, warp, lane);
+          if (warp == 0) top32 = warp_merge(top32, lists[lane], lane);
+        }
+        work_sync();
+        if (warp == 0) lists[lane] = top32;
+        work_sync();
+      }
+    }
+    work_sync();
+    // ---------------------------------------------------------------------- the blocks of the row meet in the first one
+    if (warp == 0) {
+      Stats all = lane < kWarps ? warp_stats[lane] : Stats{-CUDART_INF_F, 0.f, 0.f};
+#pragma unroll
+      for (int sh = kWarps / 2; sh > 0; sh >>= 1) {
+        Stats o;
+        o.ref = __shfl_xor_sync(0xffffffffu, all.ref, sh);
+        o.s = __shfl_xor_sync(0xffffffffu, all.s, sh);
+        o.t = __shfl_xor_sync(0xffffffffu, all.t, sh);
+        all = join(all, o, to_log2);
+      }
+      if (lane == 0) *cluster.map_shared_rank(&row_stats[part], 0) = all;
+    } else if (warp == 1) {
+      if (TOP && n_parts > 1) *cluster.map_shared_rank(&row_lists[part * 32 + lane], 0) = lists[lane];
+    } else if (warp == 2 && lane < a.n_given) {
       int sum = 0;
-      for (int p = 0; p < n_parts; ++p) sum += row_count[p][tid];
-      a.rank[(size_t)row * n_given + tid] = x == x ? sum : -1;
+      for (int w = 0; w < kWarps; ++w) sum += warp_count[w][lane];
+      *cluster.map_shared_rank(&row_count[part][lane], 0) = sum;
     }
-  }
-  if constexpr (TOP) {
-    if (n_parts > 1) merge_lists(warp < n_parts ? row_lists[warp * 32 + lane] : 0, lists, n_parts, warp, lane);
-    if (tid < a.n_top) {
-      const uint64_t k = lists[tid];
-      a.top_token[(size_t)row * a.n_top + tid] = k ? (int32_t)place_of(k) : -1;
-      a.top_logprob[(size_t)row * a.n_top + tid] = k ? logprob(from_ordered((uint32_t)(k >> 32))) : CUDART_NAN_F;
+    if (n_parts > 1) cluster.sync(); else work_sync();
+    if (part != 0) return;                                     // a cluster has one row
+    Stats all = row_stats[0];
+    for (int p = 1; p < n_parts; ++p) all = join(all, row_stats[p], to_log2);
+    // a row without a finite logit has no distribution: every log probability is -inf, the entropy 0
+    const bool none = all.s == 0.f;
+    const float log2_sum = log2f(all.s), log_sum = kLn2 * log2_sum;
+    auto logprob = [&](float x) {
+      if (none) return -CUDART_INF_F;
+      if (is_huge(all.ref) || is_huge(x)) return fmaf(x - all.ref, scale, -log_sum);
+      return kLn2 * (fmaf(x, to_log2, -__fmul_rn(all.ref, to_log2)) - log2_sum);
+    };
+    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : fmaf(-scale, all.t / all.s, log_sum);
+    if (tid >= 32 && tid - 32 < a.n_given) {
+      const int j = tid - 32;
+      const float x = given_x[j];
+      a.logprob[(size_t)row * a.n_given + j] = x == x ? logprob(x) : CUDART_NAN_F;
+      if (a.rank) {
+        int sum = 0;
+        for (int p = 0; p < n_parts; ++p) sum += row_count[p][j];
+        a.rank[(size_t)row * a.n_given + j] = x == x ? sum : -1;
+      }
     }
+    if constexpr (TOP) {
+      if (n_parts > 1) merge_lists(warp < n_parts ? row_lists[warp * 32 + lane] : 0, lists, n_parts, warp, lane);
+      if (tid < a.n_top) {
+        const uint64_t k = lists[tid];
+        a.top_token[(size_t)row * a.n_top + tid] = k ? (int32_t)place_of(k) : -1;
+        a.top_logprob[(size_t)row * a.n_top + tid] = k ? logprob(from_ordered((uint32_t)(k >> 32))) : CUDART_NAN_F;
+      }
+    }
+    work_sync();
   }
 }
 
 template <typename T, int GIVEN, bool TOP>
-cudaError_t launch_t(const Args& a, int n_rows, int n_parts, cudaStream_t stream) {
+cudaError_t launch_t(const Args& a, int n_rows, int n_parts, int n_sms, cudaStream_t stream) {
+  constexpr int smem = kStages * kStageBytes;
+  const cudaError_t e = cudaFuncSetAttribute(logprobs_kernel<T, GIVEN, TOP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(n_rows * n_parts));
-  cfg.blockDim = dim3(kThreads);
+  const int at_a_time = kBlocksPerSm * n_sms, blocks = n_parts > 1 || n_rows < at_a_time ? n_rows * n_parts : at_a_time;
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kThreads + 32);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -409,14 +625,18 @@ cudaError_t launch_t(const Args& a, int n_rows, int n_parts, cudaStream_t stream
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, GIVEN, TOP>, a);
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, GIVEN, TOP>, a, n_rows);
+}
+template <typename T, int GIVEN>
+cudaError_t launch_g(const Args& a, int n_rows, int n_parts, int n_sms, cudaStream_t stream) {
+  return a.n_top > 0 ? launch_t<T, GIVEN, true>(a, n_rows, n_parts, n_sms, stream) : launch_t<T, GIVEN, false>(a, n_rows, n_parts, n_sms, stream);
 }
 template <typename T>
-cudaError_t launch(const Args& a, int n_rows, int n_parts, cudaStream_t stream) {
-  const bool top = a.n_top > 0;
-  if (a.n_given == 0) return top ? launch_t<T, 0, true>(a, n_rows, n_parts, stream) : launch_t<T, 0, false>(a, n_rows, n_parts, stream);
-  if (a.n_given == 1) return top ? launch_t<T, 1, true>(a, n_rows, n_parts, stream) : launch_t<T, 1, false>(a, n_rows, n_parts, stream);
-  return top ? launch_t<T, kMaxGiven, true>(a, n_rows, n_parts, stream) : launch_t<T, kMaxGiven, false>(a, n_rows, n_parts, stream);
+cudaError_t launch(const Args& a, int n_rows, int n_parts, int n_sms, cudaStream_t stream) {
+  if (a.n_given == 0) return launch_g<T, 0>(a, n_rows, n_parts, n_sms, stream);
+  if (a.n_given == 1) return launch_g<T, 1>(a, n_rows, n_parts, n_sms, stream);
+  if (a.n_given <= 4) return launch_g<T, 4>(a, n_rows, n_parts, n_sms, stream);
+  return launch_g<T, kMaxGiven>(a, n_rows, n_parts, n_sms, stream);
 }
 
 }  // namespace
@@ -439,12 +659,15 @@ extern "C" int ts_token_logprobs(const ts_logprobs* p, void* cuda_stream) {
   if (cudaSetDevice(p->device) != cudaSuccess) return TS_ERR_CUDA;
   ts::Args a = {p->logits, (long long)p->row_stride, p->scale, p->tokens, p->logprob, p->entropy, p->top_logprob, p->rank, p->top_token, p->vocab,
                 p->n_given, p->n_top};
+  int n_sms = 0;
+  if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess) return TS_ERR_CUDA;
   // Few rows: a row is shared, as long as every thread still has a 16-byte block.
   int parts = 1;
   const long long blocks = (long long)p->vocab * (long long)elem / 16;
-  while (parts < ts::kMaxCluster && (long long)p->n_rows * parts * 2 <= 296 && blocks / (parts * 2) >= ts::kThreads) parts *= 2;
+  while (parts < ts::kMaxCluster && (long long)p->n_rows * parts <= n_sms && blocks / (parts * 2) >= ts::kThreads) parts *= 2;
   if ((long long)p->n_rows * parts > INT32_MAX) return TS_ERR_UNSUPPORTED;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  const cudaError_t e = p->dtype == TS_BF16 ? ts::launch<uint16_t>(a, p->n_rows, parts, stream) : ts::launch<float>(a, p->n_rows, parts, stream);
+  const cudaError_t e = p->dtype == TS_BF16 ? ts::launch<uint16_t>(a, p->n_rows, parts, n_sms, stream)
+                                              : ts::launch<float>(a, p->n_rows, parts, n_sms, stream);
   return e == cudaSuccess ? TS_OK : TS_ERR_CUDA;
 }

@@ -41,13 +41,12 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
         raise ValueError(f"at most {MAX_GIVEN} given tokens and {MAX_TOP} alternatives per row")
     if scale is not None and (scale.dtype != torch.float32 or scale.device != dev or scale.numel() != rows or not scale.is_contiguous()):
         raise ValueError(f"scale must be a contiguous float32 tensor of {rows} values on {dev}")
-    f = torch.empty(rows * (given + n_top + 1), dtype=torch.float32, device=dev)
-    i = torch.empty(rows * (given + n_top), dtype=torch.int32, device=dev)
-    a, b = rows * given, rows * (given + n_top)
-    r = TokenLogprobs(f[:a].view(rows, given), i[:a].view(rows, given), f[b:], f[a:b].view(rows, n_top), i[a:].view(rows, n_top))
-    fp, ip = f.data_ptr(), i.data_ptr()
+    # one allocation for each: a slice of a common one costs the host more
+    lp, ent, top_lp = (torch.empty(n, dtype=torch.float32, device=dev) for n in ((rows, given), rows, (rows, n_top)))
+    rank, top = (torch.empty((rows, n), dtype=torch.int32, device=dev) for n in (given, n_top))
     args = B.ts_logprobs(dev.index, rows, vocab, B.TS_BF16 if logits.dtype == torch.bfloat16 else B.TS_F32, logits.data_ptr(),
                          logits.stride(0) if rows > 1 else vocab, None if scale is None else scale.data_ptr(),
-                         None if given == 0 else tokens.data_ptr(), given, n_top, fp, ip, fp + 4 * b, fp + 4 * a, ip + 4 * a)
+                         None if given == 0 else tokens.data_ptr(), given, n_top, lp.data_ptr(), rank.data_ptr(), ent.data_ptr(),
+                         top_lp.data_ptr(), top.data_ptr())
     _check(B.ts_token_logprobs(args, _raw_stream(dev.index)), "ts_token_logprobs")
-    return r
+    return TokenLogprobs(lp, rank, ent, top_lp, top)

@@ -13,8 +13,9 @@
 //
 // Alternatives cost the pass no more than its maximum: every thread keeps the largest logit of its own part of the row and where
 // that part first has it. The n best tokens lie in the n parts that come first by (that logit, that place), since each of these
-// holds a token at least as far in front as the last part's first one. Only those parts are read again (from L2), and of them only
-// what is not behind the last part's largest is sorted.
+// holds a token at least as far in front as the last part's first one. Of those parts the 16 bytes that hold the first best token are
+// read again, the others only where the part's second best such block is not behind the last part's largest either; what is not behind
+// that is sorted.
 //
 // What bounds it: HBM for fp32 logits and few given tokens. An SM's share of HBM is 11 bf16 logits a cycle, which is 11 instructions for
 // each; the sums take 6 and every given token one more.
@@ -243,7 +244,9 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
   __shared__ uint64_t row_lists[kMaxCluster * 32];
   __shared__ float given_x[kMaxGiven];                         // of the row's given tokens: logit (a NaN for one that is none), index
   __shared__ int32_t given_tok[kMaxGiven];
-  __shared__ int32_t n_cand;
+  __shared__ float seconds[kThreads];                          // see `second`
+  __shared__ uint64_t again[kMaxTop];                          // parts that are read again in whole
+  __shared__ int32_t n_cand, n_again;
   __shared__ __align__(8) uint64_t full[kStages], empty[kStages];
   cg::cluster_group cluster = cg::this_cluster();
   const int n_parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -323,7 +326,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
       given_x[tid] = x_now;
       given_tok[tid] = tok_now;
     }
-    if (tid == 0) n_cand = 0;
+    if (tid == 0) n_cand = n_again = 0;
     work_sync();
     if (GIVEN > 0 && tid < a.n_given) {                        // these loads fly until the next row
       tok_now = tok_next;
@@ -347,6 +350,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
     float best = CUDART_NAN_F;                                 // this thread's largest logit (a NaN: none yet) and the first block that has it
     int best_block = -1;
+    float second = -CUDART_INF_F;                              // the largest of its other blocks'
     auto stats = [&]() {
       const float sum = s0 + s1, t = t0 + t1;
       return Stats{ref, sum, is_huge(ref) || ref == -CUDART_INF_F ? t : fmaf(-ref, sum, t)};
@@ -377,6 +381,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
         v[u] = blocks[u * kThreads];
         mx[u] = Vec<T>::largest(v[u]);
         top = fmaxf(top, mx[u]);
+        if (TOP) second = fmaxf(second, fminf(fmaxf(best, -CUDART_INF_F), mx[u]));
         if (TOP && !(mx[u] <= best) && mx[u] == mx[u]) {
           best = mx[u];
           best_block = b0 + u * kThreads;
@@ -469,6 +474,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     if constexpr (TOP) {
       // -------------------------------------------------------------------- alternatives of the block
       // the parts of the n threads that come first; a part is known by its first block
+      seconds[tid] = second;
       merge_lists(warp_sort(best_block < 0 ? 0 : key_of(best, (uint32_t)best_block), lane), lists, kWarps, warp, lane);
       const uint64_t last = lists[a.n_top - 1];                // 0: fewer parts than that hold a number
       const float last_x = last ? from_ordered((uint32_t)(last >> 32)) : -CUDART_INF_F;
@@ -494,28 +500,25 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
         const int t = tail + tid - 32;
         push(key_at(Vec<T>::load(r.blocks + r.off + t), (t + r.off) / N, t));
       }
-      for (int it0 = tid; it0 < n_items; it0 += 4 * kThreads) {
-        uint4 v[4];
-        int b[4];
+      auto push_block = [&](const uint4& v, int b) {
+        if (!(Vec<T>::largest(v) >= last_x)) return;
+        float x[N];
+        Vec<T>::unpack(v, x);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int it = it0 + u * kThreads;
-          b[u] = it < n_items ? block_of(lists, it) : -1;
-          if (b[u] >= 0) v[u] = load16(r.blocks + (size_t)b[u] * N);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (b[u] < 0 || !(Vec<T>::largest(v[u]) >= last_x)) continue;      // most blocks
-          float x[N];
-          Vec<T>::unpack(v[u], x);
-#pragma unroll 1
-          for (int i = 0; i < N; ++i) {
-            float y = x[0];
-#pragma unroll
-            for (int j = 1; j < N; ++j) y = i == j ? x[j] : y;
-            push(key_at(y, b[u], b[u] * N - r.off + i));
-          }
-        }
+        for (int i = 0; i < N; ++i) push(key_at(x[i], b, b * N - r.off + i));
+      };
+      // A part's first best block, and the others only where another one has something as far in front as the last part.
+      if (tid >= 64 && tid - 64 < a.n_top && lists[tid - 64] != 0) {
+        const uint64_t k = lists[tid - 64];
+        const int b = (int)place_of(k);
+        push_block(load16(r.blocks + (size_t)b * N), b);
+        const float other = seconds[(b - r.begin) % kThreads];
+        if (other > last_x || (other == last_x && b + kThreads <= last_block)) again[atomicAdd(&n_again, 1)] = k;
+      }
+      work_sync();
+      for (int it = tid; it < n_again * per_part; it += kThreads) {
+        const int b = block_of(again, it);
+        if (b >= 0 && b != (int)place_of(again[it / per_part])) push_block(load16(r.blocks + (size_t)b * N), b);
       }
       work_sync();
       const int n_found = n_cand;

@@ -1063,9 +1063,61 @@ TreePlan choose_tree(const ts_ctx* c, int nodes, int cache) {
   return p;
 }
 
-// Work items of a tree step: see ts_tree.h. Rows are cut so that the units of all rows are about as many as thread blocks run at
-// a time, none shorter than kMinTreePages pages. A row's own nodes stay together.
-constexpr int kMinTreePages = 16;
+// Pages per piece of a tree step's rows. Of steps of few units (an item's KV heads and tiles) the one of whole rows and of the shortest pieces with
+// one, two and three units per thread block that runs at a time is taken whose units, dealt out longest first, are done soonest: the
+// longest one where each has a thread block to itself, else an even share and half a unit. A unit costs kUnitPages besides its own, the
+// merge kMergePages. Steps of more units cut what is longer than an even share. (us, 8B shape, cut by the even
+// share alone / so: one row of 32768 keys x 64 nodes 85 / 57, four of 2000 x 32 31 / 24, two of 16000 and 9000 x 1 30 / 23.)
+constexpr int kMinTreePages = 16, kUnitPages = 10, kMergePages = 12;
+int64_t tree_split(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
+  const int P = c->cfg.page_size, per_unit = tp.tile_tokens * tp.tiles_per_unit;
+  const int64_t blocks = (int64_t)tp.blocks_per_sm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
+  struct Cost {
+    int64_t units, pages, partials;
+    int longest;
+  };
+  auto cost = [&](int64_t per) {
+    Cost k = {};
+    for (int r = 0; r < st->n_rows; ++r) {
+      const int pages = ceil_div(st->ctx_len[r], P) + ceil_div(st->q_len[r], P), pieces = (int)((pages + per - 1) / per);
+      const int64_t copies = (int64_t)ceil_div(st->q_len[r], per_unit) * c->cfg.n_kv_heads;
+      k.units += copies * pieces;
+      k.pages += copies * pages;
+      k.longest = std::max(k.longest, ceil_div(pages, pieces));
+      if (pieces > 1) k.partials += (int64_t)st->q_len[r] * pieces;
+    }
+    return k;
+  };
+  const Cost whole = cost(INT32_MAX);
+  int64_t per = std::max<int64_t>(kMinTreePages, (whole.pages + blocks - 1) / blocks);
+  if (whole.units < 2 * blocks) {
+    auto time_of = [&](const Cost& k) {
+      const double unit = k.longest + kUnitPages, share = (double)(k.pages + k.units * kUnitPages) / blocks;
+      const double t = k.units <= blocks ? unit : std::max(unit, share + 0.5 * ((double)k.pages / k.units + kUnitPages));
+      return t + (k.partials > 0 ? kMergePages : 0);
+    };
+    double best = time_of(whole);
+    per = std::max(whole.longest, 1);
+    for (int waves = 1; waves <= 3; ++waves) {
+      if (whole.units > waves * blocks) continue;
+      int64_t lo = kMinTreePages, hi = whole.longest;        // the units never grow with the length of a piece
+      if (lo >= hi) break;
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (cost(mid).units <= waves * blocks) hi = mid; else lo = mid + 1;
+      }
+      const double t = time_of(cost(lo));
+      if (t < best) {
+        best = t;
+        per = lo;
+      }
+    }
+  }
+  while (cost(per).partials > c->L.max_partials) per *= 2;   // the partial results have to fit
+  return per;
+}
+
+// Work items of a tree step: see ts_tree.h. A row's own nodes stay together.
 void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   c->items.clear();
   c->combines.clear();
@@ -1073,16 +1125,7 @@ void plan_tree(ts_ctx* c, const ts_step* st, const TreePlan& tp) {
   c->n_prefill_items = 0;
   const int P = c->cfg.page_size;
   auto pages_of = [&](int r) { return ceil_div(st->ctx_len[r], P) + ceil_div(st->q_len[r], P); };
-  int64_t work = 0;
-  for (int r = 0; r < st->n_rows; ++r) work += (int64_t)pages_of(r) * ceil_div(st->q_len[r], tp.tile_tokens * tp.tiles_per_unit) * c->cfg.n_kv_heads;
-  const int blocks = tp.blocks_per_sm * (c->n_sms > 0 ? c->n_sms : kSmsB200);
-  int64_t per = std::max<int64_t>(kMinTreePages, (work + blocks - 1) / blocks);
-  for (;; per *= 2) {                                        // the partial results have to fit
-    int64_t partials = 0;
-    for (int r = 0; r < st->n_rows; ++r)
-      if (pages_of(r) > per) partials += (int64_t)st->q_len[r] * ((pages_of(r) + per - 1) / per);
-    if (partials <= c->L.max_partials) break;
-  }
+  const int64_t per = tree_split(c, st, tp);
   int partial = 0;
   for (int r = 0; r < st->n_rows; ++r) {
     const int cached = ceil_div(st->ctx_len[r], P), pages = pages_of(r), T = st->q_len[r], pieces = (int)((pages + per - 1) / per);

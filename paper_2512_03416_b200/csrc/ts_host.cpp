@@ -1049,13 +1049,22 @@ struct TreePlan {
   int n_tiles;             // units of the longest row, per item and KV head
   int blocks_per_sm;       // that run at a time
 };
-// Queries per KV head of the row with most nodes above which a step runs on tcgen05 (head_dim 128). us of 37 rows of 8192 keys of the 8B shape,
-// streamed / on tcgen05, by nodes: bf16 one 188 / 203, four 195 / 207, eight 210 / 208, 16 (in two tiles) 420 / 210; 8 bits one 128 / 178, four 193 /
-// 176, eight 277 / 180.
-constexpr int kTreeTcQueries = 32, kTreeTcQueries8 = 8;
-TreePlan choose_tree(const ts_ctx* c, int nodes, int cache) {
+// A step of a head_dim of 128 runs on tcgen05 where the row with most nodes has more queries per KV head than this; in 8 bits, where a unit costs more
+// there, only if its rows have kTreeTcKeys8 cached tokens on average, more than 32 queries (two tiles when streamed) always. us, streamed / on
+// tcgen05, 8B shape (four queries a node): bf16, 37 rows of 8192 keys x 1, 4, 8, 16 nodes 194 / 207, 203 / 210, 211 / 210, 401 / 214;
+// 64 rows x 4 nodes of 500 and 4000 keys 41 / 50, 163 / 189, x 5 nodes of 500 57 / 52, 8 rows of 4000 x 5 45 / 37. 8 bits, 37 rows of 8192 keys x 1, 2,
+// 4, 8 nodes 131 / 171, 133 / 171, 188 / 160, 277 / 164; 64 rows x 4 nodes of 500, 2000 and 4000 keys 48 / 64, 114 / 112, 175 / 176, 16 rows of
+// 4000 56 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 48 / 58, 74 / 66, 112 / 85.
+constexpr int kTreeTcQueries = 16, kTreeTcQueries8 = 8;
+constexpr int kTreeTcKeys8[2] = {4000, 400};               // up to 16 queries, up to 32
+bool tree_on_tc(const ts_ctx* c, int nodes, int64_t mean_keys, int cache) {
+  const int queries = nodes * c->G;
+  if (c->cfg.head_dim != 128 || queries <= (cache == TS_CACHE_E4M3 ? kTreeTcQueries8 : kTreeTcQueries)) return false;
+  return cache != TS_CACHE_E4M3 || queries > 32 || mean_keys >= kTreeTcKeys8[queries > 16];
+}
+TreePlan choose_tree(const ts_ctx* c, int nodes, int64_t mean_keys, int cache) {
   TreePlan p = {};
-  p.tc = c->cfg.head_dim == 128 && nodes * c->G > (cache == TS_CACHE_E4M3 ? kTreeTcQueries8 : kTreeTcQueries);
+  p.tc = tree_on_tc(c, nodes, mean_keys, cache);
   p.tile_tokens = p.tc ? 128 / c->G : ts::tree_tile_tokens(c->G, nodes);
   p.tiles_per_unit = p.tc && nodes > p.tile_tokens ? 2 : 1;
   p.n_tiles = ceil_div(nodes, p.tile_tokens * p.tiles_per_unit);
@@ -1495,10 +1504,14 @@ int ts_tree_attention(ts_ctx* c, const ts_step* st, int32_t cache, const uint64_
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   ts::TreeArgs a = {};
   int nodes = 0;
-  for (int r = 0; r < st->n_rows; ++r) nodes = std::max(nodes, st->q_len[r]);
+  int64_t keys = 0;
+  for (int r = 0; r < st->n_rows; ++r) {
+    nodes = std::max(nodes, st->q_len[r]);
+    keys += st->ctx_len[r];
+  }
   a.mask = mask;
   if (cache == TS_CACHE_E4M3) a.cache = ts::Cache8{(uint8_t*)c->cache8.values, (uint8_t*)c->cache8.scales};
-  const TreePlan tp = choose_tree(c, nodes, cache);
+  const TreePlan tp = choose_tree(c, nodes, keys / st->n_rows, cache);
   a.tile_tokens = tp.tile_tokens;
   a.n_tiles = tp.n_tiles;
   plan_tree(c, st, tp);

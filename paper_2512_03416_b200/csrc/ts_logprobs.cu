@@ -6,7 +6,7 @@
 // One pass over the logits (they are what has to be read; everything else is a few values a row). A row is a thread block's, and a
 // block takes row after row; where there are few rows, one is a cluster's of up to eight blocks, which leave their sums in the first one's
 // shared memory. A warp of its own copies the row into a ring of 16 KB stages (cp.async.bulk), across the ends of rows, so
-// that memory is busy while the other sixteen warps choose a row's alternatives. Per element a thread adds up e = exp(scale (x - ref)) and x e
+// that memory is busy while the other eight warps choose a row's alternatives. Per element a thread adds up e = exp(scale (x - ref)) and x e
 // against a logit ref that only moves when one exceeds it by a factor of 2^64 (any reference is exact; fp32 has the
 // range), and counts what lies in front of the given tokens: bf16 logits two at a time, as pairs of ones that are added up, and no
 // block of 16 bytes whose largest logit is behind the token.
@@ -17,8 +17,12 @@
 // read again, the others only where the part's second best such block is not behind the last part's largest either; what is not behind
 // that is sorted.
 //
-// What bounds it: HBM for fp32 logits and few given tokens. An SM's share of HBM is 11 bf16 logits a cycle, which is 11 instructions for
-// each; the sums take 6 and every given token one more.
+// What bounds it: HBM for fp32 logits without given tokens (2000 rows of 100003: 127 us, 6.3 TB/s = 0.98 of a copy; with 20 alternatives 150). For
+// bf16 the issue of instructions: an SM's share of HBM is 11 logits a cycle, which is 11 instructions for each; the sums and the maximum take
+// about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 66 us without given
+// tokens, 84 with one and 5 alternatives, 70 % of the issue slots, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 77). One row of 32000: 14 us on
+// the device, all of it round trips (cluster launch, copies, two sorts, the cluster's barrier). Tried and dropped: blocks of 16 warps (a row's end
+// then idles the SM), sums in packed pairs (moves ate the gain).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -513,7 +517,10 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
         const int b = (int)place_of(k);
         push_block(load16(r.blocks + (size_t)b * N), b);
         const float other = seconds[(b - r.begin) % kThreads];
-        if (other > last_x || (other == last_x && b + kThreads <= last_block)) again[atomicAdd(&n_again, 1)] = k;
+        // of logits equal to the last part's largest those count that lie no further behind: in the part's blocks behind b, and, where b holds a
+        // larger one, in those in front of it
+        const int from = from_ordered((uint32_t)(k >> 32)) > other ? r.begin + (b - r.begin) % kThreads : b + kThreads;
+        if (other > last_x || (other == last_x && from <= last_block)) again[atomicAdd(&n_again, 1)] = k;
       }
       work_sync();
       for (int it = tid; it < n_again * per_part; it += kThreads) {

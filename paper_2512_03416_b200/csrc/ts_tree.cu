@@ -15,6 +15,12 @@
 // Weights are f16 there, shifted by 2^15: normal numbers down to 2^-29 of the largest. A row's own nodes are not quantised: they
 // are laid into shared memory as f16 with a power of two per row, which the same code multiplies (eight significant bits of bf16
 // fit f16's eleven; an element below 2^-28 of its row's largest rounds).
+//
+// What bounds it (37 rows of 8192 keys, 8 KV heads of 128, 4 query heads each): HBM in bf16, one node 1.24 GB in 188 to 194 us, what a copy
+// takes; four nodes 203. In 8 bits one node 0.64 GB in 129 us (4.9 TB/s): the instructions that widen the codes and the MMAs that pad 4 queries
+// to 8 (59 % of the issue slots, tensor pipe 15 %); from 9 queries on a second and fourth MMA per widened operand, 188 us for four nodes,
+// 277 for eight. Tried and dropped: K Q^T in e4m3 against two addends of Q (one node 125, but four 235), codes widened by conversion
+// instructions (163), scales by bulk copies instead of cp.async (no difference).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -514,7 +520,8 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
   }
 }
 
-// Merge of the splits of a row's nodes: a warp per (node, head), D / 32 elements a lane, eight splits' loads in flight.
+// Merge of the splits of a row's nodes: a warp per (node, head), D / 32 elements a lane, eight splits' loads in flight. Bound by its round trips:
+// 12 pages' worth of a unit in the host's rule for pieces (about 3 us behind one row of 32768 keys x 64 nodes, whose partials stay in L2).
 template <int D>
 __global__ void __launch_bounds__(256)
 tree_combine_kernel(const __grid_constant__ StepParams<kInlineWords> params) {

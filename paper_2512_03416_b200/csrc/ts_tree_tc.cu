@@ -12,8 +12,12 @@
 // take every block. A unit of one tile gives the slots its blocks in turn, as two splits, which are added up in the epilogue.
 //
 // What bounds it: a tile of 128 rows takes 1024 cycles of MMAs and as many of exponentials per block; the block's K and V take
-// 2850 cycles of an SM's share of HBM in bf16, 1430 in 8 bits. Units of one tile are HBM's, units of two tiles the chain's of a
-// tile (scores, exponentials, P V, next scores).
+// 2850 cycles of an SM's share of HBM in bf16, 1430 in 8 bits. Units of one tile are HBM's in bf16 (37 rows of 8192 keys x 16 nodes, 8 KV heads x 4
+// query heads: 1.24 GB in 207 us, 6.0 TB/s = 0.93 of a copy). In 8 bits they are their own chain's (the same: 0.64 GB in 170 us, 3.7 TB/s):
+// about 2600 cycles per block from P V over the widening of the next V to the next P V, with the looks at barriers of the one MMA issuer.
+// Units of two tiles are the chain's of a tile (scores, exponentials, P V, next scores; 4100 to 4700 cycles per block; 37 rows of 4096 keys x
+// 32 nodes, 8 KV heads x 8 query heads: 161 us, 0.58 of the MMAs' rate, in 8 bits 192). A change of units costs 5 to 10 us of latency where
+// rows are short, because a unit's epilogue and the next one's first scores follow each other.
 //
 // 8-bit cache: K goes to the tensor cores as it is (kind::f8f6f4). The queries are two e4m3 addends each, q = (q1 + q2) 2^e with
 // a power of two per row: bf16's eight significant bits are twice e4m3's four, so the sum is exact down to 2^-9 of the row's
@@ -172,7 +176,8 @@ __device__ __forceinline__ void split8(const uint4& w, float by, uint2& hi, uint
   cache8_split(w.z, w.w, by, hi.y, lo.y);
 }
 // Query q of a tile sits in this row of its operand and TMEM lane: sixteen at a time go to the four lane quarters in turn, each of which is one SM
-// sub-partition's, so that few queries use all four (37 rows of 8192 keys x 16 nodes x 4 heads in 8 bits: see the table of measurements below).
+// sub-partition's, so that few queries use all four. (Together with the second pair of transform
+// warps, which came at the same time: 64 rows of up to 16 nodes x 4 heads in 8 bits 193 -> 163 us.)
 __device__ __forceinline__ int row_of(int q) { return (q >> 4 & 3) * 32 + (q >> 6) * 16 + (q & 15); }
 // 16-byte chunk c (of eight 16-bit elements) of row r of a 16-bit operand tile; eight codes c of row r of an 8-bit one
 __device__ __forceinline__ uint32_t at16(int r, int c) { return (uint32_t)((c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4)); }

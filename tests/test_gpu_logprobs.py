@@ -145,3 +145,14 @@ def test_refusals():
             f()
     r = token_logprobs(x[:0], t[:0], 3)
     assert r.logprob.shape == (0, 1) and r.top_token.shape == (0, 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,n_top", [(200, 40000, 3), (200, 40000, 12), (40, 131072, 5), (160, 131072, 20), (3, 50001, 9)])
+def test_alternatives_with_equal_logits(rows, vocab, n_top, dtype):
+    """A few dozen logits of few sizes in front of all others, anywhere in the row: the lower index of equal ones comes first."""
+    g = torch.Generator(device="cuda").manual_seed(rows + vocab + n_top)
+    x = torch.randn(rows, vocab, generator=g, device="cuda").clamp(max=2.0)
+    at = torch.randint(0, vocab, (rows, 40), generator=g, device="cuda")
+    x.scatter_(1, at, 4.0 + torch.randint(0, 4, (rows, 40), generator=g, device="cuda").float() * 0.5)
+    _check(x.to(dtype), None, n_top)

@@ -91,9 +91,12 @@ struct Map {
     TAB_FULL = V_EMPTY + kVStages, TAB_EMPTY = TAB_FULL + kTabStages,     // Q8: the exponents of a block of cached tokens
     OWN_TAB = TAB_EMPTY + kTabStages,                                     // [2] what there is to know of a block of nodes
     K_OWN = OWN_TAB + 2,                                          // K of the row's own nodes is there
-    S_FULL, P_FULL = S_FULL + 2,                                          // [slot][half of the keys]
+    // [4] K's stage for a row's own nodes is theirs: as many as the ring has stages at most, since that barrier's phases are not followed by those who
+    // fill the stage
+    OWN_FREE, S_FULL = OWN_FREE + 4, P_FULL = S_FULL + 2,                                          // [slot][half of the keys]
     O_FULL = P_FULL + 4, O_EMPTY = O_FULL + 2, XCHG, DRAIN = XCHG + 4, COUNT
   };
+  static_assert(kKStages <= 4, "OWN_FREE");
   static constexpr int kOffMisc = kOffBar + COUNT * 8;                    // TMEM address, failure flag
   static constexpr int kBytes = kOffMisc + 16;
 };
@@ -272,7 +275,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
     for (int i = 0; i < L::COUNT; ++i) {
       int n = 1;
       if (i >= L::UNIT_EMPTY && i < L::UNIT_EMPTY + kUnitRing) n = kUnitReaders + (Q8 ? 1 : 0);
-      if (i == L::Q_FULL || i == L::K_OWN || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::OWN_TAB && i < L::K_OWN)) n = kTransformWarps;
+      if (i == L::Q_FULL || (i >= L::RAW_EMPTY && i < L::V_EMPTY) || (i >= L::OWN_TAB && i < L::K_OWN)) n = kTransformWarps;
+      if (i == L::K_OWN) n = kTransformWarps / 2;
       if (i >= L::P_FULL && i < L::O_FULL) n = 8;             // softmax warps of the slot
       if (i == L::O_EMPTY) n = 16;
       if (i >= L::XCHG && i < L::DRAIN) n = 4;                // the warps of a lane quarter, of both slots
@@ -650,18 +654,18 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           unsigned char* dst = smem + L::kOffQ + tile * kTile;
 #pragma unroll 1
           for (int i0 = 0; i0 < 8; i0 += 4) {
-            if ((w * 16 + i0 * 2) / G >= cnt) break;   // the rest of the warp's are no queries: whatever the tile holds there stays
+            if ((i0 * 16 + w * 2) / G >= cnt) break;   // the rest of the warp's are no queries: whatever the tile holds there stays
             uint4 x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int r = w * 16 + (i0 + i) * 2 + half;
+              const int r = (i0 + i) * 16 + w * 2 + half;
               x[i] = make_uint4(0, 0, 0, 0);
               if (r / G < cnt)
                 x[i] = *reinterpret_cast<const uint4*>(src + ((r / G) * s.Hq + r % G) * kD);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int r = w * 16 + (i0 + i) * 2 + half;
+              const int r = (i0 + i) * 16 + w * 2 + half;
               if constexpr (Q8) {
                 uint32_t most = max_magnitude(x[i]);
 #pragma unroll
@@ -693,8 +697,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           unsigned char* vt = smem + L::kOffV + st * kTile;
           const int end = own ? u.T : n_keys - j * kBlock;
           if constexpr (Q8) {
-            if (g >= L::kVStages && !(ok = wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1))) break;
             if (!own) {
+              if (g >= L::kVStages && !(ok = wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1))) break;
               const int tb = raw % kTabStages;
               if (!(ok = wait_both(L::TAB_FULL + tb, (raw / kTabStages) & 1, L::V_LANDED + raw % kRaw, (raw / kRaw) & 1))) break;
               const unsigned char* codes = smem + L::kOffRaw + raw % kRaw * kTile8;
@@ -726,8 +730,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               continue;
             }
           } else {
-            if (!(ok = wait(L::V_LANDED + st, (g / L::kVStages) & 1))) break;
             if (!own) {
+              if (!(ok = wait(L::V_LANDED + st, (g / L::kVStages) & 1))) break;
               // rows behind the block's last key may hold anything, and 0 * NaN is none
               for (int i = w * 32 + lane; i < (kBlock - end) * 16; i += kTransformWarps * 32) *reinterpret_cast<uint4*>(vt + at16(end + (i >> 4), i & 15)) = make_uint4(0, 0, 0, 0);
               if (end < kBlock) fence_proxy_async();
@@ -735,82 +739,104 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               continue;
             }
           }
-          // ---- the row's own nodes: warps 0 and 1 take V of 32 nodes each, warps 2 and 3 K
+          // ---- the row's own nodes: sixteen of them for each warp, V for warps 0-3, K for warps 4-7, four loads under way at a time. K does not wait for
+          // V's stage: the scores of the nodes are wanted before their V.
           const int kst = g % L::kKStages, tb = kTabStages + (n_own & 1);
           [[maybe_unused]] float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + tb * kBlock;
-          if (!(ok = wait(L::K_FULL + kst, (g / L::kKStages) & 1))) break;        // the K loader has seen the stage empty
-          unsigned char* kt = smem + L::kOffK + kst * L::kKBytes;
-          const int r0 = (w & 1) * 32;
-          const uint16_t* src = (w < 2 ? s.v_new : s.k_new) + ((size_t)u.tok0 * s.Hkv + u.head) * kD + ch * 8;
-          auto load = [&](int r) { return r < end ? *reinterpret_cast<const uint4*>(src + (size_t)r * s.Hkv * kD) : make_uint4(0, 0, 0, 0); };
-          auto row_max = [&](const uint4& x) {               // over the sixteen lanes of a row
-            uint32_t most = max_magnitude(x);
+          const int r0 = (w & 3) * 16;
+          const uint16_t* src = (w < 4 ? s.v_new : s.k_new) + ((size_t)u.tok0 * s.Hkv + u.head) * kD + ch * 8;
+          auto load4 = [&](int from, uint4 (&x)[4]) {        // two rows at a time
 #pragma unroll
-            for (int sh = 1; sh < 16; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
-            return most;
+            for (int i = 0; i < 4; ++i) {
+              const int r = from + i * 2 + half;
+              x[i] = r < end ? *reinterpret_cast<const uint4*>(src + (size_t)r * s.Hkv * kD) : make_uint4(0, 0, 0, 0);
+            }
           };
-          if (w >= 4) {
-            // nothing: the nodes are few
-          } else if (w < 2) {
+          uint4 x[4];
+          if (w < 4) {
             uint32_t bad = 0, most = 0;
-            if constexpr (Q8) {                              // the largest finite element of the 32 rows goes to 2^14 .. 2^15
-#pragma unroll 2
-              for (int i = 0; i < 16; ++i) {
-                const uint4 x = load(r0 + i * 2 + half);
-                const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x));
-                if (!(odd & (0xffffu << (half * 16)))) most = max(most, max_magnitude(x));
+            if constexpr (Q8) {                              // the largest finite element of 32 rows goes to 2^14 .. 2^15: two warps look at them all
+#pragma unroll 1
+              for (int from = r0 & ~31; from < min((r0 & ~31) + 32, end); from += 8) {
+                load4(from, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x[i]));
+                  if (!(odd & (0xffffu << (half * 16)))) most = max(most, max_magnitude(x[i]));
+                }
               }
               most = __reduce_max_sync(0xffffffffu, most);
             }
             const int e_v = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);
             const float down = power(-e_v);
-#pragma unroll 2
-            for (int i = 0; i < 16; ++i) {
-              const int r = r0 + i * 2 + half;
-              uint4 x = load(r);
-              const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x));
-              if (odd & (0xffffu << (half * 16))) x = make_uint4(0, 0, 0, 0);       // must not reach the nodes that do not see it; a NaN score for the others
-              bad |= (odd & 0xffffu ? 1u : 0u) << (i * 2) | (odd >> 16 ? 2u : 0u) << (i * 2);
-              if constexpr (Q8) {
-                auto lo = [&](uint32_t y) { return __uint_as_float(y << 16) * down; };
-                auto hi = [&](uint32_t y) { return __uint_as_float(y & 0xffff0000u) * down; };
-                x = make_uint4(pack_f16(lo(x.x), lo(x.y)), pack_f16(hi(x.x), hi(x.y)), pack_f16(lo(x.z), lo(x.w)), pack_f16(hi(x.z), hi(x.w)));
+            load4(r0, x);
+            if constexpr (Q8) ok = g < L::kVStages || wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1);
+            else ok = wait(L::V_LANDED + st, (g / L::kVStages) & 1);
+            if (!ok) break;
+#pragma unroll 1
+            for (int from = 0; from < 16; from += 8) {
+              if (from > 0) load4(r0 + from, x);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = r0 + from + i * 2 + half;
+                const uint32_t odd = __ballot_sync(0xffffffffu, not_finite(x[i]));
+                if (odd & (0xffffu << (half * 16))) x[i] = make_uint4(0, 0, 0, 0);       // must not reach the nodes that do not see it; a NaN score for the others
+                bad |= (odd & 0xffffu ? 1u : 0u) << (from + i * 2) | (odd >> 16 ? 2u : 0u) << (from + i * 2);
+                if constexpr (Q8) {
+                  auto lo = [&](uint32_t y) { return __uint_as_float(y << 16) * down; };
+                  auto hi = [&](uint32_t y) { return __uint_as_float(y & 0xffff0000u) * down; };
+                  x[i] = make_uint4(pack_f16(lo(x[i].x), lo(x[i].y)), pack_f16(hi(x[i].x), hi(x[i].y)), pack_f16(lo(x[i].z), lo(x[i].w)), pack_f16(hi(x[i].z), hi(x[i].w)));
+                }
+                *reinterpret_cast<uint4*>(vt + at16(r, ch)) = x[i];
+                *reinterpret_cast<uint4*>(vt + at16(64 + r, ch)) = make_uint4(0, 0, 0, 0);
               }
-              *reinterpret_cast<uint4*>(vt + at16(r, ch)) = x;
-              *reinterpret_cast<uint4*>(vt + at16(64 + r, ch)) = make_uint4(0, 0, 0, 0);
             }
             if (lane == 0) {
-              reinterpret_cast<uint32_t*>(smem + L::kOffBad + (n_own & 1) * 8)[w] = bad;
-              if constexpr (Q8) {
-                float* e = reinterpret_cast<float*>(smem + L::kOffExp + tb * 32);
-                e[w] = (float)e_v;
-                e[4 + w] = down;
-                e[2 + w] = 0.f;
-                e[6 + w] = 1.f;
+              reinterpret_cast<uint16_t*>(smem + L::kOffBad + (n_own & 1) * 8)[w] = (uint16_t)bad;
+              if (Q8 && (w & 1) == 0) {
+                float* e = reinterpret_cast<float*>(smem + L::kOffExp + tb * 32) + (w >> 1);
+                e[0] = (float)e_v;
+                e[4] = down;
+                e[2] = 0.f;
+                e[6] = 1.f;
               }
             }
+            fence_proxy_async();
+            arrive(L::OWN_TAB + (n_own & 1));
           } else {
-#pragma unroll 2
-            for (int i = 0; i < 16; ++i) {
-              const int r = r0 + i * 2 + half;
-              const uint4 x = load(r);
-              if constexpr (Q8) {
-                const uint32_t most = row_max(x);
-                const int e_k = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 7, -kCache8MaxExp), kCache8MaxExp);
-                uint2 hi, lo;
-                split8(x, power(-e_k), hi, lo);
-                *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
-                *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
-                if (ch == 0) tab[tab_at(r)] = power(e_k);
-              } else {
-                *reinterpret_cast<uint4*>(kt + at16(r, ch)) = x;
+            load4(r0, x);
+            if (!(ok = wait(L::OWN_FREE + (n_own & 3), (n_own >> 2) & 1))) break;
+            unsigned char* kt = smem + L::kOffK + kst * L::kKBytes;
+#pragma unroll 1
+            for (int from = 0; from < 16; from += 8) {
+              if (from > 0) load4(r0 + from, x);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = r0 + from + i * 2 + half;
+                if constexpr (Q8) {
+                  uint32_t most = max_magnitude(x[i]);       // over the sixteen lanes of a row
+#pragma unroll
+                  for (int sh = 1; sh < 16; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
+                  const int e_k = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 7, -kCache8MaxExp), kCache8MaxExp);
+                  uint2 hi, lo;
+                  split8(x[i], power(-e_k), hi, lo);
+                  *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
+                  *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
+                  if (ch == 0) tab[tab_at(r)] = power(e_k);
+                } else {
+                  *reinterpret_cast<uint4*>(kt + at16(r, ch)) = x[i];
+                }
               }
             }
+            fence_proxy_async();
+            arrive(L::OWN_TAB + (n_own & 1));
+            arrive(L::K_OWN);
+            // V's barrier counts this warp too, not before its stage's last block was multiplied
+            if constexpr (Q8) ok = g < L::kVStages || wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1);
+            else ok = wait(L::V_LANDED + st, (g / L::kVStages) & 1);
+            if (!ok) break;
           }
-          fence_proxy_async();
-          arrive(L::OWN_TAB + (n_own & 1));
           ++n_own;
-          arrive(L::K_OWN);
           arrive(L::V_FULL + st);
         }
         if (ok) arrive(L::UNIT_EMPTY + ring);
@@ -828,7 +854,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       const int stage_bytes = kv == 0 ? L::kKBytes : Q8 ? kTile8 : kTile;
       const int n_tiles = a.n_tiles, n_units = s.n_items * s.Hkv * n_tiles;
       int fetched = -1;                                      // unit that the queue has handed out (K loader)
-      int g = 0;                                             // blocks through this ring
+      int g = 0, n_own = 0;                                  // blocks through this ring; of these of nodes
       bool ok = true;
       for (int k = 0; ok; ++k) {
         if (kv == 0) {
@@ -900,7 +926,11 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           const int page_next = j + 1 < n_cached ? fetch_page(j + 1) : 0;
           if (g >= stages && !(ok = wait(empty + st, ((g / stages) & 1) ^ 1))) break;
           if (j == n_cached) {
-            if (lane == 0) mbar_arrive(bar(landed + st));    // the transform warps fill the stage
+            if (lane == 0) {                                 // the transform warps fill the stage
+              mbar_arrive(bar(landed + st));
+              if (kv == 0) mbar_arrive(bar(L::OWN_FREE + (n_own & 3)));
+            }
+            ++n_own;
           } else {
             const int n_pg = min(kBlockPages, n_pages - j * kBlockPages);
             if (lane == 0) mbar_expect_tx(bar(landed + st), n_pg * kCopyBytes * (kCopies / kBlockPages));

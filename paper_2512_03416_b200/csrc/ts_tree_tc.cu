@@ -13,11 +13,13 @@
 //
 // What bounds it: a tile of 128 rows takes 1024 cycles of MMAs and as many of exponentials per block; the block's K and V take
 // 2850 cycles of an SM's share of HBM in bf16, 1430 in 8 bits. Units of one tile are HBM's in bf16 (37 rows of 8192 keys x 16 nodes, 8 KV heads x 4
-// query heads: 1.24 GB in 207 us, 6.0 TB/s = 0.93 of a copy). In 8 bits they are their own chain's (the same: 0.64 GB in 170 us, 3.7 TB/s):
+// query heads: 1.24 GB in 206 us, 6.0 TB/s = 0.93 of a copy). In 8 bits they are their own chain's (the same: 0.64 GB in 165 to 170 us, 3.8 TB/s):
 // about 2600 cycles per block from P V over the widening of the next V to the next P V, with the looks at barriers of the one MMA issuer.
 // Units of two tiles are the chain's of a tile (scores, exponentials, P V, next scores; 4100 to 4700 cycles per block; 37 rows of 4096 keys x
-// 32 nodes, 8 KV heads x 8 query heads: 161 us, 0.58 of the MMAs' rate, in 8 bits 192). A change of units costs 5 to 10 us of latency where
-// rows are short, because a unit's epilogue and the next one's first scores follow each other.
+// 32 nodes, 8 KV heads x 8 query heads: 160 us, 0.58 of the MMAs' rate, in 8 bits 192). A change of units costs 5 us of latency where
+// rows are short, because a unit's epilogue and the next one's first scores follow each other (64 rows of 500 keys x 8 nodes 47 us, of 22 for their bytes).
+// It took 8 when four warps laid out a row's nodes two rows at a time; loads of the next unit's queries ahead of the wait for their place
+// gained 0.5 % in bf16 and lost 7 in 8 bits (the widening then keeps fewer loads under way).
 //
 // 8-bit cache: K goes to the tensor cores as it is (kind::f8f6f4). The queries are two e4m3 addends each, q = (q1 + q2) 2^e with
 // a power of two per row: bf16's eight significant bits are twice e4m3's four, so the sum is exact down to 2^-9 of the row's

@@ -22,7 +22,8 @@
 // about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 66 us without given
 // tokens, 84 with one and 5 alternatives, 70 % of the issue slots, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 77). One row of 32000: 14 us on
 // the device, all of it round trips (cluster launch, copies, two sorts, the cluster's barrier). Tried and dropped: blocks of 16 warps (a row's end
-// then idles the SM), sums in packed pairs (moves ate the gain).
+// then idles the SM), sums in packed pairs (moves ate the gain),
+// counts as sums of comparison masks (bf16 1 % at most, fp32 a third slower). Five and more given tokens with alternatives spill 5 registers, seldom read.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>

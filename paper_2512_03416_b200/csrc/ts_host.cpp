@@ -1051,12 +1051,12 @@ struct TreePlan {
 };
 // A step of a head_dim of 128 runs on tcgen05 where the row with most nodes has more queries per KV head than this; in 8 bits, where a unit costs more
 // there, only if its rows have kTreeTcKeys8 cached tokens on average, more than 32 queries (two tiles when streamed) always. us, streamed / on
-// tcgen05, 8B shape (four queries a node): bf16, 37 rows of 8192 keys x 1, 4, 8, 16 nodes 194 / 207, 203 / 210, 211 / 210, 401 / 214;
-// 64 rows x 4 nodes of 500 and 4000 keys 41 / 50, 163 / 189, x 5 nodes of 500 57 / 52, 8 rows of 4000 x 5 45 / 37. 8 bits, 37 rows of 8192 keys x 1, 2,
-// 4, 8 nodes 131 / 171, 133 / 171, 188 / 160, 277 / 164; 64 rows x 4 nodes of 500, 2000 and 4000 keys 48 / 64, 114 / 112, 175 / 176, 16 rows of
-// 4000 56 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 48 / 58, 74 / 66, 112 / 85.
+// tcgen05, 8B shape (four queries a node): bf16, 37 rows of 8192 keys x 1, 4, 8, 16 nodes 194 / 200, 203 / 201, 211 / 204, 401 / 210;
+// 64 rows x 4 nodes of 500 and 4000 keys 41 / 46, 163 / 184, x 5 nodes of 500 57 / 46, 8 rows of 4000 x 5 45 / 37. 8 bits, 37 rows of 8192 keys x 1, 2,
+// 4, 8 nodes 131 / 212, 133 / 200, 188 / 168, 277 / 169; 64 rows x 4 nodes of 500, 2000 and 4000 keys 48 / 59, 114 / 109, 175 / 170, 16 rows of
+// 4000 56 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 48 / 46, 74 / 57, 112 / 76.
 constexpr int kTreeTcQueries = 16, kTreeTcQueries8 = 8;
-constexpr int kTreeTcKeys8[2] = {4000, 400};               // up to 16 queries, up to 32
+constexpr int kTreeTcKeys8[2] = {2000, 200};               // up to 16 queries, up to 32
 bool tree_on_tc(const ts_ctx* c, int nodes, int64_t mean_keys, int cache) {
   const int queries = nodes * c->G;
   if (c->cfg.head_dim != 128 || queries <= (cache == TS_CACHE_E4M3 ? kTreeTcQueries8 : kTreeTcQueries)) return false;

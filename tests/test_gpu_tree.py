@@ -260,7 +260,7 @@ def test_large_page_numbers():
 
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 @pytest.mark.parametrize("shape,nodes", [((8, 2, 128), 3), ((8, 2, 128), 6), ((16, 2, 128), 2), ((16, 1, 128), 2)], ids=lambda v: str(v))
-@pytest.mark.parametrize("keys", [399, 401, 4100])
+@pytest.mark.parametrize("keys", [150, 399, 401, 4100])
 def test_few_nodes_of_short_and_long_rows(shape, nodes, cache, keys):
     """Nine to 32 queries per KV head, of rows on both sides of the lengths that choose a step's kernel."""
     Case(shape, cache, [(keys, nodes), (keys - 3, 1), (keys + 3, nodes)], seed=keys + nodes).check()

@@ -7,7 +7,7 @@
 // block takes row after row; where there are few rows, one is a cluster's of up to eight blocks, which leave their sums in the first one's
 // shared memory. A warp of its own copies the row into a ring of 16 KB stages (cp.async.bulk), across the ends of rows, so
 // that memory is busy while the other eight warps choose a row's alternatives. Per element a thread adds up e = exp(scale (x - ref)) and x e
-// against a logit ref that only moves when one exceeds it by a factor of 2^64 (any reference is exact; fp32 has the
+// against a logit ref that only moves when one exceeds it by a factor of 2^4 (any reference is exact; fp32 has the
 // range), and counts what lies in front of the given tokens: bf16 logits two at a time, as pairs of ones that are added up, and no
 // block of 16 bytes whose largest logit is behind the token.
 //
@@ -19,8 +19,8 @@
 //
 // What bounds it: HBM for fp32 logits without given tokens (2000 rows of 100003: 127 us, 6.3 TB/s = 0.98 of a copy; with 20 alternatives 150). For
 // bf16 the issue of instructions: an SM's share of HBM is 11 logits a cycle, which is 11 instructions for each; the sums and the maximum take
-// about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 66 us without given
-// tokens, 84 with one and 5 alternatives, 70 % of the issue slots, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 77). One row of 32000: 14 us on
+// about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 67 us without given
+// tokens, 88 with one and 5 alternatives, 70 % of the issue slots, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 77). One row of 32000: 14 us on
 // the device, all of it round trips (cluster launch, copies, two sorts, the cluster's barrier). Tried and dropped: blocks of 16 warps (a row's end
 // then idles the SM), sums in packed pairs (moves ate the gain),
 // counts as sums of comparison masks (bf16 1 % at most, fp32 a third slower). Five and more given tokens with alternatives spill 5 registers, seldom read.
@@ -45,7 +45,9 @@ constexpr int kStageBytes = 16384, kStages = 4, kStageBlocks = kStageBytes / 16,
 constexpr int kCand = 2 * kThreads;      // candidates that are sorted at a time
 constexpr int kMaxTop = 32, kMaxGiven = 8, kMaxCluster = 8;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kMove = 64.f;            // log2: how far a value may exceed the reference of its sum
+// log2: how far a value may exceed the reference of its sum. Any would do for the range; small, so that a likely token's exponent is small and
+// rounded little (a token of probability 0.999 18 log2 above the reference was off by 1.3e-6), not 0, so that moves are seldom.
+constexpr float kMove = 4.f;
 // Stands for -inf, and for what lies below it, in a row's sums (a bf16 number), as long as the reference is no larger.
 constexpr float kLowest = -0x1p126f;
 constexpr float kNothing = -200.f;       // log2 of a weight that is 0 in fp32 anyway: keeps 0 * inf out of the entropy where it is
@@ -588,11 +590,20 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     for (int p = 1; p < n_parts; ++p) all = join(all, row_stats[p], to_log2);
     // a row without a finite logit has no distribution: every log probability is -inf, the entropy 0
     const bool none = all.s == 0.f;
-    const float log2_sum = log2f(all.s), log_sum = kLn2 * log2_sum;
+    // log2 of the sum in two parts, a whole number and what is within a half: a likely token's log probability is the small difference of two
+    // numbers as large as the distance from the reference, of which only the second part is rounded. (A NaN stays whole.)
+    int sum_exp = 0;
+    float sum_part = all.s;
+    if (all.s > 0.f && all.s < CUDART_INF_F) {
+      const int bits = __float_as_int(all.s) - 0x3f3504f3;       // 2^-1/2
+      sum_exp = bits >> 23;
+      sum_part = __int_as_float((bits & 0x7fffff) + 0x3f3504f3);
+    }
+    const float sum_whole = (float)sum_exp, log2_part = log2f(sum_part), log_sum = kLn2 * (sum_whole + log2_part);
     auto logprob = [&](float x) {
       if (none) return -CUDART_INF_F;
       if (is_huge(all.ref) || is_huge(x)) return fmaf(x - all.ref, scale, -log_sum);
-      return kLn2 * (fmaf(x, to_log2, -__fmul_rn(all.ref, to_log2)) - log2_sum);
+      return kLn2 * ((fmaf(x, to_log2, -__fmul_rn(all.ref, to_log2)) - sum_whole) - log2_part);
     };
     if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : fmaf(-scale, all.t / all.s, log_sum);
     if (tid >= 32 && tid - 32 < a.n_given) {

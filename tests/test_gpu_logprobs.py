@@ -156,3 +156,20 @@ def test_alternatives_with_equal_logits(rows, vocab, n_top, dtype):
     at = torch.randint(0, vocab, (rows, 40), generator=g, device="cuda")
     x.scatter_(1, at, 4.0 + torch.randint(0, 4, (rows, 40), generator=g, device="cuda").float() * 0.5)
     _check(x.to(dtype), None, n_top)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("above", [12.0, 16.0, 20.0])
+def test_likely_tokens(above, dtype):
+    """One logit far above the others: its log probability is near 0, and the reference of the sums, a logit from the row's beginning,
+    far from it. The weight's exponent is rounded once, and the same in the sum; the weight itself carries 2^-22, the sum of up to
+    2^15 smaller ones (which are less than an e-th) 2^-23, the logarithm's part and the last products 2^-23: 2^-20 in all."""
+    x = _logits(20, 32000, torch.float32, seed=int(above), size=0.5)
+    at = _tokens(20, 1, 32000)
+    x.scatter_(1, at.long(), above + torch.arange(20, device="cuda").view(20, 1) * 0.0625)
+    x = x.to(dtype)
+    r = token_logprobs(x, at, 1)
+    want = torch.log_softmax(x.double(), -1).gather(1, at.long())
+    assert (r.top_token == at).all()
+    assert ((r.logprob.double() - want).abs() <= 2.0 ** -20).all()
+    assert ((r.top_logprob.double() - want).abs() <= 2.0 ** -20).all()

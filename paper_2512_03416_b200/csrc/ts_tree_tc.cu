@@ -78,8 +78,11 @@ struct Map {
   static constexpr int kOffTab = kOffRaw + kRawStages * kTile8;
   static constexpr int kOffExp = kOffTab + (Q8 ? (kTabStages + 2) * kBlock * 4 : 0);
   static constexpr int kOffBy = kOffExp + (Q8 ? (kTabStages + 2) * 32 : 0);
-  static constexpr int kOffQScale = kOffBy + (Q8 ? kTabStages * kBlock * 2 : 0);      // Q8: [NT][128] powers of two of the queries
-  static constexpr int kOffXchg = kOffQScale + (Q8 ? NT * 128 * 4 : 0);   // [slot][warp][16] (maximum, sum)
+  // Q8: [2][NT][128] powers of two of the queries, of units of even and of odd number: Q_EMPTY of a unit says that its operand is free, and comes before
+  // the softmax warps have looked at its powers where the unit is short (its scores are issued while they are still in the epilogue in
+  // front of it). The next but one unit's powers are written behind Q_EMPTY of the unit in between, whose scores follow all P of this one.
+  static constexpr int kOffQScale = kOffBy + (Q8 ? kTabStages * kBlock * 2 : 0);
+  static constexpr int kOffXchg = kOffQScale + (Q8 ? 2 * NT * 128 * 4 : 0);           // [slot][warp][16] (maximum, sum)
   static constexpr int kOffBad = kOffXchg + 2 * 128 * 8;                  // two blocks of nodes: those whose V is not finite, 64 bits
   static constexpr int kOffUnits = kOffBad + 32;
   static constexpr int kOffBar = kOffUnits + kUnitRing * 64;
@@ -374,7 +377,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         tc_fence_after();
         if constexpr (Q8) {
           if (first) {                                     // the queries' powers of two
-            const uint32_t qs = base + L::kOffQScale + ((two ? x : 0) * 128 + query0 + (lane >> 2)) * 4;
+            const uint32_t qs = base + L::kOffQScale + (((k8 & 1) * NT + (two ? x : 0)) * 128 + query0 + (lane >> 2)) * 4;
             q_scale[0] = scale * lds_f(qs);
             q_scale[1] = scale * lds_f(qs + 32);
           }
@@ -679,7 +682,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                   *reinterpret_cast<uint2*>(dst + at8(row_of(r) + 16 * copy, ch)) = hi;
                   *reinterpret_cast<uint2*>(dst + kTile8 + at8(row_of(r) + 16 * copy, ch)) = lo;
                 }
-                if (ch == 0) reinterpret_cast<float*>(smem + L::kOffQScale)[tile * 128 + r] = power(e);
+                if (ch == 0) reinterpret_cast<float*>(smem + L::kOffQScale)[((k & 1) * NT + tile) * 128 + r] = power(e);
               } else {
                 *reinterpret_cast<uint4*>(dst + at16(row_of(r), ch)) = x[i];
                 if (twice) *reinterpret_cast<uint4*>(dst + at16(row_of(r) + 16, ch)) = x[i];

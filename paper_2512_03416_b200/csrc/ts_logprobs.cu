@@ -69,6 +69,9 @@ __device__ __forceinline__ uint32_t place_of(uint64_t key) { return ~(uint32_t)k
 
 // Barrier of the working warps (id 1; 0 is the whole block's).
 __device__ __forceinline__ void work_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(kThreads) : "memory"); }
+// The two halves of a cluster's barrier, by all threads of its blocks in turn.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;\n" ::: "memory"); }
 // The keys of a warp sorted, largest in lane 0.
 __device__ __forceinline__ uint64_t warp_sort(uint64_t k, int lane) {
 #pragma unroll
@@ -269,6 +272,8 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     mbar_init_fence();
   }
   __syncthreads();
+  // A block's shared memory may be written by the others once it has started: all say so here, and look before they write. The pass is in between.
+  if (n_parts > 1) cluster_arrive();
   pdl_wait();
 
   // A row as 16-byte blocks of memory: block b holds the tokens b * N - off .. + N - 1, the first and the last one maybe fewer. This thread
@@ -308,7 +313,11 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
       }
     }
     for (int i = max(0, n - kStages); i < n; ++i) mbar_wait(full0 + 8 * (i % kStages), (i / kStages) & 1);      // none is left in flight
-    if (n_parts > 1) cluster.sync();
+    if (n_parts > 1) {
+      cluster_wait();
+      cluster_arrive();
+      cluster_wait();
+    }
     return;
   }
 
@@ -566,6 +575,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     }
     work_sync();
     // ---------------------------------------------------------------------- the blocks of the row meet in the first one
+    if (n_parts > 1) cluster_wait();                           // the first one has started
     if (warp == 0) {
       Stats all = lane < kWarps ? warp_stats[lane] : Stats{-CUDART_INF_F, 0.f, 0.f};
 #pragma unroll
@@ -584,7 +594,12 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
       for (int w = 0; w < kWarps; ++w) sum += warp_count[w][lane];
       *cluster.map_shared_rank(&row_count[part][lane], 0) = sum;
     }
-    if (n_parts > 1) cluster.sync(); else work_sync();
+    if (n_parts > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      work_sync();
+    }
     if (part != 0) return;                                     // a cluster has one row
     Stats all = row_stats[0];
     for (int p = 1; p < n_parts; ++p) all = join(all, row_stats[p], to_log2);

@@ -173,3 +173,16 @@ def test_likely_tokens(above, dtype):
     assert (r.top_token == at).all()
     assert ((r.logprob.double() - want).abs() <= 2.0 ** -20).all()
     assert ((r.top_logprob.double() - want).abs() <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab", [(1, 4096), (1, 8192), (1, 16384), (1, 16391), (37, 4100), (18, 17000)])
+def test_short_shares_of_a_cluster(rows, vocab, dtype):
+    """Rows shared by clusters whose blocks have one or two 16-byte blocks per thread: the pass is as short as it gets. Many such calls in a
+    row, behind each other's ends, give the same bits."""
+    x, t = _logits(rows, vocab, dtype, vocab + rows), _tokens(rows, 3, vocab)
+    want = _check(x, t, 32)
+    many = [token_logprobs(x, t, 32) for _ in range(300)]
+    torch.cuda.synchronize()
+    for r in many:
+        assert all(torch.equal(p, q) for p, q in zip(want, r))

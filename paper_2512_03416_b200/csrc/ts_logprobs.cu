@@ -6,10 +6,12 @@
 // One pass over the logits (they are what has to be read; everything else is a few values a row). A row is a thread block's, and a
 // block takes row after row; where there are few rows, one is a cluster's of up to eight blocks, which leave their sums in the first one's
 // shared memory. A warp of its own copies the row into a ring of 16 KB stages (cp.async.bulk), across the ends of rows, so
-// that memory is busy while the other eight warps choose a row's alternatives. Per element a thread adds up e = exp(scale (x - ref)) and x e
-// against a logit ref that only moves when one exceeds it by a factor of 2^4 (any reference is exact; fp32 has the
-// range), and counts what lies in front of the given tokens: bf16 logits two at a time, as pairs of ones that are added up, and no
-// block of 16 bytes whose largest logit is behind the token.
+// that memory is busy while the other eight warps choose a row's alternatives. Per element a thread adds up e = 2^u and u e, u = scale log2(e) (x - ref)
+// up to one rounding of ref's product, which is the same for all logits: H = ln 2 (log2 S - sum u e / S) does not see it, nor what a row's logits
+// have in common. The reference is a logit that only moves when one exceeds it by a factor of 2^4 (fp32 has the range); a token that has nearly all
+// the probability is the reference, and its u e nothing, so that an entropy near 0 is as exact as its small terms. The thread counts
+// what lies in front of the given tokens: bf16 logits two at a time, as pairs of ones that are added up, and no block of 16 bytes whose largest
+// logit is behind the token.
 //
 // Alternatives cost the pass no more than its maximum: every thread keeps the largest logit of its own part of the row and where
 // that part first has it. The n best tokens lie in the n parts that come first by (that logit, that place), since each of these
@@ -17,10 +19,10 @@
 // read again, the others only where the part's second best such block is not behind the last part's largest either; what is not behind
 // that is sorted.
 //
-// What bounds it: HBM for fp32 logits without given tokens (2000 rows of 100003: 127 us, 6.3 TB/s = 0.98 of a copy; with 20 alternatives 150). For
+// What bounds it: HBM for fp32 logits without given tokens (2000 rows of 100003: 127 us, 6.3 TB/s = 0.98 of a copy; with 20 alternatives 147). For
 // bf16 the issue of instructions: an SM's share of HBM is 11 logits a cycle, which is 11 instructions for each; the sums and the maximum take
 // about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 67 us without given
-// tokens, 88 with one and 5 alternatives, 70 % of the issue slots, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 77). One row of 32000: 14 us on
+// tokens, 83 with one and 5 alternatives, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 72). One row of 32000: 14 us on
 // the device, all of it round trips (cluster launch, copies, two sorts, the cluster's barrier). Tried and dropped: blocks of 16 warps (a row's end
 // then idles the SM), sums in packed pairs (moves ate the gain),
 // counts as sums of comparison masks (bf16 1 % at most, fp32 a third slower). Five and more given tokens with alternatives spill 5 registers, seldom read.
@@ -48,9 +50,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // log2: how far a value may exceed the reference of its sum. Any would do for the range; small, so that a likely token's exponent is small and
 // rounded little (a token of probability 0.999 18 log2 above the reference was off by 1.3e-6), not 0, so that moves are seldom.
 constexpr float kMove = 4.f;
-// Stands for -inf, and for what lies below it, in a row's sums (a bf16 number), as long as the reference is no larger.
-constexpr float kLowest = -0x1p126f;
-constexpr float kNothing = -200.f;       // log2 of a weight that is 0 in fp32 anyway: keeps 0 * inf out of the entropy where it is
+// A reference whose product with c = scale log2(e) is larger than this is a huge one: the product's rounding, by which all weights are off alike, would no
+// longer be near 1 (2^-5 log2 here), and from 2^32 on leave fp32. Its weights are 2^((x - ref) c). Rows that are masked throughout, and the like.
+constexpr float kHuge = 0x1p20f;
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -110,24 +112,29 @@ __device__ __forceinline__ void merge_lists(uint64_t k, uint64_t* best, int n_li
   if (warp == 0) best[lane] = k;
   work_sync();
 }
-// Whether a reference is so large that its product with the scale, or a distance from it, may leave fp32.
-__device__ __forceinline__ bool is_huge(float ref) { return fabsf(ref) > 0x1p126f && ref != -CUDART_INF_F; }
-struct Stats {                                       // of a part of a row, weights e(x) = exp(scale (x - ref))
-  float ref, s, t;                                   // a logit to refer to (any is exact), sum e(x), sum (x - ref) e(x)
+// Stands for -inf, and for what lies below, in the sums of a row whose reference is not huge (a bf16 number): its u is finite, its weight 0.
+__device__ __forceinline__ float row_lowest(float to_log2) {
+  return -__uint_as_float(__float_as_uint(fminf(0x1p126f, __fdividef(0x1p126f, to_log2))) & 0xffff0000u);
+}
+struct Stats {                                       // of a part of a row
+  float ref, s, t;                                   // a logit to refer to, sum e, sum u e
 };
-// log2 of the factor between weights against two references. The sums' weights are 2^(x c - fl(ref c)), c = scale log2(e): so are these.
+// The factor between weights against two references, as log2. The sums' weights are 2^(x c - fl(ref c)), a huge one's 2^((x - ref) c): so are these.
 __device__ __forceinline__ float log2_factor(float from, float to, float to_log2) {
-  return is_huge(from) || is_huge(to) ? (from - to) * to_log2 : __fmul_rn(from, to_log2) - __fmul_rn(to, to_log2);
+  const float f = __fmul_rn(from, to_log2), t = __fmul_rn(to, to_log2);
+  float by = f - t;                                  // -inf: from is, or nothing that counts
+  if (__builtin_expect(fabsf(t) > kHuge || (fabsf(f) > kHuge && from != -CUDART_INF_F), 0)) {
+    if (fabsf(f) > kHuge && fabsf(t) > kHuge) by = (from - to) * to_log2;
+    else if (fabsf(f) > kHuge) by += fabsf(f) < CUDART_INF_F ? fmaf(from, to_log2, -f) : 0.f;
+    else by -= fabsf(t) < CUDART_INF_F ? fmaf(to, to_log2, -t) : 0.f;
+  }
+  return by;
 }
 __device__ __forceinline__ void move_ref(Stats& a, float ref, float to_log2) {
-  const float by = a.ref - ref, f = ex2(log2_factor(a.ref, ref, to_log2));
-  if (a.s == 0.f || f == 0.f) {                      // nothing yet, or nothing that counts (ref = -inf before the first number)
-    a.t = 0.f;
-    a.s = a.s == a.s ? 0.f : a.s;                    // a NaN stays
-  } else {
-    a.t = f * fmaf(a.s, by, a.t);
-    a.s *= f;
-  }
+  const float by = log2_factor(a.ref, ref, to_log2), f = ex2(by);
+  // nothing yet, or nothing that counts (ref = -inf before the first number)
+  a.t = a.s == 0.f || f == 0.f ? 0.f : f * fmaf(a.s, by, a.t);
+  a.s *= f;                                          // a NaN stays
   a.ref = ref;
 }
 __device__ __forceinline__ Stats join(Stats a, Stats b, float to_log2) {
@@ -135,6 +142,20 @@ __device__ __forceinline__ Stats join(Stats a, Stats b, float to_log2) {
   if (a.ref != ref) move_ref(a, ref, to_log2);
   if (b.ref != ref) move_ref(b, ref, to_log2);
   return Stats{ref, a.s + b.s, a.t + b.t};
+}
+// Of all N neighbouring lanes of a warp.
+template <int N>
+__device__ __forceinline__ Stats join_lanes(Stats a, float to_log2) {
+  float ref = a.ref;
+#pragma unroll
+  for (int sh = N / 2; sh > 0; sh >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, sh));
+  if (a.ref != ref) move_ref(a, ref, to_log2);
+#pragma unroll
+  for (int sh = N / 2; sh > 0; sh >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, sh);
+    a.t += __shfl_xor_sync(0xffffffffu, a.t, sh);
+  }
+  return a;
 }
 
 struct Args {
@@ -180,11 +201,11 @@ struct Vec<float> {
   static __device__ __forceinline__ float largest(const uint4& v) {      // a NaN only where all are
     return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
-  // -inf as the lowest number: its weight is 0 all the same, and 0 times its distance is no NaN. (A NaN stays one.)
-  static __device__ __forceinline__ uint4 not_inf(const uint4& v) {
-    auto f = [](uint32_t x) {
+  // What is below `low` as that number: its weight is 0 all the same, and 0 times its u is no NaN. (A NaN stays one.)
+  static __device__ __forceinline__ uint4 not_below(const uint4& v, float low) {
+    auto f = [&](uint32_t x) {
       float y;
-      asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(__uint_as_float(x)), "f"(kLowest));
+      asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(__uint_as_float(x)), "f"(low));
       return __float_as_uint(y);
     };
     return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
@@ -217,10 +238,10 @@ struct Vec<uint16_t> {                               // bf16 bits
     const __nv_bfloat162 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
     return fmaxf(__low2float(m), __high2float(m));
   }
-  static __device__ __forceinline__ uint4 not_inf(const uint4& v) {
-    const __nv_bfloat162 low = __float2bfloat162_rn(kLowest);
+  static __device__ __forceinline__ uint4 not_below(const uint4& v, float low) {      // low is a bf16 number
+    const __nv_bfloat162 low2 = __float2bfloat162_rn(low);
     auto f = [&](uint32_t x) {
-      const __nv_bfloat162 y = __hmax2_nan(pair(x), low);
+      const __nv_bfloat162 y = __hmax2_nan(pair(x), low2);
       return *reinterpret_cast<const uint32_t*>(&y);
     };
     return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
@@ -337,7 +358,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
   bool dead = false;
   for (int row = first_row; row < n_rows; row += row_step) {
     const Row r = row_of(row);
-    const float scale = a.scale ? a.scale[row] : 1.f, to_log2 = scale * 1.4426950408889634f, lowest = kNothing / to_log2;
+    const float scale = a.scale ? a.scale[row] : 1.f, to_log2 = scale * 1.4426950408889634f, lowest = row_lowest(to_log2);
     if (GIVEN > 0 && tid < kMaxGiven) {
       given_x[tid] = x_now;
       given_tok[tid] = tok_now;
@@ -361,31 +382,25 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
       count[j] = 0.f;
     }
 
-    // The sums against ref: of e(x) and of x e(x), which is one instruction less per logit (huge references: of (x - ref) e(x)).
-    float ref = -CUDART_INF_F, neg_log2 = 0.f;                 // and -fl(ref c)
-    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    float ref = -CUDART_INF_F, neg_log2 = 0.f;                 // the reference, and -fl(ref c)
+    float sum = 0.f, usum = 0.f;                               // of e and of u e
     float best = CUDART_NAN_F;                                 // this thread's largest logit (a NaN: none yet) and the first block that has it
     int best_block = -1;
     float second = -CUDART_INF_F;                              // the largest of its other blocks'
-    auto stats = [&]() {
-      const float sum = s0 + s1, t = t0 + t1;
-      return Stats{ref, sum, is_huge(ref) || ref == -CUDART_INF_F ? t : fmaf(-ref, sum, t)};
-    };
     auto refer_to = [&](float mx) {                            // the first number too: the reference is -inf before it
       if ((mx - ref) * to_log2 > kMove) {
-        const float f = ex2(log2_factor(ref, mx, to_log2));    // 0 the first time, and where ref was or becomes a huge one
+        const float more = log2_factor(ref, mx, to_log2), f = ex2(more);      // 0 the first time
+        usum = f == 0.f ? 0.f : f * fmaf(sum, more, usum);
+        sum *= f;
         ref = mx;
         neg_log2 = -__fmul_rn(mx, to_log2);
-        s0 *= f; s1 *= f; t0 *= f; t1 *= f;
       }
     };
     // One logit, whatever its size and the reference's.
     auto take_exact = [&](float x) {
-      const float from = ref == -CUDART_INF_F ? 0.f : ref, d = x - from;
-      const bool huge = is_huge(ref);
-      const float e = ex2(huge ? d * to_log2 : fmaf(x, to_log2, neg_log2));
-      s0 += e;
-      t0 += huge ? e * fmaxf(d, lowest) : e == 0.f ? 0.f : e * x;
+      const float u = fabsf(neg_log2) > kHuge ? (x - ref) * to_log2 : fmaf(x, to_log2, neg_log2), e = ex2(u);
+      sum += e;
+      usum += e == 0.f ? 0.f : e * u;
     };
     // U blocks, kThreads apart. What seldom happens is asked for once for all of them.
     auto take = [&](auto count_tag, const uint4* blocks, int b0) {
@@ -404,23 +419,27 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
         }
       }
       refer_to(top);
-      if (is_huge(ref)) {                                      // rows of the type's lowest value, and the like
+      if (fabsf(neg_log2) > kHuge) {                           // rows of the type's lowest value, and the like
 #pragma unroll 1
         for (int i = 0; i < U * N; ++i) take_exact(Vec<T>::load(reinterpret_cast<const T*>(blocks + i / N * kThreads) + i % N));
       } else {
+        // Sums of their own first: many small weights are not added one by one to a large one.
+        float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float x[N];
-          Vec<T>::unpack(Vec<T>::not_inf(v[u]), x);
+          Vec<T>::unpack(Vec<T>::not_below(v[u], lowest), x);
 #pragma unroll
           for (int i = 0; i < N; i += 2) {
-            const float e0 = ex2(fmaf(x[i], to_log2, neg_log2)), e1 = ex2(fmaf(x[i + 1], to_log2, neg_log2));
-            s0 += e0;
-            s1 += e1;
-            t0 = fmaf(e0, x[i], t0);
-            t1 = fmaf(e1, x[i + 1], t1);
+            const float u0 = fmaf(x[i], to_log2, neg_log2), u1 = fmaf(x[i + 1], to_log2, neg_log2), e0 = ex2(u0), e1 = ex2(u1);
+            s0 = u + i == 0 ? e0 : s0 + e0;
+            s1 = u + i == 0 ? e1 : s1 + e1;
+            t0 = u + i == 0 ? e0 * u0 : fmaf(e0, u0, t0);
+            t1 = u + i == 0 ? e1 * u1 : fmaf(e1, u1, t1);
           }
         }
+        sum += s0 + s1;
+        usum += t0 + t1;
       }
 #pragma unroll
       for (int j = 0; j < GIVEN; ++j) {
@@ -469,17 +488,10 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
       __syncwarp();
       if (lane == 0) mbar_arrive(empty0 + 8 * st);
     }
-    Stats st = stats();
+    Stats st = {ref, sum, usum};
     if (dead) st.s = CUDART_NAN_F;                             // a copy that never came: no result
     // ---------------------------------------------------------------------- sums of the block
-#pragma unroll
-    for (int sh = 16; sh > 0; sh >>= 1) {
-      Stats o;
-      o.ref = __shfl_xor_sync(0xffffffffu, st.ref, sh);
-      o.s = __shfl_xor_sync(0xffffffffu, st.s, sh);
-      o.t = __shfl_xor_sync(0xffffffffu, st.t, sh);
-      st = join(st, o, to_log2);
-    }
+    st = join_lanes<32>(st, to_log2);
     if (lane == 0) warp_stats[warp] = st;
 #pragma unroll
     for (int j = 0; j < GIVEN; ++j) {                          // a thread's counts are whole numbers below 2^24
@@ -577,15 +589,7 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     // ---------------------------------------------------------------------- the blocks of the row meet in the first one
     if (n_parts > 1) cluster_wait();                           // the first one has started
     if (warp == 0) {
-      Stats all = lane < kWarps ? warp_stats[lane] : Stats{-CUDART_INF_F, 0.f, 0.f};
-#pragma unroll
-      for (int sh = kWarps / 2; sh > 0; sh >>= 1) {
-        Stats o;
-        o.ref = __shfl_xor_sync(0xffffffffu, all.ref, sh);
-        o.s = __shfl_xor_sync(0xffffffffu, all.s, sh);
-        o.t = __shfl_xor_sync(0xffffffffu, all.t, sh);
-        all = join(all, o, to_log2);
-      }
+      const Stats all = join_lanes<kWarps>(lane < kWarps ? warp_stats[lane] : Stats{-CUDART_INF_F, 0.f, 0.f}, to_log2);
       if (lane == 0) *cluster.map_shared_rank(&row_stats[part], 0) = all;
     } else if (warp == 1) {
       if (TOP && n_parts > 1) *cluster.map_shared_rank(&row_lists[part * 32 + lane], 0) = lists[lane];
@@ -617,10 +621,14 @@ __global__ void __launch_bounds__(kThreads + 32, kBlocksPerSm) logprobs_kernel(c
     const float sum_whole = (float)sum_exp, log2_part = log2f(sum_part), log_sum = kLn2 * (sum_whole + log2_part);
     auto logprob = [&](float x) {
       if (none) return -CUDART_INF_F;
-      if (is_huge(all.ref) || is_huge(x)) return fmaf(x - all.ref, scale, -log_sum);
-      return kLn2 * ((fmaf(x, to_log2, -__fmul_rn(all.ref, to_log2)) - sum_whole) - log2_part);
+      const float ref_log2 = __fmul_rn(all.ref, to_log2);
+      if (fabsf(ref_log2) > kHuge || fabsf(x) > 0x1p100f) return fmaf(x - all.ref, scale, -log_sum);
+      return kLn2 * ((fmaf(x, to_log2, -ref_log2) - sum_whole) - log2_part);
     };
-    if (tid == 0 && a.entropy) a.entropy[row] = none ? 0.f : fmaf(-scale, all.t / all.s, log_sum);
+    if (tid == 0 && a.entropy) {
+      const float h = kLn2 * ((sum_whole - all.t / all.s) + log2_part);
+      a.entropy[row] = none || h < 0.f ? 0.f : h;              // the roundings of one near 0 may leave it below
+    }
     if (tid >= 32 && tid - 32 < a.n_given) {
       const int j = tid - 32;
       const float x = given_x[j];

@@ -186,3 +186,90 @@ def test_short_shares_of_a_cluster(rows, vocab, dtype):
     torch.cuda.synchronize()
     for r in many:
         assert all(torch.equal(p, q) for p, q in zip(want, r))
+
+
+def _entropy_bound(y):
+    """For y = scale x of a row, in nats. H = ln S - sum e u / S with u = log e. The sums' reference r is a logit no more than 2.8 (4 log2) below
+    the largest one: the largest itself where the second is further behind. With A = E|y - r|, Q = E(y - r)^2: the exponents' factor and
+    roundings (2^-23 of them) move the entropy by less than 2^-22 Q, the exponentials (2^-22) and the sums (2^-21) by less than 2^-20 (1 + A)."""
+    y = np.sort(y[np.isfinite(y)])[::-1]
+    d = y[0] - y
+    p = np.exp(-d) / np.exp(-d).sum()
+    near = 2.8 if len(y) > 1 and d[1] < 2.8 else 0.0
+    return 2.0 ** -20 * (1 + (p * d).sum() + near) + 2.0 ** -22 * ((p * d * d).sum() + near * near)
+
+
+def _check_entropy(x, scale=None):
+    r = token_logprobs(x, None, 0, scale)
+    for i, (row, got) in enumerate(zip(x.double().cpu().numpy(), r.entropy.cpu().numpy().astype(np.float64))):
+        s = 1.0 if scale is None else float(scale[i])
+        want = O.token_logprobs(row, s, [], 0)[2]
+        assert got >= 0 and abs(got - want) <= _entropy_bound(row * s), (i, got, want, _entropy_bound(row * s))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [1, 300, 32000, 131072])
+@pytest.mark.parametrize("offset", [0.0, 100.0, -100.0, 2000.0, -1e5])
+def test_entropy_of_rows_far_from_zero(offset, vocab, dtype):
+    """What is added to all logits is no part of the entropy."""
+    for size in (0.3, 2.5, 40.0):
+        _check_entropy((_logits(6, vocab, torch.float32, vocab, size) + offset).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_entropy_of_likely_tokens(rows, dtype):
+    """One logit 8 to 40 nats above the others, rows far from zero among them: entropies down to nothing."""
+    x = _logits(rows, 32000, torch.float32, 17, 0.5)
+    at = _tokens(rows, 1, 32000, 3).long()
+    x.scatter_(1, at, 8.0 + torch.arange(rows, device="cuda").view(rows, 1) * (32.0 / rows))
+    _check_entropy(x.to(dtype))
+    _check_entropy((x + 1000).to(dtype))
+    _check_entropy(x.to(dtype), torch.linspace(0.5, 3.0, rows, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [50, 40000])
+def test_logits_of_the_largest_sizes(vocab, dtype):
+    """One number of any size among logits of -inf has all the probability; and numbers whose product with the scale is beyond fp32."""
+    sizes = [-(2.0 ** 127), -(2.0 ** 126), -(2.0 ** 125), -(2.0 ** 124), -1e30, 0.0, 2.0 ** 100, 2.0 ** 125, 2.0 ** 126, 2.0 ** 127]
+    for scale in (0.25, 1.0, 1000.0):
+        x = torch.full((len(sizes), vocab), -float("inf"), device="cuda")
+        at = _tokens(len(sizes), 1, vocab, 9)
+        x.scatter_(1, at.long(), torch.tensor(sizes, device="cuda").view(-1, 1))
+        r = token_logprobs(x.to(dtype), at, 1, torch.full((len(sizes),), scale, device="cuda"))
+        assert (r.logprob == 0).all() and (r.top_logprob == 0).all() and (r.entropy == 0).all() and (r.top_token == at).all()
+    x = (-torch.arange(vocab, device="cuda", dtype=torch.float64) * 2.0 ** 100 + 2.0 ** 121)[None].to(dtype)      # y to 2^130, 2^109 apart and more
+    t = torch.tensor([[0, vocab - 1]], dtype=torch.int32, device="cuda")
+    for row in (x, -x):
+        r = token_logprobs(row, t, 1, torch.full((1,), 512.0, device="cuda"))
+        lp = O.token_logprobs(row[0].double().cpu().numpy(), 512.0, t[0].cpu().numpy(), 1)
+        assert np.allclose(r.logprob[0].cpu().numpy(), lp[0], rtol=2.0 ** -20, atol=2.0 ** -20)
+        assert np.array_equal(r.top_token[0].cpu().numpy(), lp[4]) and abs(float(r.entropy[0]) - lp[2]) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [-1e9, -1e10, -3e30, 1e7])
+def test_rows_masked_throughout(offset, dtype):
+    """Every token at the same number of any size, some tokens 2^-7 of it above or below: what is left is a distribution like any other."""
+    x = torch.full((3, 20001), offset, device="cuda", dtype=torch.float64)
+    x[1, ::3] *= 1 + 2.0 ** -7
+    x[2, 5:9] *= 1 - 2.0 ** -7
+    x, t = x.to(dtype), _tokens(3, 2, 20001)
+    _check(x, t, 4)
+    _check_entropy(x)
+
+
+def test_references_on_both_sides_of_where_they_count_as_huge():
+    """Logits times log2(e) around 2^20, a few nats apart: parts of a row refer to logits on either side."""
+    base = 2.0 ** 20 / 1.4426950408889634
+    x = (base + _logits(4, 60000, torch.float32, 23, 3.0)).contiguous()
+    x[1] = -x[1]
+    x[2] *= 1024.0
+    x[3] = torch.cat([torch.linspace(base - 12, base + 6, 59999, device="cuda"), torch.tensor([base - 30.0], device="cuda")])
+    scale = torch.tensor([1.0, 1.0, 1.0 / 1024, 1.0], device="cuda")
+    r = token_logprobs(x, None, 3, scale)
+    for i in range(4):
+        _, _, ent, top_lp, top = O.token_logprobs(x[i].double().cpu().numpy(), float(scale[i]), [], 3)
+        assert np.array_equal(r.top_token[i].cpu().numpy(), top)
+        assert np.abs(r.top_logprob[i].cpu().numpy() - top_lp).max() <= 2.0 ** -18 and abs(float(r.entropy[i]) - ent) <= 2.0 ** -16, i

@@ -551,7 +551,8 @@ int ts_cache8_attach(ts_ctx* ctx, const ts_cache8* cache);
  * Node i of a row attends all ctx_len[r] cached tokens and those nodes j of the row whose bit j of its mask word is
  * set (bits from q_len[r] on are ignored); a node that sees nothing gets zeros. mask: DEVICE uint64 [N], 8-byte
  * aligned; NULL = a chain (node i sees the nodes 0..i), so that a row of one node is a decode row. The K and V of a
- * node that nobody sees may hold anything; a seen node whose V holds an infinity or a NaN makes its viewers' outputs NaN.
+ * node that nobody sees may hold anything; a seen node whose V (over the 8-bit cache: K or V) holds an infinity or a NaN makes its viewers' outputs
+ * NaN. A query that holds one gives NaN, or zeros where it sees nothing.
  * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^70), and V rows
  * more than 2^22 smaller than the largest of 32 neighbouring keys may lose bits.
  * Arithmetic as for a step: fp32 accumulation and softmax, weights rounded to bf16 (8-bit cache: f16) in front of

@@ -174,6 +174,7 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
   // ---------------------------------------------------------------- queries
   // B fragments of S^T = K Q^T: lane (g, c) holds query 8 nb + g. bf16: elements 2c, 2c + 1 and 2c + 8, 2c + 9 of each sixteen.
   // Q8: 4c, 4c + 2 and 4c + 1, 4c + 3 (the K fragments come in the same order), as f16 times a power of two per query.
+  // A query with an infinity or a NaN becomes one of NaN: it has no softmax, and scores of -inf would count as keys that are not seen.
   uint32_t qf[NB][D / 16][2];
   float q_scale[NB][2];                           // of queries 8 nb + 2c, + 1: scale * log2(e), times what takes the power out again
 #pragma unroll
@@ -193,20 +194,24 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
       }
     }
     q_scale[nb][0] = q_scale[nb][1] = s.scale_log2;
-    if constexpr (Q8) {
-      uint32_t most = 0;                          // largest magnitude of the query, as bf16 bits
+    uint32_t most = 0;                            // largest magnitude of the query, as bf16 bits
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) most = max(most, max(qf[nb][ks][i] & 0x7fffu, (qf[nb][ks][i] >> 16) & 0x7fffu));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    const bool odd = most >= 0x7f80u;
+    if constexpr (!Q8) {
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) most = max(most, max(qf[nb][ks][i] & 0x7fffu, (qf[nb][ks][i] >> 16) & 0x7fffu));
-      most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        if (odd) qf[nb][ks][0] = qf[nb][ks][1] = 0x7fc07fc0u;
+    } else {
       // to 2^8 .. 2^9: products with codes up to 448 and sums over D stay far from fp32's ends
       const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 8, -118), 118);
-      const float down = power(-e);
+      const float down = odd ? CUDART_NAN_F : power(-e);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-{
+      for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t x = qf[nb][ks][0], y = qf[nb][ks][1];
         qf[nb][ks][0] = pack_f16(__uint_as_float(x << 16) * down, __uint_as_float(y << 16) * down);
         qf[nb][ks][1] = pack_f16(__uint_as_float(x & 0xffff0000u) * down, __uint_as_float(y & 0xffff0000u) * down);
@@ -443,7 +448,8 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
           const float down = power(-e);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = pack_f16(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);
-          if (ch == 0) own_exp[kv * 16 + r] = (uint8_t)(e - 8 + 127);      // as of codes
+          // as of codes; a K row that is not finite is one of NaN, as in the tcgen05 kernel, whose codes have no infinities
+          if (ch == 0) own_exp[kv * 16 + r] = most >= 0x7f80u ? 255 : (uint8_t)(e - 8 + 127);
           // in the order that codes come in: of each sixteen elements the even ones first
           const uint32_t at0 = own - base + off16<D>(kv, r, ch & ~1) + (ch & 1) * 8, at1 = own - base + off16<D>(kv, r, ch | 1) + (ch & 1) * 8;
           *reinterpret_cast<uint2*>(smem + at0) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));

@@ -205,6 +205,12 @@ __device__ __forceinline__ float lds_f(uint32_t at) {
 __device__ __forceinline__ void lds_f4(uint32_t at, uint64_t& lo, uint64_t& hi) {      // four
   asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];\n" : "=l"(lo), "=l"(hi) : "r"(at) : "memory");
 }
+// (volatile: loads that follow each other are issued one behind the other, in front of what is done with them)
+__device__ __forceinline__ uint4 lds_u4(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
 // Place of key k's power in its table: the columns of a lane in two neighbouring eights lie together.
 __device__ __forceinline__ int tab_at(int k) { return ((k >> 4) * 4 + (k >> 1 & 3)) * 4 + (k >> 3 & 1) * 2 + (k & 1); }
 __device__ __forceinline__ uint64_t lds_f2(uint32_t at) {       // two floats
@@ -671,6 +677,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int r = (i0 + i) * 16 + w * 2 + half;
+              // A query that is not finite becomes one of NaN: it has no softmax, and scores of -inf would count as keys that are not seen.
               if constexpr (Q8) {
                 uint32_t most = max_magnitude(x[i]);
 #pragma unroll
@@ -678,12 +685,14 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                 const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 7, -118), 118);      // largest to 2^7 .. 2^8
                 uint2 hi, lo;
                 split8(x[i], power(-e), hi, lo);
+                if (most >= 0x7f80u) hi = lo = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
                 for (int copy = 0; copy < (twice ? 2 : 1); ++copy) {
                   *reinterpret_cast<uint2*>(dst + at8(row_of(r) + 16 * copy, ch)) = hi;
                   *reinterpret_cast<uint2*>(dst + kTile8 + at8(row_of(r) + 16 * copy, ch)) = lo;
                 }
                 if (ch == 0) reinterpret_cast<float*>(smem + L::kOffQScale)[((k & 1) * NT + tile) * 128 + r] = power(e);
               } else {
+                if (__ballot_sync(0xffffffffu, not_finite(x[i])) & (0xffffu << (half * 16))) x[i] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
                 *reinterpret_cast<uint4*>(dst + at16(row_of(r), ch)) = x[i];
                 if (twice) *reinterpret_cast<uint4*>(dst + at16(row_of(r) + 16, ch)) = x[i];
               }
@@ -706,7 +715,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               if (g >= L::kVStages && !(ok = wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1))) break;
               const int tb = raw % kTabStages;
               if (!(ok = wait_both(L::TAB_FULL + tb, (raw / kTabStages) & 1, L::V_LANDED + raw % kRaw, (raw / kRaw) & 1))) break;
-              const unsigned char* codes = smem + L::kOffRaw + raw % kRaw * kTile8;
+              const uint32_t codes = base + L::kOffRaw + raw % kRaw * kTile8;
               const uint16_t* by_row = reinterpret_cast<const uint16_t*>(smem + L::kOffBy) + tb * kBlock;
               // Sixteen codes -> two pieces of eight f16; eight lanes take four pieces' worth of two neighbouring rows, so that their
               // stores fall into different banks.
@@ -714,7 +723,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int r = (w & 3) * 32 + ((w >> 2) * 2 + (i >> 1)) * 8 + (lane >> 3) * 2 + ((lane >> 2) & 1), c = (i & 1) * 4 + (lane & 3);
-                x[i] = *reinterpret_cast<const uint4*>(codes + r * 128 + (((c ^ r) & 7) << 4));
+                x[i] = lds_u4(codes + r * 128 + (((c ^ r) & 7) << 4));
               }
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -827,7 +836,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
                   split8(x[i], power(-e_k), hi, lo);
                   *reinterpret_cast<uint2*>(kt + at8(r, ch)) = hi;
                   *reinterpret_cast<uint2*>(kt + at8(64 + r, ch)) = lo;
-                  if (ch == 0) tab[tab_at(r)] = power(e_k);
+                  if (ch == 0) tab[tab_at(r)] = most >= 0x7f80u ? CUDART_NAN_F : power(e_k);       // the codes have no infinities
                 } else {
                   *reinterpret_cast<uint4*>(kt + at16(r, ch)) = x[i];
                 }

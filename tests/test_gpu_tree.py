@@ -264,3 +264,57 @@ def test_large_page_numbers():
 def test_few_nodes_of_short_and_long_rows(shape, nodes, cache, keys):
     """Nine to 32 queries per KV head, of rows on both sides of the lengths that choose a step's kernel."""
     Case(shape, cache, [(keys, nodes), (keys - 3, 1), (keys + 3, nodes)], seed=keys + nodes).check()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("shape", [(8, 2, 64), (8, 2, 128), (16, 1, 128)], ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("nodes", [1, 3, 40])
+def test_queries_that_are_not_finite(shape, nodes, cache):
+    """A query with an infinity or a NaN has no softmax, not even where all its scores are -inf: NaN where it sees a key, zeros where it sees
+    none, and nothing of it in the other queries. Long and short rows, whichever kernel they are on."""
+    c = Case(shape, cache, [(37, nodes), (0, nodes), (2300, nodes)], masks="tree", seed=41)
+    c.mask[nodes] = 0                                            # the second row's first node sees nothing
+    bad = np.zeros((c.n, c.hq), bool)
+    for r, node in enumerate((0, 0, nodes - 1)):
+        for h, (at, bits) in enumerate(((0, 0x7F80), (c.d - 1, 0xFF80), (17, 0x7FC0))):
+            c.qb[r * nodes + node, h, at] = bits
+            bad[r * nodes + node, h] = True
+    # -inf times what is above 0 in all keys: every score is -inf
+    for x in [*c.k, c.kn]:
+        x[:, 0, 0] = 1.0
+    c.kb[:, 0, 0] = 0x3F80
+    for r, ctx in enumerate(c.ctx):
+        if ctx:
+            kb, vb = bf16(c.k[r])[0], bf16(c.v[r])[0]
+            c.dec.request_set_len(c.slots[r], 0)
+            c.dec.cache_append([c.slots[r]], [ctx], [0], to_dev(kb), to_dev(vb))
+            if cache == "e4m3":
+                ko, vo = (torch.empty((ctx, c.hkv, c.d), dtype=torch.int16, device="cuda") for _ in range(2))
+                c.dec.cache_read([c.slots[r]], [0], [ctx], ko, vo)
+                c.k[r], c.v[r] = (wl.bf16_bits_to_f32(t.cpu().numpy().view(np.uint16)).astype(np.float64) for t in (ko, vo))
+    c.qb[0, 0] = c.qb[nodes, 0] = 0
+    c.qb[0, 0, 0] = c.qb[nodes, 0, 0] = 0xFF80
+    got = c.run()
+    want, bound = c.want()                                       # of the finite queries from before
+    ok = np.abs(got - want) <= 2.0 ** -8 * (bound + np.abs(want))
+    assert ok[~bad].all()
+    blind = np.zeros((c.n, c.hq), bool)
+    blind[nodes] = True
+    assert np.isnan(got[bad & ~blind]).all()
+    assert (got[blind] == 0).all()
+
+
+@pytest.mark.parametrize("nodes", [2, 5, 40])
+def test_infinite_k_of_a_seen_node(nodes):
+    """Over the 8-bit cache, whose codes have no infinities: the node's viewers get NaN, whichever kernel they are on."""
+    c = Case((16, 4, 128), "e4m3", [(20, nodes), (2100, nodes)], masks=None, seed=43)
+    for r in range(2):
+        c.kb[r * nodes + 1, r, 5] = (0x7F80, 0xFF80)[r]
+    got = c.run()
+    want, bound = c.want()
+    ok = np.abs(got - want) <= 2.0 ** -8 * (bound + np.abs(want))
+    for r in range(2):
+        heads = np.arange(16) // 4 == r
+        mine = slice(r * nodes, (r + 1) * nodes)
+        assert np.isnan(got[mine][1:, heads]).all()
+        assert ok[mine][0].all() and ok[mine][:, ~heads].all()

@@ -553,8 +553,9 @@ int ts_cache8_attach(ts_ctx* ctx, const ts_cache8* cache);
  * aligned; NULL = a chain (node i sees the nodes 0..i), so that a row of one node is a decode row. The K and V of a
  * node that nobody sees may hold anything; a seen node whose V (over the 8-bit cache: K or V) holds an infinity or a NaN makes its viewers' outputs
  * NaN. A query that holds one gives NaN, or zeros where it sees nothing.
- * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^70), and V rows
- * more than 2^22 smaller than the largest of 32 neighbouring keys may lose bits.
+ * cache: TS_CACHE_*; over the 8-bit cache the nodes' own K/V are taken as they are, not quantised (magnitudes up to 2^70). There
+ * V rows more than 2^22 smaller than the largest of 32 neighbouring keys may lose bits, and so may keys whose weight times the size of
+ * their V row is less than 2^-21 of the largest such product. V rows of zeros count as the smallest there are.
  * Arithmetic as for a step: fp32 accumulation and softmax, weights rounded to bf16 (8-bit cache: f16) in front of
  * the second product, bf16 result. Asynchronous on cuda_stream; uses the context's workspace, as a step does.
  * ts_tree_masks (host): mask words of one row's nodes from their parents (parents[i] in [-1, i), -1 = attached to the

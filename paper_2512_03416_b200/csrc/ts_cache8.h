@@ -12,6 +12,9 @@ struct Cache8 {
   uint8_t* scales;
 };
 constexpr int kCache8MaxExp = 62;      // |E| at most: 2^(E of a row - E of another) then stays a normal fp32 number
+// Scale byte of a row of zeros. Other rows have it only if their largest magnitude is in (224, 448], so readers to whom a V row's exponent is its
+// size look at the codes of rows with this byte: zeros are smaller than any row.
+constexpr uint8_t kCache8ZeroByte = 127;
 
 #ifdef __CUDACC__
 // Smallest E with m <= 448 * 2^E, for m > 0 the magnitude whose bf16 bits are `bits` (infinity counts as the largest):
@@ -23,6 +26,7 @@ __device__ __forceinline__ int cache8_exponent(uint32_t bits) {
 }
 // E of a scale byte (not of 255). A byte that no row was written with is taken to the nearest that one could have been.
 __device__ __forceinline__ int cache8_exp_of(uint8_t byte) { return min(max((int)byte - 127, -kCache8MaxExp), kCache8MaxExp); }
+__device__ __forceinline__ uint32_t cache8_magnitudes(const uint4& codes) { return (codes.x | codes.y | codes.z | codes.w) & 0x7f7f7f7fu; }
 // 2^E, or NaN
 __device__ __forceinline__ float cache8_power(uint8_t byte) { return byte == 255 ? __int_as_float(0x7fc00000) : __int_as_float((cache8_exp_of(byte) + 127) << 23); }
 // Four e4m3 codes as f16 pairs (0, 2) and (1, 3), times 2^-8: a code shifted to the sign and to bits 13..7 is the f16 number 2^-8 times

@@ -273,9 +273,24 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
       // 2^8: see cache8_widen
       ks0 = 256.f * cache8_power(exps[g]);
       ks1 = 256.f * cache8_power(exps[g + 8]);
-      const int e0 = cache8_exp_of(exps[16 + g]) + 8, e1 = cache8_exp_of(exps[16 + g + 8]) + 8;
-      ve0 = exps[16 + g] == 255 ? CUDART_NAN_F : (float)e0;
-      ve1 = exps[16 + g + 8] == 255 ? CUDART_NAN_F : (float)e1;
+      const uint8_t b0 = exps[16 + g], b1 = exps[16 + g + 8];
+      int e0 = cache8_exp_of(b0) + 8, e1 = cache8_exp_of(b1) + 8;
+      if constexpr (CODES) {
+        if (__any_sync(0xffffffffu, b0 == kCache8ZeroByte || b1 == kCache8ZeroByte)) {      // rows of zeros: the smallest exponent there is
+          constexpr int CH = D / 16;
+#pragma unroll 1
+          for (int i = 0; i < CH / 2; ++i) {             // 32 / CH rows at a time
+            const int r = i * (32 / CH) + lane / CH;
+            const uint4 v = *reinterpret_cast<const uint4*>(smem + (img - base) + off8<D>(1, r, lane % CH));
+            const uint32_t some = __ballot_sync(0xffffffffu, cache8_magnitudes(v) != 0);
+            auto zeros = [&](int row) { return row / (32 / CH) == i && (some >> (row % (32 / CH) * CH) & ((1u << CH) - 1)) == 0; };
+            if (b0 == kCache8ZeroByte && zeros(g)) e0 = 8 - kCache8MaxExp;
+            if (b1 == kCache8ZeroByte && zeros(g + 8)) e1 = 8 - kCache8MaxExp;
+          }
+        }
+      }
+      ve0 = b0 == 255 ? CUDART_NAN_F : (float)e0;
+      ve1 = b1 == 255 ? CUDART_NAN_F : (float)e1;
       out0 = power(-e0);
       out1 = power(-e1);
     }
@@ -444,7 +459,7 @@ tree_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __gri
 #pragma unroll
           for (int sh = 1; sh < CH; sh <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, sh));
           // largest element to 2^14 .. 2^15 (f16 ends at 65504)
-          const int e = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, 8 - kCache8MaxExp), 8 + kCache8MaxExp);
+          const int e = min(max((int)(most >> 7) - 127 - 14, 8 - kCache8MaxExp), 8 + kCache8MaxExp);      // zeros: the smallest there is
           const float down = power(-e);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = pack_f16(__uint_as_float(x[i] << 16) * down, __uint_as_float(x[i] & 0xffff0000u) * down);

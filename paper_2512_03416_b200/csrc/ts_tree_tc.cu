@@ -781,7 +781,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
               }
               most = __reduce_max_sync(0xffffffffu, most);
             }
-            const int e_v = most == 0 ? 0 : min(max((int)(most >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);
+            const int e_v = min(max((int)(most >> 7) - 127 - 14, -kCache8MaxExp), kCache8MaxExp);      // zeros: the smallest there is
             const float down = power(-e_v);
             load4(r0, x);
             if constexpr (Q8) ok = g < L::kVStages || wait(L::V_EMPTY + st, ((g / L::kVStages) & 1) ^ 1);
@@ -973,7 +973,8 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
       while (ok) {
         if (!wait(L::UNIT_FULL + (k8 & 3), (k8 >> 2) & 1)) break;
         const uint32_t rec = base + L::kOffUnits + (k8 & 3) * 64;
-        auto field = [&](size_t off) { return __shfl_sync(0xffffffffu, lds_i(rec + (uint32_t)off), 0); };
+        // (a reduction: what it gives is known to be the same for all lanes)
+        auto field = [&](size_t off) { return (int)__reduce_or_sync(0xffffffffu, (unsigned)lds_i(rec + (uint32_t)off)); };
         const int valid = UNIT(valid), two = UNIT(cnt_b) > 0, n_cached = UNIT(n_cached), n_blocks = n_cached + UNIT(own);
         arrive(L::UNIT_EMPTY + (k8 & 3));
         if (!valid || !(ok = wait(L::Q_FULL, k8 & 1))) break;
@@ -1100,37 +1101,86 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
         fetch_page(0);
         fetch_bytes();
         fetch_page(1);
-        for (int j = 0; j < n_cached; ++j, ++c) {
-          const uint32_t bytes_k = kb, bytes_v = vb;
-          fetch_bytes();
-          fetch_page(j + 2);
-          const int st = c % kTabStages, real = n_keys - j * kBlock - lane * 4;        // keys of this lane's four
-          float kp[4];
-          int e_v[4], e_top = -kCache8MaxExp;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint8_t k_byte = (uint8_t)(bytes_k >> (8 * i)), v_byte = (uint8_t)(bytes_v >> (8 * i));
-            kp[i] = v_byte == 255 && i < real ? CUDART_NAN_F : cache8_power(k_byte);   // a row with a NaN
-            e_v[i] = i < real ? cache8_exp_of(v_byte) : -kCache8MaxExp;
-            e_top = max(e_top, e_v[i]);
+        auto table = [&](int j, uint32_t bytes_k, uint32_t bytes_v) {
+          // two keys at a time in 16-bit halves: 0 and 2, 1 and 3 of the lane's
+          constexpr uint32_t kMin = 127 - kCache8MaxExp, kMax = 127 + kCache8MaxExp;
+          const int st = c % kTabStages, left = n_keys - j * kBlock;
+          if (left < kBlock) {                               // keys behind the last one: rows of the smallest exponent (their weights are 0)
+            const int real = left - lane * 4;
+            const uint32_t keep = real >= 4 ? 0xffffffffu : real <= 0 ? 0u : (1u << (8 * real)) - 1;
+            bytes_v = (bytes_v & keep) | (kMin * 0x01010101u & ~keep);
           }
+          auto clamped = [](uint32_t two) { return __vminu2(__vmaxu2(two & 0x00ff00ffu, kMin * 0x10001u), kMax * 0x10001u); };
+          const uint32_t k02 = clamped(bytes_k), k13 = clamped(bytes_k >> 8), v02 = clamped(bytes_v), v13 = clamped(bytes_v >> 8);
+          float kp[4] = {__uint_as_float(k02 << 23), __uint_as_float(k13 << 23), __uint_as_float((k02 & 0xff0000u) << 7), __uint_as_float((k13 & 0xff0000u) << 7)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)                        // a row with a NaN
+            if ((bytes_k >> (8 * i) & 255) == 255 || (bytes_v >> (8 * i) & 255) == 255) kp[i] = CUDART_NAN_F;
           // The V rows of 32 keys are brought to the largest of their exponents: f16 has the range for rows up to 2^22 below it.
+          uint32_t top2 = __vmaxu2(v02, v13);
 #pragma unroll
-          for (int sh = 1; sh < 8; sh <<= 1) e_top = max(e_top, __shfl_xor_sync(0xffffffffu, e_top, sh));
-          uint16_t by[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) by[i] = __half_as_ushort(__float2half_rn(i < real ? power(e_v[i] - e_top + 8) : 0.f));      // 2^8: see widen4
-          if (c >= kTabStages && !(ok = wait(L::TAB_EMPTY + st, ((c / kTabStages) & 1) ^ 1))) break;
+          for (int sh = 1; sh < 8; sh <<= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, sh));
+          const int top = max(top2 & 0xffffu, top2 >> 16);
+          // 2^(v - top + 8) as f16 (8: see widen4): normal numbers where bit 7 is set here
+          const uint32_t x02 = v02 + (0x80u + 22) * 0x10001u - top * 0x10001u, x13 = v13 + (0x80u + 22) * 0x10001u - top * 0x10001u;
+          uint32_t by02 = ((x02 & 0x007f007fu) << 10) + 0x04000400u, by13 = ((x13 & 0x007f007fu) << 10) + 0x04000400u;
+          if (__any_sync(0xffffffffu, (x02 & x13 & 0x00800080u) != 0x00800080u)) {
+            auto pair = [&](uint32_t two) {
+              auto one = [&](int v) { return (uint32_t)__half_as_ushort(__float2half_rn(power(v - top + 8))); };
+              return one(two & 0xffffu) | one(two >> 16) << 16;
+            };
+            by02 = pair(v02);
+            by13 = pair(v13);
+          }
+          if (c >= kTabStages && !(ok = wait(L::TAB_EMPTY + st, ((c / kTabStages) & 1) ^ 1))) return;
           float* tab = reinterpret_cast<float*>(smem + L::kOffTab) + st * kBlock;
           *reinterpret_cast<float2*>(tab + tab_at(lane * 4)) = make_float2(kp[0], kp[1]);
           *reinterpret_cast<float2*>(tab + tab_at(lane * 4 + 2)) = make_float2(kp[2], kp[3]);
-          *reinterpret_cast<uint2*>(smem + L::kOffBy + (st * kBlock + lane * 4) * 2) = make_uint2(by[0] | by[1] << 16, by[2] | by[3] << 16);
+          *reinterpret_cast<uint2*>(smem + L::kOffBy + (st * kBlock + lane * 4) * 2) = make_uint2(__byte_perm(by02, by13, 0x5410), __byte_perm(by02, by13, 0x7632));
           if ((lane & 7) == 0) {
             float* e = reinterpret_cast<float*>(smem + L::kOffExp + st * 32);
-            e[lane >> 3] = (float)e_top;
-            e[4 + (lane >> 3)] = power(-e_top);
+            e[lane >> 3] = (float)(top - 127);
+            e[4 + (lane >> 3)] = power(127 - top);
           }
           arrive(L::TAB_FULL + st);
+          ++c;
+        };
+        int j = 0;
+        uint32_t bytes_k = 0, bytes_v = 0;
+        bool zeros = false;
+        for (; ok && j < n_cached; ++j) {
+          bytes_k = kb;
+          bytes_v = vb;
+          fetch_bytes();
+          fetch_page(j + 2);
+          zeros = __any_sync(0xffffffffu, __vcmpeq4(bytes_v, kCache8ZeroByte * 0x01010101u) != 0);
+          if (__builtin_expect(zeros, 0)) break;
+          table(j, bytes_k, bytes_v);
+        }
+        // The rest of a unit from the first block on whose V rows may be zeros, which have the smallest exponent there is. In a loop of its own: with these
+        // looks in the loop above, never taken, 37 rows of 8192 keys x 4 nodes took 195 us, not 151. (What the compiler makes of the one MMA
+        // issuer's instructions depends on the other roles'; its unit's record as uniform values, see there, gained 28 of these 44 back.)
+#pragma unroll 1
+        for (; ok && j < n_cached; ++j) {
+          if (!zeros) {
+            bytes_k = kb;
+            bytes_v = vb;
+            fetch_bytes();
+            fetch_page(j + 2);
+          }
+          zeros = false;
+#pragma unroll 1
+          for (int i = 0; i < 32; i += 8)
+            if ((bytes_v >> i & 255) == kCache8ZeroByte) {   // not of a page that is none: its bytes are 0
+              const size_t row = (scales - a.cache.scales) + ((size_t)table_row[j * kBlockPages + (lane >> 2)] * 2 + 1) * s.Hkv * kPageSize + i / 8;
+              const uint4* codes = reinterpret_cast<const uint4*>(a.cache.values + row * kD);
+              uint32_t some = 0;
+#pragma unroll 1
+              for (int ch = 0; ch < kD / 16; ++ch) some |= cache8_magnitudes(__ldg(codes + ch));
+              if (some == 0) bytes_v ^= (uint32_t)(kCache8ZeroByte ^ (127 - kCache8MaxExp)) << i;
+            }
+          __syncwarp();
+          table(j, bytes_k, bytes_v);
         }
       }
     }

@@ -318,3 +318,21 @@ def test_infinite_k_of_a_seen_node(nodes):
         mine = slice(r * nodes, (r + 1) * nodes)
         assert np.isnan(got[mine][1:, heads]).all()
         assert ok[mine][0].all() and ok[mine][:, ~heads].all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nodes", [1, 6, 12, 33])
+@pytest.mark.parametrize("size", [-6, -20, -40])
+def test_v_rows_of_zeros(size, nodes, d, cache):
+    """Some cached tokens and nodes, and a stretch of 40 tokens, whose V is zero, among small ones: zeros are smaller than any of them."""
+    def v_size(rng, n):
+        i = np.arange(n)
+        return np.where((i % 7 == 3) | ((i >= 200) & (i < 240)), 0.0, 2.0 ** size)
+    Case((8, 2, d), cache, [(700, nodes), (0, nodes), (2100, nodes), (5, nodes)], seed=51, v_size=v_size).check()
+
+
+@pytest.mark.parametrize("nodes", [1, 33])
+def test_nothing_but_zeros(nodes):
+    c = Case((8, 2, 128), "e4m3", [(300, nodes), (0, nodes)], seed=52, v_size=lambda rng, n: np.zeros(n))
+    assert (c.check() == 0).all()

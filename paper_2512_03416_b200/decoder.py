@@ -163,9 +163,9 @@ class Decoder:
 
     # ------------------------------------- trees of drafted tokens; the cache written and read back
     def _tokens(self, t, heads: int, what: str) -> int:
-        """Address of a contiguous 16-bit tensor [N, heads, head_dim] on this device."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or t.element_size() != 2:
-            raise ValueError(f"{what} must be a bf16 (or int16) tensor [N, {heads}, {self.cfg.head_dim}], not {t.dtype} {tuple(t.shape)}")
+        """Address of a contiguous bf16 tensor (or one of its bit patterns) [N, heads, head_dim] on this device."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or t.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
+            raise ValueError(f"{what} must be a bf16 (or int16, uint16) tensor [N, {heads}, {self.cfg.head_dim}], not {t.dtype} {tuple(t.shape)}")
         if t.device != self.device or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous and on {self.device}")
         return t.data_ptr()
@@ -174,7 +174,7 @@ class Decoder:
         """Attention of every request's drafted nodes over its cached tokens and, as mask says, over each other (see
         ts_tree_attention). mask: int64 CUDA tensor [N] of bit sets (tree_masks), None for chains of tokens."""
         hq, hkv, n = self.cfg.n_q_heads, self.cfg.n_kv_heads, sum(n_nodes)
-        if mask is not None and (mask.numel() < n or mask.element_size() != 8 or mask.device != self.device or not mask.is_contiguous()):
+        if mask is not None and (mask.numel() < n or mask.dtype not in (torch.int64, torch.uint64) or mask.device != self.device or not mask.is_contiguous()):
             raise ValueError(f"mask must be a contiguous int64 tensor of {n} words on {self.device}")
         if min(q.shape[0], k_new.shape[0], v_new.shape[0], out.shape[0]) < n:
             raise ValueError(f"the tensors hold fewer than {n} tokens")

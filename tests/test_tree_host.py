@@ -133,3 +133,27 @@ def test_the_oracle_of_the_attention(hq, hkv):
     for h in range(hq):                                              # one key: its V; equal scores: the mean; none: zeros
         assert np.allclose(out[0, h], v[0, h // g]) and np.allclose(out[1, h], v[:, h // g].mean(0)) and (out[2, h] == 0).all()
     assert ctypes.sizeof(B.ts_cache8) == 32
+
+
+def test_types_of_tensors():
+    """16-bit tensors are bf16, or bit patterns of it; masks are 64-bit words. A float16 or float64 tensor is not taken for one by its size."""
+    import types
+
+    import torch
+
+    from paper_2512_03416_b200.decoder import Decoder
+    dec = Decoder.__new__(Decoder)                                 # its checks alone: no device
+    dec.ctx, dec.device, dec.cache = None, torch.device("cpu"), B.TS_CACHE_BF16
+    dec.cfg = types.SimpleNamespace(n_q_heads=4, n_kv_heads=2, head_dim=64)
+    for dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        t = torch.zeros((3, 2, 64), dtype=dtype)
+        assert dec._tokens(t, 2, "k") == t.data_ptr()
+    for dtype in (torch.float16, torch.int8, torch.float32):
+        with pytest.raises(ValueError):
+            dec._tokens(torch.zeros((3, 2, 64), dtype=dtype), 2, "k")
+    q, k = (torch.zeros((3, h, 64), dtype=torch.bfloat16) for h in (4, 2))
+    dec._stream = lambda: 0
+    for mask in (torch.zeros(3, dtype=torch.float64), torch.zeros(3, dtype=torch.complex64), torch.zeros(3, dtype=torch.int32),
+                 torch.zeros(2, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            dec.tree_attention([0], [3], [0], q, k, k, q, mask=mask)

@@ -23,19 +23,24 @@ constexpr int kThreads = 256, kInFlight = 8;
 // Thread blocks per SM at most, several times those that run at a time: neighbouring tokens are then written at the same time. 32768 tokens of
 // eight heads of 128 in 8 bits, written / read back: 4 per SM 45.0 / 38.1 us, 8 43.8 / 38.9, 16 42.2 / 36.9, a warp per token 43.8 / 36.3.
 constexpr int kBlocksPerSm = 16;
+// Rows whose arrays every thread block copies to its shared memory (48 KB without asking for more). Of more rows they are looked up where they
+// are: the search for a token's row is then a dozen round trips to L2, of calls that have thousands of rows.
+constexpr int kStagedRows = 4095;
 
 // Position of a token: its row, its place in the row's request, and the page that holds it (-1: none, reported).
 struct Place {
   int page, slot;
 };
+template <bool STAGED>
 __device__ __forceinline__ Place place_of(const StepDevice& s, const int32_t* rows, int tok) {
   const int n = s.n_rows + 1;
+  auto first = [&](int r) { return STAGED ? rows[r] : s.row_tok0(r); };
   int lo = 0, hi = s.n_rows;                    // last row whose first token is <= tok
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (rows[mid] <= tok) lo = mid; else hi = mid;
+    if (first(mid) <= tok) lo = mid; else hi = mid;
   }
-  const int t = rows[n + lo] + (tok - rows[lo]), slot = rows[2 * n + lo];
+  const int t = (STAGED ? rows[n + lo] : s.row_ctx(lo)) + (tok - first(lo)), slot = STAGED ? rows[2 * n + lo] : s.row_slot(lo);
   Place p = {-1, t & (kPageSize - 1)};
   if ((unsigned)slot >= (unsigned)s.max_requests || (unsigned)(t >> 4) >= (unsigned)s.max_pages_per_req) {
     if ((threadIdx.x & 31) == 0) atomicOr(s.status, TS_DEV_BAD_INDEX);
@@ -101,7 +106,7 @@ __device__ __forceinline__ uint4 dequantise(const uint2& c, uint8_t scale) {
 }
 
 // WRITE: the step's K/V rows (or the tokens `source` names) into their pages. Else: pages into k, v.
-template <bool WRITE, bool Q8, int D>
+template <bool WRITE, bool Q8, int D, bool STAGED>
 __global__ void __launch_bounds__(kThreads)
 cache_kernel(const __grid_constant__ StepParams<kInlineWords> params, const Cache8 cache, const int32_t* __restrict__ source,
              const int n_source) {
@@ -110,8 +115,10 @@ cache_kernel(const __grid_constant__ StepParams<kInlineWords> params, const Cach
   constexpr int LPR = D / 8;                     // lanes of a row
   pdl_launch_dependents();
   pdl_wait();
-  stage_rows(s, rows, threadIdx.x, blockDim.x);
-  __syncthreads();
+  if (STAGED) {
+    stage_rows(s, rows, threadIdx.x, blockDim.x);
+    __syncthreads();
+  }
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // A lane has chunk j * 32 + lane (16 bytes of bf16) of a token's K, and of its V, for j = 0 .. per - 1: u counts K's and V's through.
   // Their places differ by multiples of that of j = 1, which spares the inner loops the address arithmetic.
@@ -140,7 +147,7 @@ cache_kernel(const __grid_constant__ StepParams<kInlineWords> params, const Cach
       }
     };
     if (WRITE) load_wide(0);
-    const Place p = place_of(s, rows, tok);
+    const Place p = place_of<STAGED>(s, rows, tok);
     const bool placed = p.page >= 0;
     // the lane's first row in the page
     const size_t row0 = (size_t)(placed ? p.page : 0) * 2 * v_rows + lane_row + p.slot;
@@ -194,8 +201,10 @@ cudaError_t launch_t(const StepDevice& s, const Cache8& cache, const int32_t* so
   const int blocks = (s.n_tokens + per_block - 1) / per_block;
   StepParams<kInlineWords> params;
   fill_params(s, &params);
-  return launch_pdl(cache_kernel<WRITE, Q8, D>, dim3(blocks < 148 * kBlocksPerSm ? blocks : 148 * kBlocksPerSm), dim3(kThreads), staged_rows_bytes(s.n_rows), stream,
-                    params, cache, source, n_source);
+  const dim3 grid(blocks < 148 * kBlocksPerSm ? blocks : 148 * kBlocksPerSm);
+  return s.n_rows <= kStagedRows
+             ? launch_pdl(cache_kernel<WRITE, Q8, D, true>, grid, dim3(kThreads), staged_rows_bytes(s.n_rows), stream, params, cache, source, n_source)
+             : launch_pdl(cache_kernel<WRITE, Q8, D, false>, grid, dim3(kThreads), 0, stream, params, cache, source, n_source);
 }
 template <bool WRITE>
 cudaError_t launch(const StepDevice& s, const Cache8& cache, const int32_t* source, int n_source, cudaStream_t stream) {

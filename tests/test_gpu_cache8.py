@@ -181,3 +181,30 @@ def test_checks_of_tensors():
         dec.tree_attention([slot], [3], [1], q, k, k, out)            # not the cached length
     with pytest.raises(ValueError):
         Decoder(8, 2, 128, n_pages=8, max_requests=2, max_pages_per_req=4, cache="int8")
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [60, 700, 4095, 4096, 9000])
+def test_many_rows(rows, cache):
+    """One call for thousands of requests: more row arrays than launch parameters (768 words) and than a thread block's default shared memory
+    (4095 rows) hold. 0 to 2 tokens each, then a tree step of a node each."""
+    dec = Decoder(2, 1, 64, n_pages=rows, max_requests=rows, max_pages_per_req=1, alloc_shuffle_seed=5, cache=cache, nan_fill=True)
+    rng = np.random.default_rng(rows)
+    count = [int(x) for x in rng.integers(0, 3, rows)]
+    slots = [dec.request_add(r, 4) for r in range(rows)]
+    for s in slots:
+        dec.alloc_pages(s, 4)
+    n = sum(count)
+    k, v = (rng.integers(-3, 4, (n, 1, 64)).astype(np.float32) for _ in range(2))          # exact in 8 bits
+    dec.cache_append(slots, count, [0] * rows, to_dev(wl.f32_to_bf16_bits(k)), to_dev(wl.f32_to_bf16_bits(v)))
+    ko, vo = (torch.empty((n, 1, 64), dtype=torch.int16, device="cuda") for _ in range(2))
+    dec.cache_read(slots, [0] * rows, count, ko, vo)
+    assert np.array_equal(_values(ko.cpu().numpy().view(np.uint16)), k) and np.array_equal(_values(vo.cpu().numpy().view(np.uint16)), v)
+    q = torch.zeros((rows, 2, 64), dtype=torch.bfloat16, device="cuda")                   # equal scores: the mean of V
+    out = torch.empty_like(q)
+    v1 = torch.ones((rows, 1, 64), dtype=torch.bfloat16, device="cuda")
+    dec.tree_attention(slots, [1] * rows, count, q, v1, v1, out)
+    assert dec.device_status() == 0
+    first = np.concatenate([[0], np.cumsum(count)])
+    want = np.stack([(v[a:b].sum(0) + 1) / (b - a + 1) for a, b in zip(first[:-1], first[1:])])
+    assert np.abs(out.float().cpu().numpy() - want).max() <= 2.0 ** -7 * 4

@@ -591,7 +591,7 @@ int ts_cache_read(ts_ctx* ctx, const ts_step* step, int32_t cache, void* k_out, 
 enum { TS_BF16 = 0, TS_F32 = 1 };
 typedef struct {
   int32_t device;
-  int32_t n_rows, vocab;     /* vocab >= 1, at most 2^30                                            */
+  int32_t n_rows, vocab;     /* vocab >= 1; both at most 2^30                                       */
   int32_t dtype;             /* TS_BF16 or TS_F32                                                   */
   const void* logits;        /* DEVICE [n_rows], rows row_stride elements apart (>= vocab), aligned to their type only */
   int64_t row_stride;

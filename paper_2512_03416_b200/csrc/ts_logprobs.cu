@@ -692,7 +692,7 @@ extern "C" int ts_token_logprobs(const ts_logprobs* p, void* cuda_stream) {
   if (p->n_rows < 0 || p->vocab < 1 || p->row_stride < p->vocab) return TS_ERR_INVALID;
   if (p->n_given < 0 || p->n_given > ts::kMaxGiven || p->n_top < 0 || p->n_top > ts::kMaxTop) return TS_ERR_INVALID;
   if (p->dtype != TS_BF16 && p->dtype != TS_F32) return TS_ERR_UNSUPPORTED;
-  if (p->vocab > (1 << 30)) return TS_ERR_UNSUPPORTED;
+  if (p->vocab > (1 << 30) || p->n_rows > (1 << 30)) return TS_ERR_UNSUPPORTED;      // the kernel counts both, and a few rows on, in 32 bits
   if (p->n_rows == 0) return TS_OK;
   const uintptr_t elem = p->dtype == TS_BF16 ? 2 : 4;
   if (!p->logits || (uintptr_t)p->logits % elem) return TS_ERR_INVALID;

@@ -157,3 +157,11 @@ def test_types_of_tensors():
                  torch.zeros(2, dtype=torch.int64)):
         with pytest.raises(ValueError):
             dec.tree_attention([0], [3], [0], q, k, k, q, mask=mask)
+
+
+def test_logprobs_of_too_many_rows():
+    """Row numbers of a call, and those a block looks ahead to, fit into 32 bits."""
+    args = dict(device=0, vocab=100, dtype=B.TS_F32, logits=256, row_stride=100, scale=None, tokens=256, n_given=1, n_top=2, logprob=256,
+                rank=256, entropy=256, top_logprob=256, top_token=256)
+    for n_rows in ((1 << 30) + 1, (1 << 31) - 1):
+        assert B.ts_token_logprobs(B.ts_logprobs(**dict(args, n_rows=n_rows)), 0) == B.TS_ERR_UNSUPPORTED

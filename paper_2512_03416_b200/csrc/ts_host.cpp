@@ -1055,7 +1055,7 @@ struct TreePlan {
 // 64 rows x 4 nodes of 500 and 4000 keys 41 / 46, 163 / 184, x 5 nodes of 500 57 / 46, 8 rows of 4000 x 5 45 / 37. 8 bits, 37 rows of 8192 keys x 1, 2,
 // 4, 8 nodes 131 / 212, 133 / 200, 188 / 168, 277 / 169; 64 rows x 4 nodes of 500, 2000 and 4000 keys 48 / 59, 114 / 109, 175 / 170, 16 rows of
 // 4000 56 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 48 / 46, 74 / 57, 112 / 76.
-constexpr int kTreeTcQueries = 16, kTreeTcQueries8 = 8;
+constexpr int kTreeTcQueries = 16, kTreeTcQueries8 = 8;     // (the streaming kernel has no bf16 variant of head_dim 128 for more than 16)
 constexpr int kTreeTcKeys8[2] = {2000, 200};               // up to 16 queries, up to 32
 bool tree_on_tc(const ts_ctx* c, int nodes, int64_t mean_keys, int cache) {
   const int queries = nodes * c->G;

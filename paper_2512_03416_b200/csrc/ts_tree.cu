@@ -609,7 +609,8 @@ cudaError_t launch_d(const StepDevice& s, const TreeArgs& a, const CUtensorMap& 
   const int queries = a.tile_tokens * (s.Hq / s.Hkv);
   if (queries <= 8) return launch_t<D, 1, Q8>(s, a, kv_map, stream);
   if (queries <= 16) return launch_t<D, 2, Q8>(s, a, kv_map, stream);
-  return launch_t<D, 4, Q8>(s, a, kv_map, stream);
+  if constexpr (D == 128 && !Q8) return cudaErrorInvalidValue;      // more than kTreeTcQueries queries: on tcgen05
+  else return launch_t<D, 4, Q8>(s, a, kv_map, stream);
 }
 
 }  // namespace

@@ -1051,10 +1051,11 @@ struct TreePlan {
 };
 // A step of a head_dim of 128 runs on tcgen05 where the row with most nodes has more queries per KV head than this; in 8 bits, where a unit costs more
 // there, only if its rows have kTreeTcKeys8 cached tokens on average, more than 32 queries (two tiles when streamed) always. us, streamed / on
-// tcgen05, 8B shape (four queries a node): bf16, 37 rows of 8192 keys x 1, 4, 8, 16 nodes 194 / 200, 203 / 201, 211 / 204, 401 / 210;
-// 64 rows x 4 nodes of 500 and 4000 keys 41 / 46, 163 / 184, x 5 nodes of 500 57 / 46, 8 rows of 4000 x 5 45 / 37. 8 bits, 37 rows of 8192 keys x 1, 2,
-// 4, 8 nodes 131 / 212, 133 / 200, 188 / 168, 277 / 169; 64 rows x 4 nodes of 500, 2000 and 4000 keys 48 / 59, 114 / 109, 175 / 170, 16 rows of
-// 4000 56 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 48 / 46, 74 / 57, 112 / 76.
+// tcgen05, 8B shape (four queries a node): bf16, 37 rows of 8192 keys x 1, 4, 8, 16 nodes 192 / 201, 200 / 202, 210 / 203, 406 / 207;
+// 64 rows x 4 nodes of 500 and 4000 keys 45 / 47, 167 / 185, x 5 nodes of 500 63 / 47, 8 rows of 500 x 5 22 / 17. 8 bits, 37 rows of 8192 keys x 1, 2,
+// 4, 8 nodes 132 / 167, 134 / 166, 192 / 154, 280 / 156; 64 rows x 4 nodes of 500, 2000 and 4000 keys 51 / 61, 117 / 109, 179 / 169, 16 rows of
+// 4000 58 / 50; 64 rows x 8 nodes of 200, 500 and 1000 keys 53 / 49, 79 / 61, 115 / 80. The rule is for the step: rows of few queries go where its largest
+// tree goes, and pay what the other kernel would have saved them.
 constexpr int kTreeTcQueries = 16, kTreeTcQueries8 = 8;     // (the streaming kernel has no bf16 variant of head_dim 128 for more than 16)
 constexpr int kTreeTcKeys8[2] = {2000, 200};               // up to 16 queries, up to 32
 bool tree_on_tc(const ts_ctx* c, int nodes, int64_t mean_keys, int cache) {

@@ -21,11 +21,11 @@
 //
 // What bounds it: HBM for fp32 logits without given tokens (2000 rows of 100003: 127 us, 6.3 TB/s = 0.98 of a copy; with 20 alternatives 147). For
 // bf16 the issue of instructions: an SM's share of HBM is 11 logits a cycle, which is 11 instructions for each; the sums and the maximum take
-// about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 10000 a row (1024 x 131072: 67 us without given
-// tokens, 83 with one and 5 alternatives, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 72). One row of 32000: 14 us on
+// about 9, a given token 1.5 more wherever something may be in front of it, the end of a row 7500 a row (1024 x 131072: 59 us for the entropy
+// alone, 83 with one and 5 alternatives, 3.2 TB/s; 2000 rows of 32001, whose ends weigh more, 72). One row of 32000: 14 us on
 // the device, all of it round trips (cluster launch, copies, two sorts, the cluster's barrier). Tried and dropped: blocks of 16 warps (a row's end
 // then idles the SM), sums in packed pairs (moves ate the gain),
-// counts as sums of comparison masks (bf16 1 % at most, fp32 a third slower). Five and more given tokens with alternatives spill 5 registers, seldom read.
+// counts as sums of comparison masks (bf16 1 % at most, fp32 a third slower). Five and more given tokens with alternatives spill 10 registers, seldom read.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>

@@ -13,10 +13,11 @@
 //
 // What bounds it: a tile of 128 rows takes 1024 cycles of MMAs and as many of exponentials per block; the block's K and V take
 // 2850 cycles of an SM's share of HBM in bf16, 1430 in 8 bits. Units of one tile are HBM's in bf16 (37 rows of 8192 keys x 16 nodes, 8 KV heads x 4
-// query heads: 1.24 GB in 206 us, 6.0 TB/s = 0.93 of a copy). In 8 bits they are their own chain's (the same: 0.64 GB in 165 to 170 us, 3.8 TB/s):
-// about 2600 cycles per block from P V over the widening of the next V to the next P V, with the looks at barriers of the one MMA issuer.
+// query heads: 1.24 GB in 206 us, 6.0 TB/s = 0.93 of a copy). In 8 bits they are their own chain's (the same: 0.64 GB in 166 to 177 us, 3.8 TB/s):
+// about 2600 cycles per block from P V over the widening of the next V to the next P V, with the looks at barriers of the one MMA issuer. There the roles' instructions
+// together are more than the instruction cache holds (stalls for no instruction 1.2 per issue): code that is never reached can cost 30 %.
 // Units of two tiles are the chain's of a tile (scores, exponentials, P V, next scores; 4100 to 4700 cycles per block; 37 rows of 4096 keys x
-// 32 nodes, 8 KV heads x 8 query heads: 160 us, 0.58 of the MMAs' rate, in 8 bits 192). A change of units costs 5 us of latency where
+// 32 nodes, 8 KV heads x 8 query heads: 157 us, 0.59 of the MMAs' rate, in 8 bits 183). A change of units costs 5 us of latency where
 // rows are short, because a unit's epilogue and the next one's first scores follow each other (64 rows of 500 keys x 8 nodes 47 us, of 22 for their bytes).
 // It took 8 when four warps laid out a row's nodes two rows at a time; loads of the next unit's queries ahead of the wait for their place
 // gained 0.5 % in bf16 and lost 7 in 8 bits (the widening then keeps fewer loads under way).
@@ -1158,8 +1159,7 @@ tree_tc_kernel(const __grid_constant__ StepParams<kInlineWords> params, const __
           table(j, bytes_k, bytes_v);
         }
         // The rest of a unit from the first block on whose V rows may be zeros, which have the smallest exponent there is. In a loop of its own: with these
-        // looks in the loop above, never taken, 37 rows of 8192 keys x 4 nodes took 195 us, not 151. (What the compiler makes of the one MMA
-        // issuer's instructions depends on the other roles'; its unit's record as uniform values, see there, gained 28 of these 44 back.)
+        // looks in the loop above, never taken, 37 rows of 8192 keys x 4 nodes took 195 us, not 151 (see the head of this file).
 #pragma unroll 1
         for (; ok && j < n_cached; ++j) {
           if (!zeros) {

@@ -607,6 +607,52 @@ typedef struct {
 } ts_logprobs;
 int ts_token_logprobs(const ts_logprobs* args, void* cuda_stream);
 
+/*
+ * Requests that are not alike: low-rank adapters, sampling of drafted tokens, shared cache pages. (The paper has no
+ * counterpart: its requests share one set of weights and no page.)
+ *
+ * Adapters of one projection W [N][K]: adapter a adds scale_a * (x . A_a^T) . B_a^T to the tokens of the requests that use it.
+ *   u = scale_a * x . A_a^T is summed in fp32 and rounded to bf16, x . W^T + u . B_a^T (+ R) is one sum in fp32, rounded once.
+ * Adapters trained on parts of a fused projection (query, key and value heads) are stacked: the A of the parts below each other,
+ * their B on the diagonal of a B of zeros. B of a gate/up projection has its rows in the order of ts_pack_gate_up (which packs B too: a
+ * matrix [intermediate][rank] for "hidden" = rank).
+ */
+typedef struct {
+  int32_t n_adapters;       /* 1 to 65536                                                       */
+  int32_t rank;             /* a multiple of 8, 8 to 256; adapters of less have rows and columns of zeros */
+  const void* a;            /* DEVICE bf16 [n_adapters][rank][K], 16-byte aligned               */
+  const void* b;            /* DEVICE bf16 [n_adapters][N][rank], 16-byte aligned               */
+  const float* scale;       /* DEVICE [n_adapters], or NULL: 1                                  */
+} ts_adapters;
+
+/*
+ * ts_adapter_project: C = (R ? R : 0) + x . W^T + the adapters' part, as ts_gemm_bf16 (arguments and limits there). Row r (a request) has the
+ * next row_tokens[r] >= 1 rows of x, M in all, and uses adapter row_adapter[r], -1 = none; both HOST arrays. C must not overlap x, R
+ * may be C. workspace: DEVICE, 256-byte aligned, ts_adapter_workspace_bytes() bytes, in use until the work enqueued here is done. Up to 1024 rows and 65536
+ * tokens, else TS_ERR_UNSUPPORTED. Asynchronous on cuda_stream; two launches, one where no row has an adapter.
+ * ts_adapter_workspace_bytes: enough for any such call; 0 for arguments outside the limits.
+ */
+size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank);
+int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const void* x, const void* W, const void* R, void* C,
+                       const ts_adapters* adapters, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, void* workspace,
+                       size_t workspace_bytes, int32_t tile_m, int32_t* device_status, void* cuda_stream);
+
+/*
+ * ts_layer_attach_adapters: gives a layer's projections adapters (each NULL or with the same n_adapters; weights and workspace are the
+ * caller's and stay in use; all NULL takes them off again). Wait for the layer's steps before changing them.
+ * ts_layer_step_adapted: ts_layer_step in which row r of the step uses adapter row_adapter[r] (HOST, -1 = none) in every projection that has
+ * adapters; row_adapter NULL = no adapters. Up to 1024 rows where one is used. ts_layer_adapters_workspace_bytes: 0 where no projection has
+ * adapters or on a bad shape.
+ */
+typedef struct {
+  const ts_adapters *qkv, *o, *gate_up, *down;
+  void* workspace;          /* DEVICE, ts_layer_adapters_workspace_bytes() bytes, 256-byte aligned */
+  size_t workspace_bytes;
+} ts_layer_adapters;
+size_t ts_layer_adapters_workspace_bytes(const ts_config* cfg, const ts_layer_adapters* adapters);
+int ts_layer_attach_adapters(ts_layer* layer, const ts_layer_adapters* adapters);
+int ts_layer_step_adapted(ts_layer* layer, const ts_step* step, const int32_t* row_adapter, const void* x_in, void* x_out, void* cuda_stream);
+
 /* The cudaError_t of the most recent failed CUDA call of this context (0 if none). */
 int ts_last_cuda_error(const ts_ctx* ctx);
 

@@ -90,6 +90,16 @@ class ts_logprobs(ctypes.Structure):
                 ("top_logprob", ctypes.c_void_p), ("top_token", ctypes.c_void_p)]
 
 
+class ts_adapters(ctypes.Structure):
+    _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
+
+
+class ts_layer_adapters(ctypes.Structure):
+    _fields_ = [(name, ctypes.POINTER(ts_adapters)) for name in ("qkv", "o", "gate_up", "down")] + \
+               [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts_request_add",
            "ts_alloc_pages", "ts_block_table", "ts_block_table_set", "ts_request_free",
            "ts_request_set_len", "ts_kv_append", "ts_mixed_step", "ts_mixed_step_host", "ts_host_fence",
@@ -101,7 +111,8 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_layer_workspace_bytes", "ts_pack_gate_up", "ts_layer_create", "ts_layer_destroy", "ts_layer_step",
            "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan", "ts_cache8_value_bytes",
            "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
-           "ts_cache_read", "ts_token_logprobs"]
+           "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project",
+           "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted"]
 
 _lib = None
 
@@ -187,6 +198,13 @@ def lib() -> ctypes.CDLL:
         L.ts_cache_append.argtypes = [vp, stepp, ctypes.c_int32, vp, ctypes.c_int32, vp]
         L.ts_cache_read.argtypes = [vp, stepp, ctypes.c_int32, vp, vp, vp]
         L.ts_token_logprobs.argtypes = [ctypes.POINTER(ts_logprobs), vp]
+        adp, i32 = ctypes.POINTER(ts_adapters), ctypes.c_int32
+        L.ts_adapter_workspace_bytes.restype = L.ts_layer_adapters_workspace_bytes.restype = ctypes.c_size_t
+        L.ts_adapter_workspace_bytes.argtypes = [i32] * 4
+        L.ts_adapter_project.argtypes = [i32] * 4 + [vp] * 4 + [adp, i32, _i32p, _i32p, vp, ctypes.c_size_t, i32, vp, vp]
+        L.ts_layer_adapters_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(ts_layer_adapters)]
+        L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
+        L.ts_layer_step_adapted.argtypes = [vp, stepp, _i32p, vp, vp, vp]
         L.ts_strerror.restype = ctypes.c_char_p
         L.ts_strerror.argtypes = [ctypes.c_int]
         for name in EXPORTS:
@@ -495,3 +513,30 @@ def ts_cache_read(ctx, step: ts_step, cache: int, k_out: int, v_out: int, stream
 
 def ts_token_logprobs(args: ts_logprobs, stream: int) -> int:
     return lib().ts_token_logprobs(ctypes.byref(args), stream)
+
+
+# --------------------------------------------------------------------------- adapters of the requests of a step
+def ts_adapter_workspace_bytes(n_tokens: int, n_rows: int, n_adapters: int, rank: int) -> int:
+    return lib().ts_adapter_workspace_bytes(n_tokens, n_rows, n_adapters, rank)
+
+
+def ts_adapter_project(device: int, M: int, N: int, K: int, x: int, W: int, R: int, C: int, adapters: ts_adapters, n_rows: int, row_tokens,
+                       row_adapter, workspace: int, workspace_bytes: int, tile_m: int, status: int, stream: int) -> int:
+    """row_tokens, row_adapter: sequences of n_rows numbers."""
+    rows = ctypes.c_int32 * max(n_rows, 1)
+    return lib().ts_adapter_project(device, M, N, K, x, W, R or None, C, ctypes.byref(adapters), n_rows, rows(*row_tokens), rows(*row_adapter),
+                                    workspace, workspace_bytes, tile_m, status, stream)
+
+
+def ts_layer_adapters_workspace_bytes(cfg: ts_config, adapters: ts_layer_adapters) -> int:
+    return lib().ts_layer_adapters_workspace_bytes(ctypes.byref(cfg), ctypes.byref(adapters))
+
+
+def ts_layer_attach_adapters(layer, adapters: ts_layer_adapters) -> int:
+    return lib().ts_layer_attach_adapters(layer, ctypes.byref(adapters))
+
+
+def ts_layer_step_adapted(layer, step: ts_step, row_adapter, x_in: int, x_out: int, stream: int) -> int:
+    """row_adapter: a sequence of step.n_rows numbers, or None."""
+    rows = None if row_adapter is None else (ctypes.c_int32 * max(step.n_rows, 1))(*row_adapter)
+    return lib().ts_layer_step_adapted(layer, ctypes.byref(step), rows, x_in, x_out, stream)

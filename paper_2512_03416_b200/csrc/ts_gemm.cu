@@ -19,6 +19,7 @@
 // accumulator row: TMEM -> registers -> bf16 -> global; in the split kernel all warps add up and write).
 // Epilogues: plain store, store + residual (C = R + A . B^T), rotary embedding of the query and key
 // heads of a fused QKV projection, and SiLU-gated product of a fused gate/up projection.
+// With ADAPT, low-rank adapters of the tokens' requests ride along as further K blocks of a tile (see AdapterTiles).
 // Every wait is bounded; a wait that runs out raises TS_DEV_TIMEOUT and the CTA drains.
 #include <cuda_bf16.h>
 
@@ -115,6 +116,47 @@ __device__ __forceinline__ void silu_mul8(float* gate, const float* up) {
     const float a = __bfloat162float(__float2bfloat16_rn(gate[e])), b = __bfloat162float(__float2bfloat16_rn(up[e]));
     gate[e] = a / silu_den(a) * b;
   }
+}
+
+// ------------------------------------------------------------------------------- low-rank adapters
+// Adapter a adds u . B_a^T to the rows of its tokens, u = scale_a x A_a^T rounded to bf16 (adapter_down_kernel). In the product that is
+// more of K: behind the K blocks of x and W a tile goes through the adapters that its tokens use, one after the other, with B_a's
+// columns as the weights' side and, as the tokens' side, u with zeros in the rows of other adapters' tokens: a row of zeros
+// adds nothing, whatever epilogue follows sees one sum in fp32, and B_a is read once per tile. A "granule" is `width` (16, 32 or 64) of
+// an adapter's rank; a stage holds 64 / width of them, each with the swizzle of its width, so that a rank of 16 moves a quarter of the
+// bytes that a padded K block would.
+template <bool ADAPT>
+struct AdapterParams {};
+template <>
+struct AdapterParams<true> {
+  AdapterTiles t;
+  CUtensorMap u, b;        // u: (width, row), box of width x the rows a thread block loads; b: see GemmMaps
+};
+// The granules of a tile: numbers first .. first + count - 1 of all granules.
+struct Granules {
+  int first, count;
+};
+__device__ __forceinline__ Granules granules_of(const AdapterTiles& t, int tile) {
+  const int first = t.tile_first[tile];
+  return Granules{first * t.granules, (t.tile_first[tile + 1] - first) * t.granules};
+}
+// K blocks that `count` granules take
+__device__ __forceinline__ int granule_blocks(const AdapterTiles& t, int count) { return (count * t.width + kBK - 1) / kBK; }
+// smem_desc for rows of `width` elements, swizzled over their width
+__device__ __forceinline__ uint64_t granule_desc(uint32_t addr, int width) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr >> 4) & 0x3FFF);
+  d |= (uint64_t)((uint32_t)width & 0x3FFF) << 32;         // 8 rows x 2 width bytes, in units of 16
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)(width == 64 ? 2 : width == 32 ? 4 : 6) << 61;   // 128-, 64-, 32-byte swizzle
+  return d;
+}
+// Calls load(granule, its place in the stage) for the granules of K block `block` of those behind x and W; returns how many.
+template <typename Load>
+__device__ __forceinline__ int for_granules(const AdapterTiles& t, Granules gr, int block, Load&& load) {
+  const int per = kBK / t.width, n = min(per, gr.count - block * per);
+  for (int j = 0; j < n; ++j) load(gr.first + block * per + j, j);
+  return n;
 }
 
 // Epilogue of one accumulator (TMEM lanes = 128 rows, 256 columns): half `hf` of this thread's row of
@@ -216,9 +258,10 @@ __device__ __forceinline__ void epilogue_row(const GemmArgs& g, uint32_t tacc, i
 }
 
 // One CTA per 128 x 256 tile, persistent; the two accumulators alternate between tiles.
-template <int EPI>
+template <int EPI, bool ADAPT>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map) {
+gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+            const __grid_constant__ AdapterParams<ADAPT> ad) {
   constexpr int kStages = kTileStages, kStageBytes = kABytes + kBBytes;
   constexpr int kOffBar = kStages * kStageBytes;
   extern __shared__ unsigned char smem_raw[];
@@ -274,6 +317,23 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
           tma_load_2d(dst + kABytes, &b_map, bar(BAR_FULL + st), kb * kBK, n0);
           tma_load_2d(dst + kABytes + kBBytes / 2, &b_map, bar(BAR_FULL + st), kb * kBK, n0 + 128);
         }
+        if constexpr (ADAPT) {
+          const Granules gr = granules_of(ad.t, t % m_tiles);
+          const int width = ad.t.width, row = width * 2;
+          for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
+            const int st = it % kStages;
+            if (it >= kStages) wait(BAR_EMPTY + st, ((it / kStages) & 1) ^ 1);
+            if (misc[1]) continue;
+            const uint32_t dst = base + st * kStageBytes;
+            mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (128 + kBN) * row);
+            for_granules(ad.t, gr, e, [&](int n, int j) {
+              const int entry = n / ad.t.granules, c = n % ad.t.granules, a = ad.t.entry_adapter[entry];
+              tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, n * ad.t.rows);
+              tma_load_3d(dst + kABytes + j * kBN * row, &ad.b, bar(BAR_FULL + st), c * width, n0, a);
+              tma_load_3d(dst + kABytes + (j * kBN + 128) * row, &ad.b, bar(BAR_FULL + st), c * width, n0 + 128, a);
+            });
+          }
+        }
       }
     }
   } else if (warp == 1) {
@@ -304,6 +364,23 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
             mma_ss(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), kIdesc,
                    (kb > 0 || ks > 0) ? 1u : 0u, issue);
           tc_commit(bar(BAR_EMPTY + st), issue);           // the stage is free once these MMAs have read it
+        }
+      }
+      if constexpr (ADAPT) {
+        const Granules gr = granules_of(ad.t, t % m_tiles);
+        const int width = ad.t.width;
+        for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
+          const int st = it % kStages;
+          iwait(BAR_FULL + st, (it / kStages) & 1);
+          tc_fence_after();
+          if (dead) continue;
+          for_granules(ad.t, gr, e, [&](int, int j) {
+            const uint64_t a_desc = granule_desc(base + st * kStageBytes + j * 128 * width * 2, width);
+            const uint64_t b_desc = granule_desc(base + st * kStageBytes + kABytes + j * kBN * width * 2, width);
+            for (int ks = 0; ks < width / 16; ++ks)
+              mma_ss(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), kIdesc, 1u, issue);
+          });
+          tc_commit(bar(BAR_EMPTY + st), issue);
         }
       }
       if (!dead) tc_commit(bar(BAR_ACC_FULL + buf), issue);
@@ -363,6 +440,13 @@ __device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap
       "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
       "[%0], [%1, {%3, %4, %5, %6, %7}], [%2];\n" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
 __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
@@ -495,9 +579,10 @@ __device__ __forceinline__ void epilogue_tokens(const GemmArgs& g, float (&v)[32
   }
 }
 
-template <int EPI>
+template <int EPI, bool ADAPT>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const int nt) {
+gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const int nt,
+                 const __grid_constant__ AdapterParams<ADAPT> ad) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
@@ -560,6 +645,28 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
             tma_load_5d_pair(dst, &w_map, full, kb * kBK, 0, 0, (int)rank * 4, nb);
           tma_load_2d_pair(dst + kABytes, &x_map, full, kb * kBK, m0);
         }
+        if constexpr (ADAPT) {
+          const Granules gr = granules_of(ad.t, t % m_tiles);
+          const int width = ad.t.width, row = width * 2;
+          for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
+            const int st = it % kPairStages;
+            if (it >= kPairStages) wait(BAR_EMPTY + st, ((it / kPairStages) & 1) ^ 1);
+            if (misc[1]) continue;
+            const uint32_t dst = base + st * kPairStageBytes, full = mapa(bar(BAR_FULL + st), 0);
+            if (rank == 0) mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (2 * 128 + nt) * row);
+            for_granules(ad.t, gr, e, [&](int n, int j) {
+              const int entry = n / ad.t.granules, c = n % ad.t.granules, a = ad.t.entry_adapter[entry];
+              const uint32_t to = dst + j * 128 * row;
+              if (EPI == GEMM_EPI_STORE)
+                tma_load_3d_pair(to, &ad.b, full, c * width, nb * kBN + (int)rank * 128, a);
+              else if (EPI == GEMM_EPI_ROPE)               // the adapters' blocks of rows lie behind one another
+                tma_load_5d_pair(to, &ad.b, full, c * width, 0, 0, 0, a * (g.N / 128) + nb * 2 + (int)rank);
+              else
+                tma_load_5d_pair(to, &ad.b, full, c * width, 0, 0, (int)rank * 4, a * (g.N / 256) + nb);
+              tma_load_2d_pair(dst + kABytes + j * (nt / 2) * row, &ad.u, full, 0, n * nt + (int)rank * (nt / 2));
+            });
+          }
+        }
       }
       // the commits that free the last stages arrive here too: they must have before this CTA may leave
       for (int i = max(0, it - kPairStages); i < it; ++i) wait(BAR_EMPTY + i % kPairStages, (i / kPairStages) & 1);
@@ -592,6 +699,23 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
             for (int ks = 0; ks < kBK / 16; ++ks)
               mma_ss_pair(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), idesc,
                           (kb > 0 || ks > 0) ? 1u : 0u, issue);
+            tc_commit_pair(bar(BAR_EMPTY + st), issue);
+          }
+        }
+        if constexpr (ADAPT) {
+          const Granules gr = granules_of(ad.t, t % m_tiles);
+          const int width = ad.t.width;
+          for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
+            const int st = it % kPairStages;
+            iwait(BAR_FULL + st, (it / kPairStages) & 1);
+            tc_fence_after();
+            if (dead) continue;
+            for_granules(ad.t, gr, e, [&](int, int j) {
+              const uint64_t a_desc = granule_desc(base + st * kPairStageBytes + j * 128 * width * 2, width);
+              const uint64_t b_desc = granule_desc(base + st * kPairStageBytes + kABytes + j * (nt / 2) * width * 2, width);
+              for (int ks = 0; ks < width / 16; ++ks)
+                mma_ss_pair(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), idesc, 1u, issue);
+            });
             tc_commit_pair(bar(BAR_EMPTY + st), issue);
           }
         }
@@ -672,9 +796,10 @@ static_assert(128 * kSplitN * 4 <= kSplitStages * kSplitStageBytes, "the accumul
 // 16-byte chunk `c` of row `row` of the accumulator image; the XOR spreads a column of rows over the banks
 __device__ __forceinline__ uint32_t image_off(int row, int c) { return (uint32_t)(row * (kSplitN * 4) + ((c ^ (row & 7)) << 4)); }
 
-template <int EPI>
+template <int EPI, bool ADAPT>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const int split) {
+gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const int split,
+                  const __grid_constant__ AdapterParams<ADAPT> ad) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
@@ -707,7 +832,7 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
   const int m0 = (t % m_tiles) * 128, n0 = (t / m_tiles) * kSplitN;
   const int rows = min(128, g.M - m0);
   const int k_blocks = (g.K + kBK - 1) / kBK;
-  const int kb0 = k_blocks * rank / split, kb1 = k_blocks * (rank + 1) / split;   // never empty: split <= k_blocks
+  int kb0 = k_blocks * rank / split, kb1 = k_blocks * (rank + 1) / split;   // never empty: split <= k_blocks
 
   // one item = 8 columns of a row, for ROPE with their partners 64 further on
   constexpr int kItems = EPI == GEMM_EPI_STORE ? 16 : 8;
@@ -733,6 +858,13 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
     tma_prefetch_desc(&b_map);
   }
   pdl_wait();                      // the activations, the residual and the positions come from the launches in front
+  Granules gr = {0, 0};
+  if constexpr (ADAPT) {           // the granules' K blocks are shared out behind those of x and W
+    gr = granules_of(ad.t, t % m_tiles);
+    const int all = k_blocks + granule_blocks(ad.t, gr.count);
+    kb0 = all * rank / split;
+    kb1 = all * (rank + 1) / split;
+  }
 
   if (warp == 0) {
     if (lane == 0) {
@@ -741,6 +873,18 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
         if (it >= kSplitStages && !mbar_wait(bar(BAR_EMPTY + st), ((it / kSplitStages) & 1) ^ 1, misc[1] ? 2000 : g.wait_cycles)) give_up();
         if (misc[1]) continue;                             // after a failure no new copies are started
         const uint32_t dst = base + st * kSplitStageBytes;
+        if constexpr (ADAPT) {
+          if (kb >= k_blocks) {
+            const int e = kb - k_blocks, width = ad.t.width, row = width * 2;
+            mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (128 + kSplitN) * row);
+            for_granules(ad.t, gr, e, [&](int n, int j) {
+              const int entry = n / ad.t.granules, c = n % ad.t.granules;
+              tma_load_3d(dst + kABytes + j * kSplitN * row, &ad.b, bar(BAR_FULL + st), c * width, n0, ad.t.entry_adapter[entry]);
+              tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, n * ad.t.rows);
+            });
+            continue;
+          }
+        }
         mbar_expect_tx(bar(BAR_FULL + st), kSplitStageBytes);
         tma_load_2d(dst + kABytes, &b_map, bar(BAR_FULL + st), kb * kBK, n0);
         tma_load_2d(dst, &a_map, bar(BAR_FULL + st), kb * kBK, m0);
@@ -757,6 +901,19 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
       }
       tc_fence_after();
       if (dead) continue;
+      if constexpr (ADAPT) {
+        if (kb >= k_blocks) {
+          const int width = ad.t.width;
+          for_granules(ad.t, gr, kb - k_blocks, [&](int, int j) {
+            const uint64_t a_desc = granule_desc(base + st * kSplitStageBytes + j * 128 * width * 2, width);
+            const uint64_t b_desc = granule_desc(base + st * kSplitStageBytes + kABytes + j * kSplitN * width * 2, width);
+            for (int ks = 0; ks < width / 16; ++ks)
+              mma_ss(tmem, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), instr_desc(false), (it > 0 || j > 0 || ks > 0) ? 1u : 0u, issue);
+          });
+          tc_commit(bar(BAR_EMPTY + st), issue);
+          continue;
+        }
+      }
       const uint64_t a_desc = smem_desc(base + st * kSplitStageBytes, 0, 1024);
       const uint64_t b_desc = smem_desc(base + st * kSplitStageBytes + kABytes, 0, 1024);
 #pragma unroll
@@ -855,12 +1012,13 @@ cudaError_t launch_cluster(void (*kernel)(Params...), int ctas, int cluster, int
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
-template <int EPI>
-cudaError_t launch_split_t(const GemmArgs& g, const CUtensorMap& a_map, const CUtensorMap& b_map, int split, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(gemm_split_kernel<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+template <int EPI, bool ADAPT>
+cudaError_t launch_split_t(const GemmArgs& g, const CUtensorMap& a_map, const CUtensorMap& b_map, int split, const AdapterParams<ADAPT>& ad,
+                           cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(gemm_split_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
   if (e != cudaSuccess) return e;
   const int tiles = ((g.M + 127) / 128) * ((g.N + kSplitN - 1) / kSplitN);
-  return launch_cluster(gemm_split_kernel<EPI>, tiles * split, split, kSplitSmem, stream, g, a_map, b_map, split);
+  return launch_cluster(gemm_split_kernel<EPI, ADAPT>, tiles * split, split, kSplitSmem, stream, g, a_map, b_map, split, ad);
 }
 
 // CTAs of gemm_split_kernel that the device runs at once in clusters of `split` (a hardware figure;
@@ -872,7 +1030,7 @@ int split_slots(int split) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
   const int have = known[dev][split].load(std::memory_order_relaxed);
   if (have > 0) return have - 1;
-  if (cudaFuncSetAttribute(gemm_split_kernel<GEMM_EPI_STORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess) return 0;
+  if (cudaFuncSetAttribute(gemm_split_kernel<GEMM_EPI_STORE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess) return 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(split);
   cfg.blockDim = dim3(kGemmThreads);
@@ -884,7 +1042,7 @@ int split_slots(int split) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int clusters = 0;
-  if (cudaOccupancyMaxActiveClusters(&clusters, gemm_split_kernel<GEMM_EPI_STORE>, &cfg) != cudaSuccess) {
+  if (cudaOccupancyMaxActiveClusters(&clusters, gemm_split_kernel<GEMM_EPI_STORE, false>, &cfg) != cudaSuccess) {
     cudaGetLastError();
     clusters = 0;
   }
@@ -892,29 +1050,40 @@ int split_slots(int split) {
   return clusters * split;
 }
 
-template <int EPI>
-cudaError_t launch_tile_t(const GemmArgs& g, const CUtensorMap& a_map, const CUtensorMap& b_map, int n_sms, cudaStream_t stream) {
+template <int EPI, bool ADAPT>
+cudaError_t launch_tile_t(const GemmArgs& g, const CUtensorMap& a_map, const CUtensorMap& b_map, int n_sms, const AdapterParams<ADAPT>& ad,
+                          cudaStream_t stream) {
   const size_t smem = (size_t)kTileStages * (kABytes + kBBytes) + (2 * kTileStages + 4) * 8 + 16 + 1024;
-  cudaError_t e = cudaFuncSetAttribute(gemm_kernel<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = cudaFuncSetAttribute(gemm_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int tiles = ((g.M + 127) / 128) * ((g.N + kBN - 1) / kBN);
-  return launch_pdl(gemm_kernel<EPI>, dim3(std::min(n_sms, tiles)), dim3(kGemmThreads), smem, stream, g, a_map, b_map);
+  return launch_pdl(gemm_kernel<EPI, ADAPT>, dim3(std::min(n_sms, tiles)), dim3(kGemmThreads), smem, stream, g, a_map, b_map, ad);
 }
 
-template <int EPI>
-cudaError_t launch_pair_t(const GemmArgs& g, const CUtensorMap& x_map, const CUtensorMap& w_map, int nt, int n_sms, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(gemm_pair_kernel<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+template <int EPI, bool ADAPT>
+cudaError_t launch_pair_t(const GemmArgs& g, const CUtensorMap& x_map, const CUtensorMap& w_map, int nt, int n_sms, const AdapterParams<ADAPT>& ad,
+                          cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(gemm_pair_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
   if (e != cudaSuccess) return e;
   const int tiles = ((g.M + nt - 1) / nt) * ((g.N + kBN - 1) / kBN);
-  return launch_cluster(gemm_pair_kernel<EPI>, 2 * std::min(n_sms / 2, tiles), 2, kPairSmem, stream, g, x_map, w_map, nt);
+  return launch_cluster(gemm_pair_kernel<EPI, ADAPT>, 2 * std::min(n_sms / 2, tiles), 2, kPairSmem, stream, g, x_map, w_map, nt, ad);
 }
 
-template <int EPI>
-cudaError_t launch_epi(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, cudaStream_t stream) {
+template <int EPI, bool ADAPT>
+cudaError_t launch_epi(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, const AdapterParams<ADAPT>& ad, cudaStream_t stream) {
   if constexpr (EPI != GEMM_EPI_SILU_MUL)                // a gate and its up column are 128 columns apart: no tile of 128 holds both
-    if (plan.split > 0) return launch_split_t<EPI>(g, *maps.x, *maps.w, plan.split, stream);
-  if (plan.tile_m == 256) return launch_pair_t<EPI>(g, *maps.x_pair, *maps.w_pair, plan.pair_tokens, n_sms, stream);
-  return launch_tile_t<EPI>(g, *maps.x, *maps.w, n_sms, stream);
+    if (plan.split > 0) return launch_split_t<EPI, ADAPT>(g, *maps.x, *maps.w, plan.split, ad, stream);
+  if (plan.tile_m == 256) return launch_pair_t<EPI, ADAPT>(g, *maps.x_pair, *maps.w_pair, plan.pair_tokens, n_sms, ad, stream);
+  return launch_tile_t<EPI, ADAPT>(g, *maps.x, *maps.w, n_sms, ad, stream);
+}
+
+template <bool ADAPT>
+cudaError_t launch_gemm_t(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, const AdapterParams<ADAPT>& ad, cudaStream_t stream) {
+  switch (g.epi) {
+    case GEMM_EPI_ROPE: return launch_epi<GEMM_EPI_ROPE, ADAPT>(g, maps, plan, n_sms, ad, stream);
+    case GEMM_EPI_SILU_MUL: return launch_epi<GEMM_EPI_SILU_MUL, ADAPT>(g, maps, plan, n_sms, ad, stream);
+    default: return launch_epi<GEMM_EPI_STORE, ADAPT>(g, maps, plan, n_sms, ad, stream);
+  }
 }
 
 }  // namespace
@@ -965,11 +1134,12 @@ GemmPlan gemm_plan(const GemmArgs& g, int n_sms) {
 
 cudaError_t launch_gemm(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, cudaStream_t stream) {
   if (g.M <= 0 || g.N <= 0) return cudaSuccess;
-  switch (g.epi) {
-    case GEMM_EPI_ROPE: return launch_epi<GEMM_EPI_ROPE>(g, maps, plan, n_sms, stream);
-    case GEMM_EPI_SILU_MUL: return launch_epi<GEMM_EPI_SILU_MUL>(g, maps, plan, n_sms, stream);
-    default: return launch_epi<GEMM_EPI_STORE>(g, maps, plan, n_sms, stream);
-  }
+  if (!maps.u) return launch_gemm_t<false>(g, maps, plan, n_sms, AdapterParams<false>{}, stream);
+  AdapterParams<true> ad;
+  ad.t = maps.adapters;
+  ad.u = *maps.u;
+  ad.b = *maps.b;
+  return launch_gemm_t<true>(g, maps, plan, n_sms, ad, stream);
 }
 
 }  // namespace ts

@@ -10,6 +10,7 @@
 #include <cstddef>
 #include <cstring>
 #include <utility>
+#include <vector>
 
 namespace ts {
 
@@ -197,10 +198,42 @@ GemmPlan gemm_plan(const GemmArgs& g, int n_sms);
 // Views of the operands as (K, row). x, w: boxes of 64 x 128. The pair kernel's: x_pair, a box of 64 x
 // pair_tokens / 2; w_pair, for STORE the same as w, else boxes of 64 x 128 whose rows come in the order the epilogue
 // pairs them in (make_paired_map). Those that the plan does not use may be null.
+// u, b: with adapters (AdapterTiles), else null. u: their tokens' side (width, row), a box as high as x's of the plan's kernel; b:
+// their weights' side (rank, row, adapter), a box of width x 128 x 1, or for the pair kernel as w_pair, the adapters' blocks behind one another.
+// The tokens' tiles and their adapters. An entry is an adapter that tokens of a tile use; it has `granules` times `rows` rows of `width` values, the
+// rank's next `width` each, rows of other adapters' tokens zero.
+struct AdapterTiles {
+  const int32_t* tile_first;      // DEVICE [tiles + 1]: a tile's first entry
+  const int32_t* entry_adapter;   // DEVICE [entries]
+  int32_t width, granules, rows;  // 16, 32 or 64; of an adapter's rank; tokens of a tile
+};
 struct GemmMaps {
   const CUtensorMap *x, *x_pair, *w, *w_pair;
+  const CUtensorMap *u, *b;
+  AdapterTiles adapters;
 };
 cudaError_t launch_gemm(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, cudaStream_t stream);
+// How the tokens of a call use adapters, for tiles of `rows` tokens: words of tile_first [tiles + 1], entry_adapter [entries] (both also
+// read by the GEMM kernels), entry_tile [entries], item_first [entries + 1] (groups of 16 tokens in front), seg_first [entries + 1], segs (place in the
+// tile | tokens << 16).
+constexpr int kAdapterWords = 7680;
+struct AdapterPlan {
+  int n_tiles, n_entries, n_groups;
+  uint32_t o_adapter, o_tile, o_item, o_seg_first, o_seg;
+  std::vector<int32_t> words;
+};
+// row_tokens[r] tokens of each row in turn, M in all; row_adapter[r] in [-1, n_adapters). False: more than kAdapterWords.
+bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int n_adapters, AdapterPlan* out);
+struct AdapterDown {
+  const uint16_t *x, *a;          // [M][K], [adapters][rank][K]
+  const float* scale;             // [adapters], or null: 1
+  uint16_t* u;                    // [entries][granules][rows][width]
+  int32_t* plan;                  // tile_first and entry_adapter go here
+  int32_t K, rank, rows;
+  int32_t granules, n_tiles, n_entries;                     // from here on set by the launcher
+  uint32_t o_adapter, o_tile, o_item, o_seg_first, o_seg;
+};
+cudaError_t launch_adapter_down(AdapterDown d, const AdapterPlan& plan, int width, int n_sms, cudaStream_t stream);
 // out[row] = x[row] / sqrt(mean(x[row]^2) + eps) * gain, bf16 in and out, fp32 inside; width % 8 == 0
 cudaError_t launch_rmsnorm(const uint16_t* x, const uint16_t* gain, uint16_t* out, int rows, int width, float eps,
                            cudaStream_t stream);

@@ -54,6 +54,73 @@ bool make_activation_maps(void* encode_fn, const void* ptr, int64_t rows, int64_
   return ok;
 }
 
+// ---- low-rank adapters
+constexpr int kMaxRank = 256, kMaxAdapters = 65536;
+constexpr int kMaxAdapterRows = 1024, kMaxAdapterTokens = 65536;   // their plan fits kAdapterWords
+int granule_width(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
+int padded_rank(int rank) { return (rank + granule_width(rank) - 1) / granule_width(rank) * granule_width(rank); }
+CUtensorMapSwizzle granule_swizzle(int width) {
+  return width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+}
+bool make_map(void* encode_fn, int dim, const void* ptr, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, int width,
+              CUtensorMap* out) {
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return ((EncodeFn)encode_fn)(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)dim, const_cast<void*>(ptr), dims, strides, box, estr,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, granule_swizzle(width), CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The tokens' side of the adapters' part of a product: rows of `width` values.
+bool make_u_map(void* encode_fn, const void* u, int64_t rows, int width, int box_rows, CUtensorMap* out) {
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)width * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)width, (cuuint32_t)box_rows};
+  return make_map(encode_fn, 2, u, dims, strides, box, width, out);
+}
+// The weights' side, b [adapters][N][rank]: (rank, row, adapter), what is beyond the rank or the rows reads as zero. apart > 0: as
+// make_paired_map, the adapters' blocks of rows one after the other.
+bool make_b_map(void* encode_fn, const ts_adapters* ad, int64_t N, int apart, CUtensorMap* out) {
+  const int width = granule_width(ad->rank);
+  const cuuint64_t row = (cuuint64_t)ad->rank * 2;
+  if (apart == 0) {
+    const cuuint64_t dims[3] = {(cuuint64_t)ad->rank, (cuuint64_t)N, (cuuint64_t)ad->n_adapters}, strides[2] = {row, row * N};
+    const cuuint32_t box[3] = {(cuuint32_t)width, 128, 1};
+    return make_map(encode_fn, 3, ad->b, dims, strides, box, width, out);
+  }
+  const cuuint64_t dims[5] = {(cuuint64_t)ad->rank, 16, 2, (cuuint64_t)apart / 16, (cuuint64_t)(N / (2 * apart)) * ad->n_adapters};
+  const cuuint64_t strides[4] = {row, row * apart, row * 16, row * 2 * apart};
+  const cuuint32_t box[5] = {(cuuint32_t)width, 16, 2, 4, 1};
+  return make_map(encode_fn, 5, ad->b, dims, strides, box, width, out);
+}
+bool adapters_ok(const ts_adapters* ad) {
+  return ad->n_adapters > 0 && ad->n_adapters <= kMaxAdapters && ad->rank > 0 && ad->rank <= kMaxRank && ad->rank % 8 == 0 && ad->a && ad->b &&
+         !(((uintptr_t)ad->a | (uintptr_t)ad->b) & 15u) && !((uintptr_t)ad->scale & 3u);
+}
+// Bytes for the plan's device words and for u, for tiles of any size: of M tokens of n_rows rows, entries of tiles of nt tokens are no more than
+// rows + tiles, than tiles * adapters, and than tokens.
+size_t adapter_plan_bytes(int64_t M, int64_t n_rows) { return align_up((size_t)(2 * (M / 16 + 2) + n_rows + 2) * sizeof(int32_t)); }
+size_t adapter_bytes(int64_t M, int64_t n_rows, int64_t n_adapters, int rank) {
+  const int64_t rows = std::min(std::min(M * 256, n_rows * 256 + M + 256), (M + 256) * n_adapters);
+  return adapter_plan_bytes(M, n_rows) + align_up((size_t)rows * padded_rank(rank) * 2);
+}
+bool adapter_rows_ok(int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int32_t n_adapters, int64_t M) {
+  int64_t n = 0;
+  for (int r = 0; r < n_rows; ++r) {
+    if (row_tokens[r] < 1 || row_adapter[r] < -1 || row_adapter[r] >= n_adapters) return false;
+    n += row_tokens[r];
+  }
+  return n == M;
+}
+// How a product with adapters is laid out: planned for the K that the adapters of a tile of 256 tokens add on average.
+ts::GemmPlan adapter_gemm_plan(ts::GemmArgs g, int n_sms, int rank, int n_rows, const int32_t* row_adapter, int n_adapters) {
+  const int tiles = (g.M + 255) / 256, k_blocks = (g.K + 63) / 64;
+  int runs = 0;
+  for (int r = 0; r < n_rows; ++r) runs += row_adapter[r] >= 0 && (r == 0 || row_adapter[r] != row_adapter[r - 1]);
+  const int per_tile = std::min(n_adapters, (runs + tiles - 1) / tiles);
+  const ts::GemmPlan without = ts::gemm_plan(g, n_sms);
+  g.K = (k_blocks + (per_tile * padded_rank(rank) + 63) / 64) * 64;
+  const ts::GemmPlan plan = ts::gemm_plan(g, n_sms);
+  return plan.split > k_blocks ? without : plan;           // every block of a cluster has K blocks also in a tile without adapters
+}
+
 struct LayerLayout {
   size_t off_table, off_pos, off_h, off_q, off_k, off_v, off_attn, off_y, off_z, total;
 };
@@ -83,6 +150,13 @@ void layer_layout(const ts_config* c, const ts_layer_config* l, int max_tokens, 
 
 }  // namespace
 
+// A projection's adapters as the layer uses them.
+struct LayerAdapters {
+  ts_adapters a = {};                          // n_adapters 0: none
+  CUtensorMap b, b_pair;
+  Activations u;                               // of width granule_width(a.rank)
+};
+
 struct ts_layer {
   ts_ctx* ctx = nullptr;
   ts_layer_config cfg;
@@ -98,6 +172,10 @@ struct ts_layer {
   bool pos_busy[kPosRing] = {};
   int pos_next = 0;
   int last_cuda_error = 0;
+  LayerAdapters adapters[4];                   // qkv, o, gate_up, down
+  int32_t n_adapters = 0;                      // 0: none attached
+  char* adapter_ws = nullptr;
+  size_t adapter_plan = 0, adapter_total = 0;  // bytes in front of u, and in all
 };
 
 namespace {
@@ -199,7 +277,64 @@ int ts_layer_destroy(ts_layer* l) {
   return TS_OK;
 }
 
+size_t ts_layer_adapters_workspace_bytes(const ts_config* cfg, const ts_layer_adapters* ad) {
+  if (!cfg || !ad || cfg->chunk_size <= 0 || cfg->chunk_size > kMaxAdapterTokens || cfg->max_requests <= 0) return 0;
+  size_t total = 0;
+  for (const ts_adapters* a : {ad->qkv, ad->o, ad->gate_up, ad->down}) {
+    if (!a) continue;
+    if (a->rank <= 0 || a->rank > kMaxRank || a->rank % 8 || a->n_adapters <= 0 || a->n_adapters > kMaxAdapters) return 0;
+    total = std::max(total, adapter_bytes(cfg->chunk_size, std::min(cfg->max_requests, kMaxAdapterRows), a->n_adapters, a->rank));
+  }
+  return total;
+}
+
+int ts_layer_attach_adapters(ts_layer* l, const ts_layer_adapters* ad) {
+  if (!l || !ad) return TS_ERR_INVALID;
+  const ts_adapters* all[4] = {ad->qkv, ad->o, ad->gate_up, ad->down};
+  int32_t n_adapters = 0;
+  for (const ts_adapters* a : all) {
+    if (!a) continue;
+    if (!adapters_ok(a) || (n_adapters && a->n_adapters != n_adapters)) return TS_ERR_INVALID;
+    n_adapters = a->n_adapters;
+  }
+  LayerAdapters made[4];
+  size_t total = 0, plan = 0;
+  const ts_config* c = l->view.cfg;
+  if (n_adapters) {
+    total = ts_layer_adapters_workspace_bytes(c, ad);
+    if (total == 0) return TS_ERR_UNSUPPORTED;
+    if (!ad->workspace || ((uintptr_t)ad->workspace & (kAlign - 1))) return TS_ERR_INVALID;
+    if (ad->workspace_bytes < total) return TS_ERR_WORKSPACE;
+    plan = adapter_plan_bytes(l->max_tokens, std::min(c->max_requests, kMaxAdapterRows));
+    const char* u = (const char*)ad->workspace + plan;
+    const int64_t qd = (int64_t)c->n_q_heads * c->head_dim, kvd = (int64_t)c->n_kv_heads * c->head_dim;
+    const int64_t out[4] = {qd + 2 * kvd, l->cfg.hidden, 2 * (int64_t)l->cfg.intermediate, l->cfg.hidden};
+    const int apart[4] = {64, 0, 128, 0};
+    TSL_CUDA(l, cudaSetDevice(c->device));
+    for (int i = 0; i < 4; ++i) {
+      if (!all[i]) continue;
+      made[i].a = *all[i];
+      const int width = granule_width(all[i]->rank);
+      const int64_t rows = (int64_t)((total - plan) / (width * 2));
+      bool ok = make_b_map(l->view.encode_fn, all[i], out[i], 0, &made[i].b) && make_b_map(l->view.encode_fn, all[i], out[i], apart[i], &made[i].b_pair) &&
+                make_u_map(l->view.encode_fn, u, rows, width, 128, &made[i].u.full);
+      for (int k = 0; k < 16; ++k) ok = ok && make_u_map(l->view.encode_fn, u, rows, width, 8 * (k + 1), &made[i].u.pair[k]);
+      if (!ok) return lfail(l, cudaErrorInvalidValue);
+    }
+  }
+  for (int i = 0; i < 4; ++i) l->adapters[i] = made[i];
+  l->n_adapters = n_adapters;
+  l->adapter_ws = n_adapters ? (char*)ad->workspace : nullptr;
+  l->adapter_plan = plan;
+  l->adapter_total = total;
+  return TS_OK;
+}
+
 int ts_layer_step(ts_layer* l, const ts_step* st, const void* x_in, void* x_out, void* cuda_stream) {
+  return ts_layer_step_adapted(l, st, nullptr, x_in, x_out, cuda_stream);
+}
+
+int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_adapter, const void* x_in, void* x_out, void* cuda_stream) {
   if (!l || !st) return TS_ERR_INVALID;
   if (st->n_rows == 0) return TS_OK;
   if (!x_in || !x_out || (((uintptr_t)x_in | (uintptr_t)x_out) & 15u)) return TS_ERR_INVALID;
@@ -213,6 +348,12 @@ int ts_layer_step(ts_layer* l, const ts_step* st, const void* x_in, void* x_out,
     n += st->q_len[r];
   }
   if (n > l->max_tokens) return TS_ERR_BUDGET;
+  bool adapted = false;
+  if (row_adapter) {
+    if (!adapter_rows_ok(st->n_rows, st->q_len, row_adapter, l->n_adapters, n)) return TS_ERR_INVALID;
+    for (int r = 0; r < st->n_rows; ++r) adapted = adapted || row_adapter[r] >= 0;
+    if (adapted && st->n_rows > kMaxAdapterRows) return TS_ERR_UNSUPPORTED;
+  }
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   const ts_config* c = l->view.cfg;
   TSL_CUDA(l, cudaSetDevice(c->device));
@@ -262,10 +403,31 @@ int ts_layer_step(ts_layer* l, const ts_step* st, const void* x_in, void* x_out,
   g.status = l->view.status;
   g.wait_cycles = l->view.wait_cycles;
   g.M = N;
-  auto project = [&](const Activations& x, const CUtensorMap& w, const CUtensorMap& w_pair) {
-    const ts::GemmPlan plan = ts::gemm_plan(g, l->view.n_sms);
-    const CUtensorMap* x_pair = plan.pair_tokens > 0 ? &x.pair[plan.pair_tokens / 16 - 1] : nullptr;
-    return ts::launch_gemm(g, ts::GemmMaps{&x.full, x_pair, &w, &w_pair}, plan, l->view.n_sms, stream);
+  ts::AdapterPlan tiles;
+  int tile_rows = 0;                                       // of the plan in `tiles`
+  auto project = [&](const Activations& x, const CUtensorMap& w, const CUtensorMap& w_pair, int which, const uint16_t* in) {
+    const LayerAdapters& ad = l->adapters[which];
+    ts::GemmPlan plan = {};
+    ts::GemmMaps maps = {&x.full, nullptr, &w, &w_pair, nullptr, nullptr, {}};
+    if (adapted && ad.a.n_adapters) {
+      plan = adapter_gemm_plan(g, l->view.n_sms, ad.a.rank, st->n_rows, row_adapter, l->n_adapters);
+      const int rows = plan.pair_tokens > 0 ? plan.pair_tokens : 128;
+      if (rows != tile_rows && !ts::plan_adapters(N, rows, st->n_rows, st->q_len, row_adapter, l->n_adapters, &tiles)) return cudaErrorInvalidValue;
+      tile_rows = rows;
+      int32_t* words = (int32_t*)l->adapter_ws;
+      const int width = granule_width(ad.a.rank);
+      const ts::AdapterDown down = {in, (const uint16_t*)ad.a.a, ad.a.scale, (uint16_t*)(l->adapter_ws + l->adapter_plan), words, g.K, ad.a.rank, rows};
+      if ((size_t)tiles.n_entries * rows * padded_rank(ad.a.rank) * 2 > l->adapter_total - l->adapter_plan) return cudaErrorInvalidValue;   // never
+      const cudaError_t e = ts::launch_adapter_down(down, tiles, width, l->view.n_sms, stream);
+      if (e != cudaSuccess) return e;
+      maps.adapters = {words, words + tiles.n_tiles + 1, width, padded_rank(ad.a.rank) / width, rows};
+      maps.b = plan.pair_tokens > 0 ? &ad.b_pair : &ad.b;
+      maps.u = plan.pair_tokens > 0 ? &ad.u.pair[plan.pair_tokens / 16 - 1] : &ad.u.full;
+    } else {
+      plan = ts::gemm_plan(g, l->view.n_sms);
+    }
+    if (plan.pair_tokens > 0) maps.x_pair = &x.pair[plan.pair_tokens / 16 - 1];
+    return ts::launch_gemm(g, maps, plan, l->view.n_sms, stream);
   };
 
   // h = rmsnorm(x); (q, k, v) = rope(h . W_qkv^T)
@@ -276,7 +438,7 @@ int ts_layer_step(ts_layer* l, const ts_step* st, const void* x_in, void* x_out,
   g.N = qd + 2 * kvd; g.K = hidden; g.epi = ts::GEMM_EPI_ROPE; g.B = (const uint16_t*)l->cfg.w_qkv;
   g.C = q; g.C2 = k; g.C3 = v; g.q_cols = qd; g.kv_cols = kvd; g.pos = pos_dev;
   g.rope_table = (const float2*)(ws + l->L.off_table);
-  TSL_CUDA(l, project(l->a_h, l->w_qkv, l->w_qkv_pair));
+  TSL_CUDA(l, project(l->a_h, l->w_qkv, l->w_qkv_pair, 0, h));
   // attention over the paged KV cache, with the append of the new K/V
   ts_step inner = *st;
   inner.q = q; inner.k_new = k; inner.v_new = v; inner.out = attn;
@@ -284,14 +446,14 @@ int ts_layer_step(ts_layer* l, const ts_step* st, const void* x_in, void* x_out,
   if (rc != TS_OK) return rc;
   // y = x + attn . W_o^T
   g.N = hidden; g.K = qd; g.epi = ts::GEMM_EPI_STORE; g.B = (const uint16_t*)l->cfg.w_o; g.C = y; g.R = (const uint16_t*)x_in; g.ldc = hidden;
-  TSL_CUDA(l, project(l->a_attn, l->w_o, l->w_o));
+  TSL_CUDA(l, project(l->a_attn, l->w_o, l->w_o, 1, attn));
   // h2 = rmsnorm(y); z = silu(h2 . W_gate^T) * (h2 . W_up^T)
   TSL_CUDA(l, ts::launch_rmsnorm(y, (const uint16_t*)l->cfg.w_norm2, h, N, hidden, l->eps, stream));
   g.N = 2 * inter; g.K = hidden; g.epi = ts::GEMM_EPI_SILU_MUL; g.B = (const uint16_t*)l->cfg.w_gate_up; g.C = z; g.R = nullptr; g.ldc = inter;
-  TSL_CUDA(l, project(l->a_h, l->w_gu, l->w_gu_pair));
+  TSL_CUDA(l, project(l->a_h, l->w_gu, l->w_gu_pair, 2, h));
   // out = y + z . W_down^T
   g.N = hidden; g.K = inter; g.epi = ts::GEMM_EPI_STORE; g.B = (const uint16_t*)l->cfg.w_down; g.C = (uint16_t*)x_out; g.R = y; g.ldc = hidden;
-  TSL_CUDA(l, project(l->a_z, l->w_down, l->w_down));
+  TSL_CUDA(l, project(l->a_z, l->w_down, l->w_down, 3, z));
   return TS_OK;
 }
 
@@ -320,7 +482,65 @@ int ts_gemm_bf16(int32_t device, int32_t M, int32_t N, int32_t K, const void* A,
   if (!make_operand_map(encode_fn, A, M, K, &x) || !make_operand_map(encode_fn, B, N, K, &w) ||
       (plan.pair_tokens > 0 && !make_operand_map(encode_fn, A, M, K, &x_pair, plan.pair_tokens / 2)))
     return TS_ERR_CUDA;
-  return ts::launch_gemm(g, ts::GemmMaps{&x, &x_pair, &w, &w}, plan, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
+  return ts::launch_gemm(g, ts::GemmMaps{&x, &x_pair, &w, &w, nullptr, nullptr, {}}, plan, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
+}
+
+size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank) {
+  if (n_tokens <= 0 || n_tokens > kMaxAdapterTokens || n_rows <= 0 || n_rows > kMaxAdapterRows || n_adapters <= 0 || n_adapters > kMaxAdapters ||
+      rank <= 0 || rank > kMaxRank || rank % 8)
+    return 0;
+  return adapter_bytes(n_tokens, n_rows, n_adapters, rank);
+}
+
+int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const void* x, const void* W, const void* R, void* C,
+                       const ts_adapters* ad, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, void* workspace,
+                       size_t workspace_bytes, int32_t tile_m, int32_t* device_status, void* cuda_stream) {
+  if (M < 0 || N <= 0 || K <= 0 || (N % 8) || (K % 8) || !ad || n_rows < 0) return TS_ERR_INVALID;
+  if (!adapters_ok(ad)) return TS_ERR_INVALID;
+  if (M == 0) return n_rows == 0 ? TS_OK : TS_ERR_INVALID;
+  if (!x || !W || !C || !device_status || !row_tokens || !row_adapter || !workspace) return TS_ERR_INVALID;
+  if (((uintptr_t)x | (uintptr_t)W | (uintptr_t)C | (uintptr_t)R) & 15u || ((uintptr_t)workspace & (kAlign - 1))) return TS_ERR_INVALID;
+  if (tile_m != 0 && tile_m != 128 && tile_m != 256) return TS_ERR_INVALID;
+  if (n_rows > kMaxAdapterRows || M > kMaxAdapterTokens) return TS_ERR_UNSUPPORTED;
+  if (!adapter_rows_ok(n_rows, row_tokens, row_adapter, ad->n_adapters, M)) return TS_ERR_INVALID;
+  bool adapted = false;
+  for (int r = 0; r < n_rows; ++r) adapted = adapted || row_adapter[r] >= 0;
+  if (!adapted) return ts_gemm_bf16(device, M, N, K, x, W, R, C, tile_m, device_status, cuda_stream);
+  if (workspace_bytes < adapter_bytes(M, n_rows, ad->n_adapters, ad->rank)) return TS_ERR_WORKSPACE;
+  if (cudaSetDevice(device) != cudaSuccess) return TS_ERR_CUDA;
+  void* encode_fn = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &encode_fn, cudaEnableDefault, &qres) != cudaSuccess || !encode_fn)
+    return TS_ERR_CUDA;
+  int n_sms = 0;
+  if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return TS_ERR_CUDA;
+  ts::GemmArgs g;
+  std::memset(&g, 0, sizeof g);
+  g.M = M; g.N = N; g.K = K; g.epi = ts::GEMM_EPI_STORE; g.B = (const uint16_t*)W;
+  g.C = (uint16_t*)C; g.R = (const uint16_t*)R; g.ldc = N;
+  g.status = device_status;
+  g.wait_cycles = ts::kWaitCycles;
+  const ts::GemmPlan plan = tile_m ? ts::GemmPlan{tile_m, 0, tile_m == 256 ? ts::pair_tokens(M, (M + 255) / 256) : 0}
+                                   : adapter_gemm_plan(g, n_sms, ad->rank, n_rows, row_adapter, ad->n_adapters);
+  const bool pair = plan.pair_tokens > 0;
+  const int rows = pair ? plan.pair_tokens : 128, width = granule_width(ad->rank);
+  ts::AdapterPlan tiles;
+  if (!ts::plan_adapters(M, rows, n_rows, row_tokens, row_adapter, ad->n_adapters, &tiles)) return TS_ERR_UNSUPPORTED;
+  const size_t plan_bytes = adapter_plan_bytes(M, n_rows);
+  int32_t* words = (int32_t*)workspace;
+  uint16_t* u = (uint16_t*)((char*)workspace + plan_bytes);
+  const int granules = padded_rank(ad->rank) / width;
+  const int64_t u_rows = (int64_t)tiles.n_entries * granules * rows;
+  if (plan_bytes + (size_t)u_rows * width * 2 > workspace_bytes) return TS_ERR_WORKSPACE;
+  CUtensorMap mx, mw, mu, mb;                              // the maps of the plan's kernel only
+  if (!make_operand_map(encode_fn, x, M, K, &mx, pair ? rows / 2 : 128) || !make_operand_map(encode_fn, W, N, K, &mw) ||
+      !make_u_map(encode_fn, u, u_rows, width, pair ? rows / 2 : 128, &mu) || !make_b_map(encode_fn, ad, N, 0, &mb))
+    return TS_ERR_CUDA;
+  const ts::AdapterDown down = {(const uint16_t*)x, (const uint16_t*)ad->a, ad->scale, u, words, K, ad->rank, rows};
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (ts::launch_adapter_down(down, tiles, width, n_sms, stream) != cudaSuccess) return TS_ERR_CUDA;
+  const ts::GemmMaps maps = {&mx, &mx, &mw, &mw, &mu, &mb, {words, words + tiles.n_tiles + 1, width, granules, rows}};
+  return ts::launch_gemm(g, maps, plan, n_sms, stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
 }
 
 int ts_gemm_plan(int32_t device, int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* tile_m, int32_t* split,

@@ -3,6 +3,8 @@ and the stream. All computation happens inside libtokenscale.so; this file only 
 """
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding as B
@@ -38,6 +40,38 @@ class DecoderLayer:
         rc, self.handle = B.ts_layer_create(dec.ctx, cfg, stream)
         _check(rc, "ts_layer_create")
 
+    def set_adapters(self, qkv=None, o=None, gate_up=None, down=None) -> None:
+        """Adapters (adapters.Adapters, one count for all) of the projections; b of gate_up in the packed order (pack_gate_up_adapters).
+        Without any: none. Synchronises, since earlier steps may still use the former ones."""
+        torch.cuda.synchronize(self.dec.device)
+        given = dict(qkv=qkv, o=o, gate_up=gate_up, down=down)
+        width = self.weights[1].shape[0], self.weights[1].shape[1], self.weights[2].shape[1], self.w_gate_up.shape[0], self.weights[4].shape[1]
+        shapes = dict(qkv=(width[0], width[1]), o=(width[1], width[2]), gate_up=(width[3], width[1]), down=(width[1], width[4]))
+        for name, ad in given.items():
+            if ad is not None and ((ad.n, ad.k) != shapes[name] or ad.device != self.dec.device):
+                raise ValueError(f"the adapters of {name} must be of a projection {list(shapes[name])} on {self.dec.device}")
+        args = B.ts_layer_adapters(*[None if ad is None else ctypes.pointer(ad.args) for ad in given.values()], None, 0)
+        workspace = None
+        if any(ad is not None for ad in given.values()):
+            nbytes = B.ts_layer_adapters_workspace_bytes(self.dec.cfg, args)
+            if nbytes == 0:
+                raise TsError(B.TS_ERR_UNSUPPORTED, "ts_layer_adapters_workspace_bytes")
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.dec.device)
+            args.workspace, args.workspace_bytes = workspace.data_ptr(), nbytes
+        _check(B.ts_layer_attach_adapters(self.handle, args), "ts_layer_attach_adapters")
+        self.adapters = (given, workspace)                             # kept alive
+
+    def pack_gate_up_adapters(self, b_gate, b_up) -> torch.Tensor:
+        """b of gate_up [adapters, 2 intermediate, rank] from those of gate and up [adapters, intermediate, rank] of one rank (their rows
+        in the order of the packed weights)."""
+        n, inter, rank = b_gate.shape
+        b_gate, b_up = b_gate.contiguous(), b_up.contiguous()
+        out = torch.empty((n, 2 * inter, rank), dtype=b_gate.dtype, device=self.dec.device)
+        for i in range(n):
+            _check(B.ts_pack_gate_up(b_gate[i].data_ptr(), b_up[i].data_ptr(), out[i].data_ptr(), inter, rank, self.dec._stream()),
+                   "ts_pack_gate_up")
+        return out
+
     def close(self) -> None:
         if getattr(self, "handle", None):
             torch.cuda.synchronize(self.dec.device)
@@ -53,10 +87,17 @@ class DecoderLayer:
     def make_step(self, slots, q_len, ctx_len, keep_len: bool = False):
         return B.make_step(slots, q_len, ctx_len, 0, 0, 0, 0, B.TS_STEP_KEEP_LEN if keep_len else 0)
 
-    def step_prepared(self, st, x_in, x_out) -> None:
-        _check(B.ts_layer_step(self.handle, st, x_in.data_ptr(), x_out.data_ptr(),
-                               self.dec._stream()), "ts_layer_step")
+    def step_prepared(self, st, x_in, x_out, adapters=None) -> None:
+        """adapters: per row of the step the adapter it uses (-1: none); None: no adapters."""
+        if adapters is None:
+            _check(B.ts_layer_step(self.handle, st, x_in.data_ptr(), x_out.data_ptr(),
+                                   self.dec._stream()), "ts_layer_step")
+            return
+        if len(adapters) != st.n_rows:
+            raise ValueError("one adapter (or -1) per row of the step")
+        _check(B.ts_layer_step_adapted(self.handle, st, adapters, x_in.data_ptr(), x_out.data_ptr(),
+                                       self.dec._stream()), "ts_layer_step_adapted")
 
-    def step(self, slots, q_len, ctx_len, x_in, x_out, keep_len: bool = False) -> None:
+    def step(self, slots, q_len, ctx_len, x_in, x_out, keep_len: bool = False, adapters=None) -> None:
         st, _keep = self.make_step(slots, q_len, ctx_len, keep_len)
-        self.step_prepared(st, x_in, x_out)
+        self.step_prepared(st, x_in, x_out, adapters)

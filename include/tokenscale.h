@@ -653,6 +653,43 @@ size_t ts_layer_adapters_workspace_bytes(const ts_config* cfg, const ts_layer_ad
 int ts_layer_attach_adapters(ts_layer* layer, const ts_layer_adapters* adapters);
 int ts_layer_step_adapted(ts_layer* layer, const ts_step* step, const int32_t* row_adapter, const void* x_in, void* x_out, void* cuda_stream);
 
+/*
+ * ts_verify_tokens: drafted tokens accepted or rejected so that what a request emits is distributed as the model's samples are, whatever drafted
+ * them. Request r has the next n_nodes[r] (1 to 64) rows: its tree, node 0 the last emitted token, parents[i] < i (in the request) that of node i.
+ * Row i of logits is the model's distribution behind node i, p = softmax(scale_i x); the children of i are drafts of the next token, drawn
+ * independently from q = softmax(draft_scale_i d) of row i of draft, or, without draft, given. From node 0 on:
+ *   r = p; the children of the node, in order: with token t accepted where u_accept[child] * q(t) < r(t) (given: u_accept[child] < r(t)): on to it;
+ *   otherwise r = max(r - q, 0) (given: r without t), normalised (as it was where nothing is left);
+ *   no child left: the token drawn is the first whose cumulative sum of r exceeds u_sample[r], and the request is done.
+ * Decided as in 64 bits. count[r] = tokens emitted (1 to the depth of the tree + 1); the request's places of emitted hold them, those of logprob their
+ * log p (natural), those of path the rows of the nodes walked (absolute; node 0 first), which ts_cache_append takes as `source`: count[r]
+ * of them are the last emitted token and the accepted ones. Behind them -1, 0 and -1.
+ * u_accept, u_sample: from [0, 1). Nodes whose parent or token does not exist are passed over, and so is a given token that comes twice below a node. A row that is no
+ * distribution (a NaN, +inf, or nothing but -inf in it; in the draft's row of a node with children) ends its request with token -1, log probability NaN.
+ * A node with no children makes this a sampler: n_nodes 1. No workspace; asynchronous on cuda_stream; calls on different streams are independent.
+ */
+typedef struct {
+  int32_t device;
+  int32_t n_requests, vocab; /* vocab 1 to 2^30                                                     */
+  int32_t dtype;             /* TS_BF16 or TS_F32, of logits and draft                              */
+  const int32_t* n_nodes;    /* HOST [n_requests]; N is their sum                                   */
+  const void* logits;        /* DEVICE [N], rows row_stride elements apart (>= vocab), aligned to their type only */
+  int64_t row_stride;
+  const void* draft;         /* DEVICE [N], or NULL; rows of nodes without children are not read    */
+  int64_t draft_stride;
+  const float* scale;        /* DEVICE [N], > 0: inverse temperatures; NULL = 1                     */
+  const float* draft_scale;  /* DEVICE [N], > 0; NULL = 1                                           */
+  const int32_t* tokens;     /* DEVICE [N]                                                          */
+  const int32_t* parents;    /* DEVICE [N]                                                          */
+  const float* u_accept;     /* DEVICE [N]                                                          */
+  const float* u_sample;     /* DEVICE [n_requests]                                                 */
+  int32_t* emitted;          /* DEVICE [N]                                                          */
+  int32_t* count;            /* DEVICE [n_requests]                                                 */
+  int32_t* path;             /* DEVICE [N]                                                          */
+  float* logprob;            /* DEVICE [N]                                                          */
+} ts_verify;
+int ts_verify_tokens(const ts_verify* args, void* cuda_stream);
+
 /* The cudaError_t of the most recent failed CUDA call of this context (0 if none). */
 int ts_last_cuda_error(const ts_ctx* ctx);
 

@@ -100,6 +100,13 @@ class ts_layer_adapters(ctypes.Structure):
                [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class ts_verify(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("n_requests", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n_nodes", _i32p), ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("draft", ctypes.c_void_p),
+                ("draft_stride", ctypes.c_int64)] + \
+               [(name, ctypes.c_void_p) for name in ("scale", "draft_scale", "tokens", "parents", "u_accept", "u_sample", "emitted", "count", "path", "logprob")]
+
+
 EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts_request_add",
            "ts_alloc_pages", "ts_block_table", "ts_block_table_set", "ts_request_free",
            "ts_request_set_len", "ts_kv_append", "ts_mixed_step", "ts_mixed_step_host", "ts_host_fence",
@@ -112,7 +119,8 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan", "ts_cache8_value_bytes",
            "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
            "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project",
-           "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted"]
+           "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted",
+           "ts_verify_tokens"]
 
 _lib = None
 
@@ -205,6 +213,7 @@ def lib() -> ctypes.CDLL:
         L.ts_layer_adapters_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_step_adapted.argtypes = [vp, stepp, _i32p, vp, vp, vp]
+        L.ts_verify_tokens.argtypes = [ctypes.POINTER(ts_verify), vp]
         L.ts_strerror.restype = ctypes.c_char_p
         L.ts_strerror.argtypes = [ctypes.c_int]
         for name in EXPORTS:
@@ -540,3 +549,8 @@ def ts_layer_step_adapted(layer, step: ts_step, row_adapter, x_in: int, x_out: i
     """row_adapter: a sequence of step.n_rows numbers, or None."""
     rows = None if row_adapter is None else (ctypes.c_int32 * max(step.n_rows, 1))(*row_adapter)
     return lib().ts_layer_step_adapted(layer, ctypes.byref(step), rows, x_in, x_out, stream)
+
+
+# ------------------------------------------------------------------------------ drafted tokens verified by sampling
+def ts_verify_tokens(args: ts_verify, stream: int) -> int:
+    return lib().ts_verify_tokens(ctypes.byref(args), stream)

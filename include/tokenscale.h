@@ -59,7 +59,8 @@ enum {
   TS_ERR_CUDA = -6,           /* a CUDA runtime call failed (ts_last_cuda_error has the code) */
   TS_ERR_DEVICE_TIMEOUT = -7, /* a bounded wait inside a kernel ran out                       */
   TS_ERR_UNSUPPORTED = -8,    /* shape outside what the kernels are built for                 */
-  TS_ERR_WORKSPACE = -9       /* kv_pool or workspace smaller than ts_pool_bytes/ts_workspace_bytes */
+  TS_ERR_WORKSPACE = -9,      /* kv_pool or workspace smaller than ts_pool_bytes/ts_workspace_bytes */
+  TS_ERR_SHARED_PAGE = -10    /* the call would write into a page that another request's table holds (ts_request_fork) */
 };
 
 typedef struct ts_ctx ts_ctx; /* opaque; host memory; one thread and one stream at a time */
@@ -689,6 +690,30 @@ typedef struct {
   float* logprob;            /* DEVICE [N]                                                          */
 } ts_verify;
 int ts_verify_tokens(const ts_verify* args, void* cuda_stream);
+
+/*
+ * Pages shared between requests, copied and moved. A page may be in the tables of several requests, which read it: whoever would write into it
+ * (a step, ts_kv_append, ts_cache_append: positions from the cached length on) is refused with TS_ERR_SHARED_PAGE and nothing changes. The calls
+ * copy in every cache that the context has (the bf16 pool, an attached 8-bit cache); copies are enqueued on cuda_stream, in whose order
+ * the steps around them have to be.
+ * ts_request_fork: for each i < n a new request (slots_out[i], id req_ids[i]) of the first n_tokens[i] cached tokens of request slots[i] (n_tokens NULL:
+ *   all of them). It shares the pages that these fill and gets a copy of its own of the last one where they fill it partly, so that both
+ *   may go on. A request may come several times. TS_ERR_NO_SLOT, TS_ERR_NO_PAGES (reserved pages are left): nothing has changed.
+ *   To go back to a length inside a shared page, fork the request at that length and free the old one.
+ * ts_requests_free: ts_request_free of n requests, each listed once. A page is free when no table holds it. (Released tokens count per request.)
+ * ts_copy_pages: page dst[i] becomes what page src[i] holds, for callers that lay tables out themselves (ts_block_table_set). Any pages of the pool;
+ *   each dst once, none a src too, none in two tables (TS_ERR_SHARED_PAGE).
+ * ts_compact_pages: moves up to max_moves pages in use from the end of the pool to free ones at its front and changes the tables. moves_out (may be
+ *   NULL, room for 2 * max_moves) gets (from, to) of each; *n_moves_out, *n_used_out (may be NULL): moves made, and one past the last page in use.
+ * ts_block_tables: the tables of n requests, rows of `width` entries, -1 behind a table's end (TS_ERR_TABLE_SHORT if one is longer).
+ * All arrays are HOST memory.
+ */
+int ts_request_fork(ts_ctx* ctx, const int32_t* slots, const int32_t* n_tokens, const int64_t* req_ids, int32_t n, int32_t* slots_out,
+                    void* cuda_stream);
+int ts_requests_free(ts_ctx* ctx, const int32_t* slots, int32_t n);
+int ts_copy_pages(ts_ctx* ctx, const int32_t* src, const int32_t* dst, int32_t n, void* cuda_stream);
+int ts_compact_pages(ts_ctx* ctx, int32_t max_moves, int32_t* moves_out, int32_t* n_moves_out, int32_t* n_used_out, void* cuda_stream);
+int ts_block_tables(ts_ctx* ctx, const int32_t* slots, int32_t n, int32_t* tables_out, int32_t width);
 
 /* The cudaError_t of the most recent failed CUDA call of this context (0 if none). */
 int ts_last_cuda_error(const ts_ctx* ctx);

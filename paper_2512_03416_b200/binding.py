@@ -23,6 +23,7 @@ TS_ERR_CUDA = -6
 TS_ERR_DEVICE_TIMEOUT = -7
 TS_ERR_UNSUPPORTED = -8
 TS_ERR_WORKSPACE = -9
+TS_ERR_SHARED_PAGE = -10
 TS_STEP_KEEP_LEN = 1
 TS_STEP_HOST_ASYNC = 2
 TS_DEV_BAD_PAGE = 1
@@ -120,7 +121,7 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
            "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project",
            "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted",
-           "ts_verify_tokens"]
+           "ts_verify_tokens", "ts_request_fork", "ts_requests_free", "ts_copy_pages", "ts_compact_pages", "ts_block_tables"]
 
 _lib = None
 
@@ -214,6 +215,12 @@ def lib() -> ctypes.CDLL:
         L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_step_adapted.argtypes = [vp, stepp, _i32p, vp, vp, vp]
         L.ts_verify_tokens.argtypes = [ctypes.POINTER(ts_verify), vp]
+        i64p = ctypes.POINTER(ctypes.c_int64)
+        L.ts_request_fork.argtypes = [vp, _i32p, _i32p, i64p, i32, _i32p, vp]
+        L.ts_requests_free.argtypes = [vp, _i32p, i32]
+        L.ts_copy_pages.argtypes = [vp, _i32p, _i32p, i32, vp]
+        L.ts_compact_pages.argtypes = [vp, i32, _i32p, _i32p, _i32p, vp]
+        L.ts_block_tables.argtypes = [vp, _i32p, i32, _i32p, i32]
         L.ts_strerror.restype = ctypes.c_char_p
         L.ts_strerror.argtypes = [ctypes.c_int]
         for name in EXPORTS:
@@ -554,3 +561,34 @@ def ts_layer_step_adapted(layer, step: ts_step, row_adapter, x_in: int, x_out: i
 # ------------------------------------------------------------------------------ drafted tokens verified by sampling
 def ts_verify_tokens(args: ts_verify, stream: int) -> int:
     return lib().ts_verify_tokens(ctypes.byref(args), stream)
+
+
+# ------------------------------------------------------------- pages shared between requests, copied and moved
+# Arrays are contiguous numpy int32 (req_ids: int64).
+def _i32(a):
+    return None if a is None else a.ctypes.data_as(_i32p)
+
+
+def ts_request_fork(ctx, slots, n_tokens, req_ids, slots_out, stream: int) -> int:
+    """n_tokens may be None; slots_out is written."""
+    return lib().ts_request_fork(ctx, _i32(slots), _i32(n_tokens), req_ids.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), len(slots), _i32(slots_out), stream)
+
+
+def ts_requests_free(ctx, slots) -> int:
+    return lib().ts_requests_free(ctx, _i32(slots), len(slots))
+
+
+def ts_copy_pages(ctx, src, dst, stream: int) -> int:
+    return lib().ts_copy_pages(ctx, _i32(src), _i32(dst), len(src), stream)
+
+
+def ts_compact_pages(ctx, max_moves: int, moves_out, stream: int):
+    """Returns (code, moves made, one past the last page in use); moves_out [max_moves, 2] is written."""
+    n, used = ctypes.c_int32(0), ctypes.c_int32(0)
+    rc = lib().ts_compact_pages(ctx, max_moves, _i32(moves_out), ctypes.byref(n), ctypes.byref(used), stream)
+    return rc, n.value, used.value
+
+
+def ts_block_tables(ctx, slots, tables_out) -> int:
+    """tables_out [len(slots), width] is written."""
+    return lib().ts_block_tables(ctx, _i32(slots), len(slots), _i32(tables_out), tables_out.shape[1])

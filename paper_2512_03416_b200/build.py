@@ -8,7 +8,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libtokenscale.so")
 SOURCES = ["ts_host.cpp", "ts_layer.cpp", "ts_kernels.cu", "ts_decode.cu", "ts_mixed.cu", "ts_gemm.cu", "ts_layer_kernels.cu",
-           "ts_cache.cu", "ts_tree.cu", "ts_tree_tc.cu", "ts_logprobs.cu", "ts_adapters.cu", "ts_verify.cu"]
+           "ts_cache.cu", "ts_tree.cu", "ts_tree_tc.cu", "ts_logprobs.cu", "ts_adapters.cu", "ts_verify.cu",
+           "ts_pages.cu"]
 HEADERS = [os.path.join(CSRC, "ts_internal.h"), os.path.join(CSRC, "ts_tma.h"), os.path.join(CSRC, "ts_ptx.h"), os.path.join(CSRC, "ts_tc.h"), os.path.join(CSRC, "ts_units.h"), os.path.join(CSRC, "ts_decode_body.h"),
            os.path.join(CSRC, "ts_cache8.h"), os.path.join(CSRC, "ts_tree.h"),
            os.path.join(PKG_DIR, "..", "include", "tokenscale.h")]

@@ -124,7 +124,9 @@ struct ts_ctx {
   std::vector<int32_t> table;       // [max_requests][max_pages_per_req]
   std::vector<Slot> slots;
   std::vector<int32_t> free_pages;  // stack, next page at the back
-  std::vector<int32_t> page_owner;  // -1 = free
+  std::vector<int32_t> page_uses;   // tables that hold the page, 0 = free
+  std::vector<int32_t> page_mark;   // scratch: -1 between calls
+  std::vector<int32_t> pairs;       // scratch: pages to copy
   std::vector<int32_t> free_slots;  // stack
   ts_velocity_counters cnt;
   RingBuf ring[kRing];              // block-table deltas
@@ -192,8 +194,7 @@ void release_pages(ts_ctx* c, int slot) {
   Slot& s = c->slots[slot];
   int32_t* row = table_row(c, slot);
   for (int i = s.n_pages - 1; i >= 0; --i) {
-    c->page_owner[row[i]] = -1;
-    c->free_pages.push_back(row[i]);
+    if (--c->page_uses[row[i]] == 0) c->free_pages.push_back(row[i]);
   }
   s.n_pages = 0;
   s.synced_pages = 0;
@@ -332,6 +333,14 @@ int ring_send(ts_ctx* c, RingBuf* r, size_t dst_off, size_t bytes, cudaStream_t 
   return TS_OK;
 }
 
+// Whether n tokens written from position `from` on would change a page that another request's table holds too.
+bool writes_shared(ts_ctx* c, int slot, int from, int n) {
+  const int32_t* row = table_row(c, slot);
+  for (int i = from / c->cfg.page_size; n > 0 && i <= (from + n - 1) / c->cfg.page_size; ++i)
+    if (c->page_uses[row[i]] > 1) return true;
+  return false;
+}
+
 // Checks shared by ts_kv_append, ts_mixed_step and ts_plan_step. Fills tok0 (prefix sums).
 int validate(ts_ctx* c, const ts_step* st, bool attention, bool need_tensors, int64_t* n_tokens_out,
              int* n_decode_out, int64_t* n_prefill_out) {
@@ -356,6 +365,7 @@ int validate(ts_ctx* c, const ts_step* st, bool attention, bool need_tensors, in
     if (ql < 1 || ctx < 0) return TS_ERR_INVALID;
     if (ctx != s.n_tokens) return TS_ERR_INVALID;
     if ((int64_t)ctx + ql > (int64_t)s.n_pages * P) return TS_ERR_TABLE_SHORT;
+    if (writes_shared(c, slot, ctx, ql)) return TS_ERR_SHARED_PAGE;
     n += ql;
     if (n > INT32_MAX / 2) return TS_ERR_INVALID;
     c->tok0[r + 1] = (int32_t)n;
@@ -1014,11 +1024,38 @@ int check_rows(ts_ctx* c, const ts_step* st, int min_len, int max_len, bool any_
     if (len < min_len || len > max_len || ctx < 0) return TS_ERR_INVALID;
     if (!any_start && ctx != s.n_tokens) return TS_ERR_INVALID;
     if ((int64_t)ctx + (cover ? len : 0) > (int64_t)s.n_pages * c->cfg.page_size) return TS_ERR_TABLE_SHORT;
+    if (cover && !any_start && writes_shared(c, slot, ctx, len)) return TS_ERR_SHARED_PAGE;   // ts_cache_append
     n += len;
     if (n > INT32_MAX / 2) return TS_ERR_INVALID;
     c->tok0[r + 1] = (int32_t)n;
   }
   *n_tokens_out = n;
+  return TS_OK;
+}
+
+// Copies the pages of `pairs` in every cache that the context has.
+int copy_page_pairs(ts_ctx* c, void* cuda_stream) {
+  if (c->pairs.empty()) return TS_OK;
+  const cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const size_t page8 = ts_cache8_value_bytes(&c->cfg) / c->cfg.n_pages;
+  ts::PageRegions r = {};
+  auto add = [&](void* base, size_t bytes) {
+    r.base[r.n] = (char*)base;
+    r.bytes[r.n++] = bytes;
+  };
+  if (c->cfg.kv_pool || !c->cache8.values) {
+    const int rc = ensure_cuda(c, stream, TS_CACHE_BF16);
+    if (rc != TS_OK) return rc;
+    add(c->cfg.kv_pool, 2 * page8);
+  }
+  if (c->cache8.values) {
+    const int rc = ensure_cuda(c, stream, TS_CACHE_E4M3);
+    if (rc != TS_OK) return rc;
+    add(c->cache8.values, page8);
+    add(c->cache8.scales, page8 / c->cfg.head_dim);
+  }
+  TS_CUDA(c, ts::launch_copy_pages(r, c->pairs.data(), (int)(c->pairs.size() / 2), stream));
+  ++c->cnt.kernel_launches;
   return TS_OK;
 }
 
@@ -1208,7 +1245,8 @@ int ts_create(const ts_config* cfg, ts_ctx** out) {
   c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim);
   c->table.assign((size_t)cfg->max_requests * cfg->max_pages_per_req, -1);
   c->slots.assign(cfg->max_requests, Slot());
-  c->page_owner.assign(cfg->n_pages, -1);
+  c->page_uses.assign(cfg->n_pages, 0);
+  c->page_mark.assign(cfg->n_pages, -1);
   c->free_pages.resize(cfg->n_pages);
   for (int i = 0; i < cfg->n_pages; ++i) c->free_pages[i] = cfg->n_pages - 1 - i;  // page 0 on top
   if (cfg->alloc_shuffle_seed) {
@@ -1290,7 +1328,7 @@ int ts_alloc_pages(ts_ctx* c, int32_t slot, int32_t total_tokens, int32_t for_pr
   for (int i = 0; i < need; ++i) {
     const int32_t p = c->free_pages.back();
     c->free_pages.pop_back();
-    c->page_owner[p] = slot;
+    c->page_uses[p] = 1;
     row[s.n_pages++] = p;
   }
   return TS_OK;
@@ -1323,23 +1361,25 @@ int ts_block_table_set(ts_ctx* c, int32_t slot, const int32_t* pages, int32_t n_
   ++c->stamp;
   std::vector<char> seen;  // small helper bitmap only for this call
   seen.assign(c->cfg.n_pages, 0);
+  const int32_t* held = table_row(c, slot);
+  for (int i = 0; i < c->slots[slot].n_pages; ++i) seen[held[i]] = 2;
   for (int i = 0; i < n_pages; ++i) {
     const int32_t p = pages[i];
-    if (p < 0 || p >= c->cfg.n_pages || seen[p]) return TS_ERR_INVALID;
-    if (c->page_owner[p] != -1 && c->page_owner[p] != slot) return TS_ERR_INVALID;
+    if (p < 0 || p >= c->cfg.n_pages || seen[p] == 1) return TS_ERR_INVALID;
+    if (c->page_uses[p] > 0 && seen[p] != 2) return TS_ERR_INVALID;
     seen[p] = 1;
   }
   release_pages(c, slot);
   // remove the requested pages from the free stack, keeping the order of the rest
   size_t w = 0;
   for (size_t i = 0; i < c->free_pages.size(); ++i)
-    if (!seen[c->free_pages[i]]) c->free_pages[w++] = c->free_pages[i];
+    if (seen[c->free_pages[i]] != 1) c->free_pages[w++] = c->free_pages[i];
   c->free_pages.resize(w);
   Slot& s = c->slots[slot];
   int32_t* row = table_row(c, slot);
   for (int i = 0; i < n_pages; ++i) {
     row[i] = pages[i];
-    c->page_owner[pages[i]] = slot;
+    ++c->page_uses[pages[i]];
   }
   s.n_pages = n_pages;
   s.synced_pages = 0;
@@ -1357,6 +1397,155 @@ int ts_request_free(ts_ctx* c, int32_t slot) {
   s.n_tokens = 0;
   c->free_slots.push_back(slot);
   return TS_OK;
+}
+
+int ts_requests_free(ts_ctx* c, const int32_t* slots, int32_t n) {
+  if (!c || n < 0 || (n > 0 && !slots)) return TS_ERR_INVALID;
+  if (++c->stamp == 0) {
+    for (auto& s : c->slots) s.stamp = 0;
+    c->stamp = 1;
+  }
+  for (int i = 0; i < n; ++i) {
+    if (!slot_ok(c, slots[i]) || c->slots[slots[i]].stamp == c->stamp) return TS_ERR_INVALID;
+    c->slots[slots[i]].stamp = c->stamp;
+  }
+  for (int i = 0; i < n; ++i) ts_request_free(c, slots[i]);
+  return TS_OK;
+}
+
+int ts_block_tables(ts_ctx* c, const int32_t* slots, int32_t n, int32_t* tables_out, int32_t width) {
+  if (!c || n < 0 || width < 0 || (n > 0 && (!slots || (width > 0 && !tables_out)))) return TS_ERR_INVALID;
+  for (int i = 0; i < n; ++i) {
+    if (!slot_ok(c, slots[i])) return TS_ERR_INVALID;
+    if (c->slots[slots[i]].n_pages > width) return TS_ERR_TABLE_SHORT;
+  }
+  for (int i = 0; i < n; ++i) {
+    const int have = c->slots[slots[i]].n_pages;
+    int32_t* out = tables_out + (size_t)i * width;
+    std::copy_n(table_row(c, slots[i]), have, out);
+    std::fill(out + have, out + width, -1);
+  }
+  return TS_OK;
+}
+
+int ts_request_fork(ts_ctx* c, const int32_t* slots, const int32_t* n_tokens, const int64_t* req_ids, int32_t n, int32_t* slots_out,
+                    void* cuda_stream) try {
+  if (!c || n < 0 || (n > 0 && (!slots || !req_ids || !slots_out))) return TS_ERR_INVALID;
+  const int P = c->cfg.page_size;
+  auto length = [&](int i) { return n_tokens ? n_tokens[i] : c->slots[slots[i]].n_tokens; };
+  c->pairs.clear();
+  const int64_t free = (int64_t)c->free_pages.size(), usable = free - c->cfg.reserved_pages;
+  for (int i = 0; i < n; ++i) {
+    if (!slot_ok(c, slots[i])) return TS_ERR_INVALID;
+    if (length(i) < 0 || length(i) > c->slots[slots[i]].n_tokens) return TS_ERR_INVALID;
+    if (length(i) % P == 0) continue;
+    const int64_t used = (int64_t)c->pairs.size() / 2;
+    if (used >= usable) return TS_ERR_NO_PAGES;
+    c->pairs.push_back(table_row(c, slots[i])[length(i) / P]);
+    c->pairs.push_back(c->free_pages[free - 1 - used]);
+  }
+  if ((int64_t)n > (int64_t)c->free_slots.size()) return TS_ERR_NO_SLOT;
+  const int rc = copy_page_pairs(c, cuda_stream);
+  if (rc != TS_OK) return rc;
+  for (int i = 0; i < n; ++i) {
+    const int from = slots[i], len = length(i), whole = len / P, slot = c->free_slots.back();
+    c->free_slots.pop_back();
+    Slot& s = c->slots[slot];
+    s = Slot();
+    s.live = true;
+    s.req_id = req_ids[i];
+    s.prompt_len = len;
+    s.expected_output_len = c->slots[from].expected_output_len;
+    s.n_tokens = len;
+    s.n_pages = whole;
+    const int32_t* parent = table_row(c, from);
+    int32_t* row = table_row(c, slot);
+    for (int k = 0; k < whole; ++k) {
+      row[k] = parent[k];
+      ++c->page_uses[row[k]];
+    }
+    if (len % P) {
+      const int32_t p = c->free_pages.back();
+      c->free_pages.pop_back();
+      c->page_uses[p] = 1;
+      row[s.n_pages++] = p;
+    }
+    slots_out[i] = slot;
+  }
+  return TS_OK;
+} catch (const std::bad_alloc&) {        // of the list of pages: nothing has changed
+  return TS_ERR_INVALID;
+}
+
+int ts_copy_pages(ts_ctx* c, const int32_t* src, const int32_t* dst, int32_t n, void* cuda_stream) try {
+  if (!c || n < 0 || (n > 0 && (!src || !dst))) return TS_ERR_INVALID;
+  c->pairs.clear();
+  c->pairs.reserve(2 * (size_t)n);
+  int rc = TS_OK;
+  int marked = 0;
+  for (; marked < n && rc == TS_OK; ++marked) {
+    const int32_t p = dst[marked];
+    if (p < 0 || p >= c->cfg.n_pages || c->page_mark[p] != -1) rc = TS_ERR_INVALID;
+    else if (c->page_uses[p] > 1) rc = TS_ERR_SHARED_PAGE;
+    if (rc != TS_OK) break;
+    c->page_mark[p] = 0;
+  }
+  for (int i = 0; i < n && rc == TS_OK; ++i) {
+    if (src[i] < 0 || src[i] >= c->cfg.n_pages || c->page_mark[src[i]] != -1) rc = TS_ERR_INVALID;
+    c->pairs.push_back(src[i]);
+    c->pairs.push_back(dst[i]);
+  }
+  for (int i = 0; i < marked; ++i) c->page_mark[dst[i]] = -1;
+  return rc == TS_OK ? copy_page_pairs(c, cuda_stream) : rc;
+} catch (const std::bad_alloc&) {
+  return TS_ERR_INVALID;
+}
+
+int ts_compact_pages(ts_ctx* c, int32_t max_moves, int32_t* moves_out, int32_t* n_moves_out, int32_t* n_used_out, void* cuda_stream) try {
+  if (!c || max_moves < 0) return TS_ERR_INVALID;
+  const int n = c->cfg.n_pages, live = n - (int)c->free_pages.size();
+  c->pairs.clear();
+  int to = 0, from = n - 1;                                // the highest pages in use go to the lowest free ones
+  while ((int)c->pairs.size() / 2 < max_moves) {
+    while (to < live && c->page_uses[to] > 0) ++to;
+    while (from >= live && c->page_uses[from] == 0) --from;
+    if (to >= live || from < live) break;
+    c->pairs.push_back(from--);
+    c->pairs.push_back(to++);
+  }
+  const int rc = copy_page_pairs(c, cuda_stream);
+  if (rc != TS_OK) return rc;
+  const int moves = (int)c->pairs.size() / 2;
+  if (moves > 0) {
+    for (int i = 0; i < moves; ++i) {
+      const int32_t a = c->pairs[2 * i], b = c->pairs[2 * i + 1];
+      c->page_mark[a] = b;
+      c->page_mark[b] = a;
+      std::swap(c->page_uses[a], c->page_uses[b]);
+    }
+    for (int slot = 0; slot < c->cfg.max_requests; ++slot) {
+      Slot& s = c->slots[slot];
+      int32_t* row = table_row(c, slot);
+      for (int i = 0; s.live && i < s.n_pages; ++i) {
+        if (c->page_mark[row[i]] == -1) continue;
+        row[i] = c->page_mark[row[i]];
+        s.synced_pages = std::min(s.synced_pages, i);      // the device's table is sent again from here on
+      }
+    }
+    for (int32_t& p : c->free_pages)
+      if (c->page_mark[p] != -1) p = c->page_mark[p];
+    for (int32_t p : c->pairs) c->page_mark[p] = -1;
+  }
+  if (moves_out) std::copy(c->pairs.begin(), c->pairs.end(), moves_out);
+  if (n_moves_out) *n_moves_out = moves;
+  if (n_used_out) {
+    int used = n;
+    while (used > 0 && c->page_uses[used - 1] == 0) --used;
+    *n_used_out = used;
+  }
+  return TS_OK;
+} catch (const std::bad_alloc&) {        // of the list of pages: nothing has changed
+  return TS_ERR_INVALID;
 }
 
 int ts_request_set_len(ts_ctx* c, int32_t slot, int32_t n_tokens) {
@@ -1776,6 +1965,7 @@ const char* ts_strerror(int code) {
     case TS_ERR_DEVICE_TIMEOUT: return "a bounded wait inside a kernel ran out";
     case TS_ERR_UNSUPPORTED: return "unsupported shape";
     case TS_ERR_WORKSPACE: return "pool or workspace too small";
+    case TS_ERR_SHARED_PAGE: return "a page that another request reads would be written";
     default: return "unknown error";
   }
 }

@@ -154,6 +154,15 @@ cudaError_t launch_mixed(const StepDevice& s, const CUtensorMap& q_map, const CU
                          const CUtensorMap& kv_tile_map, const NewKvMaps& new_maps, int n_ctas, int n_prefill_ctas, cudaStream_t stream);
 cudaError_t launch_decode(const StepDevice& s, const CUtensorMap& kv_map, int n_sms, cudaStream_t stream);
 
+// Copies pages src, dst = pairs[2 i], pairs[2 i + 1] of each region (HOST, n of them, no page in both lists).
+struct PageRegions {
+  int32_t n;
+  int32_t pieces[3];              // set by the launcher
+  char* base[3];
+  size_t bytes[3];                // of a page, a multiple of 16
+};
+cudaError_t launch_copy_pages(PageRegions r, const int32_t* pairs, int n, cudaStream_t stream);
+
 // ---- the decoder layer around the attention step: GEMMs and small kernels (ts_gemm.cu, ts_layer_kernels.cu)
 enum { GEMM_EPI_STORE = 0, GEMM_EPI_ROPE = 1, GEMM_EPI_SILU_MUL = 2 };
 // C = A . B^T (+ R), A [M][K], B [N][K] bf16 K-major (their tensor maps travel beside this struct).

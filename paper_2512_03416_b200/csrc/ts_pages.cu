@@ -1,0 +1,67 @@
+// Cache pages copied (sm_100a): page dst[i] of every region (the bf16 pool; codes and scales of the 8-bit cache) becomes what page src[i] holds. No
+// page is in both lists, so the order does not matter.
+//
+// Bound by memory: every byte is read and written once. A thread block moves a piece of a page, every thread four 16-byte chunks with all
+// loads in flight before the first store. The page ids are launch parameters.
+#include "../../include/tokenscale.h"
+#include "ts_internal.h"
+
+namespace ts {
+namespace {
+
+constexpr int kThreads = 256, kInFlight = 4, kPiece = kThreads * kInFlight * 16;
+
+template <int W>
+struct CopyParams {
+  PageRegions r;
+  int32_t words[W];                      // src, dst of each pair
+};
+
+template <int W>
+__global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyParams<W> p) {
+  pdl_launch_dependents();
+  const int pair = blockIdx.y, src = p.words[2 * pair], dst = p.words[2 * pair + 1];
+  int piece = blockIdx.x, i = 0;
+  while (i + 1 < p.r.n && piece >= p.r.pieces[i]) piece -= p.r.pieces[i++];
+  const size_t bytes = p.r.bytes[i];
+  const char* const from = p.r.base[i] + (size_t)src * bytes;
+  char* const to = p.r.base[i] + (size_t)dst * bytes;
+  const size_t at = (size_t)piece * kPiece + threadIdx.x * 16;
+  pdl_wait();
+  uint4 v[kInFlight];
+#pragma unroll
+  for (int k = 0; k < kInFlight; ++k)
+    if (at + k * kThreads * 16 < bytes) v[k] = *reinterpret_cast<const uint4*>(from + at + k * kThreads * 16);
+#pragma unroll
+  for (int k = 0; k < kInFlight; ++k)
+    if (at + k * kThreads * 16 < bytes) *reinterpret_cast<uint4*>(to + at + k * kThreads * 16) = v[k];
+}
+
+template <int W>
+cudaError_t launch(const PageRegions& r, int pieces, const int32_t* pairs, int n, cudaStream_t stream) {
+  CopyParams<W> p;
+  p.r = r;
+  std::memcpy(p.words, pairs, sizeof(int32_t) * 2 * (size_t)n);
+  return launch_pdl(copy_pages_kernel<W>, dim3((unsigned)pieces, (unsigned)n), dim3(kThreads), 0, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_copy_pages(PageRegions r, const int32_t* pairs, int n, cudaStream_t stream) {
+  int pieces = 0;
+  for (int i = 0; i < r.n; ++i) {
+    r.pieces[i] = (int32_t)((r.bytes[i] + kPiece - 1) / kPiece);
+    pieces += r.pieces[i];
+  }
+  if (pieces == 0) return cudaSuccess;
+  for (int at = 0; at < n;) {
+    const int some = n - at < kInlineWordsMax / 2 ? n - at : kInlineWordsMax / 2;
+    const cudaError_t e = some <= kInlineWords / 2 ? launch<kInlineWords>(r, pieces, pairs + 2 * (size_t)at, some, stream)
+                                                   : launch<kInlineWordsMax>(r, pieces, pairs + 2 * (size_t)at, some, stream);
+    if (e != cudaSuccess) return e;
+    at += some;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace ts

@@ -118,6 +118,43 @@ class Decoder:
     def request_set_len(self, slot: int, n_tokens: int) -> None:
         _check(B.ts_request_set_len(self.ctx, slot, n_tokens), "ts_request_set_len")
 
+    # ------------------------------------------------- pages shared between requests, copied and moved
+    def fork(self, slots, req_ids, n_tokens=None) -> np.ndarray:
+        """New requests (their slots, int32) of the first n_tokens[i] cached tokens of slots[i] (None: all of them): whole pages are shared, the last
+        partly filled one is copied on the current stream. See ts_request_fork."""
+        slots, req_ids = np.ascontiguousarray(slots, dtype=np.int32), np.ascontiguousarray(req_ids, dtype=np.int64)
+        n_tokens = None if n_tokens is None else np.ascontiguousarray(n_tokens, dtype=np.int32)
+        if slots.ndim != 1 or req_ids.shape != slots.shape or (n_tokens is not None and n_tokens.shape != slots.shape):
+            raise ValueError("slots, req_ids and n_tokens must be lists of one length")
+        out = np.empty_like(slots)
+        _check(B.ts_request_fork(self.ctx, slots, n_tokens, req_ids, out, self._stream()), "ts_request_fork")
+        return out
+
+    def requests_free(self, slots) -> None:
+        _check(B.ts_requests_free(self.ctx, np.ascontiguousarray(slots, dtype=np.int32).reshape(-1)), "ts_requests_free")
+
+    def copy_pages(self, src, dst) -> None:
+        """Page dst[i] becomes what page src[i] holds, on the current stream. See ts_copy_pages."""
+        src, dst = np.ascontiguousarray(src, dtype=np.int32), np.ascontiguousarray(dst, dtype=np.int32)
+        if src.ndim != 1 or src.shape != dst.shape:
+            raise ValueError("src and dst must be lists of one length")
+        _check(B.ts_copy_pages(self.ctx, src, dst, self._stream()), "ts_copy_pages")
+
+    def compact(self, max_moves=None):
+        """Moves pages in use to the front of the pool, on the current stream. Returns ((from, to) of each move, one past the last page in use)."""
+        most = self.cfg.n_pages if max_moves is None else max_moves
+        moves = np.empty((max(most, 0), 2), dtype=np.int32)
+        rc, n, used = B.ts_compact_pages(self.ctx, most, moves, self._stream())
+        _check(rc, "ts_compact_pages")
+        return moves[:n], used
+
+    def block_tables(self, slots) -> np.ndarray:
+        """int32 [len(slots), max_pages_per_req], -1 behind a table's end."""
+        slots = np.ascontiguousarray(slots, dtype=np.int32).reshape(-1)
+        out = np.empty((len(slots), self.cfg.max_pages_per_req), dtype=np.int32)
+        _check(B.ts_block_tables(self.ctx, slots, out), "ts_block_tables")
+        return out
+
     # ------------------------------------------------------------------------------- steps
     def _stream(self) -> int:
         return _raw_stream(self.device.index)

@@ -20,17 +20,20 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/tokenscale.h"
 #include "ts_internal.h"
+#include "ts_ptx.h"
 
 namespace ts {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kTile = 256;               // logits of a warp at a time: eight neighbouring ones per lane
-constexpr int kStrips = 512;             // of a block's part of a row
-constexpr int kNodes = 64, kMaxCluster = 8;
+constexpr int kStrips = 256;             // of a block's part of a row
+constexpr int kMostWarps = 16;
+constexpr double kNothing = 1e-250;      // what is not more than this is as good as nothing
+constexpr int kNodes = 64, kMaxCluster = 8, kValues = 6;
 constexpr int kWords = 767;              // requests of a launch
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -46,19 +49,52 @@ struct VerifyParams {
   int32_t first[kWords + 1];             // of each request's nodes
 };
 
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// The distributions behind a node in 64 bits: probability of a logit x e^(x scale - top) inv.
+struct Exact {
+  double scale, top, inv, dscale, dtop, dinv;
+};
+// A block's part of a row.
+struct Row {
+  const void *row, *drow;                // the model's, the draft's
+  int32_t vocab, shift;                  // the row's first 16-byte boundary is `shift` logits in front of it
+  int32_t from, to;                      // tiles, counted from there
+  int32_t dvec;                          // the draft's row has its boundaries at the same places
+  int32_t per, n;                        // tiles of a strip, strips
+};
+__shared__ struct {
+  double strips[3][kStrips];
+  double part[kMostWarps][kValues];
+  double box[2][kMaxCluster][kValues];   // the blocks' values, by turns
+  double norm[kNodes];                   // 1 / Z of the rejections at this node
+  Exact e;
+  Row row;
+  int32_t gone[kNodes];                  // tokens rejected at this node (no draft)
+  int32_t token[kNodes], child[kNodes], sibling[kNodes];     // child, sibling: a node's first one, the next of the same parent; -1: none
+  float chance[kNodes], scale[kNodes], dscale[kNodes];
+  float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (max, s of the model; of the draft), by turns
+  float4 part32[kMostWarps];
+  int32_t found;
+} sh;
+
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ double ld_cluster(uint32_t addr) {
-  double v;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];\n" : "=d"(v) : "r"(addr));
-  return v;
+__device__ __forceinline__ void st_cluster(uint32_t addr, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;\n" ::"r"(addr), "d"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, int32_t v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;\n" ::"r"(addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;\n" ::: "memory");
+}
+__device__ __forceinline__ void sync_all(int cluster) {
+  if (cluster > 1) cluster_sync(); else __syncthreads();
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -67,430 +103,586 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float value(const float* p) { return *p; }
-// Elements of a row from `at` on (at may be negative): -inf outside [0, n). `vec`: address at + row is 16-byte aligned.
-__device__ __forceinline__ void load8(const __nv_bfloat16* row, int at, int n, bool vec, float (&x)[8]) {
-  if (vec && at >= 0 && at + 8 <= n) {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + at));
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ uint32_t bits(const __nv_bfloat16& x) { return *reinterpret_cast<const uint16_t*>(&x); }
+__device__ __forceinline__ uint32_t bits(const float& x) { return __float_as_uint(x); }
+
+// N neighbouring logits as they lie in memory, in words.
+template <typename T, int N>
+struct Raw {
+  uint32_t w[N * sizeof(T) / 4];
+};
+// Those of a row from `at` on (at may be negative): -inf outside [0, n). `vec`: address at + row is a multiple of N logits' bytes, 16 at most.
+template <int N, typename T>
+__device__ __forceinline__ Raw<T, N> load(const T* row, int at, int n, bool vec) {
+  constexpr int kWide = (int)(N * sizeof(T)) / 4;
+  Raw<T, N> r;
+  if (vec && at >= 0 && at + N <= n) {
+    if constexpr (kWide == 2) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(row + at));
+      r.w[0] = v.x; r.w[1] = v.y;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      for (int i = 0; i < kWide / 4; ++i) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(row + at) + i);
+        r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+      }
     }
   } else {
+    constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
+    constexpr int kEach = 4 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (unsigned)(at + i) < (unsigned)n ? __bfloat162float(row[at + i]) : -CUDART_INF_F;
+    for (int i = 0; i < kWide; ++i) {
+      r.w[i] = 0;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int a = at + i * kEach + k;
+        r.w[i] |= ((unsigned)a < (unsigned)n ? bits(row[a]) : kNone) << (16 * k);
+      }
+    }
   }
+  return r;
 }
-__device__ __forceinline__ void load8(const float* row, int at, int n, bool vec, float (&x)[8]) {
-  if (vec && at >= 0 && at + 8 <= n) {
+template <typename T, int N>
+__device__ __forceinline__ void unpack(const Raw<T, N>& r, float (&x)[N]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 w = __ldg(reinterpret_cast<const float4*>(row + at) + i);
-      x[4 * i] = w.x; x[4 * i + 1] = w.y; x[4 * i + 2] = w.z; x[4 * i + 3] = w.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (unsigned)(at + i) < (unsigned)n ? row[at + i] : -CUDART_INF_F;
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(r.w[i]);
+    else x[i] = __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
   }
 }
 
-// A distribution's sum: weights 2^((x - max) c). (As x c - max c in one rounding they would overflow for the largest logits.)
-struct Sum {
-  float max, s;
+// A warp's tiles on their way: every lane copies its own eight logits (and the draft's) into shared memory, kRing tiles ahead of their use, and
+// waits for its own copies only. kRing tiles of both rows are 8 KB a warp, 128 KB an SM under way.
+template <typename T>
+struct Ring {
+  static constexpr int kLane = 8 * sizeof(T), kRing = 8192 / (2 * 32 * kLane);
+  static constexpr int kBytes = 2 * kRing * 32 * kLane;      // of a warp
+  const T *row, *drow;
+  int vocab;
+  bool both, dvec;
+  uint32_t mine;                         // this lane's first slot
+  __device__ Ring(const T* r, const T* d, int n, bool b, bool v, unsigned char* all, int warp, int lane)
+      : row(r), drow(d), vocab(n), both(b), dvec(v), mine(smem_u32(all) + warp * kBytes + lane * kLane) {}
+  __device__ __forceinline__ uint32_t slot(int k, int which) const { return mine + ((k % kRing) * 2 + which) * 32 * kLane; }
+  __device__ __forceinline__ void one(const T* from, int at, bool vec, uint32_t to) const {
+    if (vec && at >= 0 && at + 8 <= vocab) {
+#pragma unroll
+      for (int i = 0; i < kLane / 16; ++i) cp_async16(to + 16 * i, from + at + i * (16 / sizeof(T)), 16);
+    } else {                             // the row's ends, rows of another alignment
+      const Raw<T, 8> r = load<8>(from, at, vocab, false);
+#pragma unroll
+      for (int i = 0; i < kLane / 16; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(to + 16 * i), "r"(r.w[4 * i]), "r"(r.w[4 * i + 1]), "r"(r.w[4 * i + 2]), "r"(r.w[4 * i + 3]) : "memory");
+    }
+  }
+  // The k-th tile that is asked for, logits from `at` on in this lane. Called for every k in turn, `some` false behind the last one.
+  __device__ __forceinline__ void ask(int k, int at, bool some) const {
+    if (some) {
+      one(row, at, true, slot(k, 0));
+      if (both) one(drow, at, dvec, slot(k, 1));
+    }
+    cp_async_commit();
+  }
+  __device__ __forceinline__ void get(int k, float (&x)[8], float (&y)[8]) const {
+    cp_async_wait<kRing - 1>();
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      if (which && !both) break;
+      Raw<T, 8> r;
+#pragma unroll
+      for (int i = 0; i < kLane / 16; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3]) : "r"(slot(k, which) + 16 * i) : "memory");
+      unpack(r, which ? y : x);
+    }
+  }
 };
-__device__ __forceinline__ float weight(float x, float max, float c) { return ex2((x - max) * c); }
-__device__ __forceinline__ void add8(Sum& a, const float (&x)[8], float c) {
-  float m = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, x[i]);
-  if (m > a.max) {
-    a.s *= weight(a.max, m, c);          // of nothing: 2^-inf
-    a.max = m;
-  }
-  if (a.max == -CUDART_INF_F) {          // nothing but -inf and NaN yet
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a.s += x[i] != x[i] ? x[i] : 0.f;
-    return;
-  }
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s += weight(x[i], a.max, c);
-  a.s += s;
-}
-__device__ __forceinline__ void join(Sum& a, const Sum& b, float c) {
-  if (b.max > a.max) {
-    a.s = a.s * weight(a.max, b.max, c) + b.s;
-    a.max = b.max;
-  } else {
-    a.s += b.max == -CUDART_INF_F ? b.s : b.s * weight(b.max, a.max, c);
-  }
-}
-__device__ __forceinline__ Sum warp_join(Sum a, float c) {
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) {
-    const Sum b = {__shfl_xor_sync(0xffffffffu, a.max, sh), __shfl_xor_sync(0xffffffffu, a.s, sh)};
-    // both lanes add the same two in the same order
-    const bool lower = !(threadIdx.x & sh);
-    Sum lo = lower ? a : b;
-    join(lo, lower ? b : a, c);
-    a = lo;
-  }
-  return a;
-}
+
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) v += __shfl_xor_sync(0xffffffffu, v, sh);
+  for (int sh_ = 16; sh_ > 0; sh_ >>= 1) v += __shfl_xor_sync(0xffffffffu, v, sh_);
   return v;
 }
+// The block's values (part[0][0 .. n - 1], by warp 0's lanes) go to every block of the cluster.
+__device__ __forceinline__ void publish(int n, double (&v)[kValues], int rank, int cluster, int turn, int lane) {
+  if (lane < cluster) {
+    const uint32_t to = smem_u32(&sh.box[turn][rank][0]);
+    const uint32_t there = cluster > 1 ? mapa(to, lane) : to;
+#pragma unroll
+    for (int i = 0; i < kValues; ++i)
+      if (i < n) st_cluster(there + 8 * i, v[i]);
+  }
+}
 
-// The distribution behind a node in 64 bits.
-struct Exact {
-  double scale, top, inv, dscale, dtop, dinv;
+// ---- sums in fp32
+// Weights 2^(x c - top), top = ref c rounded, the same for all: it is as if ref were another number nearby. Where it would not be (kHuge), top is a
+// NaN, and weights are 2^((x - ref) c). ref is a logit that moves when weights get large, so that most logits are one fma, one exponential, one sum.
+struct Sum {
+  float ref, top, s;
 };
+constexpr float kLarge = 0x1p60f, kHuge = 0x1p20f;
+__device__ __forceinline__ Sum nothing() { return Sum{-CUDART_INF_F, CUDART_NAN_F, 0.f}; }
+__device__ __forceinline__ float top_of(float ref, float c) {
+  const float top = __fmul_rn(ref, c);
+  return fabsf(top) < kHuge ? top : CUDART_NAN_F;
+}
+__device__ __forceinline__ float exponent(float x, const Sum& a, float c) { return a.top == a.top ? fmaf(x, c, -a.top) : (x - a.ref) * c; }
+__device__ __forceinline__ float weight(float x, const Sum& a, float c) { return ex2(exponent(x, a, c)); }
+// The sum in weights of another reference.
+__device__ __forceinline__ float moved(const Sum& a, float ref, float top, float c) {
+  if (a.ref == -CUDART_INF_F || a.ref == ref) return a.s;                    // nothing, or a NaN
+  return a.s * ex2(a.top == a.top && top == top ? a.top - top : (a.ref - ref) * c);
+}
+__device__ __noinline__ Sum add_slow(Sum a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float c) {
+  const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
+  float m = a.ref;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i]);
+  const float top = top_of(m, c);
+  Sum b = {m, top, moved(a, m, top, c)};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b.s += m != -CUDART_INF_F ? weight(x[i], b, c) : x[i] != x[i] ? x[i] : 0.f;
+  return b;
+}
+__device__ __forceinline__ void refer(Sum& a, const float (&x)[8], float c) {      // the first reference
+  a.ref = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) a.ref = fmaxf(a.ref, x[i]);
+  a.top = top_of(a.ref, c);
+}
+__device__ __forceinline__ void add(Sum& a, const float (&x)[8], float c) {
+  float s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c, -a.top));
+  const float sum = s[0] + s[1];
+  if (__builtin_expect(sum < kLarge, 1)) a.s += sum;
+  else a = add_slow(a, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], c);  // large, or no numbers; a huge reference
+}
+// Over groups of 2 * WIDEST lanes.
+template <int WIDEST>
+__device__ __forceinline__ void lanes_sum(Sum& a, float c) {
+  float m = a.ref;
+#pragma unroll
+  for (int s = WIDEST; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+  const float top = top_of(m, c);
+  a = Sum{m, top, moved(a, m, top, c)};
+#pragma unroll
+  for (int s = WIDEST; s > 0; s >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, s);
+}
 
+// ---- sums in 64 bits
+// e^v in 64 bits for v up to 700: 2^n e^f with n the nearest whole number to v / ln 2, |f| <= ln 2 / 2, e^f by its Taylor series up to f^10, 3e-13
+// off. Below e^-690 it stays there (kNothing). Half the operations of a library function that serves all arguments. (With sixteenths of n, a table
+// of roots and the series up to f^5, 10 operations instead of 14, a pass takes 1.25 times as long.)
+__device__ __forceinline__ double exp64(double v) {
+  v = __hiloint2double((int)min((unsigned)__double2hiint(v), 0xc0859000u), __double2loint(v));      // not below -690; -inf neither
+  const double magic = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to whole numbers, which are then its lowest bits
+  const double y = fma(v, 1.4426950408889634, magic);
+  const double f = fma(y - magic, -0.6931471805599453, v);
+  double s = 1.0 / 3628800;
+  s = fma(s, f, 1.0 / 362880);
+  s = fma(s, f, 1.0 / 40320);
+  s = fma(s, f, 1.0 / 5040);
+  s = fma(s, f, 1.0 / 720);
+  s = fma(s, f, 1.0 / 120);
+  s = fma(s, f, 1.0 / 24);
+  s = fma(s, f, 1.0 / 6);
+  s = fma(s, f, 0.5);
+  s = fma(s, f, 1.0);
+  s = fma(s, f, 1.0);
+  return __hiloint2double(__double2hiint(s) + (int)((unsigned)__double2loint(y) << 20), __double2loint(s));
+}
+__device__ __forceinline__ double weight64(float x, double scale, double top) { return exp64(fma((double)x, scale, -top)); }
+// The sum over the blocks of value i.
+__device__ __forceinline__ double total(int i, int cluster, int turn) {
+  double v = 0.0;
+  for (int r = 0; r < cluster; ++r) v += sh.box[turn][r][i];
+  return v;
+}
+// What is left of the probability of a token whose logits are x (the model's) and y (the draft's) behind the rejections so far.
+template <bool DRAFT>
+__device__ __noinline__ double left(float x, float y, int rejected) {
+  double r = weight64(x, sh.e.scale, sh.e.top) * sh.e.inv;
+  if (DRAFT && rejected > 0) {
+    const double q = weight64(y, sh.e.dscale, sh.e.dtop) * sh.e.dinv;
+    for (int i = 0; i < rejected; ++i)
+      if (sh.norm[i] > 0.0) r = fmax(r - q, 0.0) * sh.norm[i];
+  }
+  return r;
+}
+
+// One pass over (a part of) the block's part of the row in 64 bits. The exponentials are the bulk of the work and of the code, which every SM has to
+// fetch: all uses but for single tokens are modes of this one loop. A warp has strips from, from + step, ... below to.
+//   SUMS    values 0, 1: the sums of e^(x scale - top) of the model and of the draft
+//   REST    value 0: what one more rejection leaves
+//   STRIPS  what is left, per strip, and value 0: in all
+//   FIRST   what the first rejection leaves, with e.inv and e.dinv known to 2^-21 only: strips and values 3, 4, 5 of max(p - q, 0), and of
+//           e^.. of the model and of the draft where that is not 0, by which it is corrected; values 0, 1 as SUMS; value 2: p + q of tokens whose
+//           p and q are alike to 2^-19, of which it may not be known which is larger
+// Values are published. find, by one warp: the token at `want` of a strip, or the last one there that has anything.
+enum { SUMS, REST, STRIPS, FIRST };
 template <typename T, bool DRAFT>
-struct Walk {
-  const VerifyParams& p;
-  const int rank, tid, lane, warp;
-  // shared memory
-  double* strips;                        // [kStrips]
-  double* norm;                          // [kNodes] 1 / Z of the rejections at this node
-  int32_t* gone;                         // [kNodes] tokens rejected at this node (no draft)
-  double* warps;                         // [kWarps][2]
-  double* box;                           // [2][4]: what the blocks exchange, by turns
-  int32_t* found;
-  int turn = 0;
-  const T* row;
-  const T* drow;
-  int shift, tile0, tile1;               // the row's first 16-byte boundary is `shift` elements in front of it; this block's tiles
-  bool dvec;
-  int rejected = 0;
-
-  __device__ Walk(const VerifyParams& p_, int rank_) : p(p_), rank(rank_), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5) {}
-
-  __device__ void at_row(int64_t r) {
-    row = static_cast<const T*>(p.logits) + r * p.stride;
-    shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    if (DRAFT) {
-      drow = static_cast<const T*>(p.draft) + r * p.draft_stride;
-      dvec = (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(T)) == shift;
+__device__ __noinline__ int find(int rejected, int strip, double want) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool both = DRAFT && rejected > 0;
+  const T* const row = static_cast<const T*>(sh.row.row);
+  const T* const drow = static_cast<const T*>(sh.row.drow);
+  const int vocab = sh.row.vocab, first = sh.row.from + strip * sh.row.per, end = min(sh.row.to, first + sh.row.per);
+  extern __shared__ __align__(16) unsigned char copies[];
+  const Ring<T> ring(row, drow, vocab, both, sh.row.dvec, copies, warp, lane);
+  const int base = lane * 8 - sh.row.shift;
+  for (int k = 0; k < Ring<T>::kRing; ++k) ring.ask(k, (first + k) * kTile + base, first + k < end);
+  double cum = 0.0;
+  int some_tile = -1;
+  auto given = [&](int token) {          // no such token, or one that is rejected
+    bool no = (unsigned)token >= (unsigned)vocab;
+    if (!DRAFT)
+      for (int k = 0; k < rejected; ++k) no = no || sh.gone[k] == token;
+    return no;
+  };
+#pragma unroll 1
+  for (int tile = first, k = 0; tile < end; ++tile, ++k) {
+    float x[8], y[8] = {};
+    ring.get(k, x, y);
+    ring.ask(k + Ring<T>::kRing, (tile + Ring<T>::kRing) * kTile + base, tile + Ring<T>::kRing < end);
+    double mine = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < 8; i += 2) {     // short code: it is gone through once or twice, and has to be fetched first
+      float xi = x[0], xj = x[1], yi = y[0], yj = y[1];
+#pragma unroll
+      for (int k = 2; k < 8; k += 2) {
+        xi = i == k ? x[k] : xi;
+        xj = i == k ? x[k + 1] : xj;
+        yi = i == k ? y[k] : yi;
+        yj = i == k ? y[k + 1] : yj;
+      }
+      const double r = left<DRAFT>(xi, yi, rejected), s = left<DRAFT>(xj, yj, rejected);
+      mine += DRAFT || !given(tile * kTile + base + i) ? r : 0.0;
+      mine += DRAFT || !given(tile * kTile + base + i + 1) ? s : 0.0;
     }
-    const int tiles = (p.vocab + shift + kTile - 1) / kTile;
-    tile0 = (int)((int64_t)tiles * rank / p.cluster);
-    tile1 = (int)((int64_t)tiles * (rank + 1) / p.cluster);
-    rejected = 0;
-  }
-  __device__ int place(int tile) const { return tile * kTile + lane * 8 - shift; }
-
-  // Sums over the cluster of up to two values per block, by every thread.
-  __device__ void total(double a, double b, double& ta, double& tb) {
-    a = warp_sum(a);
-    b = warp_sum(b);
-    __syncthreads();                     // the former use of `warps` is over
-    if (lane == 0) {
-      warps[2 * warp] = a;
-      warps[2 * warp + 1] = b;
+    double upto = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const double o = __shfl_up_sync(0xffffffffu, upto, s);
+      if (lane >= s) upto += o;
     }
-    __syncthreads();
-    ta = tb = 0.0;
-    for (int w = 0; w < kWarps; ++w) {
-      ta += warps[2 * w];
-      tb += warps[2 * w + 1];
-    }
-    if (p.cluster == 1) return;
-    double* mine = box + turn * 4;
-    if (tid == 0) {
-      mine[0] = ta;
-      mine[1] = tb;
-    }
-    cluster_sync();
-    ta = tb = 0.0;
-    for (int r = 0; r < p.cluster; ++r) {
-      const uint32_t from = mapa(smem_at(mine), r);
-      ta += ld_cluster(from);
-      tb += ld_cluster(from + 8);
-    }
-    turn ^= 1;
-  }
-
-  // A part's sum over the block; which: 0 the model's, 1 the draft's, into one turn of the box.
-  __device__ Sum whole(Sum a, float c, int which) {
-    a = warp_join(a, c);
-    float* f = reinterpret_cast<float*>(strips);
-    __syncthreads();
-    if (lane == 0) {
-      f[warp * 2] = a.max;
-      f[warp * 2 + 1] = a.s;
-    }
-    __syncthreads();
-    a = Sum{-CUDART_INF_F, 0.f};
-    for (int w = 0; w < kWarps; ++w) join(a, Sum{f[w * 2], f[w * 2 + 1]}, c);
-    double* mine = box + turn * 4 + which * 2;
-    if (p.cluster > 1 && tid == 0) {
-      mine[0] = a.max;
-      mine[1] = a.s;
-    }
-    return a;
-  }
-  __device__ Sum gathered(Sum a, float c, int which) {
-    if (p.cluster == 1) return a;
-    a = Sum{-CUDART_INF_F, 0.f};
-    for (int r = 0; r < p.cluster; ++r) {
-      const uint32_t from = mapa(smem_at(box + turn * 4 + which * 2), r);
-      join(a, Sum{(float)ld_cluster(from), (float)ld_cluster(from + 8)}, c);
-    }
-    return a;
-  }
-  // The row's sums in fp32.
-  __device__ void sums(float c, float dc, bool children, Sum& a, Sum& b) {
-    const bool both = DRAFT && children;
-    a = b = Sum{-CUDART_INF_F, 0.f};
-    for (int tile = tile0 + warp; tile < tile1; tile += kWarps) {
-      float x[8], y[8];
-      load8(row, place(tile), p.vocab, true, x);
-      if (both) load8(drow, place(tile), p.vocab, dvec, y);
-      add8(a, x, c);
-      if (both) add8(b, y, dc);
-    }
-    a = whole(a, c, 0);
-    if (both) b = whole(b, dc, 1);
-    if (p.cluster > 1) cluster_sync();
-    a = gathered(a, c, 0);
-    if (both) b = gathered(b, dc, 1);
-    if (p.cluster > 1) turn ^= 1;
-  }
-  // The same in 64 bits.
-  __device__ void exact(Exact& e) {
-    double s = 0.0, t = 0.0;
-    for (int tile = tile0 + warp; tile < tile1; tile += kWarps) {
-      float x[8], y[8];
-      load8(row, place(tile), p.vocab, true, x);
-      if (DRAFT) load8(drow, place(tile), p.vocab, dvec, y);
+    const uint32_t there = __ballot_sync(0xffffffffu, cum + upto > want && mine > kNothing);
+    const bool any = __any_sync(0xffffffffu, mine > kNothing);
+    if (there != 0) {                    // in the first of these lanes: lane i < 8 looks at its i-th token
+      const int lead = __ffs(there) - 1;
+      float xi = 0.f, yi = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        s += exp(fma((double)x[i], e.scale, -e.top));
-        if (DRAFT) t += exp(fma((double)y[i], e.dscale, -e.dtop));
+        const float xs = __shfl_sync(0xffffffffu, x[i], lead), ys = __shfl_sync(0xffffffffu, y[i], lead);
+        xi = lane == i ? xs : xi;
+        yi = lane == i ? ys : yi;
       }
-    }
-    double ts, tt;
-    total(s, t, ts, tt);
-    e.inv = 1.0 / ts;
-    e.dinv = DRAFT ? 1.0 / tt : 0.0;
-  }
-  // What is left of the probability of a token whose logits are x (the model's) and y (the draft's) behind `rejections`, in units that are the
-  // same for all tokens.
-  __device__ double left(const Exact& e, float x, float y, int rejections) const {
-    double r = exp(fma((double)x, e.scale, -e.top)) * e.inv;
-    if (DRAFT && rejections > 0) {
-      const double q = exp(fma((double)y, e.dscale, -e.dtop)) * e.dinv;
-      for (int i = 0; i < rejections; ++i)
-        if (norm[i] > 0.0) r = fmax(r - q, 0.0) * norm[i];
-    }
-    return r;
-  }
-  __device__ bool is_gone(int token) const {
-    for (int i = 0; i < rejected; ++i)
-      if (gone[i] == token) return true;
-    return false;
-  }
-  __device__ void left8(const Exact& e, int tile, double (&w)[8]) const {
-    float x[8], y[8];
-    const int at = place(tile);
-    load8(row, at, p.vocab, true, x);
-    if (DRAFT && rejected > 0) load8(drow, at, p.vocab, dvec, y);
+      const int token = tile * kTile + lead * 8 - sh.row.shift + lane;
+      const double r = lane >= 8 || given(token) ? 0.0 : left<DRAFT>(xi, yi, rejected);
+      double c = r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = left(e, x[i], DRAFT ? y[i] : 0.f, rejected);
-    if (!DRAFT && rejected > 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (is_gone(at + i)) w[i] = 0.0;
-    }
-  }
-  // Z behind one more rejection: norm[rejected] is set, by all.
-  __device__ void reject(const Exact& e) {
-    double s = 0.0, ts, unused;
-    for (int tile = tile0 + warp; tile < tile1; tile += kWarps) {
-      float x[8], y[8];
-      load8(row, place(tile), p.vocab, true, x);
-      load8(drow, place(tile), p.vocab, dvec, y);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += fmax(left(e, x[i], y[i], rejected) - exp(fma((double)y[i], e.dscale, -e.dtop)) * e.dinv, 0.0);
-    }
-    total(s, 0.0, ts, unused);
-    if (tid == 0) norm[rejected] = ts > 0.0 ? 1.0 / ts : 0.0;
-    __syncthreads();
-    ++rejected;
-  }
-  // The token at u of what is left; -1 where nothing is.
-  __device__ int draw(const Exact& e, float u) {
-    const int tiles = tile1 - tile0, per = max(1, (tiles + kStrips - 1) / kStrips), n = (tiles + per - 1) / per;
-    double sum = 0.0;
-    __syncthreads();                     // `strips` also holds what sums() exchanged
-    for (int s = warp; s < n; s += kWarps) {
-      double v = 0.0;
-      for (int tile = tile0 + s * per; tile < min(tile1, tile0 + (s + 1) * per); ++tile) {
-        double w[8];
-        left8(e, tile, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v += w[i];
+      for (int s = 1; s < 8; s <<= 1) {
+        const double o = __shfl_up_sync(0xffffffffu, c, s);
+        if (lane >= s) c += o;
       }
-      v = warp_sum(v);
-      if (lane == 0) strips[s] = v;
+      c += __shfl_sync(0xffffffffu, cum + (upto - mine), lead);
+      const uint32_t some = __ballot_sync(0xffffffffu, r > kNothing), hit = __ballot_sync(0xffffffffu, r > kNothing && c > want);
+      return __shfl_sync(0xffffffffu, token, hit ? __ffs(hit) - 1 : 31 - __clz(some));
     }
-    __syncthreads();
-    for (int s = 0; s < n; ++s) sum += strips[s];          // every thread the same
-    double* mine = box + turn * 4;
-    double front = 0.0, all = sum;
-    int last = 0, holder = -1;           // the last block with anything; the one that holds the place
-    if (p.cluster > 1) {
-      if (tid == 0) mine[0] = sum;
-      cluster_sync();
-      all = 0.0;
-      for (int r = 0; r < p.cluster; ++r) all += ld_cluster(mapa(smem_at(mine), r));
-      const double want = (double)u * all;
-      double cum = 0.0;
-      for (int r = 0; r < p.cluster; ++r) {
-        const double v = ld_cluster(mapa(smem_at(mine), r));
-        if (v > 0.0) last = r;
-        if (holder < 0 && cum + v > want) {
-          holder = r;
-          front = cum;
-        }
-        cum += v;
-      }
-      turn ^= 1;
-    } else {
-      holder = 0;
-    }
-    const bool beyond = holder < 0;      // u not below 1, or a rounding: the last token with anything
-    if (beyond) holder = last;
-    if (!(all > 0.0) || !(all < CUDART_INF)) return -1;
-    if (holder == rank && warp == 0) {
-      const double want = beyond ? CUDART_INF : (double)u * all - front;
-      // the strip, by all lanes alike
-      double cum = 0.0;
-      int strip = -1, final = -1;
-      double before = 0.0;
-      for (int s = 0; s < n; ++s) {
-        const double v = strips[s];
-        if (v > 0.0) final = s;
-        if (strip < 0 && cum + v > want) {
-          strip = s;
-          before = cum;
-        }
-        cum += v;
-      }
-      double place_in = want - before;
-      if (strip < 0) {
-        strip = final;
-        place_in = CUDART_INF;
-      }
-      int token = -1, some = -1;         // found; the last one with anything
-      cum = 0.0;
-      for (int tile = tile0 + strip * per; tile < min(tile1, tile0 + (strip + 1) * per) && token < 0; ++tile) {
-        double w[8], mine8 = 0.0;
-        left8(e, tile, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mine8 += w[i];
-        double upto = mine8;
-#pragma unroll
-        for (int sh = 1; sh < 32; sh <<= 1) {
-          const double o = __shfl_up_sync(0xffffffffu, upto, sh);
-          if (lane >= sh) upto += o;
-        }
-        double c = cum + (upto - mine8);
-        int hit = 0x7fffffff, any = -1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          c += w[i];
-          if (w[i] > 0.0) {
-            any = place(tile) + i;
-            if (c > place_in && hit == 0x7fffffff) hit = any;
-          }
-        }
-        hit = __reduce_min_sync(0xffffffffu, hit);
-        any = __reduce_max_sync(0xffffffffu, any);
-        if (any >= 0) some = any;
-        if (hit != 0x7fffffff) token = hit;
-        cum += __shfl_sync(0xffffffffu, upto, 31);
-      }
-      if (token < 0) token = some;
-      if (lane == 0) *found = token;
-    }
-    if (p.cluster > 1) cluster_sync(); else __syncthreads();
-    int token;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(token) : "r"(mapa(smem_at(found), holder)));
-    return token;
+    if (any) some_tile = tile;
+    cum += __shfl_sync(0xffffffffu, upto, 31);
   }
-};
+  int last = -1;
+#pragma unroll 1
+  for (int i = 0; i < 8 && some_tile >= 0; ++i) {
+    const int token = some_tile * kTile + base + i;
+    if (!given(token) && left<DRAFT>(value(row + token), both ? value(drow + token) : 0.f, rejected) > kNothing) last = token;
+  }
+  return __reduce_max_sync(0xffffffffu, last);
+}
 
-template <typename T, bool DRAFT>
-__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyParams p) {
-  __shared__ double strips[kStrips], norm[kNodes], warps[kWarps * 2], box[8];
-  __shared__ int32_t gone[kNodes], token_of[kNodes], parent_of[kNodes], found;
-  __shared__ float chance_of[kNodes];
-  const int request = blockIdx.x / p.cluster, rank = blockIdx.x % p.cluster;
-  Walk<T, DRAFT> w(p, rank);
-  w.strips = strips; w.norm = norm; w.gone = gone; w.warps = warps; w.box = box; w.found = &found;
-  const int first = p.first[request], nodes = p.first[request + 1] - first, tid = threadIdx.x;
-  pdl_launch_dependents();
-  pdl_wait();
-  if (tid < nodes) {
-    token_of[tid] = p.tokens[first + tid];
-    parent_of[tid] = p.parents[first + tid];
-    chance_of[tid] = p.u_accept[first + tid];
+template <typename T, bool DRAFT, int WARPS, int MODE>
+__device__ __noinline__ void pass(int rejected, int to, int rank, int cluster, int turn) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const T* const row = static_cast<const T*>(sh.row.row);
+  const T* const drow = static_cast<const T*>(sh.row.drow);
+  const int vocab = sh.row.vocab, per = sh.row.per, tile0 = sh.row.from, tile1 = sh.row.to, base = lane * 8 - sh.row.shift;
+  const bool dvec = sh.row.dvec, both = DRAFT && (MODE != STRIPS || rejected > 0);
+  const double scale = sh.e.scale, top = sh.e.top, inv = sh.e.inv, dscale = sh.e.dscale, dtop = sh.e.dtop, dinv = sh.e.dinv;
+  extern __shared__ __align__(16) unsigned char copies[];
+  const Ring<T> ring(row, drow, vocab, both, dvec, copies, warp, lane);
+  // tiles in turn, strip after strip; `ahead` is the one to ask for
+  int ahead_strip = warp, ahead = tile0 + warp * per, asked = 0;
+  auto ask = [&]() {
+    ring.ask(asked++, ahead * kTile + base, ahead_strip < to);
+    if (++ahead >= min(tile1, tile0 + (ahead_strip + 1) * per)) {
+      ahead_strip += WARPS;
+      ahead = tile0 + ahead_strip * per;
+    }
+  };
+#pragma unroll 1
+  for (int k = 0; k < Ring<T>::kRing; ++k) ask();
+  double v[kValues] = {};
+  int k_tile = 0;
+#pragma unroll 1
+  for (int strip = warp; strip < to; strip += WARPS) {
+    const int end = min(tile1, tile0 + (strip + 1) * per);
+    double in_strip = 0.0, p_strip = 0.0, q_strip = 0.0;
+#pragma unroll 1
+    for (int tile = tile0 + strip * per; tile < end; ++tile) {
+      float x[8], y[8];
+      ring.get(k_tile++, x, y);
+      ask();
+      const int at = tile * kTile + base;
+#pragma unroll
+      for (int part = 0; part < 8; part += 4) {
+        double w[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = weight64(x[part + i], scale, top);
+        if (both) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[i] = weight64(y[part + i], dscale, dtop);
+        }
+        if (MODE == SUMS || MODE == FIRST) {
+          v[0] += (w[0] + w[1]) + (w[2] + w[3]);
+          if (both) v[1] += (q[0] + q[1]) + (q[2] + q[3]);
+          if (DRAFT && MODE == FIRST) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const double p = w[i] * inv, d = fma(-q[i], dinv, p);
+              if ((__double2hiint(d) & 0x7fffffff) + (19 << 20) <= __double2hiint(p)) v[2] += 2.0 * p;
+              const int keep = ~(__double2hiint(d) >> 31);
+              in_strip += __hiloint2double(__double2hiint(d) & keep, __double2loint(d) & keep);
+              p_strip += __hiloint2double(__double2hiint(w[i]) & keep, __double2loint(w[i]) & keep);
+              q_strip += __hiloint2double(__double2hiint(q[i]) & keep, __double2loint(q[i]) & keep);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] *= inv;
+          if (both) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] *= dinv;
+          }
+#pragma unroll 1
+          for (int k = 0; k < rejected; ++k) {
+            if (DRAFT) {
+              const double z = sh.norm[k];
+              if (z > 0.0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = fmax(w[i] - q[i], 0.0) * z;
+              }
+            } else {
+              const int d = sh.gone[k] - at - part;
+              if ((unsigned)d < 4u) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (d == i) w[i] = 0.0;
+              }
+            }
+          }
+          if (DRAFT && MODE == REST) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = fmax(w[i] - q[i], 0.0);
+          }
+          const double sum = (w[0] + w[1]) + (w[2] + w[3]);
+          in_strip += sum;
+        }
+      }
+    }
+    if (MODE == FIRST) {
+      v[3] += in_strip;
+      v[4] += p_strip;
+      v[5] += q_strip;
+      in_strip = warp_sum(in_strip);
+      p_strip = warp_sum(p_strip);
+      q_strip = warp_sum(q_strip);
+      if (lane == 0) {
+        sh.strips[0][strip] = in_strip;
+        sh.strips[1][strip] = p_strip;
+        sh.strips[2][strip] = q_strip;
+      }
+    } else if (MODE == STRIPS || MODE == REST) {
+      v[0] += in_strip;
+      in_strip = warp_sum(in_strip);
+      if (lane == 0) sh.strips[0][strip] = in_strip;
+    }
+  }
+  constexpr int n = MODE == FIRST ? 6 : MODE == SUMS ? 2 : 1;
+#pragma unroll
+  for (int i = 0; i < kValues; ++i) {
+    if (i < n) {
+      v[i] = warp_sum(v[i]);
+      if (lane == 0) sh.part[warp][i] = v[i];
+    }
   }
   __syncthreads();
-  if (p.cluster > 1) cluster_sync();     // all blocks of the cluster run: they may be written to and read
-  int cur = 0, emitted = 0;
+  if (warp == 0) {
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      if (i < n) {
+        v[i] = sh.part[lane & (WARPS - 1)][i];
+#pragma unroll
+        for (int s = WARPS / 2; s > 0; s >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
+      }
+    }
+    publish(n, v, rank, cluster, turn, lane);
+  }
+  sync_all(cluster);
+}
+
+// THREADS: 512 where there are few requests, so that what runs of them has the threads of an SM each; else 128, four blocks of which an SM runs.
+template <typename T, bool DRAFT, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __grid_constant__ VerifyParams p) {
+  constexpr int kWarps = THREADS / 32;
+  extern __shared__ __align__(16) unsigned char copies[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cluster = p.cluster;
+  const int request = blockIdx.x / cluster, rank = blockIdx.x % cluster;
+  const int first = p.first[request], nodes = p.first[request + 1] - first;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (tid < kNodes) {                    // gone: here, the nodes' parents
+    const bool node = tid < nodes;
+    const int token = node ? p.tokens[first + tid] : -1, parent = node && tid > 0 ? p.parents[first + tid] : -1;
+    sh.token[tid] = token;
+    sh.gone[tid] = (unsigned)token < (unsigned)p.vocab && parent >= 0 && parent < tid ? parent : -1;      // -1: passed over
+    sh.chance[tid] = node ? p.u_accept[first + tid] : 0.f;
+    sh.scale[tid] = node && p.scale ? p.scale[first + tid] : 1.f;
+    sh.dscale[tid] = DRAFT && node && p.draft_scale ? p.draft_scale[first + tid] : 1.f;
+  }
+  __syncthreads();
+  if (tid < nodes) {
+    int child = -1, sibling = -1;
+    const int parent = sh.gone[tid];
+    for (int j = nodes - 1; j > tid; --j) {
+      if (sh.gone[j] == tid) child = j;
+      if (parent >= 0 && sh.gone[j] == parent) sibling = j;
+    }
+    sh.child[tid] = child;
+    sh.sibling[tid] = sibling;
+  }
+  sync_all(cluster);                     // all blocks of the cluster run: they may be written to
+  int cur = 0, emitted = 0, turn = 0;
   for (;;) {
     const int64_t r = first + cur;
-    const float scale = p.scale ? p.scale[r] : 1.f, dscale = DRAFT && p.draft_scale ? p.draft_scale[r] : 1.f;
+    const float scale = sh.scale[cur], dscale = sh.dscale[cur];
     const float c = scale * kLog2e, dc = dscale * kLog2e;
-    w.at_row(r);
-    bool children = false;               // the draft's row of a node without any is not read
-    for (int j = cur + 1; j < nodes; ++j) children = children || (parent_of[j] == cur && (unsigned)token_of[j] < (unsigned)p.vocab);
-    Sum a, b;
-    w.sums(c, dc, children, a, b);
-    bool valid = a.s > 0.f && a.s < CUDART_INF_F;
-    if (DRAFT && children) valid = valid && b.s > 0.f && b.s < CUDART_INF_F;
+    const T* const row = static_cast<const T*>(p.logits) + r * p.stride;
+    const T* const drow = DRAFT ? static_cast<const T*>(p.draft) + r * p.draft_stride : nullptr;
+    const int vocab = p.vocab, shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    const bool dvec = DRAFT && (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(T)) == shift;
+    const int tiles = (vocab + shift + kTile - 1) / kTile;
+    const int from = (int)((int64_t)tiles * rank / cluster), to = (int)((int64_t)tiles * (rank + 1) / cluster);
+    const int child = sh.child[cur];
+    const bool both = DRAFT && child >= 0;           // the draft's row of a node without children is not read
+    // the first child's logits: asked for before the sums
+    const float x0 = child >= 0 ? value(row + sh.token[child]) : 0.f, y0 = both ? value(drow + sh.token[child]) : 0.f;
+
+    // the row's sums in fp32
+    Sum a = nothing(), b = nothing();
+    {
+      const Ring<T> ring(row, drow, vocab, both, dvec, copies, warp, lane);
+      const int base = lane * 8 - shift;
+      for (int k = 0; k < Ring<T>::kRing; ++k) ring.ask(k, (from + warp + k * kWarps) * kTile + base, from + warp + k * kWarps < to);
+#pragma unroll 1
+      for (int k = 0, tile = from + warp; tile < to; ++k, tile += kWarps) {
+        float x[8], y[8];
+        ring.get(k, x, y);
+        const int next = tile + Ring<T>::kRing * kWarps;
+        ring.ask(k, next * kTile + base, next < to);
+        if (k == 0) {
+          refer(a, x, c);
+          if (both) refer(b, y, dc);
+        }
+        add(a, x, c);
+        if (both) add(b, y, dc);
+      }
+      lanes_sum<16>(a, c);
+      if (both) lanes_sum<16>(b, dc);
+      if (lane == 0) sh.part32[warp] = make_float4(a.ref, a.s, b.ref, b.s);
+      __syncthreads();
+      auto join = [&](const float4& v, auto widest) {
+        a = Sum{v.x, top_of(v.x, c), v.y};
+        b = Sum{v.z, top_of(v.z, dc), v.w};
+        lanes_sum<widest.value>(a, c);
+        if (both) lanes_sum<widest.value>(b, dc);
+      };
+      if (cluster > 1) {
+        if (warp == 0) {
+          join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
+          if (lane < cluster) st_cluster(mapa(smem_u32(&sh.sums[turn][rank]), lane), make_float4(a.ref, a.s, b.ref, b.s));
+        }
+        cluster_sync();
+        join(lane % kMaxCluster < cluster ? sh.sums[turn][lane % kMaxCluster] : make_float4(-CUDART_INF_F, 0.f, -CUDART_INF_F, 0.f),
+             std::integral_constant<int, kMaxCluster / 2>{});
+        turn ^= 1;
+      } else {
+        join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
+      }
+      if (!both) b = Sum{0.f, 0.f, 1.f};
+    }
+    const bool valid = a.s > 0.f && a.s < CUDART_INF_F && b.s > 0.f && b.s < CUDART_INF_F;
     int chosen = -1, out = -1;
     if (valid) {
-      Exact e;
-      e.scale = scale; e.top = (double)a.max * scale; e.inv = 1.0;
-      e.dscale = dscale; e.dtop = DRAFT && children ? (double)b.max * dscale : 0.0; e.dinv = 0.0;
-      bool precise = false;
+      // strips as short as there is room for, but a few for every warp at most: their sums cost a strip as much as a tile does
+      const int per = max(1, max((to - from + kStrips - 1) / kStrips, min(2, (to - from) / (4 * kWarps)))), n = (to - from + per - 1) / per;
+      bool precise = false;              // sh.e holds sums of 64 bits
+      int rejected = 0;
       float rest = 1.f;                  // no draft: what the rejected tokens leave
       double rest64 = 1.0;
       bool pending = false;              // draft: a rejection whose Z is not summed yet
-      for (int j = cur + 1; j < nodes; ++j) {
-        if (parent_of[j] != cur) continue;
-        const int t = token_of[j];
-        if ((unsigned)t >= (unsigned)p.vocab) continue;
-        const float u = chance_of[j], x = value(w.row + t), y = DRAFT ? value(w.drow + t) : 0.f;
-        if (!DRAFT && w.is_gone(t)) {    // given twice: nothing is left of it
-          continue;
+      bool ready = false;
+      auto prepare = [&]() {             // what the passes read; e.inv, e.dinv: to 2^-21 or so
+        if (ready) return;
+        ready = true;
+        if (tid == 0) {
+          sh.row = Row{row, drow, vocab, shift, from, to, dvec, per, n};
+          sh.e = Exact{scale, (double)a.ref * scale, (double)(1.f / a.s), dscale, (double)b.ref * dscale, (double)(1.f / b.s)};
         }
-        bool accept;
-        bool close = precise;
-        if (!precise) {
-          const float have = weight(x, a.max, c) / a.s;
-          const float need = DRAFT ? u * (weight(y, b.max, dc) / b.s) : u * rest;
+        __syncthreads();
+      };
+      auto sum64 = [&](auto mode) {      // SUMS or FIRST: the distributions' sums become those of 64 bits
+        prepare();
+        pass<T, DRAFT, kWarps, mode.value>(rejected, n, rank, cluster, turn);
+        if (tid == 0) {
+          sh.e.inv = 1.0 / total(0, cluster, turn);
+          if (DRAFT) sh.e.dinv = 1.0 / total(1, cluster, turn);
+        }
+        __syncthreads();
+        turn ^= 1;
+        precise = true;
+      };
+      auto reject = [&]() {              // Z of the pending rejection
+        if constexpr (DRAFT) pass<T, DRAFT, kWarps, REST>(rejected, n, rank, cluster, turn);
+        const double z = total(0, cluster, turn);
+        turn ^= 1;
+        if (tid == 0) sh.norm[rejected] = z > kNothing ? 1.0 / z : 0.0;
+        __syncthreads();
+        ++rejected;
+        pending = false;
+      };
+      for (int j = child; j >= 0; j = sh.sibling[j]) {
+        const int t = sh.token[j];
+        const float u = sh.chance[j], x = j == child ? x0 : value(row + t), y = j == child ? y0 : DRAFT ? value(drow + t) : 0.f;
+        bool again = false;              // given twice: nothing is left of it
+        if (!DRAFT)
+          for (int i = 0; i < rejected; ++i) again = again || sh.gone[i] == t;
+        if (again) continue;
+        bool accept = false, close = precise || pending;
+        if (!close) {
+          const float have = weight(x, a, c) / a.s;
+          const float need = DRAFT ? u * (weight(y, b, dc) / b.s) : u * rest;
           accept = need < have;
-          close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + w.rejected));
+          close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + rejected));
         }
         if (close) {
           if (!precise) {
-            w.exact(e);
-            precise = true;
+            sum64(std::integral_constant<int, SUMS>{});
             if (!DRAFT)
-              for (int i = 0; i < w.rejected; ++i) rest64 -= w.left(e, value(w.row + gone[i]), 0.f, 0);
+              for (int i = 0; i < rejected; ++i) rest64 -= weight64(value(row + sh.gone[i]), sh.e.scale, sh.e.top) * sh.e.inv;
           }
-          if (pending) w.reject(e);
-          pending = false;
-          const double have = w.left(e, x, y, w.rejected);
-          accept = DRAFT ? (double)u * (exp(fma((double)y, e.dscale, -e.dtop)) * e.dinv) < have : (double)u * rest64 < have;
+          if (pending) reject();
+          const double have = left<DRAFT>(x, y, rejected);
+          accept = have > kNothing && (DRAFT ? (double)u * (weight64(y, sh.e.dscale, sh.e.dtop) * sh.e.dinv) : (double)u * rest64) < have;
         }
         if (accept) {
           chosen = j;
@@ -498,36 +690,124 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
           break;
         }
         if (DRAFT) {
-          if (!precise) w.exact(e);
-          precise = pending = true;
+          pending = true;
         } else {
-          rest -= weight(x, a.max, c) / a.s;
-          if (precise) rest64 -= w.left(e, x, 0.f, 0);
+          rest -= weight(x, a, c) / a.s;
+          if (precise) rest64 -= weight64(x, sh.e.scale, sh.e.top) * sh.e.inv;
           __syncthreads();               // the others may still look through the list
-          if (tid == 0) gone[w.rejected] = t;
-          ++w.rejected;
+          if (tid == 0) sh.gone[rejected] = t;
+          ++rejected;
           __syncthreads();
         }
       }
       if (chosen < 0) {
-        if (pending) {                   // its Z is a factor of all that is left: not needed, unless nothing is
+        const float at = p.u_sample[request];
+        // the last rejection's Z is a factor of all that is left: it is not needed, unless nothing is
+        prepare();
+        const bool one = DRAFT && pending && rejected == 0 && !precise;
+        bool done = false;
+        double fix_p = 0.0, fix_q = 0.0;
+        const double inv = sh.e.inv, dinv = sh.e.dinv;
+        if (DRAFT && pending) {
           __syncthreads();
-          if (tid == 0) norm[w.rejected] = 1.0;
-          ++w.rejected;
+          if (tid == 0) sh.norm[rejected] = 1.0;
           __syncthreads();
         }
-        out = w.draw(e, p.u_sample[request]);
-        if (out < 0 && pending) {        // p = q up to roundings: as if not rejected
-          --w.rejected;
-          out = w.draw(e, p.u_sample[request]);
+        if constexpr (DRAFT) if (one) {
+          // One rejection and none before: the sums of 64 bits and what it leaves in one pass. The latter is linear in the sums' reciprocals as long
+          // as the corrections change no sign.
+          sum64(std::integral_constant<int, FIRST>{});
+          turn ^= 1;                     // its values are read here
+          fix_p = sh.e.inv - inv;
+          fix_q = sh.e.dinv - dinv;
+          const double off = fmax(fabs(fix_p) * a.s, fabs(fix_q) * b.s);
+          done = off < 0x1p-20 && off * total(2, cluster, turn) <= 1e-12 * total(3, cluster, turn);
+          if (!done) turn ^= 1;
+        } else if (pending && !precise) {
+          sum64(std::integral_constant<int, SUMS>{});
+        }
+        const int all_rejected = rejected + pending;
+        for (int tries = 0; tries < 2 && out < 0; ++tries) {
+          const int gone = tries ? rejected : all_rejected;          // nothing left: p = q up to roundings, as if not rejected
+          if (tries && !pending) break;
+          if (!done) pass<T, DRAFT, kWarps, STRIPS>(gone, n, rank, cluster, turn);
+          // the blocks' sums; the last block with anything, the one that holds the place
+          auto sum_of = [&](int k) {
+            const double* v = sh.box[turn][k];
+            return done ? fmax(0.0, v[3] + fix_p * v[4] - fix_q * v[5]) : v[0];
+          };
+          double all = 0.0, front = 0.0, cum = 0.0;
+          for (int k = 0; k < cluster; ++k) all += sum_of(k);
+          const double want = (double)at * all;
+          int holder = -1, last = 0;
+          for (int k = 0; k < cluster; ++k) {
+            const double v = sum_of(k);
+            if (v > kNothing) last = k;
+            if (holder < 0 && cum + v > want) {
+              holder = k;
+              front = cum;
+            }
+            cum += v;
+          }
+          turn ^= 1;
+          const bool fixed = done;
+          done = false;
+          if (!(all > kNothing) || !(all < CUDART_INF)) continue;
+          const bool beyond = holder < 0;            // u not below 1, or a rounding: the last token with anything
+          if (beyond) holder = last;
+          if (holder == rank && warp == 0) {
+            // the strip: a lane has n / 32 neighbouring ones
+            const double here = beyond ? CUDART_INF : want - front;
+            const int each = (n + 31) / 32, s0 = min(n, lane * each), s1 = min(n, s0 + each);
+            auto strip_of = [&](int s) {
+              return fixed ? fmax(0.0, sh.strips[0][s] + fix_p * sh.strips[1][s] - fix_q * sh.strips[2][s]) : sh.strips[0][s];
+            };
+            double own = 0.0;
+            int final = -1;
+            for (int s = s0; s < s1; ++s) {
+              const double v = strip_of(s);
+              own += v;
+              if (v > kNothing) final = s;
+            }
+            double upto = own;
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) {
+              const double o = __shfl_up_sync(0xffffffffu, upto, s);
+              if (lane >= s) upto += o;
+            }
+            const uint32_t behind = __ballot_sync(0xffffffffu, upto > here);
+            final = __reduce_max_sync(0xffffffffu, final);
+            double before = upto - own, place = CUDART_INF;
+            int strip = -1;
+            const int lead = behind != 0 ? __ffs(behind) - 1 : 0;
+            if (behind != 0 && lane == lead) {
+              for (int s = s0; s < s1 && strip < 0; ++s) {
+                const double v = strip_of(s);
+                if (before + v > here) strip = s; else before += v;
+              }
+              place = here - before;
+            }
+            strip = __shfl_sync(0xffffffffu, strip, lead);
+            place = __shfl_sync(0xffffffffu, place, lead);
+            if (strip < 0) {
+              strip = final;
+              place = CUDART_INF;
+            }
+            const int token = find<T, DRAFT>(gone, strip, place);
+            if (lane < cluster) {
+              const uint32_t found = smem_u32(&sh.found);
+              st_cluster(cluster > 1 ? mapa(found, lane) : found, token);
+            }
+          }
+          sync_all(cluster);
+          out = sh.found;
         }
       }
     }
     if (rank == 0 && tid == 0) {
-      const bool some = out >= 0;
       p.emitted[first + emitted] = out;
       p.path[first + emitted] = first + cur;
-      p.logprob[first + emitted] = some ? ((value(w.row + out) - a.max) * c - log2f(a.s)) * kLn2 : CUDART_NAN_F;
+      p.logprob[first + emitted] = out >= 0 ? (exponent(value(row + out), a, c) - log2f(a.s)) * kLn2 : CUDART_NAN_F;
     }
     ++emitted;
     if (chosen < 0) break;
@@ -535,19 +815,22 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
   }
   if (rank == 0) {
     if (tid == 0) p.count[request] = emitted;
-    for (int i = emitted + tid; i < nodes; i += kThreads) {
+    for (int i = emitted + tid; i < nodes; i += THREADS) {
       p.emitted[first + i] = p.path[first + i] = -1;
       p.logprob[first + i] = 0.f;
     }
   }
-  if (p.cluster > 1) cluster_sync();     // no block leaves while another one reads its sums
+  if (cluster > 1) cluster_sync();       // no block leaves while another one may write to it
 }
 
-template <typename T, bool DRAFT>
-cudaError_t launch(const VerifyParams& p, int requests, cudaStream_t stream) {
+template <typename T, bool DRAFT, int THREADS>
+cudaError_t launch_t(const VerifyParams& p, int requests, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(requests * p.cluster));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = THREADS / 32 * Ring<T>::kBytes;
+  const cudaError_t e = cudaFuncSetAttribute(verify_kernel<T, DRAFT, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  if (e != cudaSuccess) return e;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -557,7 +840,11 @@ cudaError_t launch(const VerifyParams& p, int requests, cudaStream_t stream) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T, DRAFT>, p);
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, DRAFT, THREADS>, p);
+}
+template <typename T, bool DRAFT>
+cudaError_t launch(const VerifyParams& p, int requests, bool wide, cudaStream_t stream) {
+  return wide ? launch_t<T, DRAFT, 512>(p, requests, stream) : launch_t<T, DRAFT, 128>(p, requests, stream);
 }
 
 }  // namespace
@@ -587,9 +874,10 @@ extern "C" int ts_verify_tokens(const ts_verify* v, void* cuda_stream) {
   p.logits = v->logits; p.draft = v->draft; p.stride = v->row_stride; p.draft_stride = v->draft_stride;
   p.scale = v->scale; p.draft_scale = v->draft_scale; p.tokens = v->tokens; p.parents = v->parents;
   p.u_accept = v->u_accept; p.emitted = v->emitted; p.path = v->path; p.logprob = v->logprob; p.vocab = v->vocab;
-  // as many blocks of a request as run at once, two per SM, each with a few tiles for every warp
+  // as many blocks of a request as run at once, four of 128 threads per SM or one of 512, each with a few tiles for every warp
+  const bool wide = (int64_t)v->n_requests * kMaxCluster <= n_sms;
   p.cluster = 1;
-  while (p.cluster < kMaxCluster && (int64_t)v->n_requests * p.cluster * 2 <= 2 * n_sms && v->vocab / (p.cluster * 2) >= kTile * kWarps / 2) p.cluster *= 2;
+  while (p.cluster < kMaxCluster && (wide || (int64_t)v->n_requests * p.cluster * 2 <= 4 * n_sms) && v->vocab / (p.cluster * 2) >= kTile * (wide ? 4 : 2)) p.cluster *= 2;
   int32_t at = 0;
   for (int r0 = 0; r0 < v->n_requests; r0 += kWords) {
     const int some = std::min(kWords, v->n_requests - r0);
@@ -600,8 +888,8 @@ extern "C" int ts_verify_tokens(const ts_verify* v, void* cuda_stream) {
       if (r < some) at += v->n_nodes[r0 + r];
     }
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const cudaError_t e = v->dtype == TS_BF16 ? (v->draft ? launch<__nv_bfloat16, true>(p, some, stream) : launch<__nv_bfloat16, false>(p, some, stream))
-                                              : (v->draft ? launch<float, true>(p, some, stream) : launch<float, false>(p, some, stream));
+    const cudaError_t e = v->dtype == TS_BF16 ? (v->draft ? launch<__nv_bfloat16, true>(p, some, wide, stream) : launch<__nv_bfloat16, false>(p, some, wide, stream))
+                                              : (v->draft ? launch<float, true>(p, some, wide, stream) : launch<float, false>(p, some, wide, stream));
     if (e != cudaSuccess) return TS_ERR_CUDA;
   }
   return TS_OK;

@@ -622,15 +622,25 @@ typedef struct {
   int32_t n_adapters;       /* 1 to 65536                                                       */
   int32_t rank;             /* a multiple of 8, 8 to 256; adapters of less have rows and columns of zeros */
   const void* a;            /* DEVICE bf16 [n_adapters][rank][K], 16-byte aligned               */
-  const void* b;            /* DEVICE bf16 [n_adapters][N][rank], 16-byte aligned               */
+  const void* b;            /* DEVICE, B [n_adapters][N][rank] as ts_adapter_pack writes it in TS_ROWS_PLAIN, 128-byte aligned */
+  const void* b_pair;       /* the same in the order of a layer's qkv or gate/up projection, for those; else not read */
   const float* scale;       /* DEVICE [n_adapters], or NULL: 1                                  */
 } ts_adapters;
 
 /*
+ * ts_adapter_pack: B (DEVICE bf16 [n_adapters][N][rank], row-major) as the kernels read it, to ts_adapter_packed_bytes() bytes (128-byte aligned; 0 for
+ * arguments outside the limits): ranks padded to 16, 32 or a multiple of 64 and rows to a multiple of 128 with zeros. order: which rows lie together.
+ * TS_ROWS_QKV needs N a multiple of 128, TS_ROWS_GATE_UP (B's rows in the order of ts_pack_gate_up) of 256. Asynchronous on cuda_stream, on the current device.
+ */
+enum { TS_ROWS_PLAIN = 0, TS_ROWS_QKV = 1, TS_ROWS_GATE_UP = 2 };
+size_t ts_adapter_packed_bytes(int32_t n_adapters, int32_t N, int32_t rank);
+int ts_adapter_pack(const void* b, int32_t n_adapters, int32_t N, int32_t rank, int32_t order, void* packed, void* cuda_stream);
+
+/*
  * ts_adapter_project: C = (R ? R : 0) + x . W^T + the adapters' part, as ts_gemm_bf16 (arguments and limits there). Row r (a request) has the
  * next row_tokens[r] >= 1 rows of x, M in all, and uses adapter row_adapter[r], -1 = none; both HOST arrays. C must not overlap x, R
- * may be C. workspace: DEVICE, 256-byte aligned, ts_adapter_workspace_bytes() bytes, in use until the work enqueued here is done. Up to 1024 rows and 65536
- * tokens, else TS_ERR_UNSUPPORTED. Asynchronous on cuda_stream; two launches, one where no row has an adapter.
+ * may be C. workspace: DEVICE, 256-byte aligned, ts_adapter_workspace_bytes() bytes, in use until the work enqueued here is done. Up to 1024 rows and 8192
+ * tokens, or 512 rows and 32768 tokens, else TS_ERR_UNSUPPORTED. Asynchronous on cuda_stream; two launches, one where no row has an adapter.
  * ts_adapter_workspace_bytes: enough for any such call; 0 for arguments outside the limits.
  */
 size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank);
@@ -642,7 +652,7 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
  * ts_layer_attach_adapters: gives a layer's projections adapters (each NULL or with the same n_adapters; weights and workspace are the
  * caller's and stay in use; all NULL takes them off again). Wait for the layer's steps before changing them.
  * ts_layer_step_adapted: ts_layer_step in which row r of the step uses adapter row_adapter[r] (HOST, -1 = none) in every projection that has
- * adapters; row_adapter NULL = no adapters. Up to 1024 rows where one is used. ts_layer_adapters_workspace_bytes: 0 where no projection has
+ * adapters; row_adapter NULL = no adapters. Limits as for ts_adapter_project where one is used. ts_layer_adapters_workspace_bytes: 0 where no projection has
  * adapters or on a bad shape.
  */
 typedef struct {

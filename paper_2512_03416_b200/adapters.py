@@ -10,6 +10,7 @@ import torch
 from . import binding as B
 from .decoder import _check, _raw_stream
 
+ROWS = {"plain": B.TS_ROWS_PLAIN, "qkv": B.TS_ROWS_QKV, "gate_up": B.TS_ROWS_GATE_UP}
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
 
 
@@ -23,10 +24,13 @@ def _matrix(t: torch.Tensor, shape, device, what: str) -> int:
 
 
 class Adapters:
-    """The adapters of one projection [N, K]: a [adapters, rank, K], b [adapters, N, rank] bf16, scale float32 [adapters] (None: 1). The
-    tensors are kept, not copied. status: int32, TS_DEV_TIMEOUT where a bounded wait of a projection ran out."""
+    """The adapters of one projection [N, K]: a [adapters, rank, K], b [adapters, N, rank] bf16, scale float32 [adapters] (None: 1). a and
+    scale are kept, not copied; b is laid out anew here, so that an adapter that changes needs new Adapters. rows: which projection of a layer (see
+    ts_adapter_pack): "qkv", "gate_up" (b's rows in its packed order), or "plain" for others and for adapted_project. status: int32, TS_DEV_TIMEOUT where a bounded wait of a projection ran out."""
 
-    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None):
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None, rows: str = "plain"):
+        if rows not in ROWS:
+            raise ValueError(f"rows must be one of {sorted(ROWS)}")
         if not a.is_cuda or a.dim() != 3 or b.dim() != 3:
             raise ValueError("a and b must be CUDA tensors [adapters, rank, K] and [adapters, N, rank]")
         n, rank, self.k = a.shape
@@ -36,10 +40,22 @@ class Adapters:
         if scale is not None and (scale.dtype != torch.float32 or scale.device != a.device or scale.numel() != n or not scale.is_contiguous()):
             raise ValueError(f"scale must be a contiguous float32 tensor of {n} values on {a.device}")
         self.device, self.rank, self.count = a.device, rank, n
-        self.tensors = (a, b, scale)
-        self.args = B.ts_adapters(n, rank, _matrix(a, (n, rank, self.k), a.device, "a"), _matrix(b, (n, self.n, rank), a.device, "b"),
-                                  None if scale is None else scale.data_ptr())
+        self.rows, pa, pb = rows, _matrix(a, (n, rank, self.k), a.device, "a"), _matrix(b, (n, self.n, rank), a.device, "b")
+        self.tensors = [a, scale]
+        with torch.cuda.device(a.device):
+            packed = [self._pack(pb, order) for order in ([B.TS_ROWS_PLAIN] if rows == "plain" else [B.TS_ROWS_PLAIN, ROWS[rows]])]
+        self.args = B.ts_adapters(n, rank, pa, packed[0], packed[-1], None if scale is None else scale.data_ptr())
         self.status = torch.zeros(1, dtype=torch.int32, device=a.device)
+
+
+    def _pack(self, b: int, order: int) -> int:
+        nbytes = B.ts_adapter_packed_bytes(self.count, self.n, self.rank)
+        if nbytes == 0:
+            raise ValueError("too many adapters")
+        out = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        _check(B.ts_adapter_pack(b, self.count, self.n, self.rank, order, out.data_ptr(), _raw_stream(self.device.index)), "ts_adapter_pack")
+        self.tensors.append(out)
+        return out.data_ptr()
 
 
 def stack_adapters(parts) -> tuple:

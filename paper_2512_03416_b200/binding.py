@@ -32,6 +32,7 @@ TS_DEV_BAD_INDEX = 4
 TS_DEBUG_LOSE_APPEND_ARRIVAL = 1
 TS_CACHE_BF16, TS_CACHE_E4M3 = 0, 1
 TS_BF16, TS_F32 = 0, 1
+TS_ROWS_PLAIN, TS_ROWS_QKV, TS_ROWS_GATE_UP = 0, 1, 2
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 
@@ -93,7 +94,7 @@ class ts_logprobs(ctypes.Structure):
 
 class ts_adapters(ctypes.Structure):
     _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
-                ("scale", ctypes.c_void_p)]
+                ("b_pair", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class ts_layer_adapters(ctypes.Structure):
@@ -119,7 +120,7 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_layer_workspace_bytes", "ts_pack_gate_up", "ts_layer_create", "ts_layer_destroy", "ts_layer_step",
            "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan", "ts_cache8_value_bytes",
            "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
-           "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project",
+           "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project", "ts_adapter_packed_bytes", "ts_adapter_pack",
            "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted",
            "ts_verify_tokens", "ts_request_fork", "ts_requests_free", "ts_copy_pages", "ts_compact_pages", "ts_block_tables"]
 
@@ -208,8 +209,10 @@ def lib() -> ctypes.CDLL:
         L.ts_cache_read.argtypes = [vp, stepp, ctypes.c_int32, vp, vp, vp]
         L.ts_token_logprobs.argtypes = [ctypes.POINTER(ts_logprobs), vp]
         adp, i32 = ctypes.POINTER(ts_adapters), ctypes.c_int32
-        L.ts_adapter_workspace_bytes.restype = L.ts_layer_adapters_workspace_bytes.restype = ctypes.c_size_t
+        L.ts_adapter_workspace_bytes.restype = L.ts_adapter_packed_bytes.restype = L.ts_layer_adapters_workspace_bytes.restype = ctypes.c_size_t
         L.ts_adapter_workspace_bytes.argtypes = [i32] * 4
+        L.ts_adapter_packed_bytes.argtypes = [i32] * 3
+        L.ts_adapter_pack.argtypes = [vp, i32, i32, i32, i32, vp, vp]
         L.ts_adapter_project.argtypes = [i32] * 4 + [vp] * 4 + [adp, i32, _i32p, _i32p, vp, ctypes.c_size_t, i32, vp, vp]
         L.ts_layer_adapters_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
@@ -534,6 +537,14 @@ def ts_token_logprobs(args: ts_logprobs, stream: int) -> int:
 # --------------------------------------------------------------------------- adapters of the requests of a step
 def ts_adapter_workspace_bytes(n_tokens: int, n_rows: int, n_adapters: int, rank: int) -> int:
     return lib().ts_adapter_workspace_bytes(n_tokens, n_rows, n_adapters, rank)
+
+
+def ts_adapter_packed_bytes(n_adapters: int, N: int, rank: int) -> int:
+    return lib().ts_adapter_packed_bytes(n_adapters, N, rank)
+
+
+def ts_adapter_pack(b: int, n_adapters: int, N: int, rank: int, order: int, packed: int, stream: int) -> int:
+    return lib().ts_adapter_pack(b, n_adapters, N, rank, order, packed, stream)
 
 
 def ts_adapter_project(device: int, M: int, N: int, K: int, x: int, W: int, R: int, C: int, adapters: ts_adapters, n_rows: int, row_tokens,

@@ -2,11 +2,13 @@
 // an adapter a, rounded to bf16 and laid out as the GEMM kernels read it (AdapterTiles): an entry per tile of tokens and adapter,
 // zeros in the rows of other adapters' tokens. The second half, u . B_a^T, is part of the projection itself (ts_gemm.cu).
 //
-// A thread block takes up to 16 tokens of an entry and one granule (16, 32 or 64) of the rank: 16 x width sums over K with mma.sync
-// (m16n8k16, fp32), eight warps and, where there are few of these, a cluster of up to eight blocks sharing K. Nothing is staged:
-// a sum over K may take its elements in any order as long as x and A agree, so a lane loads 16 bytes of a row of x and of the rows of A
-// and these are the operands of two MMAs. In a decode batch a block reads A_a (its only user), so that the launch is bound by the bytes of the
-// adapters in use; in a prompt's chunk x and A come from L2, each A once per 16 tokens.
+// A thread block takes up to 16 or 64 tokens of an entry and one granule (16, 32 or 64) of the rank, and, where there are few of these blocks, a cluster
+// of up to eight shares K. Rows of x (gathered) and of A go through a ring of stages in shared memory by 16-byte asynchronous copies to
+// mma.sync (m16n8k16, fp32); a warp has 16 tokens, or a share of each stage's K. In a decode batch a block reads A_a (its only
+// user), so that the launch is bound by the bytes of the adapters in use; in a prompt's chunk x and A come from L2, each A once per 64 tokens.
+// The launch runs next to the product behind it, whose main loop does not need u: a block is small enough (128 threads, 56 KB) to share an SM
+// with one of the product's, and there is one per SM where that is enough. Blocks of 256 threads with 64 to 96 KB of copies under way were faster by
+// themselves, but the product waited for them: MEASURED.
 // The partial sums are added up in a fixed order (warps, then blocks): equal calls give equal bits.
 #include <cuda_bf16.h>
 
@@ -20,8 +22,9 @@
 namespace ts {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kGroup = 16;                      // tokens of a thread block
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kRingBytes = 56 * 1024;           // next to 162 KB of a GEMM kernel's stages
+constexpr int kGroup = 64;                      // most tokens of a thread block
 constexpr int kMaxCluster = 8;
 
 template <int W>
@@ -44,106 +47,195 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
-// WIDTH: ranks of a granule. U: steps of 32 of K whose loads a warp has in flight.
-template <int WIDTH, int U, int W>
-__global__ void __launch_bounds__(kThreads) adapter_down_kernel(const __grid_constant__ DownParams<W> p, const int split) {
-  constexpr int NT = WIDTH / 8;
-  __shared__ float part[kWarps][kGroup][WIDTH + 2];
-  __shared__ float sums[kGroup * WIDTH];
-  __shared__ int16_t member[kGroup];            // places in the tile of the block's tokens
+// WIDTH: ranks of a granule. MT: sixteens of tokens of a block.
+template <int WIDTH, int MT>
+struct Down {
+  static constexpr int kTokens = 16 * MT, kParts = kWarps / MT;      // of a stage's K, a warp each
+  static constexpr int kDepth = MT == 1 && WIDTH < 64 ? 128 : 64;     // K of a stage
+  static constexpr int kChunks = kDepth / 8;                         // of 16 bytes in a row
+  static constexpr int kStageBytes = (kTokens + WIDTH) * kDepth * 2;
+  static constexpr int kStages = kRingBytes / kStageBytes < 8 ? kRingBytes / kStageBytes : 8;
+  static constexpr int kSteps = kDepth / 16 / kParts;                // sixteens of K of a warp and stage
+  static constexpr int kPartBytes = kParts * kTokens * (WIDTH + 2) * 4;
+  static constexpr int kBytes = kStages * kStageBytes > kPartBytes ? kStages * kStageBytes : kPartBytes;
+  static_assert(kStages >= 2 && kSteps >= 1, "a stage is read while another one is filled");
+  // Place of a 16-byte chunk of a row, such that eight rows' chunks lie in different banks.
+  static __device__ __forceinline__ uint32_t place(int stage, int row, int chunk) {
+    return (uint32_t)(stage % kStages * kStageBytes + row * kDepth * 2 + ((chunk ^ (row & 7)) << 4));
+  }
+};
+
+template <int WIDTH, int MT, int W>
+__global__ void __launch_bounds__(kThreads, 5) adapter_down_kernel(const __grid_constant__ DownParams<W> p, const int split) {
+  using D = Down<WIDTH, MT>;
+  constexpr int NT = WIDTH / 8, kTokens = D::kTokens, kPitch = WIDTH + 2;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ int32_t token_of[kTokens], entry_of[kTokens];   // the block's tokens and their entries
+  float* const part = reinterpret_cast<float*>(smem);      // [kParts][kTokens][kPitch], when the stages are done with
   const AdapterDown& d = p.d;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  pdl_launch_dependents();
-  const int32_t* entry_adapter = p.words + d.o_adapter;
-  const int32_t* item_first = p.words + d.o_item;
+  const int32_t* const words = p.words;
   const int item = blockIdx.x / split, rank_of = blockIdx.x % split;   // the cluster's blocks are consecutive
-  const int c = item % d.granules, group_at = item / d.granules;
-  int e = 0;                                    // the entry: last one whose first group is <= group_at
-  for (int hi = d.n_entries; hi - e > 1;) {
-    const int mid = (e + hi) >> 1;
-    if (item_first[mid] <= group_at) e = mid; else hi = mid;
+  const int c = item % d.granules, group = item / d.granules;
+  const uint32_t what = (uint32_t)words[d.o_item + 2 * group], where = (uint32_t)words[d.o_item + 2 * group + 1];
+  const int adapter = what & 0xffff, n = what >> 16;                   // tokens of the group
+  const uint32_t base = smem_u32(smem);
+  const int stages = (d.K + D::kDepth - 1) / D::kDepth, first = stages * rank_of / split, end = stages * (rank_of + 1) / split;
+  const uint16_t* const a = d.a + ((size_t)adapter * d.rank + c * WIDTH) * d.K;
+  const int ranks = min(WIDTH, d.rank - c * WIDTH);
+  // 16-byte chunks of a stage's rows of A, or of x; what is not there is zero
+  auto copy_a = [&](int stage) {
+#pragma unroll
+    for (int i = tid; i < WIDTH * D::kChunks; i += kThreads) {
+      const int row = i / D::kChunks, ch = i % D::kChunks, k = stage * D::kDepth + ch * 8;
+      const bool in = row < ranks && k < d.K;
+      cp_async16(base + D::place(stage, kTokens + row, ch), in ? a + (size_t)row * d.K + k : a, in ? 16 : 0);
+    }
+  };
+#pragma unroll 1
+  for (int s = first; s < min(end, first + D::kStages); ++s) copy_a(s);      // the adapters are not the launch in front's: they fly while it ends
+
+  for (int got = 0, run = where & 0xffff, skip = where >> 16; got < n; ++run, skip = 0) {      // the group's tokens
+    const uint32_t place = (uint32_t)words[d.o_run + 2 * run];
+    const int t0 = place & 0xffff, len = min((int)(place >> 16) - skip, n - got), e = words[d.o_run + 2 * run + 1];
+    for (int k = tid; k < len; k += kThreads) {
+      token_of[got + k] = t0 + skip + k;
+      entry_of[got + k] = e;
+    }
+    got += len;
   }
-  const int group = group_at - item_first[e];
-  const int adapter = entry_adapter[e], t0 = p.words[d.o_tile + e] * d.rows;
-  // this thread's place in the tile: its number among the entry's tokens, or -1
-  int mine = -1, count = 0;
-  for (int s = p.words[d.o_seg_first + e]; s < p.words[d.o_seg_first + e + 1]; ++s) {
-    const int from = p.words[d.o_seg + s] & 0xffff, len = p.words[d.o_seg + s] >> 16;
-    if (tid >= from && tid < from + len) mine = count + tid - from;
-    count += len;
-  }
-  if (mine >= group * kGroup && mine < (group + 1) * kGroup) member[mine - group * kGroup] = (int16_t)tid;
-  const int n = min(kGroup, count - group * kGroup);
   __syncthreads();
   pdl_wait();                                   // x comes from the launch in front; the one before may still read u and the plan
-  if (blockIdx.x == 0)
-    for (int i = tid; i <= d.n_tiles + d.n_entries; i += kThreads) d.plan[i] = p.words[i];
-  uint16_t* const u = d.u + (size_t)(e * d.granules + c) * d.rows * WIDTH;
-  if (group == 0 && rank_of == 0 && mine < 0 && tid < d.rows) {
+  // The product behind this launch may start: what was before is done, which is all that its main loop reads.
+  pdl_launch_dependents();
+  auto copy_x = [&](int stage) {
 #pragma unroll
-    for (int i = 0; i < WIDTH / 8; ++i) reinterpret_cast<uint4*>(u + (size_t)tid * WIDTH)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kTokens * D::kChunks; i += kThreads) {
+      const int row = i / D::kChunks, ch = i % D::kChunks, k = stage * D::kDepth + ch * 8;
+      const bool in = row < n && k < d.K;
+      cp_async16(base + D::place(stage, row, ch), in ? d.x + (size_t)token_of[row] * d.K + k : d.x, in ? 16 : 0);
+    }
+  };
+#pragma unroll 1
+  for (int s = first; s < first + D::kStages; ++s) {
+    if (s < end) copy_x(s);
+    cp_async_commit();                          // a group per stage, the last ones empty
+  }
+  if (blockIdx.x == 0 && d.plan)
+    for (int i = tid; i <= d.n_tiles + d.n_entries; i += kThreads) d.plan[i] = words[i];
+  auto u_of = [&](int entry, int granule) { return reinterpret_cast<char*>(d.u + (size_t)(entry * d.granules + granule) * d.rows * WIDTH); };
+  for (int i = blockIdx.x; i < d.n_entries * d.granules; i += gridDim.x) {      // the rows of other adapters' tokens
+    const int e = i / d.granules;
+    char* const u = u_of(e, i % d.granules);
+    for (int row = tid; row < d.rows; row += kThreads) {
+      bool member = false;
+      for (int s = words[d.o_seg_first + e]; s < words[d.o_seg_first + e + 1]; ++s) {
+        const int k = row - (words[d.o_seg + s] & 0xffff);
+        member = member || (k >= 0 && k < words[d.o_seg + s] >> 16);
+      }
+      if (member) continue;
+#pragma unroll
+      for (int k = 0; k < WIDTH / 8; ++k) *reinterpret_cast<uint4*>(u + granule_place(WIDTH, row, k)) = make_uint4(0, 0, 0, 0);
+    }
   }
 
-  const int g = lane >> 2, t = lane & 3;
-  const int chunks = (d.K + 31) / 32, first = chunks * rank_of / split, end = chunks * (rank_of + 1) / split;
-  const uint16_t* x0 = d.x + (size_t)(t0 + (g < n ? member[g] : 0)) * d.K;
-  const uint16_t* x1 = d.x + (size_t)(t0 + (g + 8 < n ? member[g + 8] : 0)) * d.K;
-  const uint16_t* a0 = d.a + ((size_t)adapter * d.rank + c * WIDTH + g) * d.K;
-  const int ranks = d.rank - c * WIDTH - g;     // row j * 8 of a0 is there where j * 8 < ranks
+  const int g = lane >> 2, t = lane & 3, mt = warp % MT, kp = warp / MT;
   float acc[NT][4] = {};
-  for (int ch = first + warp; ch < end; ch += kWarps * U) {
-    uint4 xa[U][2], w[U][NT];
+#pragma unroll 1
+  for (int s = first; s < end; ++s) {
+    cp_async_wait<D::kStages - 1>();
+    __syncthreads();                            // the stage is there
+    if (mt * 16 < n) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int k = (ch + i * kWarps) * 32 + t * 8;
-      const bool in = ch + i * kWarps < end && k < d.K;
-      xa[i][0] = xa[i][1] = make_uint4(0, 0, 0, 0);
-      if (in && g < n) xa[i][0] = *reinterpret_cast<const uint4*>(x0 + k);
-      if (in && g + 8 < n) xa[i][1] = *reinterpret_cast<const uint4*>(x1 + k);
+      for (int i = 0; i < D::kSteps; ++i) {
+        const int ch = (kp * D::kSteps + i) * 2;
+        uint32_t xa[4];
+        ldmatrix_x4(xa, base + D::place(s, mt * 16 + (lane & 15), ch + (lane >> 4)));
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        w[i][j] = make_uint4(0, 0, 0, 0);
-        if (in && j * 8 < ranks) w[i][j] = *reinterpret_cast<const uint4*>(a0 + (size_t)(j * 8) * d.K + k);
+        for (int j = 0; j < NT; j += 2) {       // sixteen rows of A: lanes 0-7, 8-15 the halves of K of the first eight, 16-31 of the others
+          uint32_t w[4];
+          ldmatrix_x4(w, base + D::place(s, kTokens + j * 8 + (lane & 7) + (lane >> 4) * 8, ch + (lane >> 3 & 1)));
+          mma_bf16(acc[j], xa, w[0], w[1]);
+          mma_bf16(acc[j + 1], xa, w[2], w[3]);
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const uint32_t lo[4] = {xa[i][0].x, xa[i][1].x, xa[i][0].y, xa[i][1].y}, hi[4] = {xa[i][0].z, xa[i][1].z, xa[i][0].w, xa[i][1].w};
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        mma_bf16(acc[j], lo, w[i][j].x, w[i][j].y);
-        mma_bf16(acc[j], hi, w[i][j].z, w[i][j].w);
-      }
+    __syncthreads();                            // and read
+    if (s + D::kStages < end) {
+      copy_a(s + D::kStages);
+      copy_x(s + D::kStages);
     }
+    cp_async_commit();
   }
+  cp_async_wait<0>();
+  __syncthreads();                              // the sums take the stages' place
+  auto at = [&](int k, int row, int col) { return (k * kTokens + row) * kPitch + col; };
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    *reinterpret_cast<float2*>(&part[warp][g][j * 8 + 2 * t]) = make_float2(acc[j][0], acc[j][1]);
-    *reinterpret_cast<float2*>(&part[warp][g + 8][j * 8 + 2 * t]) = make_float2(acc[j][2], acc[j][3]);
+    *reinterpret_cast<float2*>(part + at(kp, mt * 16 + g, j * 8 + 2 * t)) = make_float2(acc[j][0], acc[j][1]);
+    *reinterpret_cast<float2*>(part + at(kp, mt * 16 + g + 8, j * 8 + 2 * t)) = make_float2(acc[j][2], acc[j][3]);
   }
   __syncthreads();
-  for (int i = tid; i < kGroup * WIDTH; i += kThreads) {
+  for (int i = tid; i < n * WIDTH; i += kThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += part[w][i / WIDTH][i % WIDTH];
-    sums[i] = v;
+    for (int k = 0; k < D::kParts; ++k) v += part[at(k, i / WIDTH, i % WIDTH)];
+    part[at(0, i / WIDTH, i % WIDTH)] = v;      // this thread's alone
   }
   const float scale = d.scale ? d.scale[adapter] : 1.f;
   if (split > 1) cluster_sync(); else __syncthreads();
-  const uint32_t at = smem_u32(sums);
   for (int i = (rank_of * kThreads + tid) * 2; i < n * WIDTH; i += split * kThreads * 2) {
-    float lo = 0.f, hi = 0.f;
-    for (int r = 0; r < split; ++r) {
-      const uint32_t from = split > 1 ? mapa(at, r) : at;
-      lo += ld_cluster(from + i * 4);
-      hi += ld_cluster(from + i * 4 + 4);
+    float lo[kMaxCluster], hi[kMaxCluster];
+    const uint32_t own = smem_u32(part + at(0, i / WIDTH, i % WIDTH));
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r) {      // all loads fly at once
+      lo[r] = hi[r] = 0.f;
+      if (r < split) {
+        const uint32_t from = split > 1 ? mapa(own, r) : own;
+        lo[r] = ld_cluster(from);
+        hi[r] = ld_cluster(from + 4);
+      }
     }
-    *reinterpret_cast<uint32_t*>(u + (size_t)member[i / WIDTH] * WIDTH + i % WIDTH) = pack_bf16(lo * scale, hi * scale);
+#pragma unroll
+    for (int r = 1; r < kMaxCluster; ++r) {
+      lo[0] += lo[r];
+      hi[0] += hi[r];
+    }
+    const int col = i % WIDTH, entry = entry_of[i / WIDTH], row = token_of[i / WIDTH] % d.tile;
+    *reinterpret_cast<uint32_t*>(u_of(entry, c) + granule_place(WIDTH, row, col / 8) + (col % 8) * 2) = pack_bf16(lo[0] * scale, hi[0] * scale);
   }
   if (split > 1) cluster_sync();                // no block leaves while another one reads its sums
 }
 
-template <int WIDTH, int U, int W>
+// One thread per 16 bytes of the packed form.
+__global__ void __launch_bounds__(256) adapter_pack_kernel(const uint16_t* __restrict__ b, char* __restrict__ out, int N, int rank, int width, int granules,
+                                                                int blocks, int apart, size_t chunks) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  const int per_row = width / 8, chunk = (int)(i % per_row), r = (int)(i / per_row % 128);
+  const size_t image = i / per_row / 128;       // (adapter, granule, block)
+  const int block = (int)(image % blocks), c = (int)(image / blocks % granules);
+  const size_t adapter = image / blocks / granules;
+  int row = block * 128 + r;
+  if (apart > 0) {                              // sixteen rows and the sixteen `apart` behind them, in turn
+    const int span = 2 * apart, first = block * 128 / span * span, s = block * 128 % span / 32 + r / 32;
+    row = first + (r / 16 % 2) * apart + s * 16 + r % 16;
+  }
+  uint32_t v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int col = c * width + chunk * 8 + k * 2 + h;
+      if (row < N && col < rank) word |= (uint32_t)b[(adapter * N + row) * rank + col] << (16 * h);
+    }
+    v[k] = word;
+  }
+  *reinterpret_cast<uint4*>(out + image * 128 * width * 2 + granule_place(width, r, chunk)) = make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+template <int WIDTH, int MT, int W>
 cudaError_t launch_w(const AdapterDown& d, const int32_t* words, int n_words, int items, int split, cudaStream_t stream) {
   DownParams<W> p;
   p.d = d;
@@ -151,6 +243,12 @@ cudaError_t launch_w(const AdapterDown& d, const int32_t* words, int n_words, in
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * split));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Down<WIDTH, MT>::kBytes;
+  // the SM's memory divided as the product behind this launch needs it: it cannot be divided anew while a block runs
+  const cudaError_t e = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e != cudaSuccess) return e;
+  const cudaError_t e2 = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  if (e2 != cudaSuccess) return e2;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -160,21 +258,28 @@ cudaError_t launch_w(const AdapterDown& d, const int32_t* words, int n_words, in
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, adapter_down_kernel<WIDTH, U, W>, p, split);
+  return cudaLaunchKernelEx(&cfg, adapter_down_kernel<WIDTH, MT, W>, p, split);
 }
-template <int WIDTH, int U>
-cudaError_t launch_t(const AdapterDown& d, const int32_t* words, int n_words, int items, int split, cudaStream_t stream) {
-  return n_words <= kInlineWords ? launch_w<WIDTH, U, kInlineWords>(d, words, n_words, items, split, stream)
-                                 : launch_w<WIDTH, U, kAdapterWords>(d, words, n_words, items, split, stream);
+template <int WIDTH>
+cudaError_t launch_t(const AdapterDown& d, const AdapterPlan& plan, int items, int split, cudaStream_t stream) {
+  const int n = (int)plan.words.size();
+  const int32_t* words = plan.words.data();
+  if (plan.group == 16)
+    return n <= kInlineWords ? launch_w<WIDTH, 1, kInlineWords>(d, words, n, items, split, stream)
+                             : launch_w<WIDTH, 1, kAdapterWords>(d, words, n, items, split, stream);
+  return n <= kInlineWords ? launch_w<WIDTH, 4, kInlineWords>(d, words, n, items, split, stream)
+                           : launch_w<WIDTH, 4, kAdapterWords>(d, words, n, items, split, stream);
 }
 
 }  // namespace
 
 bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int n_adapters, AdapterPlan* out) try {
   struct Run { int entry, from, len; };
-  std::vector<int32_t> tile_first{0}, adapter, tile, groups{0}, seg_first{0}, segs;
+  std::vector<int32_t> tile_first{0}, adapter, seg_first{0}, segs;
   std::vector<Run> runs;                        // of the current tile
   std::vector<int32_t> entry_of((size_t)n_adapters, -1);
+  struct Part { int32_t adapter, token, len, entry; };
+  std::vector<Part> parts;                      // all tiles' runs
   int r = 0, left = n_rows > 0 ? row_tokens[0] : 0;
   for (int t0 = 0; t0 < M; t0 += rows) {
     const int first = (int)adapter.size();
@@ -186,7 +291,6 @@ bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const
         if (entry_of[a] < first) {
           entry_of[a] = (int)adapter.size();
           adapter.push_back(a);
-          tile.push_back(t0 / rows);
         }
         if (!runs.empty() && runs.back().entry == entry_of[a] && runs.back().from + runs.back().len == at) runs.back().len += len;
         else runs.push_back({entry_of[a], at, len});
@@ -197,19 +301,44 @@ bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const
     std::stable_sort(runs.begin(), runs.end(), [](const Run& x, const Run& y) { return x.entry < y.entry; });
     size_t i = 0;
     for (int e = first; e < (int)adapter.size(); ++e) {
-      int tokens = 0;
       for (; i < runs.size() && runs[i].entry == e; ++i) {
+        parts.push_back({adapter[e], t0 + runs[i].from, runs[i].len, e});
         segs.push_back(runs[i].from | runs[i].len << 16);
-        tokens += runs[i].len;
       }
       seg_first.push_back((int32_t)segs.size());
-      groups.push_back(groups.back() + (tokens + kGroup - 1) / kGroup);
     }
     tile_first.push_back((int32_t)adapter.size());
   }
+  std::stable_sort(parts.begin(), parts.end(), [](const Part& x, const Part& y) { return x.adapter < y.adapter; });
+  int64_t all = 0;
+  int used = 0;
+  for (size_t i = 0; i < parts.size(); ++i) {
+    all += parts[i].len;
+    used += i == 0 || parts[i].adapter != parts[i - 1].adapter;
+  }
+  // Blocks of 64 tokens where an adapter has more than 16 on average: each A is then read once per 64, but no warps share a stage's K.
+  out->group = all > 16 * (int64_t)used ? kGroup : 16;
+  std::vector<int32_t> items, run;
+  int room = 0;                                 // left in the last item
+  for (size_t i = 0; i < parts.size(); ++i) {
+    if (i > 0 && parts[i].adapter != parts[i - 1].adapter) room = 0;
+    for (int skip = 0; skip < parts[i].len;) {
+      if (room == 0) {
+        items.push_back(parts[i].adapter);
+        items.push_back((int32_t)i | skip << 16);
+        room = out->group;
+      }
+      const int take = std::min(room, parts[i].len - skip);
+      items[items.size() - 2] += take << 16;
+      skip += take;
+      room -= take;
+    }
+    run.push_back(parts[i].token | parts[i].len << 16);
+    run.push_back(parts[i].entry);
+  }
   out->n_tiles = (int)tile_first.size() - 1;
   out->n_entries = (int)adapter.size();
-  out->n_groups = groups.back();
+  out->n_groups = (int)items.size() / 2;
   out->words.clear();
   auto put = [&](const std::vector<int32_t>& v) {
     const uint32_t at = (uint32_t)out->words.size();
@@ -218,30 +347,37 @@ bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const
   };
   put(tile_first);
   out->o_adapter = put(adapter);
-  out->o_tile = put(tile);
-  out->o_item = put(groups);
   out->o_seg_first = put(seg_first);
   out->o_seg = put(segs);
+  out->o_item = put(items);
+  out->o_run = put(run);
   return out->words.size() <= (size_t)kAdapterWords;
 } catch (const std::bad_alloc&) {
   return false;
 }
 
-cudaError_t launch_adapter_down(AdapterDown d, const AdapterPlan& plan, int width, int n_sms, cudaStream_t stream) {
+cudaError_t launch_adapter_down(AdapterDown d, const AdapterPlan& plan, int tile, int width, int n_sms, cudaStream_t stream) {
   if (plan.n_entries == 0) return cudaSuccess;
   d.n_tiles = plan.n_tiles;
   d.n_entries = plan.n_entries;
   d.granules = (d.rank + width - 1) / width;
-  d.o_adapter = plan.o_adapter; d.o_tile = plan.o_tile; d.o_item = plan.o_item; d.o_seg_first = plan.o_seg_first; d.o_seg = plan.o_seg;
+  d.tile = tile;
+  d.o_seg_first = plan.o_seg_first; d.o_seg = plan.o_seg; d.o_item = plan.o_item; d.o_run = plan.o_run;
   const int items = plan.n_groups * d.granules;
-  // two blocks per SM, each with a step of 32 of K for every warp at least
-  const int split = std::max(1, std::min({kMaxCluster, 2 * n_sms / items, (d.K + 32 * kWarps - 1) / (32 * kWarps)}));
-  const int n = (int)plan.words.size();
+  // a block per SM, each with a few stages at least
+  const int split = std::max(1, std::min({kMaxCluster, n_sms / items, (d.K + 255) / 256}));
   switch (width) {
-    case 16: return launch_t<16, 4>(d, plan.words.data(), n, items, split, stream);
-    case 32: return launch_t<32, 4>(d, plan.words.data(), n, items, split, stream);
-    default: return launch_t<64, 2>(d, plan.words.data(), n, items, split, stream);
+    case 16: return launch_t<16>(d, plan, items, split, stream);
+    case 32: return launch_t<32>(d, plan, items, split, stream);
+    default: return launch_t<64>(d, plan, items, split, stream);
   }
+}
+
+cudaError_t launch_adapter_pack(const uint16_t* b, uint16_t* out, int n_adapters, int N, int rank, int width, int apart, cudaStream_t stream) {
+  const int granules = (rank + width - 1) / width, blocks = (N + 127) / 128;
+  const size_t chunks = (size_t)n_adapters * granules * blocks * 128 * (width / 8);
+  adapter_pack_kernel<<<(unsigned)((chunks + 255) / 256), 256, 0, stream>>>(b, (char*)out, N, rank, width, granules, blocks, apart, chunks);
+  return cudaGetLastError();
 }
 
 }  // namespace ts

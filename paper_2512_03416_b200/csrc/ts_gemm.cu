@@ -124,21 +124,27 @@ __device__ __forceinline__ void silu_mul8(float* gate, const float* up) {
 // columns as the weights' side and, as the tokens' side, u with zeros in the rows of other adapters' tokens: a row of zeros
 // adds nothing, whatever epilogue follows sees one sum in fp32, and B_a is read once per tile. A "granule" is `width` (16, 32 or 64) of
 // an adapter's rank; a stage holds 64 / width of them, each with the swizzle of its width, so that a rank of 16 moves a quarter of the
-// bytes that a padded K block would.
+// bytes that a padded K block would. Both sides lie in memory as they have to lie in shared memory, so that a copy is runs of 256 bytes: as tensor
+// copies of rows of 32 bytes, of which the copy engine does one in two cycles, 64 adapters of rank 16 took 16 us of a product of 15.
+// The launch in front is the one that makes u, and it starts this one only when everything before it is done: the main loop does not wait for it,
+// only the granules do. The launch behind is told to start at the end: its blocks, small ones, would otherwise be put on the SMs that this grid leaves free,
+// several on each (192 tokens, 48 adapters of rank 32: 94 us instead of 66).
 template <bool ADAPT>
 struct AdapterParams {};
 template <>
 struct AdapterParams<true> {
   AdapterTiles t;
-  CUtensorMap u, b;        // u: (width, row), box of width x the rows a thread block loads; b: see GemmMaps
+  CUtensorMap u, b;        // runs of 128 values: a granule's tokens, a granule's 128 weight rows
 };
 // The granules of a tile: numbers first .. first + count - 1 of all granules.
 struct Granules {
   int first, count;
 };
+__device__ __forceinline__ int tile_word(const AdapterTiles& t, int i) { return t.n_inline > 0 ? t.words[i] : t.plan[i]; }
 __device__ __forceinline__ Granules granules_of(const AdapterTiles& t, int tile) {
-  const int first = t.tile_first[tile];
-  return Granules{first * t.granules, (t.tile_first[tile + 1] - first) * t.granules};
+  if (t.n_inline == 0) pdl_wait();         // the plan too is the launch in front's
+  const int first = tile_word(t, tile);
+  return Granules{first * t.granules, (tile_word(t, tile + 1) - first) * t.granules};
 }
 // K blocks that `count` granules take
 __device__ __forceinline__ int granule_blocks(const AdapterTiles& t, int count) { return (count * t.width + kBK - 1) / kBK; }
@@ -151,12 +157,32 @@ __device__ __forceinline__ uint64_t granule_desc(uint32_t addr, int width) {
   d |= (uint64_t)(width == 64 ? 2 : width == 32 ? 4 : 6) << 61;   // 128-, 64-, 32-byte swizzle
   return d;
 }
-// Calls load(granule, its place in the stage) for the granules of K block `block` of those behind x and W; returns how many.
-template <typename Load>
-__device__ __forceinline__ int for_granules(const AdapterTiles& t, Granules gr, int block, Load&& load) {
-  const int per = kBK / t.width, n = min(per, gr.count - block * per);
-  for (int j = 0; j < n; ++j) load(gr.first + block * per + j, j);
-  return n;
+// Runs of the tensor maps: where granule n's tokens begin, and rows 128 * block .. of its adapter's B (the former's are next to them).
+__device__ __forceinline__ int u_run(const AdapterTiles& t, int n) { return n * (t.rows * t.width / 128); }
+__device__ __forceinline__ int b_run(const AdapterTiles& t, int n, int block) {
+  const int entry = n / t.granules, c = n - entry * t.granules;
+  return ((tile_word(t, t.n_tiles + 1 + entry) * t.granules + c) * t.blocks + block) * t.width;
+}
+// Granules in K block `block` of those behind x and W
+__device__ __forceinline__ int granules_in(const AdapterTiles& t, Granules gr, int block) { return min(kBK / t.width, gr.count - block * (kBK / t.width)); }
+// The producer warp's part of K blocks e0 .. e1 - 1 of those: begin(block) on lane 0 makes room for a block and tells its barrier, copy(block, place in
+// the stage, run of u, run of b) starts a granule's copies, on a lane of its own. Where they lie is found for 32 granules at a time: one after the other on one
+// lane, a granule took 400 cycles.
+template <typename Begin, typename Copy>
+__device__ __forceinline__ void copy_granules(const AdapterTiles& t, Granules gr, int e0, int e1, int b_block, int lane, Begin&& begin, Copy&& copy) {
+  const int per = kBK / t.width, at_once = 32 / per;
+  for (int first = e0; first < e1; first += at_once) {
+    const int block = first + lane / per, k = block * per + lane % per;
+    const bool mine = block < e1 && k < gr.count;
+    const int u = mine ? u_run(t, gr.first + k) : 0, b = mine ? b_run(t, gr.first + k, b_block) : 0;
+    for (int e = first; e < min(e1, first + at_once); ++e) {
+      bool go = true;
+      if (lane == 0) go = begin(e);
+      go = __shfl_sync(0xffffffffu, go, 0);
+      if (go && mine && block == e) copy(e, lane % per, u, b);
+      __syncwarp();
+    }
+  }
 }
 
 // Epilogue of one accumulator (TMEM lanes = 128 rows, 256 columns): half `hf` of this thread's row of
@@ -268,7 +294,7 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  pdl_launch_dependents();
+  if (!ADAPT) pdl_launch_dependents();
   // barriers: full[kStages], empty[kStages], acc_full[2], acc_empty[2]
   auto bar = [&](int i) { return base + kOffBar + (uint32_t)i * 8u; };
   const int BAR_FULL = 0, BAR_EMPTY = kStages, BAR_ACC_FULL = 2 * kStages, BAR_ACC_EMPTY = 2 * kStages + 2;
@@ -300,14 +326,17 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
 
   if (warp == 0) {
     // ---------------------------------------------------------------------- TMA producer
-    if (lane == 0) {
-      tma_prefetch_desc(&a_map);
-      tma_prefetch_desc(&b_map);
-      pdl_wait();                  // the activations come from the kernel in front of this one
+    if (ADAPT || lane == 0) {
+      if (lane == 0) {
+        tma_prefetch_desc(&a_map);
+        tma_prefetch_desc(&b_map);
+      }
+      if (!ADAPT) pdl_wait();      // the activations come from the kernel in front of this one
       int it = 0;                                          // K blocks issued so far (ring position)
       for (int t = blockIdx.x; t < n_work; t += gridDim.x) {
         const int m0 = (t % m_tiles) * 128, n0 = (t / m_tiles) * kBN;
         for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+          if (ADAPT && lane > 0) continue;
           const int st = it % kStages;
           if (it >= kStages) wait(BAR_EMPTY + st, ((it / kStages) & 1) ^ 1);
           if (misc[1]) continue;                           // after a failure no new copies are started
@@ -319,26 +348,31 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
         }
         if constexpr (ADAPT) {
           const Granules gr = granules_of(ad.t, t % m_tiles);
-          const int width = ad.t.width, row = width * 2;
-          for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
-            const int st = it % kStages;
-            if (it >= kStages) wait(BAR_EMPTY + st, ((it / kStages) & 1) ^ 1);
-            if (misc[1]) continue;
-            const uint32_t dst = base + st * kStageBytes;
-            mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (128 + kBN) * row);
-            for_granules(ad.t, gr, e, [&](int n, int j) {
-              const int entry = n / ad.t.granules, c = n % ad.t.granules, a = ad.t.entry_adapter[entry];
-              tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, n * ad.t.rows);
-              tma_load_3d(dst + kABytes + j * kBN * row, &ad.b, bar(BAR_FULL + st), c * width, n0, a);
-              tma_load_3d(dst + kABytes + (j * kBN + 128) * row, &ad.b, bar(BAR_FULL + st), c * width, n0 + 128, a);
-            });
-          }
+          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, gr.count);
+          __syncwarp();
+          pdl_wait();
+          copy_granules(ad.t, gr, 0, blocks, n0 / 128, lane,
+                        [&](int e) {
+                          const int st = (it + e) % kStages;
+                          if (it + e >= kStages) wait(BAR_EMPTY + st, (((it + e) / kStages) & 1) ^ 1);
+                          if (misc[1]) return false;
+                          mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (ad.t.rows + kBN) * row);
+                          return true;
+                        },
+                        [&](int e, int j, int u, int b) {    // of an odd last block the second half is no column's
+                          const int st = (it + e) % kStages;
+                          const uint32_t dst = base + st * kStageBytes;
+                          tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, u);
+                          tma_load_2d(dst + kABytes + j * kBN * row, &ad.b, bar(BAR_FULL + st), 0, b);
+                          tma_load_2d(dst + kABytes + (j * kBN + 128) * row, &ad.b, bar(BAR_FULL + st), 0, b + width);
+                        });
+          it += blocks;
         }
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------------ MMA issuer
-    pdl_wait();                    // the time limits of its waits are for this launch, not for what the one in front still has to do
+    if (!ADAPT) pdl_wait();        // the time limits of its waits are for this launch, not for what the one in front still has to do
     const uint32_t issue = elect_one();
     bool dead = false;
     auto iwait = [&](int i, uint32_t parity) {
@@ -374,12 +408,12 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
           iwait(BAR_FULL + st, (it / kStages) & 1);
           tc_fence_after();
           if (dead) continue;
-          for_granules(ad.t, gr, e, [&](int, int j) {
+          for (int j = 0; j < granules_in(ad.t, gr, e); ++j) {
             const uint64_t a_desc = granule_desc(base + st * kStageBytes + j * 128 * width * 2, width);
             const uint64_t b_desc = granule_desc(base + st * kStageBytes + kABytes + j * kBN * width * 2, width);
             for (int ks = 0; ks < width / 16; ++ks)
               mma_ss(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), kIdesc, 1u, issue);
-          });
+          }
           tc_commit(bar(BAR_EMPTY + st), issue);
         }
       }
@@ -389,7 +423,7 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
     // --------------------------------------------------------------------------- epilogue
     const int q = warp & 3, hf = (warp - 2) >> 2;          // the TMEM lanes this warp can reach, its half of the columns
     prefetch_weights(g, ((int)blockIdx.x / m_tiles) * kBN + tid - 64, 0, g.K);
-    pdl_wait();                    // the residual or the positions may come from the kernel in front of this one
+    if (!ADAPT) pdl_wait();        // the residual or the positions may come from the kernel in front of this one
     int n_done = 0;
     for (int t = blockIdx.x; t < n_work; t += gridDim.x, ++n_done) {
       const int m0 = (t % m_tiles) * 128, n0 = (t / m_tiles) * kBN;
@@ -402,6 +436,7 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
       });
     }
   }
+  if (ADAPT) pdl_launch_dependents();
   settle(misc[1] != 0);
   tc_fence_before();
   __syncthreads();
@@ -442,13 +477,6 @@ __device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
       : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
 __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t issue) {
   asm volatile(
       "{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
@@ -468,9 +496,10 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
 
-constexpr int kPairStages = 6, kPairStageBytes = 2 * kABytes;
-constexpr int kPairBars = 2 * kPairStages + 4;
-constexpr int kPairSmem = kPairStages * kPairStageBytes + kPairBars * 8 + 16 + 1024;
+constexpr int kPairStageBytes = 2 * kABytes;
+__host__ __device__ constexpr int pair_stages(bool adapt) { return adapt ? 5 : 6; }          // the launch that makes u has room beside five
+__host__ __device__ constexpr int pair_bars(bool adapt) { return 2 * pair_stages(adapt) + 4; }
+__host__ __device__ constexpr int pair_smem(bool adapt) { return pair_stages(adapt) * kPairStageBytes + pair_bars(adapt) * 8 + 16 + 1024; }
 constexpr uint32_t kIdescPair = (1u << 4) | (1u << 7) | (1u << 10) | ((256u >> 4) << 24);   // M = 256; N is added
 
 // One word of a token's row, read or written where at < n, by a predicate: with a branch around each, the sixteen
@@ -588,8 +617,8 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = blockIdx.x & 1;                    // in the cluster
-  constexpr int kOffBar = kPairStages * kPairStageBytes, kOffMisc = kOffBar + kPairBars * 8;
-  pdl_launch_dependents();
+  constexpr int kPairStages = pair_stages(ADAPT), kOffBar = kPairStages * kPairStageBytes, kOffMisc = kOffBar + pair_bars(ADAPT) * 8;
+  if (!ADAPT) pdl_launch_dependents();
   auto bar = [&](int i) { return base + kOffBar + (uint32_t)i * 8u; };
   constexpr int BAR_FULL = 0, BAR_EMPTY = kPairStages, BAR_ACC_FULL = 2 * kPairStages, BAR_ACC_EMPTY = 2 * kPairStages + 2;
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + kOffMisc);   // [0] TMEM base, [1] failure flag
@@ -623,15 +652,18 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
   const int k_blocks = (g.K + kBK - 1) / kBK;
 
   if (warp == 0) {
-    if (lane == 0) {
-      tma_prefetch_desc(&x_map);
-      tma_prefetch_desc(&w_map);
-      pdl_wait();
+    if (ADAPT || lane == 0) {
+      if (lane == 0) {
+        tma_prefetch_desc(&x_map);
+        tma_prefetch_desc(&w_map);
+      }
+      if (!ADAPT) pdl_wait();
       const uint32_t bytes = 2u * (kABytes + (uint32_t)nt * (kBK * 2 / 2));
       int it = 0;
       for (int t = first; t < n_work; t += stride) {
         const int m0 = (t % m_tiles) * nt + (int)rank * (nt / 2), nb = t / m_tiles;
         for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+          if (ADAPT && lane > 0) continue;
           const int st = it % kPairStages;
           if (it >= kPairStages) wait(BAR_EMPTY + st, ((it / kPairStages) & 1) ^ 1);
           if (misc[1]) continue;                           // after a failure no new copies are started
@@ -647,33 +679,33 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
         }
         if constexpr (ADAPT) {
           const Granules gr = granules_of(ad.t, t % m_tiles);
-          const int width = ad.t.width, row = width * 2;
-          for (int e = 0; e < granule_blocks(ad.t, gr.count); ++e, ++it) {
-            const int st = it % kPairStages;
-            if (it >= kPairStages) wait(BAR_EMPTY + st, ((it / kPairStages) & 1) ^ 1);
-            if (misc[1]) continue;
-            const uint32_t dst = base + st * kPairStageBytes, full = mapa(bar(BAR_FULL + st), 0);
-            if (rank == 0) mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (2 * 128 + nt) * row);
-            for_granules(ad.t, gr, e, [&](int n, int j) {
-              const int entry = n / ad.t.granules, c = n % ad.t.granules, a = ad.t.entry_adapter[entry];
-              const uint32_t to = dst + j * 128 * row;
-              if (EPI == GEMM_EPI_STORE)
-                tma_load_3d_pair(to, &ad.b, full, c * width, nb * kBN + (int)rank * 128, a);
-              else if (EPI == GEMM_EPI_ROPE)               // the adapters' blocks of rows lie behind one another
-                tma_load_5d_pair(to, &ad.b, full, c * width, 0, 0, 0, a * (g.N / 128) + nb * 2 + (int)rank);
-              else
-                tma_load_5d_pair(to, &ad.b, full, c * width, 0, 0, (int)rank * 4, a * (g.N / 256) + nb);
-              tma_load_2d_pair(dst + kABytes + j * (nt / 2) * row, &ad.u, full, 0, n * nt + (int)rank * (nt / 2));
-            });
-          }
+          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, gr.count);
+          __syncwarp();
+          pdl_wait();
+          copy_granules(ad.t, gr, 0, blocks, nb * 2 + (int)rank, lane,
+                        [&](int e) {
+                          const int st = (it + e) % kPairStages;
+                          if (it + e >= kPairStages) wait(BAR_EMPTY + st, (((it + e) / kPairStages) & 1) ^ 1);
+                          if (misc[1]) return false;
+                          if (rank == 0) mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (2 * 128 + nt) * row);
+                          return true;
+                        },
+                        [&](int e, int j, int u, int b) {
+                          const int st = (it + e) % kPairStages;
+                          const uint32_t dst = base + st * kPairStageBytes, full = mapa(bar(BAR_FULL + st), 0);
+                          tma_load_2d_pair(dst + j * 128 * row, &ad.b, full, 0, b);
+                          tma_load_2d_pair(dst + kABytes + j * (nt / 2) * row, &ad.u, full, 0, u + (int)rank * (nt / 2) * width / 128);
+                        });
+          it += blocks;
         }
       }
       // the commits that free the last stages arrive here too: they must have before this CTA may leave
-      for (int i = max(0, it - kPairStages); i < it; ++i) wait(BAR_EMPTY + i % kPairStages, (i / kPairStages) & 1);
+      for (int i = max(0, it - kPairStages); i < it; ++i)
+        if (!ADAPT || lane == 0) wait(BAR_EMPTY + i % kPairStages, (i / kPairStages) & 1);
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      pdl_wait();                  // as in gemm_kernel
+      if (!ADAPT) pdl_wait();      // as in gemm_kernel
       const uint32_t issue = elect_one();
       bool dead = false;
       auto iwait = [&](int i, uint32_t parity) {
@@ -710,12 +742,12 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
             iwait(BAR_FULL + st, (it / kPairStages) & 1);
             tc_fence_after();
             if (dead) continue;
-            for_granules(ad.t, gr, e, [&](int, int j) {
+            for (int j = 0; j < granules_in(ad.t, gr, e); ++j) {
               const uint64_t a_desc = granule_desc(base + st * kPairStageBytes + j * 128 * width * 2, width);
               const uint64_t b_desc = granule_desc(base + st * kPairStageBytes + kABytes + j * (nt / 2) * width * 2, width);
               for (int ks = 0; ks < width / 16; ++ks)
                 mma_ss_pair(tmem + buf * 256, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), idesc, 1u, issue);
-            });
+            }
             tc_commit_pair(bar(BAR_EMPTY + st), issue);
           }
         }
@@ -724,7 +756,7 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
     }
   } else {
     if (tid - 64 < 128) prefetch_weights(g, (first / m_tiles) * kBN + (int)rank * 128 + tid - 64, 0, g.K);
-    pdl_wait();                    // the residual or the positions may come from the kernel in front of this one
+    if (!ADAPT) pdl_wait();                    // the residual or the positions may come from the kernel in front of this one
     const int q = warp & 3, hf = (warp - 2) >> 2;
     int n_done = 0;
     for (int t = first; t < n_work; t += stride, ++n_done) {
@@ -764,6 +796,7 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
       }
     }
   }
+  if (ADAPT) pdl_launch_dependents();
   settle(misc[1] != 0);
   tc_fence_before();
   __syncwarp();
@@ -790,9 +823,10 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   return v;
 }
 constexpr int kSplitN = 128;
-constexpr int kSplitStages = 6, kSplitStageBytes = kABytes + kBBytes / 2;
-constexpr int kSplitSmem = kSplitStages * kSplitStageBytes + (2 * kSplitStages + 1) * 8 + 16 + 1024;
-static_assert(128 * kSplitN * 4 <= kSplitStages * kSplitStageBytes, "the accumulator image takes the place of the operand stages");
+constexpr int kSplitStageBytes = kABytes + kBBytes / 2;
+__host__ __device__ constexpr int split_stages(bool adapt) { return adapt ? 5 : 6; }         // as pair_stages
+__host__ __device__ constexpr int split_smem(bool adapt) { return split_stages(adapt) * kSplitStageBytes + (2 * split_stages(adapt) + 1) * 8 + 16 + 1024; }
+static_assert(128 * kSplitN * 4 <= split_stages(true) * kSplitStageBytes, "the accumulator image takes the place of the operand stages");
 // 16-byte chunk `c` of row `row` of the accumulator image; the XOR spreads a column of rows over the banks
 __device__ __forceinline__ uint32_t image_off(int row, int c) { return (uint32_t)(row * (kSplitN * 4) + ((c ^ (row & 7)) << 4)); }
 
@@ -804,8 +838,8 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* smem = smem_raw + (base - smem_u32(smem_raw));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kOffBar = kSplitStages * kSplitStageBytes;
-  pdl_launch_dependents();
+  constexpr int kSplitStages = split_stages(ADAPT), kOffBar = kSplitStages * kSplitStageBytes;
+  if (!ADAPT) pdl_launch_dependents();
   // barriers: full[kSplitStages], empty[kSplitStages], accumulator full
   auto bar = [&](int i) { return base + kOffBar + (uint32_t)i * 8u; };
   constexpr int BAR_FULL = 0, BAR_EMPTY = kSplitStages, BAR_ACC = 2 * kSplitStages;
@@ -857,14 +891,17 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
     tma_prefetch_desc(&a_map);
     tma_prefetch_desc(&b_map);
   }
-  pdl_wait();                      // the activations, the residual and the positions come from the launches in front
+  if (!ADAPT) pdl_wait();          // the activations, the residual and the positions come from the launches in front
   Granules gr = {0, 0};
-  if constexpr (ADAPT) {           // the granules' K blocks are shared out behind those of x and W
+  // Every block of the cluster has its share of the granules' K blocks behind its share of those of x and W: they wait for u in the end.
+  int e0 = 0, e1 = 0;
+  if constexpr (ADAPT) {
     gr = granules_of(ad.t, t % m_tiles);
-    const int all = k_blocks + granule_blocks(ad.t, gr.count);
-    kb0 = all * rank / split;
-    kb1 = all * (rank + 1) / split;
+    const int all = granule_blocks(ad.t, gr.count);
+    e0 = all * rank / split;
+    e1 = all * (rank + 1) / split;
   }
+  const int n_blocks = kb1 - kb0 + e1 - e0;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -873,27 +910,34 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
         if (it >= kSplitStages && !mbar_wait(bar(BAR_EMPTY + st), ((it / kSplitStages) & 1) ^ 1, misc[1] ? 2000 : g.wait_cycles)) give_up();
         if (misc[1]) continue;                             // after a failure no new copies are started
         const uint32_t dst = base + st * kSplitStageBytes;
-        if constexpr (ADAPT) {
-          if (kb >= k_blocks) {
-            const int e = kb - k_blocks, width = ad.t.width, row = width * 2;
-            mbar_expect_tx(bar(BAR_FULL + st), min(kBK / width, gr.count - e * (kBK / width)) * (128 + kSplitN) * row);
-            for_granules(ad.t, gr, e, [&](int n, int j) {
-              const int entry = n / ad.t.granules, c = n % ad.t.granules;
-              tma_load_3d(dst + kABytes + j * kSplitN * row, &ad.b, bar(BAR_FULL + st), c * width, n0, ad.t.entry_adapter[entry]);
-              tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, n * ad.t.rows);
-            });
-            continue;
-          }
-        }
         mbar_expect_tx(bar(BAR_FULL + st), kSplitStageBytes);
         tma_load_2d(dst + kABytes, &b_map, bar(BAR_FULL + st), kb * kBK, n0);
         tma_load_2d(dst, &a_map, bar(BAR_FULL + st), kb * kBK, m0);
       }
     }
+    if constexpr (ADAPT) {
+      const int row = ad.t.width * 2, it = kb1 - kb0 - e0;
+      __syncwarp();
+      if (e1 > e0) pdl_wait();
+      copy_granules(ad.t, gr, e0, e1, n0 / 128, lane,
+                    [&](int e) {
+                      const int st = (it + e) % kSplitStages;
+                      if (it + e >= kSplitStages && !mbar_wait(bar(BAR_EMPTY + st), (((it + e) / kSplitStages) & 1) ^ 1, misc[1] ? 2000 : g.wait_cycles)) give_up();
+                      if (misc[1]) return false;
+                      mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (ad.t.rows + kSplitN) * row);
+                      return true;
+                    },
+                    [&](int e, int j, int u, int b) {
+                      const int st = (it + e) % kSplitStages;
+                      const uint32_t dst = base + st * kSplitStageBytes;
+                      tma_load_2d(dst + kABytes + j * kSplitN * row, &ad.b, bar(BAR_FULL + st), 0, b);
+                      tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, u);
+                    });
+    }
   } else if (warp == 1) {
     const uint32_t issue = elect_one();
     bool dead = false;
-    for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+    for (int kb = kb0, it = 0; it < n_blocks; ++kb, ++it) {
       const int st = it % kSplitStages;
       if (!mbar_poll(bar(BAR_FULL + st), (it / kSplitStages) & 1, dead ? 2000 : g.wait_cycles)) {
         dead = true;
@@ -902,14 +946,14 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
       tc_fence_after();
       if (dead) continue;
       if constexpr (ADAPT) {
-        if (kb >= k_blocks) {
+        if (kb >= kb1) {
           const int width = ad.t.width;
-          for_granules(ad.t, gr, kb - k_blocks, [&](int, int j) {
+          for (int j = 0; j < granules_in(ad.t, gr, e0 + kb - kb1); ++j) {
             const uint64_t a_desc = granule_desc(base + st * kSplitStageBytes + j * 128 * width * 2, width);
             const uint64_t b_desc = granule_desc(base + st * kSplitStageBytes + kABytes + j * kSplitN * width * 2, width);
             for (int ks = 0; ks < width / 16; ++ks)
               mma_ss(tmem, a_desc + (uint64_t)(ks * 2), b_desc + (uint64_t)(ks * 2), instr_desc(false), (it > 0 || j > 0 || ks > 0) ? 1u : 0u, issue);
-          });
+          }
           tc_commit(bar(BAR_EMPTY + st), issue);
           continue;
         }
@@ -943,6 +987,7 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
       }
     }
   }
+  if (ADAPT) pdl_launch_dependents();
   settle(misc[1] != 0);
   __syncwarp();
   if (warp < 2) fetch(first_item, extra);
@@ -1015,10 +1060,10 @@ cudaError_t launch_cluster(void (*kernel)(Params...), int ctas, int cluster, int
 template <int EPI, bool ADAPT>
 cudaError_t launch_split_t(const GemmArgs& g, const CUtensorMap& a_map, const CUtensorMap& b_map, int split, const AdapterParams<ADAPT>& ad,
                            cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(gemm_split_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+  cudaError_t e = cudaFuncSetAttribute(gemm_split_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, split_smem(ADAPT));
   if (e != cudaSuccess) return e;
   const int tiles = ((g.M + 127) / 128) * ((g.N + kSplitN - 1) / kSplitN);
-  return launch_cluster(gemm_split_kernel<EPI, ADAPT>, tiles * split, split, kSplitSmem, stream, g, a_map, b_map, split, ad);
+  return launch_cluster(gemm_split_kernel<EPI, ADAPT>, tiles * split, split, split_smem(ADAPT), stream, g, a_map, b_map, split, ad);
 }
 
 // CTAs of gemm_split_kernel that the device runs at once in clusters of `split` (a hardware figure;
@@ -1030,11 +1075,11 @@ int split_slots(int split) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
   const int have = known[dev][split].load(std::memory_order_relaxed);
   if (have > 0) return have - 1;
-  if (cudaFuncSetAttribute(gemm_split_kernel<GEMM_EPI_STORE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess) return 0;
+  if (cudaFuncSetAttribute(gemm_split_kernel<GEMM_EPI_STORE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, split_smem(false)) != cudaSuccess) return 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(split);
   cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = kSplitSmem;
+  cfg.dynamicSmemBytes = split_smem(false);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)split;
@@ -1063,10 +1108,10 @@ cudaError_t launch_tile_t(const GemmArgs& g, const CUtensorMap& a_map, const CUt
 template <int EPI, bool ADAPT>
 cudaError_t launch_pair_t(const GemmArgs& g, const CUtensorMap& x_map, const CUtensorMap& w_map, int nt, int n_sms, const AdapterParams<ADAPT>& ad,
                           cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(gemm_pair_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+  cudaError_t e = cudaFuncSetAttribute(gemm_pair_kernel<EPI, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, pair_smem(ADAPT));
   if (e != cudaSuccess) return e;
   const int tiles = ((g.M + nt - 1) / nt) * ((g.N + kBN - 1) / kBN);
-  return launch_cluster(gemm_pair_kernel<EPI, ADAPT>, 2 * std::min(n_sms / 2, tiles), 2, kPairSmem, stream, g, x_map, w_map, nt, ad);
+  return launch_cluster(gemm_pair_kernel<EPI, ADAPT>, 2 * std::min(n_sms / 2, tiles), 2, pair_smem(ADAPT), stream, g, x_map, w_map, nt, ad);
 }
 
 template <int EPI, bool ADAPT>
@@ -1136,7 +1181,7 @@ cudaError_t launch_gemm(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, 
   if (g.M <= 0 || g.N <= 0) return cudaSuccess;
   if (!maps.u) return launch_gemm_t<false>(g, maps, plan, n_sms, AdapterParams<false>{}, stream);
   AdapterParams<true> ad;
-  ad.t = maps.adapters;
+  ad.t = *maps.adapters;
   ad.u = *maps.u;
   ad.b = *maps.b;
   return launch_gemm_t<true>(g, maps, plan, n_sms, ad, stream);

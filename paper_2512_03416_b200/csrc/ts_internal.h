@@ -207,28 +207,41 @@ GemmPlan gemm_plan(const GemmArgs& g, int n_sms);
 // Views of the operands as (K, row). x, w: boxes of 64 x 128. The pair kernel's: x_pair, a box of 64 x
 // pair_tokens / 2; w_pair, for STORE the same as w, else boxes of 64 x 128 whose rows come in the order the epilogue
 // pairs them in (make_paired_map). Those that the plan does not use may be null.
-// u, b: with adapters (AdapterTiles), else null. u: their tokens' side (width, row), a box as high as x's of the plan's kernel; b:
-// their weights' side (rank, row, adapter), a box of width x 128 x 1, or for the pair kernel as w_pair, the adapters' blocks behind one another.
-// The tokens' tiles and their adapters. An entry is an adapter that tokens of a tile use; it has `granules` times `rows` rows of `width` values, the
-// rank's next `width` each, rows of other adapters' tokens zero.
+// The tokens' tiles and their adapters. An entry is an adapter that tokens of a tile use; its tokens' side is `granules` times `rows` rows of `width`
+// values, of the rank's next `width` each, rows of other adapters' tokens zero. The weights' side: per adapter and granule `blocks` times 128
+// rows of `width`. Both swizzled over the width (granule_place).
+constexpr int kInlineTiles = 512;
 struct AdapterTiles {
-  const int32_t* tile_first;      // DEVICE [tiles + 1]: a tile's first entry
-  const int32_t* entry_adapter;   // DEVICE [entries]
-  int32_t width, granules, rows;  // 16, 32 or 64; of an adapter's rank; tokens of a tile
+  const int32_t* plan;            // DEVICE: a tile's first entry [n_tiles + 1], an entry's adapter [entries]; or, n_inline of them, in `words`
+  int32_t n_tiles, width, granules, rows, blocks, n_inline;
+  int32_t words[kInlineTiles];
 };
+// Place, in bytes, of the 16 bytes `chunk` of row `row` among rows of `width` values: the 128-, 64- or 32-byte swizzle.
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline int granule_place(int width, int row, int chunk) {
+  const int at = row * width * 2 + chunk * 16;
+  return at ^ ((at >> 3) & (width * 2 - 16));
+}
+// u, b: with adapters, else null. Both views are runs of 128 values; boxes of what a thread block loads of an entry's granule, and of 128 rows. b of the
+// pair kernel has its rows in w_pair's order.
 struct GemmMaps {
   const CUtensorMap *x, *x_pair, *w, *w_pair;
   const CUtensorMap *u, *b;
-  AdapterTiles adapters;
+  const AdapterTiles* adapters;
 };
 cudaError_t launch_gemm(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, int n_sms, cudaStream_t stream);
-// How the tokens of a call use adapters, for tiles of `rows` tokens: words of tile_first [tiles + 1], entry_adapter [entries] (both also
-// read by the GEMM kernels), entry_tile [entries], item_first [entries + 1] (groups of 16 tokens in front), seg_first [entries + 1], segs (place in the
-// tile | tokens << 16).
+// How the tokens of a call use adapters, for tiles of `rows` tokens: words of
+//   tile_first [tiles + 1], entry_adapter [entries]         (both also read by the GEMM kernels)
+//   seg_first [entries + 1], segs [segments]                an entry's tokens: place in the tile | tokens << 16
+//   items [groups][2]                                       `group` tokens of an adapter, whatever tiles they are in: adapter | tokens << 16, first run |
+//                                                           its tokens that come before << 16
+//   runs [segments][2]                                      by adapter: first token | tokens << 16, entry
 constexpr int kAdapterWords = 7680;
 struct AdapterPlan {
-  int n_tiles, n_entries, n_groups;
-  uint32_t o_adapter, o_tile, o_item, o_seg_first, o_seg;
+  int n_tiles, n_entries, n_groups, group;
+  uint32_t o_adapter, o_seg_first, o_seg, o_item, o_run;
   std::vector<int32_t> words;
 };
 // row_tokens[r] tokens of each row in turn, M in all; row_adapter[r] in [-1, n_adapters). False: more than kAdapterWords.
@@ -236,13 +249,16 @@ bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const
 struct AdapterDown {
   const uint16_t *x, *a;          // [M][K], [adapters][rank][K]
   const float* scale;             // [adapters], or null: 1
-  uint16_t* u;                    // [entries][granules][rows][width]
-  int32_t* plan;                  // tile_first and entry_adapter go here
+  uint16_t* u;                    // [entries][granules][rows][width], see AdapterTiles
+  int32_t* plan;                  // tile_first and entry_adapter go here, or null
   int32_t K, rank, rows;
-  int32_t granules, n_tiles, n_entries;                     // from here on set by the launcher
-  uint32_t o_adapter, o_tile, o_item, o_seg_first, o_seg;
+  int32_t granules, n_tiles, n_entries, tile;               // from here on set by the launcher; tile: tokens of one
+  uint32_t o_seg_first, o_seg, o_item, o_run;
 };
-cudaError_t launch_adapter_down(AdapterDown d, const AdapterPlan& plan, int width, int n_sms, cudaStream_t stream);
+// b [adapters][N][rank] as the GEMM kernels read it: rows and rank padded with zeros. apart: 0, or how far apart the rows lie that the pair kernel's
+// epilogue brings together.
+cudaError_t launch_adapter_pack(const uint16_t* b, uint16_t* out, int n_adapters, int N, int rank, int width, int apart, cudaStream_t stream);
+cudaError_t launch_adapter_down(AdapterDown d, const AdapterPlan& plan, int tile, int width, int n_sms, cudaStream_t stream);
 // out[row] = x[row] / sqrt(mean(x[row]^2) + eps) * gain, bf16 in and out, fp32 inside; width % 8 == 0
 cudaError_t launch_rmsnorm(const uint16_t* x, const uint16_t* gain, uint16_t* out, int rows, int width, float eps,
                            cudaStream_t stream);

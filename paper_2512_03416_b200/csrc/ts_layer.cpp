@@ -56,43 +56,28 @@ bool make_activation_maps(void* encode_fn, const void* ptr, int64_t rows, int64_
 
 // ---- low-rank adapters
 constexpr int kMaxRank = 256, kMaxAdapters = 65536;
-constexpr int kMaxAdapterRows = 1024, kMaxAdapterTokens = 65536;   // their plan fits kAdapterWords
+constexpr int kMaxAdapterRows = 1024, kMaxAdapterTokens = 32768, kManyAdapterRows = 512, kManyAdapterTokens = 8192;
+// their plan fits kAdapterWords: 5 words for each of up to (rows + tiles) segments, 2 for each of (segments, or segments + tokens / 64) groups, 1 per tile
+bool adapter_size_ok(int64_t tokens, int64_t rows) {
+  return rows <= kMaxAdapterRows && tokens <= kMaxAdapterTokens && (rows <= kManyAdapterRows || tokens <= kManyAdapterTokens);
+}
 int granule_width(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
 int padded_rank(int rank) { return (rank + granule_width(rank) - 1) / granule_width(rank) * granule_width(rank); }
-CUtensorMapSwizzle granule_swizzle(int width) {
-  return width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
-}
-bool make_map(void* encode_fn, int dim, const void* ptr, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, int width,
-              CUtensorMap* out) {
-  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return ((EncodeFn)encode_fn)(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)dim, const_cast<void*>(ptr), dims, strides, box, estr,
-                               CU_TENSOR_MAP_INTERLEAVE_NONE, granule_swizzle(width), CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+// Either side of the adapters' part of a product: runs of 128 values, boxes of `runs` of them.
+bool make_runs_map(void* encode_fn, const void* ptr, int64_t values, int runs, CUtensorMap* out) {
+  const cuuint64_t dims[2] = {128, (cuuint64_t)(values / 128)}, strides[1] = {256};
+  const cuuint32_t box[2] = {128, (cuuint32_t)runs}, estr[2] = {1, 1};
+  return ((EncodeFn)encode_fn)(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// The tokens' side of the adapters' part of a product: rows of `width` values.
-bool make_u_map(void* encode_fn, const void* u, int64_t rows, int width, int box_rows, CUtensorMap* out) {
-  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)width * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)width, (cuuint32_t)box_rows};
-  return make_map(encode_fn, 2, u, dims, strides, box, width, out);
-}
-// The weights' side, b [adapters][N][rank]: (rank, row, adapter), what is beyond the rank or the rows reads as zero. apart > 0: as
-// make_paired_map, the adapters' blocks of rows one after the other.
-bool make_b_map(void* encode_fn, const ts_adapters* ad, int64_t N, int apart, CUtensorMap* out) {
-  const int width = granule_width(ad->rank);
-  const cuuint64_t row = (cuuint64_t)ad->rank * 2;
-  if (apart == 0) {
-    const cuuint64_t dims[3] = {(cuuint64_t)ad->rank, (cuuint64_t)N, (cuuint64_t)ad->n_adapters}, strides[2] = {row, row * N};
-    const cuuint32_t box[3] = {(cuuint32_t)width, 128, 1};
-    return make_map(encode_fn, 3, ad->b, dims, strides, box, width, out);
-  }
-  const cuuint64_t dims[5] = {(cuuint64_t)ad->rank, 16, 2, (cuuint64_t)apart / 16, (cuuint64_t)(N / (2 * apart)) * ad->n_adapters};
-  const cuuint64_t strides[4] = {row, row * apart, row * 16, row * 2 * apart};
-  const cuuint32_t box[5] = {(cuuint32_t)width, 16, 2, 4, 1};
-  return make_map(encode_fn, 5, ad->b, dims, strides, box, width, out);
+int64_t packed_values(int64_t n_adapters, int64_t N, int rank) { return n_adapters * padded_rank(rank) * ((N + 127) / 128 * 128); }
+bool make_b_map(void* encode_fn, const void* packed, const ts_adapters* ad, int64_t N, CUtensorMap* out) {
+  return make_runs_map(encode_fn, packed, packed_values(ad->n_adapters, N, ad->rank), granule_width(ad->rank), out);
 }
 bool adapters_ok(const ts_adapters* ad) {
   return ad->n_adapters > 0 && ad->n_adapters <= kMaxAdapters && ad->rank > 0 && ad->rank <= kMaxRank && ad->rank % 8 == 0 && ad->a && ad->b &&
-         !(((uintptr_t)ad->a | (uintptr_t)ad->b) & 15u) && !((uintptr_t)ad->scale & 3u);
+         !((uintptr_t)ad->a & 15u) && !(((uintptr_t)ad->b | (uintptr_t)ad->b_pair) & 127u) && !((uintptr_t)ad->scale & 3u);
 }
 // Bytes for the plan's device words and for u, for tiles of any size: of M tokens of n_rows rows, entries of tiles of nt tokens are no more than
 // rows + tiles, than tiles * adapters, and than tokens.
@@ -100,6 +85,16 @@ size_t adapter_plan_bytes(int64_t M, int64_t n_rows) { return align_up((size_t)(
 size_t adapter_bytes(int64_t M, int64_t n_rows, int64_t n_adapters, int rank) {
   const int64_t rows = std::min(std::min(M * 256, n_rows * 256 + M + 256), (M + 256) * n_adapters);
   return adapter_plan_bytes(M, n_rows) + align_up((size_t)rows * padded_rank(rank) * 2);
+}
+// Rows of a tile as the adapters' part has them: all that a kernel's tile holds, or of a single tile what its tokens need.
+int entry_rows(const ts::GemmPlan& plan, int M) { return plan.pair_tokens > 0 ? plan.pair_tokens : std::min(128, (M + 15) / 16 * 16); }
+void fill_tiles(const ts::AdapterPlan& plan, int rank, int rows, int64_t N, const int32_t* words, ts::AdapterTiles* out) {
+  const int width = granule_width(rank), n = plan.n_tiles + 1 + plan.n_entries;
+  out->plan = words;
+  out->n_tiles = plan.n_tiles; out->width = width; out->granules = padded_rank(rank) / width; out->rows = rows;
+  out->blocks = (int32_t)((N + 127) / 128);
+  out->n_inline = n <= ts::kInlineTiles ? n : 0;
+  std::memcpy(out->words, plan.words.data(), sizeof(int32_t) * (size_t)out->n_inline);
 }
 bool adapter_rows_ok(int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int32_t n_adapters, int64_t M) {
   int64_t n = 0;
@@ -153,8 +148,7 @@ void layer_layout(const ts_config* c, const ts_layer_config* l, int max_tokens, 
 // A projection's adapters as the layer uses them.
 struct LayerAdapters {
   ts_adapters a = {};                          // n_adapters 0: none
-  CUtensorMap b, b_pair;
-  Activations u;                               // of width granule_width(a.rank)
+  CUtensorMap b, b_pair, u[16];                // u[i]: boxes of 8 (i + 1) tokens of width granule_width(a.rank)
 };
 
 struct ts_layer {
@@ -297,6 +291,9 @@ int ts_layer_attach_adapters(ts_layer* l, const ts_layer_adapters* ad) {
     if (!adapters_ok(a) || (n_adapters && a->n_adapters != n_adapters)) return TS_ERR_INVALID;
     n_adapters = a->n_adapters;
   }
+  const bool paired[4] = {true, false, true, false};       // the pair kernel has these weights' rows in another order
+  for (int i = 0; i < 4; ++i)
+    if (all[i] && paired[i] && !all[i]->b_pair) return TS_ERR_INVALID;
   LayerAdapters made[4];
   size_t total = 0, plan = 0;
   const ts_config* c = l->view.cfg;
@@ -309,16 +306,14 @@ int ts_layer_attach_adapters(ts_layer* l, const ts_layer_adapters* ad) {
     const char* u = (const char*)ad->workspace + plan;
     const int64_t qd = (int64_t)c->n_q_heads * c->head_dim, kvd = (int64_t)c->n_kv_heads * c->head_dim;
     const int64_t out[4] = {qd + 2 * kvd, l->cfg.hidden, 2 * (int64_t)l->cfg.intermediate, l->cfg.hidden};
-    const int apart[4] = {64, 0, 128, 0};
     TSL_CUDA(l, cudaSetDevice(c->device));
     for (int i = 0; i < 4; ++i) {
       if (!all[i]) continue;
       made[i].a = *all[i];
       const int width = granule_width(all[i]->rank);
-      const int64_t rows = (int64_t)((total - plan) / (width * 2));
-      bool ok = make_b_map(l->view.encode_fn, all[i], out[i], 0, &made[i].b) && make_b_map(l->view.encode_fn, all[i], out[i], apart[i], &made[i].b_pair) &&
-                make_u_map(l->view.encode_fn, u, rows, width, 128, &made[i].u.full);
-      for (int k = 0; k < 16; ++k) ok = ok && make_u_map(l->view.encode_fn, u, rows, width, 8 * (k + 1), &made[i].u.pair[k]);
+      bool ok = make_b_map(l->view.encode_fn, all[i]->b, all[i], out[i], &made[i].b) &&
+                make_b_map(l->view.encode_fn, paired[i] ? all[i]->b_pair : all[i]->b, all[i], out[i], &made[i].b_pair);
+      for (int k = 0; k < 16; ++k) ok = ok && make_runs_map(l->view.encode_fn, u, (int64_t)(total - plan) / 2, 8 * (k + 1) * width / 128, &made[i].u[k]);
       if (!ok) return lfail(l, cudaErrorInvalidValue);
     }
   }
@@ -352,7 +347,7 @@ int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_ada
   if (row_adapter) {
     if (!adapter_rows_ok(st->n_rows, st->q_len, row_adapter, l->n_adapters, n)) return TS_ERR_INVALID;
     for (int r = 0; r < st->n_rows; ++r) adapted = adapted || row_adapter[r] >= 0;
-    if (adapted && st->n_rows > kMaxAdapterRows) return TS_ERR_UNSUPPORTED;
+    if (adapted && !adapter_size_ok(n, st->n_rows)) return TS_ERR_UNSUPPORTED;
   }
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   const ts_config* c = l->view.cfg;
@@ -405,24 +400,26 @@ int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_ada
   g.M = N;
   ts::AdapterPlan tiles;
   int tile_rows = 0;                                       // of the plan in `tiles`
+  ts::AdapterTiles at;
   auto project = [&](const Activations& x, const CUtensorMap& w, const CUtensorMap& w_pair, int which, const uint16_t* in) {
     const LayerAdapters& ad = l->adapters[which];
     ts::GemmPlan plan = {};
-    ts::GemmMaps maps = {&x.full, nullptr, &w, &w_pair, nullptr, nullptr, {}};
+    ts::GemmMaps maps = {&x.full, nullptr, &w, &w_pair, nullptr, nullptr, nullptr};
     if (adapted && ad.a.n_adapters) {
       plan = adapter_gemm_plan(g, l->view.n_sms, ad.a.rank, st->n_rows, row_adapter, l->n_adapters);
-      const int rows = plan.pair_tokens > 0 ? plan.pair_tokens : 128;
-      if (rows != tile_rows && !ts::plan_adapters(N, rows, st->n_rows, st->q_len, row_adapter, l->n_adapters, &tiles)) return cudaErrorInvalidValue;
-      tile_rows = rows;
+      const int rows = entry_rows(plan, N), tile = plan.pair_tokens > 0 ? rows : 128;
+      if (tile != tile_rows && !ts::plan_adapters(N, tile, st->n_rows, st->q_len, row_adapter, l->n_adapters, &tiles)) return cudaErrorInvalidValue;
+      tile_rows = tile;
       int32_t* words = (int32_t*)l->adapter_ws;
-      const int width = granule_width(ad.a.rank);
-      const ts::AdapterDown down = {in, (const uint16_t*)ad.a.a, ad.a.scale, (uint16_t*)(l->adapter_ws + l->adapter_plan), words, g.K, ad.a.rank, rows};
+      fill_tiles(tiles, ad.a.rank, rows, g.N, words, &at);
+      const ts::AdapterDown down = {in, (const uint16_t*)ad.a.a, ad.a.scale, (uint16_t*)(l->adapter_ws + l->adapter_plan), at.n_inline ? nullptr : words,
+                                    g.K, ad.a.rank, rows};
       if ((size_t)tiles.n_entries * rows * padded_rank(ad.a.rank) * 2 > l->adapter_total - l->adapter_plan) return cudaErrorInvalidValue;   // never
-      const cudaError_t e = ts::launch_adapter_down(down, tiles, width, l->view.n_sms, stream);
+      const cudaError_t e = ts::launch_adapter_down(down, tiles, tile, at.width, l->view.n_sms, stream);
       if (e != cudaSuccess) return e;
-      maps.adapters = {words, words + tiles.n_tiles + 1, width, padded_rank(ad.a.rank) / width, rows};
+      maps.adapters = &at;
       maps.b = plan.pair_tokens > 0 ? &ad.b_pair : &ad.b;
-      maps.u = plan.pair_tokens > 0 ? &ad.u.pair[plan.pair_tokens / 16 - 1] : &ad.u.full;
+      maps.u = &ad.u[(plan.pair_tokens > 0 ? rows / 2 : rows) / 8 - 1];
     } else {
       plan = ts::gemm_plan(g, l->view.n_sms);
     }
@@ -482,11 +479,11 @@ int ts_gemm_bf16(int32_t device, int32_t M, int32_t N, int32_t K, const void* A,
   if (!make_operand_map(encode_fn, A, M, K, &x) || !make_operand_map(encode_fn, B, N, K, &w) ||
       (plan.pair_tokens > 0 && !make_operand_map(encode_fn, A, M, K, &x_pair, plan.pair_tokens / 2)))
     return TS_ERR_CUDA;
-  return ts::launch_gemm(g, ts::GemmMaps{&x, &x_pair, &w, &w, nullptr, nullptr, {}}, plan, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
+  return ts::launch_gemm(g, ts::GemmMaps{&x, &x_pair, &w, &w, nullptr, nullptr, nullptr}, plan, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
 }
 
 size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank) {
-  if (n_tokens <= 0 || n_tokens > kMaxAdapterTokens || n_rows <= 0 || n_rows > kMaxAdapterRows || n_adapters <= 0 || n_adapters > kMaxAdapters ||
+  if (n_tokens <= 0 || n_rows <= 0 || !adapter_size_ok(n_tokens, n_rows) || n_adapters <= 0 || n_adapters > kMaxAdapters ||
       rank <= 0 || rank > kMaxRank || rank % 8)
     return 0;
   return adapter_bytes(n_tokens, n_rows, n_adapters, rank);
@@ -501,7 +498,7 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
   if (!x || !W || !C || !device_status || !row_tokens || !row_adapter || !workspace) return TS_ERR_INVALID;
   if (((uintptr_t)x | (uintptr_t)W | (uintptr_t)C | (uintptr_t)R) & 15u || ((uintptr_t)workspace & (kAlign - 1))) return TS_ERR_INVALID;
   if (tile_m != 0 && tile_m != 128 && tile_m != 256) return TS_ERR_INVALID;
-  if (n_rows > kMaxAdapterRows || M > kMaxAdapterTokens) return TS_ERR_UNSUPPORTED;
+  if (!adapter_size_ok(M, n_rows)) return TS_ERR_UNSUPPORTED;
   if (!adapter_rows_ok(n_rows, row_tokens, row_adapter, ad->n_adapters, M)) return TS_ERR_INVALID;
   bool adapted = false;
   for (int r = 0; r < n_rows; ++r) adapted = adapted || row_adapter[r] >= 0;
@@ -523,24 +520,40 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
   const ts::GemmPlan plan = tile_m ? ts::GemmPlan{tile_m, 0, tile_m == 256 ? ts::pair_tokens(M, (M + 255) / 256) : 0}
                                    : adapter_gemm_plan(g, n_sms, ad->rank, n_rows, row_adapter, ad->n_adapters);
   const bool pair = plan.pair_tokens > 0;
-  const int rows = pair ? plan.pair_tokens : 128, width = granule_width(ad->rank);
+  const int rows = entry_rows(plan, M);
   ts::AdapterPlan tiles;
-  if (!ts::plan_adapters(M, rows, n_rows, row_tokens, row_adapter, ad->n_adapters, &tiles)) return TS_ERR_UNSUPPORTED;
+  if (!ts::plan_adapters(M, pair ? rows : 128, n_rows, row_tokens, row_adapter, ad->n_adapters, &tiles)) return TS_ERR_UNSUPPORTED;
   const size_t plan_bytes = adapter_plan_bytes(M, n_rows);
   int32_t* words = (int32_t*)workspace;
   uint16_t* u = (uint16_t*)((char*)workspace + plan_bytes);
-  const int granules = padded_rank(ad->rank) / width;
-  const int64_t u_rows = (int64_t)tiles.n_entries * granules * rows;
-  if (plan_bytes + (size_t)u_rows * width * 2 > workspace_bytes) return TS_ERR_WORKSPACE;
+  ts::AdapterTiles at;
+  fill_tiles(tiles, ad->rank, rows, N, words, &at);
+  const int64_t values = (int64_t)tiles.n_entries * rows * padded_rank(ad->rank);
+  if (plan_bytes + (size_t)values * 2 > workspace_bytes) return TS_ERR_WORKSPACE;
   CUtensorMap mx, mw, mu, mb;                              // the maps of the plan's kernel only
   if (!make_operand_map(encode_fn, x, M, K, &mx, pair ? rows / 2 : 128) || !make_operand_map(encode_fn, W, N, K, &mw) ||
-      !make_u_map(encode_fn, u, u_rows, width, pair ? rows / 2 : 128, &mu) || !make_b_map(encode_fn, ad, N, 0, &mb))
+      !make_runs_map(encode_fn, u, values, (pair ? rows / 2 : rows) * at.width / 128, &mu) || !make_b_map(encode_fn, ad->b, ad, N, &mb))
     return TS_ERR_CUDA;
-  const ts::AdapterDown down = {(const uint16_t*)x, (const uint16_t*)ad->a, ad->scale, u, words, K, ad->rank, rows};
+  const ts::AdapterDown down = {(const uint16_t*)x, (const uint16_t*)ad->a, ad->scale, u, at.n_inline ? nullptr : words, K, ad->rank, rows};
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (ts::launch_adapter_down(down, tiles, width, n_sms, stream) != cudaSuccess) return TS_ERR_CUDA;
-  const ts::GemmMaps maps = {&mx, &mx, &mw, &mw, &mu, &mb, {words, words + tiles.n_tiles + 1, width, granules, rows}};
+  if (ts::launch_adapter_down(down, tiles, pair ? rows : 128, at.width, n_sms, stream) != cudaSuccess) return TS_ERR_CUDA;
+  const ts::GemmMaps maps = {&mx, &mx, &mw, &mw, &mu, &mb, &at};
   return ts::launch_gemm(g, maps, plan, n_sms, stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
+}
+
+size_t ts_adapter_packed_bytes(int32_t n_adapters, int32_t N, int32_t rank) {
+  if (n_adapters <= 0 || n_adapters > kMaxAdapters || N <= 0 || rank <= 0 || rank > kMaxRank || rank % 8) return 0;
+  return (size_t)packed_values(n_adapters, N, rank) * 2;
+}
+
+int ts_adapter_pack(const void* b, int32_t n_adapters, int32_t N, int32_t rank, int32_t order, void* packed, void* cuda_stream) {
+  const size_t bytes = ts_adapter_packed_bytes(n_adapters, N, rank);
+  if (bytes == 0 || !b || !packed || ((uintptr_t)b & 1u) || ((uintptr_t)packed & 127u) || order < TS_ROWS_PLAIN || order > TS_ROWS_GATE_UP) return TS_ERR_INVALID;
+  const int apart = order == TS_ROWS_QKV ? 64 : order == TS_ROWS_GATE_UP ? 128 : 0;
+  if (apart && N % (2 * apart)) return TS_ERR_INVALID;
+  if (bytes / 16 / 256 > 0x7fffffffu) return TS_ERR_UNSUPPORTED;
+  return ts::launch_adapter_pack((const uint16_t*)b, (uint16_t*)packed, n_adapters, N, rank, granule_width(rank), apart, (cudaStream_t)cuda_stream) == cudaSuccess
+             ? TS_OK : TS_ERR_CUDA;
 }
 
 int ts_gemm_plan(int32_t device, int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* tile_m, int32_t* split,

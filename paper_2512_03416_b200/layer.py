@@ -50,6 +50,8 @@ class DecoderLayer:
         for name, ad in given.items():
             if ad is not None and ((ad.n, ad.k) != shapes[name] or ad.device != self.dec.device):
                 raise ValueError(f"the adapters of {name} must be of a projection {list(shapes[name])} on {self.dec.device}")
+            if ad is not None and ad.rows != (name if name in ("qkv", "gate_up") else "plain"):
+                raise ValueError(f"the adapters of {name} are laid out for rows={ad.rows!r}")
         args = B.ts_layer_adapters(*[None if ad is None else ctypes.pointer(ad.args) for ad in given.values()], None, 0)
         workspace = None
         if any(ad is not None for ad in given.values()):

@@ -28,12 +28,18 @@ def make(seed, tokens, which, n, k, rank, count, residual=False, scale=True):
     m = sum(tokens)
     a, b = normal(count, rank, k, std=k ** -0.5), normal(count, n, rank, std=rank ** -0.5)
     s = 0.5 + torch.rand(count, generator=gen, device="cuda") if scale else None
-    return normal(m, k), normal(n, k, std=k ** -0.5), Adapters(a, b, s), (normal(m, n) if residual else None)
+    return normal(m, k), normal(n, k, std=k ** -0.5), made(a, b, s), (normal(m, n) if residual else None)
+
+
+def made(a, b, scale=None):
+    ad = Adapters(a, b, scale)
+    ad.given = (a, b, scale)                             # what the definition is taken of
+    return ad
 
 
 def definition(x, w, ad, tokens, which, residual):
     """y in 64 bits and, per element, how far rounding u to bf16 may move it: half a step 2^-9 of every |u| times |B|."""
-    a, b, s = ad.tensors
+    a, b, s = ad.given
     y, slack, at = x.double() @ w.double().T, torch.zeros(x.shape[0], w.shape[0], dtype=torch.float64, device="cuda"), 0
     for t, i in zip(tokens, which):
         if i >= 0:
@@ -90,7 +96,7 @@ def test_foreign_nan_stays_with_its_adapter_and_its_tokens():
     tokens, which = [3, 1, 70, 2], [0, 1, 2, -1]
     x, w, ad, _ = make(4, tokens, which, 384, 512, 16, 3)
     clean = adapted_project(x, w, ad, tokens, which)
-    ad.tensors[0][1].fill_(math.nan)
+    ad.given[0][1].fill_(math.nan)
     x[5] = math.inf
     y = adapted_project(x, w, ad, tokens, which)
     bad = ~torch.isfinite(y.float()).all(1)
@@ -131,8 +137,8 @@ def test_stacked_adapters_are_those_of_the_parts():
     at = 0
     for part in parts:
         n = part[1].shape[1]
-        alone = adapted_project(x, (w / 16)[at:at + n].contiguous(), Adapters(*part), [2, 3], [1, 0])
-        want, slack = definition(x, (w / 16)[at:at + n], Adapters(*part), [2, 3], [1, 0], None)
+        alone = adapted_project(x, (w / 16)[at:at + n].contiguous(), made(*part), [2, 3], [1, 0])
+        want, slack = definition(x, (w / 16)[at:at + n], made(*part), [2, 3], [1, 0], None)
         check(y[:, at:at + n], want, slack, 256, 32)
         check(alone, want, slack, 256, 16)
         at += n
@@ -151,10 +157,24 @@ def test_refusals():
         adapted_project(x, w.float(), ad, [4], [0])
     with pytest.raises(ValueError):
         Adapters(torch.zeros(1, 12, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 256, 12, dtype=torch.bfloat16, device="cuda"))
-    assert B.ts_adapter_workspace_bytes(4, 1, 2, 12) == 0 and B.ts_adapter_workspace_bytes(4, 1025, 2, 8) == 0
+    assert B.ts_adapter_workspace_bytes(4, 1, 2, 12) == 0 and B.ts_adapter_workspace_bytes(4000, 1025, 2, 8) == 0
     need = B.ts_adapter_workspace_bytes(4, 1, 2, 8)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     rc = B.ts_adapter_project(0, 4, 256, 64, x.data_ptr(), w.data_ptr(), 0, w.data_ptr(), ad.args, 1, [4], [0], ws.data_ptr(), need - 1, 0,
                               ad.status.data_ptr(), 0)
     assert rc == B.TS_ERR_WORKSPACE
     assert adapted_project(x[:0], w, ad, [], []).shape == (0, 256)
+
+
+@pytest.mark.parametrize("rows,tokens", [(1024, 1), (512, 64), (300, 27)])
+def test_as_many_rows_as_are_served(rows, tokens):
+    """The longest plans: every row another adapter than its neighbours, or its own."""
+    for which in ([r % 7 - 1 for r in range(rows)], list(range(rows))):
+        count = max(which) + 1
+        x, w, ad, _ = make(rows, [tokens] * rows, which, 128, 64, 8, count)
+        y = adapted_project(x, w, ad, [tokens] * rows, which)
+        want, slack = definition(x, w, ad, [tokens] * rows, which, None)
+        check(y, want, slack, 64, 8)
+        assert int(ad.status.item()) == 0
+    with pytest.raises(TsError):
+        adapted_project(x.new_zeros(9000, 64), w, ad, [9] * 1000, [0] * 1000)

@@ -101,11 +101,11 @@ def test_layer_step_with_adapters_matches_the_oracle(case, only):
     step = (lb.slots, b.q_len.tolist(), b.ctx_len.tolist(), x_in)
     layer.step(*step, outs[0], keep_len=True)
     gpu_scale = torch.from_numpy(scale).cuda()
-    given = {name: Adapters(to_dev(ads[name][0]), to_dev(ads[name][1]), gpu_scale) for name in ("qkv", "o", "down") if name in ads}
+    given = {name: Adapters(to_dev(ads[name][0]), to_dev(ads[name][1]), gpu_scale, "qkv" if name == "qkv" else "plain") for name in ("qkv", "o", "down") if name in ads}
     if "gate" in ads:                                     # adapters of their own: A below each other, B next to zeros
         zeros = np.zeros_like(ads["gate"][1])
         packed = layer.pack_gate_up_adapters(to_dev(np.concatenate([ads["gate"][1], zeros], 2)), to_dev(np.concatenate([zeros, ads["up"][1]], 2)))
-        given["gate_up"] = Adapters(to_dev(np.concatenate([ads["gate"][0], ads["up"][0]], 1)), packed, gpu_scale)
+        given["gate_up"] = Adapters(to_dev(np.concatenate([ads["gate"][0], ads["up"][0]], 1)), packed, gpu_scale, "gate_up")
     layer.set_adapters(**given)
     layer.step(*step, outs[1], keep_len=True)             # attached, not used
     for _ in range(2):

@@ -6,6 +6,8 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2512_03416_b200 import speculative
+from paper_2512_03416_b200.adapters import Adapters
 from paper_2512_03416_b200.speculative import SpeculativeDecoder, main, random_adapters, random_weights
 
 pytestmark = pytest.mark.gpu
@@ -13,11 +15,21 @@ HQ, HKV, D, HIDDEN, VOCAB = 8, 2, 128, 256, 512
 PROMPTS, WHICH = ([3], [5, 6, 7, 8, 9], list(range(100, 141))), (1, -1, 0)
 
 
+class Kept(Adapters):
+    def __init__(self, a, b):
+        super().__init__(a, b)
+        self.given = a, b
+
+
 def made(cache, depth, width, temperature, seed=3, attention=0.5, forks=2):
     if not torch.cuda.is_available():
         pytest.fail("a CUDA device is required")
     w = random_weights(VOCAB, HIDDEN, HQ, HKV, D, seed=7, attention=attention)
-    ads = random_adapters(w, 2, 16, seed=8)
+    speculative.Adapters = Kept
+    try:
+        ads = random_adapters(w, 2, 16, seed=8)
+    finally:
+        speculative.Adapters = Adapters
     sd = SpeculativeDecoder(w, HQ, HKV, D, max_requests=3 * (1 + forks), max_tokens=160, depth=depth, width=width, cache=cache, temperature=temperature,
                             seed=seed, adapters=ads)
     for p, a in zip(PROMPTS, WHICH):
@@ -33,7 +45,7 @@ def logits64(w, ads, which, tokens, first):
     m = [t.double().cpu().numpy() for t in w]
     if which >= 0:
         for i, name in ((1, "q"), (2, "k"), (3, "v"), (4, "o")):
-            a, b, _ = ads[name].tensors
+            a, b = ads[name].given
             m[i] = m[i] + (b[which].double() @ a[which].double()).cpu().numpy()
     x = m[0][tokens]
     q, k, v = ((x @ a.T).reshape(len(tokens), -1, D) for a in m[1:4])

@@ -218,12 +218,11 @@ def lib() -> ctypes.CDLL:
         L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_step_adapted.argtypes = [vp, stepp, _i32p, vp, vp, vp]
         L.ts_verify_tokens.argtypes = [ctypes.POINTER(ts_verify), vp]
-        i64p = ctypes.POINTER(ctypes.c_int64)
-        L.ts_request_fork.argtypes = [vp, _i32p, _i32p, i64p, i32, _i32p, vp]
-        L.ts_requests_free.argtypes = [vp, _i32p, i32]
-        L.ts_copy_pages.argtypes = [vp, _i32p, _i32p, i32, vp]
-        L.ts_compact_pages.argtypes = [vp, i32, _i32p, _i32p, _i32p, vp]
-        L.ts_block_tables.argtypes = [vp, _i32p, i32, _i32p, i32]
+        L.ts_request_fork.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+        L.ts_requests_free.argtypes = [vp, vp, i32]
+        L.ts_copy_pages.argtypes = [vp, vp, vp, i32, vp]
+        L.ts_compact_pages.argtypes = [vp, i32, vp, _i32p, _i32p, vp]
+        L.ts_block_tables.argtypes = [vp, vp, i32, vp, i32]
         L.ts_strerror.restype = ctypes.c_char_p
         L.ts_strerror.argtypes = [ctypes.c_int]
         for name in EXPORTS:
@@ -575,31 +574,28 @@ def ts_verify_tokens(args: ts_verify, stream: int) -> int:
 
 
 # ------------------------------------------------------------- pages shared between requests, copied and moved
-# Arrays are contiguous numpy int32 (req_ids: int64).
-def _i32(a):
-    return None if a is None else a.ctypes.data_as(_i32p)
-
-
+# Arrays are contiguous numpy int32 (req_ids: int64). Their addresses go as numbers: a typed pointer costs 3 us to make.
 def ts_request_fork(ctx, slots, n_tokens, req_ids, slots_out, stream: int) -> int:
     """n_tokens may be None; slots_out is written."""
-    return lib().ts_request_fork(ctx, _i32(slots), _i32(n_tokens), req_ids.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), len(slots), _i32(slots_out), stream)
+    return lib().ts_request_fork(ctx, slots.ctypes.data, None if n_tokens is None else n_tokens.ctypes.data, req_ids.ctypes.data, len(slots),
+                                 slots_out.ctypes.data, stream)
 
 
 def ts_requests_free(ctx, slots) -> int:
-    return lib().ts_requests_free(ctx, _i32(slots), len(slots))
+    return lib().ts_requests_free(ctx, slots.ctypes.data, len(slots))
 
 
 def ts_copy_pages(ctx, src, dst, stream: int) -> int:
-    return lib().ts_copy_pages(ctx, _i32(src), _i32(dst), len(src), stream)
+    return lib().ts_copy_pages(ctx, src.ctypes.data, dst.ctypes.data, len(src), stream)
 
 
 def ts_compact_pages(ctx, max_moves: int, moves_out, stream: int):
     """Returns (code, moves made, one past the last page in use); moves_out [max_moves, 2] is written."""
     n, used = ctypes.c_int32(0), ctypes.c_int32(0)
-    rc = lib().ts_compact_pages(ctx, max_moves, _i32(moves_out), ctypes.byref(n), ctypes.byref(used), stream)
+    rc = lib().ts_compact_pages(ctx, max_moves, moves_out.ctypes.data, ctypes.byref(n), ctypes.byref(used), stream)
     return rc, n.value, used.value
 
 
 def ts_block_tables(ctx, slots, tables_out) -> int:
     """tables_out [len(slots), width] is written."""
-    return lib().ts_block_tables(ctx, _i32(slots), len(slots), _i32(tables_out), tables_out.shape[1])
+    return lib().ts_block_tables(ctx, slots.ctypes.data, len(slots), tables_out.ctypes.data, tables_out.shape[1])

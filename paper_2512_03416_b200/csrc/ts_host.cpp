@@ -333,6 +333,18 @@ int ring_send(ts_ctx* c, RingBuf* r, size_t dst_off, size_t bytes, cudaStream_t 
   return TS_OK;
 }
 
+// How many of the first n numbers are the same, sixteen at a time (which the compiler makes vectors of).
+int common_prefix(const int32_t* a, const int32_t* b, int n) {
+  int k = 0;
+  for (; k + 16 <= n; k += 16) {
+    int32_t differ = 0;
+    for (int i = 0; i < 16; ++i) differ |= a[k + i] ^ b[k + i];
+    if (differ) break;
+  }
+  while (k < n && a[k] == b[k]) ++k;
+  return k;
+}
+
 // Whether n tokens written from position `from` on would change a page that another request's table holds too.
 bool writes_shared(ts_ctx* c, int slot, int from, int n) {
   const int32_t* row = table_row(c, slot);
@@ -1409,7 +1421,23 @@ int ts_requests_free(ts_ctx* c, const int32_t* slots, int32_t n) {
     if (!slot_ok(c, slots[i]) || c->slots[slots[i]].stamp == c->stamp) return TS_ERR_INVALID;
     c->slots[slots[i]].stamp = c->stamp;
   }
-  for (int i = 0; i < n; ++i) ts_request_free(c, slots[i]);
+  // As ts_request_free of one after the other, in whose order pages become free. Neighbours in the list that hold the same first pages (forks of one
+  // request) leave these to the last of them, which frees them in either case: `left` of them have left their first `held` pages to slot i.
+  for (int i = 0, left = 0, held = 0; i < n; ++i) {
+    Slot& s = c->slots[slots[i]];
+    const int32_t* row = table_row(c, slots[i]);
+    int keep = 0;                                          // pages left to the next one
+    if (i + 1 < n) {
+      const int most = std::min(left > 0 ? held : s.n_pages, c->slots[slots[i + 1]].n_pages);
+      keep = common_prefix(row, table_row(c, slots[i + 1]), most);
+    }
+    for (int k = s.n_pages - 1; k >= keep; --k)
+      if ((c->page_uses[row[k]] -= 1 + (k < held ? left : 0)) == 0) c->free_pages.push_back(row[k]);
+    left = keep > 0 ? left + 1 : 0;
+    held = keep;
+    s.n_pages = 0;                                         // what is left of them is the next one's
+    ts_request_free(c, slots[i]);
+  }
   return TS_OK;
 }
 
@@ -1447,8 +1475,13 @@ int ts_request_fork(ts_ctx* c, const int32_t* slots, const int32_t* n_tokens, co
   if ((int64_t)n > (int64_t)c->free_slots.size()) return TS_ERR_NO_SLOT;
   const int rc = copy_page_pairs(c, cuda_stream);
   if (rc != TS_OK) return rc;
-  for (int i = 0; i < n; ++i) {
+  for (int i = 0, counted = 0; i < n; ++i) {
     const int from = slots[i], len = length(i), whole = len / P, slot = c->free_slots.back();
+    const int32_t* parent = table_row(c, from);
+    if (i == counted) {                                    // the uses of forks alike, together
+      while (counted < n && slots[counted] == from && length(counted) == len) ++counted;
+      for (int k = 0; k < whole; ++k) c->page_uses[parent[k]] += counted - i;
+    }
     c->free_slots.pop_back();
     Slot& s = c->slots[slot];
     s = Slot();
@@ -1458,12 +1491,8 @@ int ts_request_fork(ts_ctx* c, const int32_t* slots, const int32_t* n_tokens, co
     s.expected_output_len = c->slots[from].expected_output_len;
     s.n_tokens = len;
     s.n_pages = whole;
-    const int32_t* parent = table_row(c, from);
     int32_t* row = table_row(c, slot);
-    for (int k = 0; k < whole; ++k) {
-      row[k] = parent[k];
-      ++c->page_uses[row[k]];
-    }
+    std::copy_n(parent, whole, row);
     if (len % P) {
       const int32_t p = c->free_pages.back();
       c->free_pages.pop_back();

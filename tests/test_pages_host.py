@@ -159,3 +159,34 @@ def test_counts_hold_over_random_calls(seed):
         used = set().union(*[B.ts_block_table(h, s)[1] for s in live]) if live else set()
         assert B.ts_velocity(h)[1]["pages_in_use"] == len(used)
     B.ts_destroy(h)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_requests_freed_together_leave_what_they_leave_one_by_one(seed):
+    """Forks of forks at any lengths, freed in any order: the free pages come in the same order, so that new requests get the same pages."""
+    tables = []
+    for together in (False, True):
+        rng, h = np.random.default_rng(seed), ctx(n_pages=60, max_requests=40)
+        live = [request(h, 16 * int(rng.integers(1, 9))) for _ in range(3)]
+        for _ in range(12):
+            s = int(rng.choice(live))
+            rc, new = fork(h, [s] * 3, [16 * int(rng.integers(0, B.ts_block_table(h, s)[2] // 16 + 1)) for _ in range(3)])
+            assert rc == B.TS_OK
+            live += new
+            B.ts_alloc_pages(h, new[0], B.ts_block_table(h, new[0])[2] + 16, 0)
+        gone = rng.permutation(live)[:int(rng.integers(5, 30))] if seed % 2 else np.array(live[3:][::-1])
+        gone = gone.astype(np.int32)
+        if together:
+            assert B.ts_requests_free(h, gone) == B.TS_OK
+        else:
+            for s in gone:
+                assert B.ts_request_free(h, int(s)) == B.TS_OK
+        rest = [s for s in live if s not in gone]
+        used = set().union(*[B.ts_block_table(h, s)[1] for s in rest]) if rest else set()
+        assert free_pages(h) == 60 - len(used)
+        new = [request(h, 16 * k) for k in (3, 1, 5)]
+        tables.append([B.ts_block_table(h, s)[1] for s in new] + [new])
+        B.ts_requests_free(h, i32(*rest, *new))
+        assert free_pages(h) == 60
+        B.ts_destroy(h)
+    assert tables[0] == tables[1]

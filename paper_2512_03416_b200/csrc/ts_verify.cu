@@ -71,8 +71,9 @@ __shared__ struct {
   int32_t gone[kNodes];                  // tokens rejected at this node (no draft)
   int32_t token[kNodes], child[kNodes], sibling[kNodes];     // child, sibling: a node's first one, the next of the same parent; -1: none
   float chance[kNodes], scale[kNodes], dscale[kNodes];
-  float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (max, s of the model; of the draft), by turns
+  float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (reference, sum of the model; of the draft), by turns
   float4 part32[kMostWarps];
+  float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference
   int32_t found;
 } sh;
 
@@ -86,6 +87,9 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, double v) {
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};\n" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, int32_t v) {
   asm volatile("st.shared::cluster.s32 [%0], %1;\n" ::"r"(addr), "r"(v) : "memory");
@@ -164,22 +168,26 @@ struct Ring {
   __device__ Ring(const T* r, const T* d, int n, bool b, bool v, unsigned char* all, int warp, int lane)
       : row(r), drow(d), vocab(n), both(b), dvec(v), mine(smem_u32(all) + warp * kBytes + lane * kLane) {}
   __device__ __forceinline__ uint32_t slot(int k, int which) const { return mine + ((k % kRing) * 2 + which) * 32 * kLane; }
-  __device__ __forceinline__ void one(const T* from, int at, bool vec, uint32_t to) const {
-    if (vec && at >= 0 && at + 8 <= vocab) {
+  __device__ __forceinline__ void copy(const T* from, uint32_t to) const {
 #pragma unroll
-      for (int i = 0; i < kLane / 16; ++i) cp_async16(to + 16 * i, from + at + i * (16 / sizeof(T)), 16);
-    } else {                             // the row's ends, rows of another alignment
-      const Raw<T, 8> r = load<8>(from, at, vocab, false);
+    for (int i = 0; i < kLane / 16; ++i) cp_async16(to + 16 * i, from + i * (16 / sizeof(T)), 16);
+  }
+  __device__ __forceinline__ void by_hand(const T* from, int at, uint32_t to) const {      // the row's ends, rows of another alignment
+    const Raw<T, 8> r = load<8>(from, at, vocab, false);
 #pragma unroll
-      for (int i = 0; i < kLane / 16; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(to + 16 * i), "r"(r.w[4 * i]), "r"(r.w[4 * i + 1]), "r"(r.w[4 * i + 2]), "r"(r.w[4 * i + 3]) : "memory");
-    }
+    for (int i = 0; i < kLane / 16; ++i)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(to + 16 * i), "r"(r.w[4 * i]), "r"(r.w[4 * i + 1]), "r"(r.w[4 * i + 2]), "r"(r.w[4 * i + 3]) : "memory");
   }
   // The k-th tile that is asked for, logits from `at` on in this lane. Called for every k in turn, `some` false behind the last one.
   __device__ __forceinline__ void ask(int k, int at, bool some) const {
     if (some) {
-      one(row, at, true, slot(k, 0));
-      if (both) one(drow, at, dvec, slot(k, 1));
+      if (at >= 0 && at + 8 <= vocab && (!both || dvec)) {
+        copy(row + at, slot(k, 0));
+        if (both) copy(drow + at, slot(k, 1));
+      } else {
+        by_hand(row, at, slot(k, 0));
+        if (both) by_hand(drow, at, slot(k, 1));
+      }
     }
     cp_async_commit();
   }
@@ -215,7 +223,7 @@ __device__ __forceinline__ void publish(int n, double (&v)[kValues], int rank, i
 
 // ---- sums in fp32
 // Weights 2^(x c - top), top = ref c rounded, the same for all: it is as if ref were another number nearby. Where it would not be (kHuge), top is a
-// NaN, and weights are 2^((x - ref) c). ref is a logit that moves when weights get large, so that most logits are one fma, one exponential, one sum.
+// NaN, and weights are 2^((x - ref) c).
 struct Sum {
   float ref, top, s;
 };
@@ -232,7 +240,7 @@ __device__ __forceinline__ float moved(const Sum& a, float ref, float top, float
   if (a.ref == -CUDART_INF_F || a.ref == ref) return a.s;                    // nothing, or a NaN
   return a.s * ex2(a.top == a.top && top == top ? a.top - top : (a.ref - ref) * c);
 }
-__device__ __noinline__ Sum add_slow(Sum a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float c) {
+__device__ __noinline__ Sum add(Sum a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float c) {
   const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
   float m = a.ref;
 #pragma unroll
@@ -242,20 +250,6 @@ __device__ __noinline__ Sum add_slow(Sum a, float x0, float x1, float x2, float 
 #pragma unroll
   for (int i = 0; i < 8; ++i) b.s += m != -CUDART_INF_F ? weight(x[i], b, c) : x[i] != x[i] ? x[i] : 0.f;
   return b;
-}
-__device__ __forceinline__ void refer(Sum& a, const float (&x)[8], float c) {      // the first reference
-  a.ref = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) a.ref = fmaxf(a.ref, x[i]);
-  a.top = top_of(a.ref, c);
-}
-__device__ __forceinline__ void add(Sum& a, const float (&x)[8], float c) {
-  float s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c, -a.top));
-  const float sum = s[0] + s[1];
-  if (__builtin_expect(sum < kLarge, 1)) a.s += sum;
-  else a = add_slow(a, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], c);  // large, or no numbers; a huge reference
 }
 // Over groups of 2 * WIDEST lanes.
 template <int WIDEST>
@@ -315,9 +309,9 @@ __device__ __noinline__ double left(float x, float y, int rejected) {
 //   SUMS    values 0, 1: the sums of e^(x scale - top) of the model and of the draft
 //   REST    value 0: what one more rejection leaves
 //   STRIPS  what is left, per strip, and value 0: in all
-//   FIRST   what the first rejection leaves, with e.inv and e.dinv known to 2^-21 only: strips and values 3, 4, 5 of max(p - q, 0), and of
+//   FIRST   what the first rejection leaves, with e.inv and e.dinv known to 2^-19 only: strips and values 3, 4, 5 of max(p - q, 0), and of
 //           e^.. of the model and of the draft where that is not 0, by which it is corrected; values 0, 1 as SUMS; value 2: p + q of tokens whose
-//           p and q are alike to 2^-19, of which it may not be known which is larger
+//           p and q are alike to 2^-18, of which it may not be known which is larger
 // Values are published. find, by one warp: the token at `want` of a strip, or the last one there that has anything.
 enum { SUMS, REST, STRIPS, FIRST };
 template <typename T, bool DRAFT>
@@ -346,18 +340,24 @@ __device__ __noinline__ int find(int rejected, int strip, double want) {
     ring.ask(k + Ring<T>::kRing, (tile + Ring<T>::kRing) * kTile + base, tile + Ring<T>::kRing < end);
     double mine = 0.0;
 #pragma unroll 1
-    for (int i = 0; i < 8; i += 2) {     // short code: it is gone through once or twice, and has to be fetched first
-      float xi = x[0], xj = x[1], yi = y[0], yj = y[1];
+    for (int half = 0; half < 8; half += 4) {       // short code: it is gone through a few times, and has to be fetched first
+      double r[4], q[4];
 #pragma unroll
-      for (int k = 2; k < 8; k += 2) {
-        xi = i == k ? x[k] : xi;
-        xj = i == k ? x[k + 1] : xj;
-        yi = i == k ? y[k] : yi;
-        yj = i == k ? y[k + 1] : yj;
+      for (int i = 0; i < 4; ++i) {
+        r[i] = weight64(half ? x[i + 4] : x[i], sh.e.scale, sh.e.top) * sh.e.inv;
+        q[i] = both ? weight64(half ? y[i + 4] : y[i], sh.e.dscale, sh.e.dtop) * sh.e.dinv : 0.0;
       }
-      const double r = left<DRAFT>(xi, yi, rejected), s = left<DRAFT>(xj, yj, rejected);
-      mine += DRAFT || !given(tile * kTile + base + i) ? r : 0.0;
-      mine += DRAFT || !given(tile * kTile + base + i + 1) ? s : 0.0;
+      if (both) {
+        for (int k = 0; k < rejected; ++k) {
+          const double z = sh.norm[k];
+          if (z > 0.0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = fmax(r[i] - q[i], 0.0) * z;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine += DRAFT || !given(tile * kTile + base + half + i) ? r[i] : 0.0;
     }
     double upto = mine;
 #pragma unroll
@@ -427,8 +427,26 @@ __device__ __noinline__ void pass(int rejected, int to, int rank, int cluster, i
   for (int strip = warp; strip < to; strip += WARPS) {
     const int end = min(tile1, tile0 + (strip + 1) * per);
     double in_strip = 0.0, p_strip = 0.0, q_strip = 0.0;
+    int tile = tile0 + strip * per;
+    if (MODE == STRIPS && !both) {       // without a rejected token in the strip: sums of weights, short code
+      bool plain = true;
+      if (!DRAFT)
+        for (int k = 0; k < rejected; ++k) plain = plain && (unsigned)(sh.gone[k] + sh.row.shift - tile * kTile) >= (unsigned)((end - tile) * kTile);
+      if (plain) {
+        double s[2] = {0.0, 0.0};
 #pragma unroll 1
-    for (int tile = tile0 + strip * per; tile < end; ++tile) {
+        for (; tile < end; ++tile) {
+          float x[8], y[8];
+          ring.get(k_tile++, x, y);
+          ask();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[i & 1] += weight64(x[i], scale, top);
+        }
+        in_strip = (s[0] + s[1]) * inv;
+      }
+    }
+#pragma unroll 1
+    for (; tile < end; ++tile) {
       float x[8], y[8];
       ring.get(k_tile++, x, y);
       ask();
@@ -449,11 +467,12 @@ __device__ __noinline__ void pass(int rejected, int to, int rank, int cluster, i
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const double p = w[i] * inv, d = fma(-q[i], dinv, p);
-              if ((__double2hiint(d) & 0x7fffffff) + (19 << 20) <= __double2hiint(p)) v[2] += 2.0 * p;
-              const int keep = ~(__double2hiint(d) >> 31);
-              in_strip += __hiloint2double(__double2hiint(d) & keep, __double2loint(d) & keep);
-              p_strip += __hiloint2double(__double2hiint(w[i]) & keep, __double2loint(w[i]) & keep);
-              q_strip += __hiloint2double(__double2hiint(q[i]) & keep, __double2loint(q[i]) & keep);
+              if ((__double2hiint(d) & 0x7fffffff) + (18 << 20) <= __double2hiint(p)) v[2] += 2.0 * p;
+              if (d > 0.0) {
+                in_strip += d;
+                p_strip += w[i];
+                q_strip += q[i];
+              }
             }
           }
         } else {
@@ -561,62 +580,143 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
     sh.sibling[tid] = sibling;
   }
   sync_all(cluster);                     // all blocks of the cluster run: they may be written to
-  int cur = 0, emitted = 0, turn = 0;
+  const int shares = 31 - __clz(cluster);            // log2
+  // A node's rows and this block's tiles of them.
+  struct Place {
+    const T *row, *drow;
+    int shift, from, to;
+    bool both, dvec;                     // the draft's row of a node without children is not read
+  };
+  auto place_of = [&](int node) {
+    Place s;
+    s.row = static_cast<const T*>(p.logits) + (int64_t)(first + node) * p.stride;
+    s.drow = DRAFT ? static_cast<const T*>(p.draft) + (int64_t)(first + node) * p.draft_stride : nullptr;
+    s.shift = (int)((reinterpret_cast<uintptr_t>(s.row) & 15) / sizeof(T));
+    s.dvec = DRAFT && (int)((reinterpret_cast<uintptr_t>(s.drow) & 15) / sizeof(T)) == s.shift;
+    s.both = DRAFT && sh.child[node] >= 0;
+    const int tiles = (p.vocab + s.shift + kTile - 1) / kTile;
+    s.from = tiles * rank >> shares;
+    s.to = tiles * (rank + 1) >> shares;
+    return s;
+  };
+  auto ring_of = [&](const Place& s) { return Ring<T>(s.row, s.drow, p.vocab, s.both, s.dvec, copies, warp, lane); };
+  auto ask_first = [&](const Place& s) {
+    const Ring<T> ring = ring_of(s);
+    const int at = (s.from + warp) * kTile + lane * 8 - s.shift;
+#pragma unroll 2
+    for (int k = 0; k < Ring<T>::kRing; ++k) ring.ask(k, at + k * kWarps * kTile, s.from + warp + k * kWarps < s.to);
+  };
+  int cur = 0, emitted = 0, turn = 0, asked = -1;    // asked: the node whose first tiles are on their way
+  float ref = 0.f, dref = 0.f;           // logits of likely tokens: the last accepted one's, where it was accepted
   for (;;) {
-    const int64_t r = first + cur;
     const float scale = sh.scale[cur], dscale = sh.dscale[cur];
     const float c = scale * kLog2e, dc = dscale * kLog2e;
-    const T* const row = static_cast<const T*>(p.logits) + r * p.stride;
-    const T* const drow = DRAFT ? static_cast<const T*>(p.draft) + r * p.draft_stride : nullptr;
-    const int vocab = p.vocab, shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    const bool dvec = DRAFT && (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(T)) == shift;
-    const int tiles = (vocab + shift + kTile - 1) / kTile;
-    const int from = (int)((int64_t)tiles * rank / cluster), to = (int)((int64_t)tiles * (rank + 1) / cluster);
+    const Place here = place_of(cur);
+    const T *const row = here.row, *const drow = here.drow;
+    const int vocab = p.vocab, shift = here.shift, from = here.from, to = here.to;
+    const bool both = here.both, dvec = here.dvec;
+    if (asked != cur) {
+      if (asked >= 0) cp_async_wait<0>();
+      ask_first(here);
+    }
+    asked = -1;
     const int child = sh.child[cur];
-    const bool both = DRAFT && child >= 0;           // the draft's row of a node without children is not read
     // the first child's logits: asked for before the sums
     const float x0 = child >= 0 ? value(row + sh.token[child]) : 0.f, y0 = both ? value(drow + sh.token[child]) : 0.f;
 
-    // the row's sums in fp32
-    Sum a = nothing(), b = nothing();
+    // The row's sums in fp32. All threads first take one reference, a logit that may be far from the row's largest but seldom is: then a logit is a
+    // product, an exponential and a sum, and sums are joined by adding. Where the whole sum says that it was too far, or no number, once more with
+    // references that move.
+    if (emitted == 0) {
+      ref = child >= 0 ? x0 : value(row);
+      dref = y0;
+    }
+    Sum a = {ref, top_of(ref, c), 0.f}, b = {dref, top_of(dref, dc), 0.f};
+    const int base = lane * 8 - shift;
+    auto ask_child = [&]() {             // the first child is the likeliest to be next: its tiles fly while this row's sums are joined
+      if (child < 0) return;
+      ask_first(place_of(child));
+      asked = child;
+    };
     {
-      const Ring<T> ring(row, drow, vocab, both, dvec, copies, warp, lane);
-      const int base = lane * 8 - shift;
-      for (int k = 0; k < Ring<T>::kRing; ++k) ring.ask(k, (from + warp + k * kWarps) * kTile + base, from + warp + k * kWarps < to);
+      const Ring<T> ring = ring_of(here);
+      float s[2] = {0.f, 0.f}, d[2] = {0.f, 0.f};
 #pragma unroll 1
       for (int k = 0, tile = from + warp; tile < to; ++k, tile += kWarps) {
         float x[8], y[8];
         ring.get(k, x, y);
         const int next = tile + Ring<T>::kRing * kWarps;
         ring.ask(k, next * kTile + base, next < to);
-        if (k == 0) {
-          refer(a, x, c);
-          if (both) refer(b, y, dc);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c, -a.top));
+        if (both) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i & 1] += ex2(fmaf(y[i], dc, -b.top));
         }
-        add(a, x, c);
-        if (both) add(b, y, dc);
       }
-      lanes_sum<16>(a, c);
-      if (both) lanes_sum<16>(b, dc);
-      if (lane == 0) sh.part32[warp] = make_float4(a.ref, a.s, b.ref, b.s);
+      ask_child();
+      float sa = s[0] + s[1], sb = d[0] + d[1];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        sa += __shfl_xor_sync(0xffffffffu, sa, o);
+        sb += __shfl_xor_sync(0xffffffffu, sb, o);
+      }
+      if (lane == 0) sh.part_even[warp] = make_float2(sa, sb);
       __syncthreads();
+      sa = sb = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        sa += sh.part_even[w].x;
+        sb += sh.part_even[w].y;
+      }
+      if (cluster > 1) {
+        if (tid < cluster) st_cluster(mapa(smem_u32(&sh.even[turn][rank]), tid), make_float2(sa, sb));
+        cluster_sync();
+        sa = sb = 0.f;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+          if (r < cluster) {
+            sa += sh.even[turn][r].x;
+            sb += sh.even[turn][r].y;
+          }
+        }
+        turn ^= 1;
+      }
+      a.s = sa;
+      b.s = both ? sb : 1.f;
+    }
+    if (__builtin_expect(!(a.s > 1.f / kLarge && a.s < kLarge && b.s > 1.f / kLarge && b.s < kLarge), 0)) {
+      a = b = nothing();
+      cp_async_wait<0>();
+      __syncthreads();
+      ask_first(here);
+      asked = -1;
+      const Ring<T> ring = ring_of(here);
+#pragma unroll 1
+      for (int k = 0, tile = from + warp; tile < to; ++k, tile += kWarps) {
+        float x[8], y[8];
+        ring.get(k, x, y);
+        const int next = tile + Ring<T>::kRing * kWarps;
+        ring.ask(k, next * kTile + base, next < to);
+        a = add(a, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], c);
+        if (both) b = add(b, y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7], dc);
+      }
       auto join = [&](const float4& v, auto widest) {
         a = Sum{v.x, top_of(v.x, c), v.y};
         b = Sum{v.z, top_of(v.z, dc), v.w};
         lanes_sum<widest.value>(a, c);
         if (both) lanes_sum<widest.value>(b, dc);
       };
+      join(make_float4(a.ref, a.s, b.ref, b.s), std::integral_constant<int, 16>{});
+      if (lane == 0) sh.part32[warp] = make_float4(a.ref, a.s, b.ref, b.s);
+      __syncthreads();
+      join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
       if (cluster > 1) {
-        if (warp == 0) {
-          join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
-          if (lane < cluster) st_cluster(mapa(smem_u32(&sh.sums[turn][rank]), lane), make_float4(a.ref, a.s, b.ref, b.s));
-        }
+        if (tid < cluster) st_cluster(mapa(smem_u32(&sh.sums[turn][rank]), tid), make_float4(a.ref, a.s, b.ref, b.s));
         cluster_sync();
         join(lane % kMaxCluster < cluster ? sh.sums[turn][lane % kMaxCluster] : make_float4(-CUDART_INF_F, 0.f, -CUDART_INF_F, 0.f),
              std::integral_constant<int, kMaxCluster / 2>{});
         turn ^= 1;
-      } else {
-        join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
       }
       if (!both) b = Sum{0.f, 0.f, 1.f};
     }
@@ -631,12 +731,16 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       double rest64 = 1.0;
       bool pending = false;              // draft: a rejection whose Z is not summed yet
       bool ready = false;
-      auto prepare = [&]() {             // what the passes read; e.inv, e.dinv: to 2^-21 or so
+      auto prepare = [&]() {             // what the passes read; e.inv, e.dinv: to 2^-19 or so (a sum's c is rounded)
         if (ready) return;
         ready = true;
+        if (asked >= 0) cp_async_wait<0>();          // the passes use the same slots
+        asked = -1;
         if (tid == 0) {
           sh.row = Row{row, drow, vocab, shift, from, to, dvec, per, n};
-          sh.e = Exact{scale, (double)a.ref * scale, (double)(1.f / a.s), dscale, (double)b.ref * dscale, (double)(1.f / b.s)};
+          // the sums are of 2^(x c - top): what rounding ref c has changed them by is known
+          auto less = [](const Sum& v, float scale) { return v.top == v.top ? 1.0 - 0.6931471805599453 * ((double)v.top - (double)v.ref * scale * 1.4426950408889634) : 1.0; };
+          sh.e = Exact{scale, (double)a.ref * scale, less(a, scale) / a.s, dscale, (double)b.ref * dscale, less(b, dscale) / b.s};
         }
         __syncthreads();
       };
@@ -669,10 +773,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         if (again) continue;
         bool accept = false, close = precise || pending;
         if (!close) {
-          const float have = weight(x, a, c) / a.s;
-          const float need = DRAFT ? u * (weight(y, b, dc) / b.s) : u * rest;
+          // p and u q, or p and u times what is left, both times the sums: no divisions. (What underflows is close.)
+          const float have = DRAFT ? weight(x, a, c) * b.s : weight(x, a, c);
+          const float need = DRAFT ? u * weight(y, b, dc) * a.s : u * rest * a.s;
           accept = need < have;
-          close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + rejected));
+          close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + rejected) * a.s);
         }
         if (close) {
           if (!precise) {
@@ -687,6 +792,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         if (accept) {
           chosen = j;
           out = t;
+          ref = x;
+          dref = y;
           break;
         }
         if (DRAFT) {
@@ -721,7 +828,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           fix_p = sh.e.inv - inv;
           fix_q = sh.e.dinv - dinv;
           const double off = fmax(fabs(fix_p) * a.s, fabs(fix_q) * b.s);
-          done = off < 0x1p-20 && off * total(2, cluster, turn) <= 1e-12 * total(3, cluster, turn);
+          done = off < 0x1p-19 && off * total(2, cluster, turn) <= 1e-12 * total(3, cluster, turn);
           if (!done) turn ^= 1;
         } else if (pending && !precise) {
           sum64(std::integral_constant<int, SUMS>{});

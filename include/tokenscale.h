@@ -628,7 +628,7 @@ typedef struct {
 } ts_adapters;
 
 /*
- * ts_adapter_pack: B (DEVICE bf16 [n_adapters][N][rank], row-major) as the kernels read it, to ts_adapter_packed_bytes() bytes (128-byte aligned; 0 for
+ * ts_adapter_pack: B (DEVICE bf16 [n_adapters][N][rank], row-major, finite: tokens of other adapters take zeros times it) as the kernels read it, to ts_adapter_packed_bytes() bytes (128-byte aligned; 0 for
  * arguments outside the limits): ranks padded to 16, 32 or a multiple of 64 and rows to a multiple of 128 with zeros. order: which rows lie together.
  * TS_ROWS_QKV needs N a multiple of 128, TS_ROWS_GATE_UP (B's rows in the order of ts_pack_gate_up) of 256. Asynchronous on cuda_stream, on the current device.
  */

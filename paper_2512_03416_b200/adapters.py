@@ -3,6 +3,7 @@ computation happens inside libtokenscale.so.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional, Sequence
 
 import torch
@@ -14,9 +15,9 @@ ROWS = {"plain": B.TS_ROWS_PLAIN, "qkv": B.TS_ROWS_QKV, "gate_up": B.TS_ROWS_GAT
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
 
 
-def _matrix(t: torch.Tensor, shape, device, what: str) -> int:
+def _matrix(t: torch.Tensor, shape: tuple, device, what: str) -> int:
     """Address of a contiguous bf16 tensor (or one of its bit patterns) of this shape on this device."""
-    if t.dtype not in _BF16 or tuple(t.shape) != tuple(shape):
+    if t.shape != shape or t.dtype not in _BF16:
         raise ValueError(f"{what} must be a bf16 (or int16, uint16) tensor {list(shape)}, not {t.dtype} {list(t.shape)}")
     if t.device != device or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous and on {device}")
@@ -41,12 +42,13 @@ class Adapters:
             raise ValueError(f"scale must be a contiguous float32 tensor of {n} values on {a.device}")
         self.device, self.rank, self.count = a.device, rank, n
         self.rows, pa, pb = rows, _matrix(a, (n, rank, self.k), a.device, "a"), _matrix(b, (n, self.n, rank), a.device, "b")
+        if b.numel() and not all(math.isfinite(v) for v in torch.aminmax(b.view(torch.bfloat16))):
+            raise ValueError("b must be finite: tokens of other adapters take zeros times it")
         self.tensors = [a, scale]
         with torch.cuda.device(a.device):
             packed = [self._pack(pb, order) for order in ([B.TS_ROWS_PLAIN] if rows == "plain" else [B.TS_ROWS_PLAIN, ROWS[rows]])]
         self.args = B.ts_adapters(n, rank, pa, packed[0], packed[-1], None if scale is None else scale.data_ptr())
         self.status = torch.zeros(1, dtype=torch.int32, device=a.device)
-
 
     def _pack(self, b: int, order: int) -> int:
         nbytes = B.ts_adapter_packed_bytes(self.count, self.n, self.rank)
@@ -82,12 +84,14 @@ def adapted_project(x: torch.Tensor, w: torch.Tensor, adapters: Adapters, row_to
         raise ValueError("row_tokens and row_adapter must be of one length")
     pr = 0 if residual is None else _matrix(residual, (m, n), dev, "residual")
     if out is None:
-        out = torch.empty((m, n), dtype=x.dtype, device=dev)
-    po = _matrix(out, (m, n), dev, "out")
+        out = x.new_empty((m, n))
+        po = out.data_ptr()
+    else:
+        po = _matrix(out, (m, n), dev, "out")
     if m == 0 and rows == 0:
         return out
     nbytes = B.ts_adapter_workspace_bytes(m, rows, adapters.count, adapters.rank)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)          # torch's allocator keeps it until the stream has passed this call
+    ws = x.new_empty((nbytes + 1) // 2)          # torch's allocator keeps it until the stream has passed this call
     _check(B.ts_adapter_project(dev.index, m, n, k, px, pw, pr, po, adapters.args, rows, row_tokens, row_adapter, ws.data_ptr(), nbytes,
                                 tile_m, adapters.status.data_ptr(), _raw_stream(dev.index)), "ts_adapter_project")
     return out

@@ -7,8 +7,12 @@
 // mma.sync (m16n8k16, fp32); a warp has 16 tokens, or a share of each stage's K. In a decode batch a block reads A_a (its only
 // user), so that the launch is bound by the bytes of the adapters in use; in a prompt's chunk x and A come from L2, each A once per 64 tokens.
 // The launch runs next to the product behind it, whose main loop does not need u: a block is small enough (128 threads, 56 KB) to share an SM
-// with one of the product's, and there is one per SM where that is enough. Blocks of 256 threads with 64 to 96 KB of copies under way were faster by
-// themselves, but the product waited for them: MEASURED.
+// with one of the product's, and there is one per SM where that is enough. Blocks of 256 threads with 64 to 96 KB of copies under way take less
+// by themselves, but the product waited for them: both together 29.5 and 70.5 us where these take 27 and 62.4 (below).
+//
+// Measured, this launch alone / the product without adapters / both together, us: 64 tokens, 64 adapters of rank 16, K = 4096, N = 6144: 7.6 / 15.8 / 27;
+// 192 tokens, 48 adapters of rank 32, K = N = 8192: 12.2 / 41.4 / 62.4; 2112 tokens, 16 adapters of rank 64, K = 4096, N = 28672: 22.8 / 321 / 363;
+// 2319 tokens, 5 adapters of rank 24, K = 14336, N = 4096: 34.2 / 213 / 236.
 // The partial sums are added up in a fixed order (warps, then blocks): equal calls give equal bits.
 #include <cuda_bf16.h>
 
@@ -92,8 +96,11 @@ __global__ void __launch_bounds__(kThreads, 5) adapter_down_kernel(const __grid_
       cp_async16(base + D::place(stage, kTokens + row, ch), in ? a + (size_t)row * d.K + k : a, in ? 16 : 0);
     }
   };
-#pragma unroll 1
-  for (int s = first; s < min(end, first + D::kStages); ++s) copy_a(s);      // the adapters are not the launch in front's: they fly while it ends
+  // The rows of A go to L2 while the launch in front ends: a hint only, nothing is read before the wait.
+  if (tid < ranks) {
+    const int k0 = first * D::kDepth, ahead = min(min(end, first + D::kStages) * D::kDepth, d.K) - k0;
+    if (ahead > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(a + (size_t)tid * d.K + k0), "r"(ahead * 2) : "memory");
+  }
 
   for (int got = 0, run = where & 0xffff, skip = where >> 16; got < n; ++run, skip = 0) {      // the group's tokens
     const uint32_t place = (uint32_t)words[d.o_run + 2 * run];
@@ -118,7 +125,10 @@ __global__ void __launch_bounds__(kThreads, 5) adapter_down_kernel(const __grid_
   };
 #pragma unroll 1
   for (int s = first; s < first + D::kStages; ++s) {
-    if (s < end) copy_x(s);
+    if (s < end) {
+      copy_a(s);
+      copy_x(s);
+    }
     cp_async_commit();                          // a group per stage, the last ones empty
   }
   if (blockIdx.x == 0 && d.plan)

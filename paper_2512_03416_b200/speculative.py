@@ -179,6 +179,8 @@ class SpeculativeDecoder:
         counts = got.count.tolist()
         keep = got.path >= 0                                     # count of each request, in order: what the cache takes
         tokens, lps = got.emitted[keep].tolist(), got.logprob[keep].tolist()
+        if -1 in tokens:
+            raise FloatingPointError("logits or draft logits that are no distribution")
         for r in range(R):
             self.dec.alloc_pages(self.slots[r], self.cached[r] + counts[r])
         self.dec.cache_append(self.slots, counts, self.cached, k, v, source=got.path[keep])

@@ -127,6 +127,22 @@ def test_equal_calls_give_equal_bits_and_a_captured_call_follows_its_inputs():
     assert torch.equal(out, want)
 
 
+def test_an_adapter_changed_in_place_counts_from_the_next_call_on():
+    """a and scale are not copied: a call reads what the work enqueued in front of it has written."""
+    tokens, which = [1] * 64, [r % 16 for r in range(64)]
+    x, w, ad, _ = make(8, tokens, which, 512, 4096, 32, 16)
+    a, b, s = ad.given
+    others = [(torch.randn_like(a.float()) / 64).to(torch.bfloat16) for _ in range(4)]
+    torch.cuda.synchronize()
+    got = []
+    for o in others:
+        a.copy_(o)
+        s.mul_(1.25)
+        got.append((adapted_project(x, w, ad, tokens, which), s.clone()))
+    for y, o, scale in ((y, o, scale) for (y, scale), o in zip(got, others)):
+        assert torch.equal(y, adapted_project(x, w, made(o, b, scale), tokens, which))
+
+
 def test_stacked_adapters_are_those_of_the_parts():
     gen = torch.Generator(device="cuda").manual_seed(6)
     parts = [((torch.randn(2, r, 256, generator=gen, device="cuda") / 16).to(torch.bfloat16), (torch.randn(2, n, r, generator=gen, device="cuda") / 4).to(torch.bfloat16))
@@ -157,6 +173,13 @@ def test_refusals():
         adapted_project(x, w.float(), ad, [4], [0])
     with pytest.raises(ValueError):
         Adapters(torch.zeros(1, 12, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 256, 12, dtype=torch.bfloat16, device="cuda"))
+    for bad in (math.nan, math.inf, -math.inf):          # B is in the products of tokens that it is not for
+        a, b, _ = ad.given
+        b = b.clone()
+        b[1, 255, 7] = bad
+        for form in (b, b.view(torch.int16)):
+            with pytest.raises(ValueError):
+                Adapters(a, form)
     assert B.ts_adapter_workspace_bytes(4, 1, 2, 12) == 0 and B.ts_adapter_workspace_bytes(4000, 1025, 2, 8) == 0
     need = B.ts_adapter_workspace_bytes(4, 1, 2, 8)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")

@@ -111,6 +111,17 @@ def test_refusals():
     plain.close()
 
 
+def test_logits_that_are_no_distribution_end_the_loop_with_an_error():
+    w, _, sd, _ = made("bf16", 2, 2, 0.5)
+    sd.step()
+    cached = list(sd.cached)
+    w.w_head[7].fill_(math.nan)
+    with pytest.raises(FloatingPointError):
+        sd.step()
+    assert sd.cached == cached
+    sd.close()
+
+
 def test_command(capsys):
     assert main(["--requests", "2", "--samples", "2", "--prompt", "20", "--tokens", "4", "--temperature", "0.8", "--adapters", "2", "--rank", "8"]) == 0
     line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])

@@ -160,26 +160,38 @@ __device__ __forceinline__ uint64_t granule_desc(uint32_t addr, int width) {
 // Runs of the tensor maps: where granule n's tokens begin, and rows 128 * block .. of its adapter's B (the former's are next to them).
 __device__ __forceinline__ int u_run(const AdapterTiles& t, int n) { return n * (t.rows * t.width / 128); }
 __device__ __forceinline__ int b_run(const AdapterTiles& t, int n, int block) {
-  const int entry = n / t.granules, c = n - entry * t.granules;
+  const int entry = t.granules == 1 ? n : t.granules == 2 ? n >> 1 : t.granules == 3 ? n / 3 : n >> 2, c = n - entry * t.granules;
   return ((tile_word(t, t.n_tiles + 1 + entry) * t.granules + c) * t.blocks + block) * t.width;
 }
-// Granules in K block `block` of those behind x and W
-__device__ __forceinline__ int granules_in(const AdapterTiles& t, Granules gr, int block) { return min(kBK / t.width, gr.count - block * (kBK / t.width)); }
+// Granules of a stage, and in K block `block` of those behind x and W
+__device__ __forceinline__ int per_stage(const AdapterTiles& t) { return t.width == 16 ? 4 : t.width == 32 ? 2 : 1; }
+__device__ __forceinline__ int granules_in(const AdapterTiles& t, Granules gr, int block) { return min(per_stage(t), gr.count - block * per_stage(t)); }
 // The producer warp's part of K blocks e0 .. e1 - 1 of those: begin(block) on lane 0 makes room for a block and tells its barrier, copy(block, place in
-// the stage, run of u, run of b) starts a granule's copies, on a lane of its own. Where they lie is found for 32 granules at a time: one after the other on one
-// lane, a granule took 400 cycles.
+// the stage, which side, run) starts one of a granule's copies, on a lane of its own: issued one after the other by one lane, they took 1.4 times as long.
+// The runs of as many blocks as a warp has lanes for are found at once (400 cycles a granule otherwise), the first ones' before the main loop.
+__device__ __forceinline__ int granule_run(const AdapterTiles& t, Granules gr, int first, int e1, int b_block, int lane) {
+  const int per = per_stage(t), block = first + lane / (2 * per), k = block * per + lane % (2 * per) / 2;
+  if (block >= e1 || k >= gr.count) return -1;
+  return lane & 1 ? b_run(t, gr.first + k, b_block) : u_run(t, gr.first + k);
+}
+struct TileGranules {
+  Granules gr;
+  int run;                 // this lane's first one
+};
+__device__ __forceinline__ TileGranules find_granules(const AdapterTiles& t, int tile, int b_block, int lane) {
+  const Granules gr = granules_of(t, tile);
+  return TileGranules{gr, granule_run(t, gr, 0, granule_blocks(t, gr.count), b_block, lane)};
+}
 template <typename Begin, typename Copy>
-__device__ __forceinline__ void copy_granules(const AdapterTiles& t, Granules gr, int e0, int e1, int b_block, int lane, Begin&& begin, Copy&& copy) {
-  const int per = kBK / t.width, at_once = 32 / per;
+__device__ __forceinline__ void copy_granules(const AdapterTiles& t, Granules gr, int e0, int e1, int b_block, int lane, int run, Begin&& begin, Copy&& copy) {
+  const int lanes = 2 * per_stage(t), at_once = 32 / lanes, mine = lane / lanes, j = lane % lanes / 2;
   for (int first = e0; first < e1; first += at_once) {
-    const int block = first + lane / per, k = block * per + lane % per;
-    const bool mine = block < e1 && k < gr.count;
-    const int u = mine ? u_run(t, gr.first + k) : 0, b = mine ? b_run(t, gr.first + k, b_block) : 0;
+    if (first > e0) run = granule_run(t, gr, first, e1, b_block, lane);
     for (int e = first; e < min(e1, first + at_once); ++e) {
       bool go = true;
       if (lane == 0) go = begin(e);
       go = __shfl_sync(0xffffffffu, go, 0);
-      if (go && mine && block == e) copy(e, lane % per, u, b);
+      if (go && run >= 0 && first + mine == e) copy(e, j, lane & 1, run);
       __syncwarp();
     }
   }
@@ -320,6 +332,9 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
   auto wait = [&](int i, uint32_t parity) {
     if (!mbar_wait(bar(i), parity, misc[1] ? 2000 : g.wait_cycles)) give_up();
   };
+  auto spin = [&](int i, uint32_t parity) {                // without the time that a parked thread takes to wake up; not after a failure
+    if (!mbar_poll(bar(i), parity, g.wait_cycles)) give_up();
+  };
   const int m_tiles = (g.M + 127) / 128, n_tiles = (g.N + kBN - 1) / kBN;
   const int n_work = m_tiles * n_tiles;
   const int k_blocks = (g.K + kBK - 1) / kBK;
@@ -335,6 +350,9 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
       int it = 0;                                          // K blocks issued so far (ring position)
       for (int t = blockIdx.x; t < n_work; t += gridDim.x) {
         const int m0 = (t % m_tiles) * 128, n0 = (t / m_tiles) * kBN;
+        TileGranules tg = {};
+        if constexpr (ADAPT)                               // while lane 0 copies
+          if (lane > 0 && ad.t.n_inline > 0) tg = find_granules(ad.t, t % m_tiles, n0 / 128, lane);
         for (int kb = 0; kb < k_blocks; ++kb, ++it) {
           if (ADAPT && lane > 0) continue;
           const int st = it % kStages;
@@ -347,24 +365,25 @@ gemm_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, const _
           tma_load_2d(dst + kABytes + kBBytes / 2, &b_map, bar(BAR_FULL + st), kb * kBK, n0 + 128);
         }
         if constexpr (ADAPT) {
-          const Granules gr = granules_of(ad.t, t % m_tiles);
-          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, gr.count);
+          __syncwarp();
+          if (lane == 0 || ad.t.n_inline == 0) tg = find_granules(ad.t, t % m_tiles, n0 / 128, lane);
+          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, tg.gr.count);
           __syncwarp();
           pdl_wait();
-          copy_granules(ad.t, gr, 0, blocks, n0 / 128, lane,
+          copy_granules(ad.t, tg.gr, 0, blocks, n0 / 128, lane, tg.run,
                         [&](int e) {
                           const int st = (it + e) % kStages;
-                          if (it + e >= kStages) wait(BAR_EMPTY + st, (((it + e) / kStages) & 1) ^ 1);
                           if (misc[1]) return false;
-                          mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (ad.t.rows + kBN) * row);
+                          if (it + e >= kStages) spin(BAR_EMPTY + st, (((it + e) / kStages) & 1) ^ 1);
+                          if (misc[1]) return false;
+                          mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, tg.gr, e) * (ad.t.rows + kBN) * row);
                           return true;
                         },
-                        [&](int e, int j, int u, int b) {    // of an odd last block the second half is no column's
+                        [&](int e, int j, bool of_b, int run) {    // of an odd last block the second half is no column's
                           const int st = (it + e) % kStages;
-                          const uint32_t dst = base + st * kStageBytes;
-                          tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, u);
-                          tma_load_2d(dst + kABytes + j * kBN * row, &ad.b, bar(BAR_FULL + st), 0, b);
-                          tma_load_2d(dst + kABytes + (j * kBN + 128) * row, &ad.b, bar(BAR_FULL + st), 0, b + width);
+                          const uint32_t dst = base + st * kStageBytes + (of_b ? kABytes + j * kBN * row : j * 128 * row);
+                          tma_load_2d(dst, of_b ? &ad.b : &ad.u, bar(BAR_FULL + st), 0, run);
+                          if (of_b) tma_load_2d(dst + 128 * row, &ad.b, bar(BAR_FULL + st), 0, run + width);
                         });
           it += blocks;
         }
@@ -647,6 +666,9 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
   auto wait = [&](int i, uint32_t parity) {
     if (!mbar_wait(bar(i), parity, misc[1] ? 2000 : g.wait_cycles)) give_up();
   };
+  auto spin = [&](int i, uint32_t parity) {                // without the time that a parked thread takes to wake up; not after a failure
+    if (!mbar_poll(bar(i), parity, g.wait_cycles)) give_up();
+  };
   const int m_tiles = (g.M + nt - 1) / nt, n_tiles = (g.N + kBN - 1) / kBN;
   const int n_work = m_tiles * n_tiles, first = blockIdx.x >> 1, stride = gridDim.x >> 1;
   const int k_blocks = (g.K + kBK - 1) / kBK;
@@ -662,6 +684,9 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
       int it = 0;
       for (int t = first; t < n_work; t += stride) {
         const int m0 = (t % m_tiles) * nt + (int)rank * (nt / 2), nb = t / m_tiles;
+        TileGranules tg = {};
+        if constexpr (ADAPT)
+          if (lane > 0 && ad.t.n_inline > 0) tg = find_granules(ad.t, t % m_tiles, nb * 2 + (int)rank, lane);
         for (int kb = 0; kb < k_blocks; ++kb, ++it) {
           if (ADAPT && lane > 0) continue;
           const int st = it % kPairStages;
@@ -678,23 +703,25 @@ gemm_pair_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap x_map, co
           tma_load_2d_pair(dst + kABytes, &x_map, full, kb * kBK, m0);
         }
         if constexpr (ADAPT) {
-          const Granules gr = granules_of(ad.t, t % m_tiles);
-          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, gr.count);
+          __syncwarp();
+          if (lane == 0 || ad.t.n_inline == 0) tg = find_granules(ad.t, t % m_tiles, nb * 2 + (int)rank, lane);
+          const int width = ad.t.width, row = width * 2, blocks = granule_blocks(ad.t, tg.gr.count);
+          const uint32_t full0 = mapa(bar(BAR_FULL), 0);
           __syncwarp();
           pdl_wait();
-          copy_granules(ad.t, gr, 0, blocks, nb * 2 + (int)rank, lane,
+          copy_granules(ad.t, tg.gr, 0, blocks, nb * 2 + (int)rank, lane, tg.run,
                         [&](int e) {
                           const int st = (it + e) % kPairStages;
-                          if (it + e >= kPairStages) wait(BAR_EMPTY + st, (((it + e) / kPairStages) & 1) ^ 1);
                           if (misc[1]) return false;
-                          if (rank == 0) mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (2 * 128 + nt) * row);
+                          if (it + e >= kPairStages) spin(BAR_EMPTY + st, (((it + e) / kPairStages) & 1) ^ 1);
+                          if (misc[1]) return false;
+                          if (rank == 0) mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, tg.gr, e) * (2 * 128 + nt) * row);
                           return true;
                         },
-                        [&](int e, int j, int u, int b) {
+                        [&](int e, int j, bool of_b, int run) {
                           const int st = (it + e) % kPairStages;
-                          const uint32_t dst = base + st * kPairStageBytes, full = mapa(bar(BAR_FULL + st), 0);
-                          tma_load_2d_pair(dst + j * 128 * row, &ad.b, full, 0, b);
-                          tma_load_2d_pair(dst + kABytes + j * (nt / 2) * row, &ad.u, full, 0, u + (int)rank * (nt / 2) * width / 128);
+                          const uint32_t dst = base + st * kPairStageBytes + (of_b ? j * 128 * row : kABytes + j * (nt / 2) * row);
+                          tma_load_2d_pair(dst, of_b ? &ad.b : &ad.u, full0 + 8 * st, 0, of_b ? run : run + (int)rank * (nt / 2) * width / 128);
                         });
           it += blocks;
         }
@@ -904,6 +931,9 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
   const int n_blocks = kb1 - kb0 + e1 - e0;
 
   if (warp == 0) {
+    int run = -1;
+    if constexpr (ADAPT)
+      if (lane > 0) run = granule_run(ad.t, gr, e0, e1, n0 / 128, lane);       // while lane 0 copies
     if (lane == 0) {
       for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
         const int st = it % kSplitStages;
@@ -918,20 +948,21 @@ gemm_split_kernel(const GemmArgs g, const __grid_constant__ CUtensorMap a_map, c
     if constexpr (ADAPT) {
       const int row = ad.t.width * 2, it = kb1 - kb0 - e0;
       __syncwarp();
+      if (lane == 0) run = granule_run(ad.t, gr, e0, e1, n0 / 128, lane);
+      __syncwarp();
       if (e1 > e0) pdl_wait();
-      copy_granules(ad.t, gr, e0, e1, n0 / 128, lane,
+      copy_granules(ad.t, gr, e0, e1, n0 / 128, lane, run,
                     [&](int e) {
                       const int st = (it + e) % kSplitStages;
-                      if (it + e >= kSplitStages && !mbar_wait(bar(BAR_EMPTY + st), (((it + e) / kSplitStages) & 1) ^ 1, misc[1] ? 2000 : g.wait_cycles)) give_up();
+                      if (misc[1]) return false;
+                      if (it + e >= kSplitStages && !mbar_poll(bar(BAR_EMPTY + st), (((it + e) / kSplitStages) & 1) ^ 1, g.wait_cycles)) give_up();
                       if (misc[1]) return false;
                       mbar_expect_tx(bar(BAR_FULL + st), granules_in(ad.t, gr, e) * (ad.t.rows + kSplitN) * row);
                       return true;
                     },
-                    [&](int e, int j, int u, int b) {
+                    [&](int e, int j, bool of_b, int run) {
                       const int st = (it + e) % kSplitStages;
-                      const uint32_t dst = base + st * kSplitStageBytes;
-                      tma_load_2d(dst + kABytes + j * kSplitN * row, &ad.b, bar(BAR_FULL + st), 0, b);
-                      tma_load_2d(dst + j * 128 * row, &ad.u, bar(BAR_FULL + st), 0, u);
+                      tma_load_2d(base + st * kSplitStageBytes + (of_b ? kABytes + j * kSplitN * row : j * 128 * row), of_b ? &ad.b : &ad.u, bar(BAR_FULL + st), 0, run);
                     });
     }
   } else if (warp == 1) {

@@ -6,6 +6,7 @@ is no fallback implementation.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -104,7 +105,7 @@ class ts_layer_adapters(ctypes.Structure):
 
 class ts_verify(ctypes.Structure):
     _fields_ = [("device", ctypes.c_int32), ("n_requests", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("n_nodes", _i32p), ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("draft", ctypes.c_void_p),
+                ("n_nodes", ctypes.c_void_p), ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("draft", ctypes.c_void_p),
                 ("draft_stride", ctypes.c_int64)] + \
                [(name, ctypes.c_void_p) for name in ("scale", "draft_scale", "tokens", "parents", "u_accept", "u_sample", "emitted", "count", "path", "logprob")]
 
@@ -213,10 +214,10 @@ def lib() -> ctypes.CDLL:
         L.ts_adapter_workspace_bytes.argtypes = [i32] * 4
         L.ts_adapter_packed_bytes.argtypes = [i32] * 3
         L.ts_adapter_pack.argtypes = [vp, i32, i32, i32, i32, vp, vp]
-        L.ts_adapter_project.argtypes = [i32] * 4 + [vp] * 4 + [adp, i32, _i32p, _i32p, vp, ctypes.c_size_t, i32, vp, vp]
+        L.ts_adapter_project.argtypes = [i32] * 4 + [vp] * 4 + [adp, i32, vp, vp, vp, ctypes.c_size_t, i32, vp, vp]
         L.ts_layer_adapters_workspace_bytes.argtypes = [cfgp, ctypes.POINTER(ts_layer_adapters)]
         L.ts_layer_attach_adapters.argtypes = [vp, ctypes.POINTER(ts_layer_adapters)]
-        L.ts_layer_step_adapted.argtypes = [vp, stepp, _i32p, vp, vp, vp]
+        L.ts_layer_step_adapted.argtypes = [vp, stepp, vp, vp, vp, vp]
         L.ts_verify_tokens.argtypes = [ctypes.POINTER(ts_verify), vp]
         L.ts_request_fork.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         L.ts_requests_free.argtypes = [vp, vp, i32]
@@ -534,6 +535,11 @@ def ts_token_logprobs(args: ts_logprobs, stream: int) -> int:
 
 
 # --------------------------------------------------------------------------- adapters of the requests of a step
+def int32_array(numbers) -> array.array:
+    """A C array of a sequence; buffer_info()[0] is its address. (A ctypes array made from a list takes five times as long.)"""
+    return array.array("i", numbers)
+
+
 def ts_adapter_workspace_bytes(n_tokens: int, n_rows: int, n_adapters: int, rank: int) -> int:
     return lib().ts_adapter_workspace_bytes(n_tokens, n_rows, n_adapters, rank)
 
@@ -549,9 +555,11 @@ def ts_adapter_pack(b: int, n_adapters: int, N: int, rank: int, order: int, pack
 def ts_adapter_project(device: int, M: int, N: int, K: int, x: int, W: int, R: int, C: int, adapters: ts_adapters, n_rows: int, row_tokens,
                        row_adapter, workspace: int, workspace_bytes: int, tile_m: int, status: int, stream: int) -> int:
     """row_tokens, row_adapter: sequences of n_rows numbers."""
-    rows = ctypes.c_int32 * max(n_rows, 1)
-    return lib().ts_adapter_project(device, M, N, K, x, W, R or None, C, ctypes.byref(adapters), n_rows, rows(*row_tokens), rows(*row_adapter),
-                                    workspace, workspace_bytes, tile_m, status, stream)
+    tokens, which = int32_array(row_tokens), int32_array(row_adapter)
+    if len(tokens) != n_rows or len(which) != n_rows:
+        return TS_ERR_INVALID
+    return lib().ts_adapter_project(device, M, N, K, x, W, R or None, C, ctypes.byref(adapters), n_rows, tokens.buffer_info()[0],
+                                    which.buffer_info()[0], workspace, workspace_bytes, tile_m, status, stream)
 
 
 def ts_layer_adapters_workspace_bytes(cfg: ts_config, adapters: ts_layer_adapters) -> int:
@@ -564,8 +572,10 @@ def ts_layer_attach_adapters(layer, adapters: ts_layer_adapters) -> int:
 
 def ts_layer_step_adapted(layer, step: ts_step, row_adapter, x_in: int, x_out: int, stream: int) -> int:
     """row_adapter: a sequence of step.n_rows numbers, or None."""
-    rows = None if row_adapter is None else (ctypes.c_int32 * max(step.n_rows, 1))(*row_adapter)
-    return lib().ts_layer_step_adapted(layer, ctypes.byref(step), rows, x_in, x_out, stream)
+    rows = None if row_adapter is None else int32_array(row_adapter)
+    if rows is not None and len(rows) != step.n_rows:
+        return TS_ERR_INVALID
+    return lib().ts_layer_step_adapted(layer, ctypes.byref(step), None if rows is None else rows.buffer_info()[0], x_in, x_out, stream)
 
 
 # ------------------------------------------------------------------------------ drafted tokens verified by sampling

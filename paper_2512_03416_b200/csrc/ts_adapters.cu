@@ -17,6 +17,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 
 #include "../../include/tokenscale.h"
@@ -254,11 +255,17 @@ cudaError_t launch_w(const AdapterDown& d, const int32_t* words, int n_words, in
   cfg.gridDim = dim3((unsigned)(items * split));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Down<WIDTH, MT>::kBytes;
-  // the SM's memory divided as the product behind this launch needs it: it cannot be divided anew while a block runs
-  const cudaError_t e = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  static std::atomic<uint64_t> ready{0};        // devices on which these are set
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  const cudaError_t e2 = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
-  if (e2 != cudaSuccess) return e2;
+  if (device >= 64 || !(ready.load(std::memory_order_acquire) >> device & 1)) {
+    // the SM's memory divided as the product behind this launch needs it: it cannot be divided anew while a block runs
+    e = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_down_kernel<WIDTH, MT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+    if (e != cudaSuccess) return e;
+    if (device < 64) ready.fetch_or(1ull << device, std::memory_order_release);
+  }
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -2,6 +2,7 @@
 // rotary embedding, ts_mixed_step, output projection, gated MLP. The public ABI is documented in
 // include/tokenscale.h.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -505,10 +506,13 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
   if (!adapted) return ts_gemm_bf16(device, M, N, K, x, W, R, C, tile_m, device_status, cuda_stream);
   if (workspace_bytes < adapter_bytes(M, n_rows, ad->n_adapters, ad->rank)) return TS_ERR_WORKSPACE;
   if (cudaSetDevice(device) != cudaSuccess) return TS_ERR_CUDA;
-  void* encode_fn = nullptr;
+  static std::atomic<void*> encode{nullptr};               // the driver's function: looked up once
+  void* encode_fn = encode.load(std::memory_order_relaxed);
   cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &encode_fn, cudaEnableDefault, &qres) != cudaSuccess || !encode_fn)
-    return TS_ERR_CUDA;
+  if (!encode_fn) {
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &encode_fn, cudaEnableDefault, &qres) != cudaSuccess || !encode_fn) return TS_ERR_CUDA;
+    encode.store(encode_fn, std::memory_order_relaxed);
+  }
   int n_sms = 0;
   if (cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return TS_ERR_CUDA;
   ts::GemmArgs g;

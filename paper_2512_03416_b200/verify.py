@@ -3,7 +3,6 @@ stream; all computation happens inside libtokenscale.so.
 """
 from __future__ import annotations
 
-import ctypes
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -48,8 +47,8 @@ def verify_tokens(logits: torch.Tensor, tokens: torch.Tensor, parents: torch.Ten
     count, logprob = torch.empty(requests, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
     if requests == 0:
         return Verified(emitted, count, path, logprob)
-    nodes = (ctypes.c_int32 * requests)(*n_nodes)
-    args = B.ts_verify(dev.index, requests, vocab, B.TS_BF16 if logits.dtype == torch.bfloat16 else B.TS_F32, nodes, logits.data_ptr(),
+    nodes = B.int32_array(n_nodes)
+    args = B.ts_verify(dev.index, requests, vocab, B.TS_BF16 if logits.dtype == torch.bfloat16 else B.TS_F32, nodes.buffer_info()[0], logits.data_ptr(),
                        logits.stride(0) if n > 1 else vocab, None if draft is None else draft.data_ptr(),
                        vocab if draft is None or n == 1 else draft.stride(0), None if scale is None else scale.data_ptr(),
                        None if draft_scale is None else draft_scale.data_ptr(), tokens.data_ptr(), parents.data_ptr(), u_accept.data_ptr(),

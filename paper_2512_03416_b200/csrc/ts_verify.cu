@@ -16,6 +16,11 @@
 // would draw a neighbour of the token once in a hundred times. Its cumulative sums are kept per strip of the row; one warp then goes through
 // the strip that holds the place.
 // Sums are added up in a fixed order: equal calls give equal results.
+//
+// A launch lasts as long as its longest request. A level of a walk (131072 bf16 logits and the draft's, 64 requests) takes 9 us: some 5 that the row's
+// exponentials take an SM's four blocks, the rest joins; a rejection's pass in 64 bits 33, a draw without one 22, finding the token in its strip 2 to 5.
+// Measured: 64 chains of 6 nodes 95 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 145 to 175 (267),
+// 256 trees of 8 given tokens 107 (300), one chain of 4 over 32000 23.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -549,7 +554,8 @@ __device__ __noinline__ void pass(int rejected, int to, int rank, int cluster, i
   sync_all(cluster);
 }
 
-// THREADS: 512 where there are few requests, so that what runs of them has the threads of an SM each; else 128, four blocks of which an SM runs.
+// THREADS: 512 where there are few requests, so that what runs of them has the threads of an SM each; else 128, four blocks of which an SM runs (128
+// registers): blocks of different requests then pass through their joins and draws at different times.
 template <typename T, bool DRAFT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __grid_constant__ VerifyParams p) {
   constexpr int kWarps = THREADS / 32;

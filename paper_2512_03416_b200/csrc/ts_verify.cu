@@ -19,8 +19,8 @@
 //
 // A launch lasts as long as its longest request. A level of a walk (131072 bf16 logits and the draft's, 64 requests) takes 9 us: some 5 that the row's
 // exponentials take an SM's four blocks, the rest joins; a rejection's pass in 64 bits 33, a draw without one 22, finding the token in its strip 2 to 5.
-// Measured: 64 chains of 6 nodes 95 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 145 to 175 (267),
-// 256 trees of 8 given tokens 107 (300), one chain of 4 over 32000 23.
+// Measured: 64 chains of 6 nodes 97 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 150 to 165 (267),
+// 256 trees of 8 given tokens 111 (300), one chain of 4 over 32000 23.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -40,7 +40,7 @@ constexpr int kMostWarps = 16;
 constexpr double kNothing = 1e-250;      // what is not more than this is as good as nothing
 constexpr int kNodes = 64, kMaxCluster = 8, kValues = 6;
 constexpr int kWords = 767;              // requests of a launch
-constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr double kLog2e = 1.4426950408889634;
 
 struct VerifyParams {
   const void *logits, *draft;
@@ -80,6 +80,8 @@ __shared__ struct {
   float4 part32[kMostWarps];
   float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference
   int32_t found;
+  float ref[kNodes], top[kNodes], sum[kNodes], c[kNodes], c_rest[kNodes];      // of the rows walked: the sums (see Sum) and what they were taken with
+  int32_t out[kNodes], walked[kNodes];
 } sh;
 
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
@@ -238,8 +240,10 @@ __device__ __forceinline__ float top_of(float ref, float c) {
   const float top = __fmul_rn(ref, c);
   return fabsf(top) < kHuge ? top : CUDART_NAN_F;
 }
-__device__ __forceinline__ float exponent(float x, const Sum& a, float c) { return a.top == a.top ? fmaf(x, c, -a.top) : (x - a.ref) * c; }
-__device__ __forceinline__ float weight(float x, const Sum& a, float c) { return ex2(exponent(x, a, c)); }
+__device__ __forceinline__ float exponent(float x, const Sum& a, float c, float c_rest) {
+  return a.top == a.top ? fmaf(x, c_rest, fmaf(x, c, -a.top)) : (x - a.ref) * c;
+}
+__device__ __forceinline__ float weight(float x, const Sum& a, float c, float c_rest) { return ex2(exponent(x, a, c, c_rest)); }
 // The sum in weights of another reference.
 __device__ __forceinline__ float moved(const Sum& a, float ref, float top, float c) {
   if (a.ref == -CUDART_INF_F || a.ref == ref) return a.s;                    // nothing, or a NaN
@@ -253,7 +257,7 @@ __device__ __noinline__ Sum add(Sum a, float x0, float x1, float x2, float x3, f
   const float top = top_of(m, c);
   Sum b = {m, top, moved(a, m, top, c)};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) b.s += m != -CUDART_INF_F ? weight(x[i], b, c) : x[i] != x[i] ? x[i] : 0.f;
+  for (int i = 0; i < 8; ++i) b.s += m != -CUDART_INF_F ? weight(x[i], b, c, 1e-37f) : x[i] != x[i] ? x[i] : 0.f;
   return b;
 }
 // Over groups of 2 * WIDEST lanes.
@@ -314,7 +318,7 @@ __device__ __noinline__ double left(float x, float y, int rejected) {
 //   SUMS    values 0, 1: the sums of e^(x scale - top) of the model and of the draft
 //   REST    value 0: what one more rejection leaves
 //   STRIPS  what is left, per strip, and value 0: in all
-//   FIRST   what the first rejection leaves, with e.inv and e.dinv known to 2^-19 only: strips and values 3, 4, 5 of max(p - q, 0), and of
+//   FIRST   what the first rejection leaves, with e.inv and e.dinv known to 2^-19 or so: strips and values 3, 4, 5 of max(p - q, 0), and of
 //           e^.. of the model and of the draft where that is not 0, by which it is corrected; values 0, 1 as SUMS; value 2: p + q of tokens whose
 //           p and q are alike to 2^-18, of which it may not be known which is larger
 // Values are published. find, by one warp: the token at `want` of a strip, or the last one there that has anything.
@@ -616,7 +620,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
   float ref = 0.f, dref = 0.f;           // logits of likely tokens: the last accepted one's, where it was accepted
   for (;;) {
     const float scale = sh.scale[cur], dscale = sh.dscale[cur];
-    const float c = scale * kLog2e, dc = dscale * kLog2e;
+    // c, rounded down, and what is missing of it, always something (-inf times it stays -inf): left out, all terms of a sum would share an error of 1e-6
+    const float c = __double2float_rd(scale * kLog2e * (1.0 - 0x1p-30)), dc = __double2float_rd(dscale * kLog2e * (1.0 - 0x1p-30));
+    float c_rest = (float)(scale * kLog2e - c), dc_rest = (float)(dscale * kLog2e - dc);
     const Place here = place_of(cur);
     const T *const row = here.row, *const drow = here.drow;
     const int vocab = p.vocab, shift = here.shift, from = here.from, to = here.to;
@@ -654,10 +660,10 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         const int next = tile + Ring<T>::kRing * kWarps;
         ring.ask(k, next * kTile + base, next < to);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c, -a.top));
+        for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c_rest, fmaf(x[i], c, -a.top)));
         if (both) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[i & 1] += ex2(fmaf(y[i], dc, -b.top));
+          for (int i = 0; i < 8; ++i) d[i & 1] += ex2(fmaf(y[i], dc_rest, fmaf(y[i], dc, -b.top)));
         }
       }
       ask_child();
@@ -693,6 +699,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
     }
     if (__builtin_expect(!(a.s > 1.f / kLarge && a.s < kLarge && b.s > 1.f / kLarge && b.s < kLarge), 0)) {
       a = b = nothing();
+      c_rest = dc_rest = 1e-37f;         // nothing: references move, the same c everywhere
       cp_async_wait<0>();
       __syncthreads();
       ask_first(here);
@@ -780,8 +787,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         bool accept = false, close = precise || pending;
         if (!close) {
           // p and u q, or p and u times what is left, both times the sums: no divisions. (What underflows is close.)
-          const float have = DRAFT ? weight(x, a, c) * b.s : weight(x, a, c);
-          const float need = DRAFT ? u * weight(y, b, dc) * a.s : u * rest * a.s;
+          const float have = DRAFT ? weight(x, a, c, c_rest) * b.s : weight(x, a, c, c_rest);
+          const float need = DRAFT ? u * weight(y, b, dc, dc_rest) * a.s : u * rest * a.s;
           accept = need < have;
           close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + rejected) * a.s);
         }
@@ -805,7 +812,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         if (DRAFT) {
           pending = true;
         } else {
-          rest -= weight(x, a, c) / a.s;
+          rest -= weight(x, a, c, c_rest) / a.s;
           if (precise) rest64 -= weight64(x, sh.e.scale, sh.e.top) * sh.e.inv;
           __syncthreads();               // the others may still look through the list
           if (tid == 0) sh.gone[rejected] = t;
@@ -918,9 +925,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       }
     }
     if (rank == 0 && tid == 0) {
-      p.emitted[first + emitted] = out;
-      p.path[first + emitted] = first + cur;
-      p.logprob[first + emitted] = out >= 0 ? (exponent(value(row + out), a, c) - log2f(a.s)) * kLn2 : CUDART_NAN_F;
+      sh.out[emitted] = out;
+      sh.walked[emitted] = cur;
+      sh.ref[emitted] = a.ref;
+      sh.top[emitted] = a.top;
+      sh.sum[emitted] = a.s;
+      sh.c[emitted] = c;
+      sh.c_rest[emitted] = c_rest;
     }
     ++emitted;
     if (chosen < 0) break;
@@ -928,9 +939,17 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
   }
   if (rank == 0) {
     if (tid == 0) p.count[request] = emitted;
-    for (int i = emitted + tid; i < nodes; i += THREADS) {
-      p.emitted[first + i] = p.path[first + i] = -1;
-      p.logprob[first + i] = 0.f;
+    __syncthreads();
+    if (tid < nodes) {
+      const int out = tid < emitted ? sh.out[tid] : -1, at = tid < emitted ? sh.walked[tid] : -1;
+      p.emitted[first + tid] = out;
+      p.path[first + tid] = at >= 0 ? first + at : -1;
+      float lp = at >= 0 ? CUDART_NAN_F : 0.f;
+      if (out >= 0) {                    // the exponent as it went into the sum: of a token that has nearly all, their roundings cancel
+        const Sum a = {sh.ref[tid], sh.top[tid], sh.sum[tid]};
+        lp = (float)(exponent(value(place_of(at).row + out), a, sh.c[tid], sh.c_rest[tid]) * 0.6931471805599453 - log((double)a.s));
+      }
+      p.logprob[first + tid] = lp;
     }
   }
   if (cluster > 1) cluster_sync();       // no block leaves while another one may write to it

@@ -30,6 +30,7 @@
 #include "../../include/tokenscale.h"
 #include "ts_internal.h"
 #include "ts_ptx.h"
+#include "ts_tma.h"
 
 namespace ts {
 namespace {
@@ -78,9 +79,11 @@ __shared__ struct {
   float chance[kNodes], scale[kNodes], dscale[kNodes];
   float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (reference, sum of the model; of the draft), by turns
   float4 part32[kMostWarps];
-  float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference
+  float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference; by turns of their own
+  uint64_t even_bar[2];                  // a phase for each of these turns: eight bytes from every block
   int32_t found;
-  float ref[kNodes], top[kNodes], sum[kNodes], c[kNodes], c_rest[kNodes];      // of the rows walked: the sums (see Sum) and what they were taken with
+  float c[kNodes], c_rest[kNodes], dc[kNodes], dc_rest[kNodes];
+  float ref[kNodes], top[kNodes], sum[kNodes], rest_used[kNodes];      // of the rows walked: the sums (see Sum), the c_rest they were taken with
   int32_t out[kNodes], walked[kNodes];
 } sh;
 
@@ -100,6 +103,10 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, float2 v) {
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, int32_t v) {
   asm volatile("st.shared::cluster.s32 [%0], %1;\n" ::"r"(addr), "r"(v) : "memory");
+}
+// Eight bytes into another block's shared memory, counted by a barrier there: neither side needs a fence for what else is under way.
+__device__ __forceinline__ void st_async(uint32_t addr, uint32_t bar, float2 v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];\n" ::"r"(addr), "f"(v.x), "f"(v.y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;\n" ::: "memory");
@@ -577,6 +584,18 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
     sh.chance[tid] = node ? p.u_accept[first + tid] : 0.f;
     sh.scale[tid] = node && p.scale ? p.scale[first + tid] : 1.f;
     sh.dscale[tid] = DRAFT && node && p.draft_scale ? p.draft_scale[first + tid] : 1.f;
+    // c, rounded down, and what is missing of it, always something (-inf times it stays -inf): left out, all terms of a sum would share an error of 1e-6
+    auto split = [](float scale, float& c, float& rest) {
+      const double exact = scale * kLog2e;
+      c = __double2float_rd(exact * (1.0 - 0x1p-30));
+      rest = (float)(exact - c);
+    };
+    split(sh.scale[tid], sh.c[tid], sh.c_rest[tid]);
+    split(sh.dscale[tid], sh.dc[tid], sh.dc_rest[tid]);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.even_bar[i]), 1);
+    mbar_init_fence();
   }
   __syncthreads();
   if (tid < nodes) {
@@ -613,16 +632,18 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
   auto ask_first = [&](const Place& s) {
     const Ring<T> ring = ring_of(s);
     const int at = (s.from + warp) * kTile + lane * 8 - s.shift;
-#pragma unroll 2
-    for (int k = 0; k < Ring<T>::kRing; ++k) ring.ask(k, at + k * kWarps * kTile, s.from + warp + k * kWarps < s.to);
+    int k = 0;
+#pragma unroll 1
+    for (; k < Ring<T>::kRing && s.from + warp + k * kWarps < s.to; ++k) ring.ask(k, at + k * kWarps * kTile, true);
+#pragma unroll 1
+    for (; k < Ring<T>::kRing; ++k) cp_async_commit();
   };
-  int cur = 0, emitted = 0, turn = 0, asked = -1;    // asked: the node whose first tiles are on their way
+  int cur = 0, emitted = 0, turn = 0, joins = 0, asked = -1;    // asked: the node whose first tiles are on their way
   float ref = 0.f, dref = 0.f;           // logits of likely tokens: the last accepted one's, where it was accepted
   for (;;) {
     const float scale = sh.scale[cur], dscale = sh.dscale[cur];
-    // c, rounded down, and what is missing of it, always something (-inf times it stays -inf): left out, all terms of a sum would share an error of 1e-6
-    const float c = __double2float_rd(scale * kLog2e * (1.0 - 0x1p-30)), dc = __double2float_rd(dscale * kLog2e * (1.0 - 0x1p-30));
-    float c_rest = (float)(scale * kLog2e - c), dc_rest = (float)(dscale * kLog2e - dc);
+    const float c = sh.c[cur], dc = sh.dc[cur];
+    float c_rest = sh.c_rest[cur], dc_rest = sh.dc_rest[cur];
     const Place here = place_of(cur);
     const T *const row = here.row, *const drow = here.drow;
     const int vocab = p.vocab, shift = here.shift, from = here.from, to = here.to;
@@ -650,6 +671,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       ask_first(place_of(child));
       asked = child;
     };
+    bool lost = false;                   // a block of the cluster has not answered: never, and if it does, the request ends
     {
       const Ring<T> ring = ring_of(here);
       float s[2] = {0.f, 0.f}, d[2] = {0.f, 0.f};
@@ -675,29 +697,43 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       }
       if (lane == 0) sh.part_even[warp] = make_float2(sa, sb);
       __syncthreads();
-      sa = sb = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        sa += sh.part_even[w].x;
-        sb += sh.part_even[w].y;
-      }
       if (cluster > 1) {
-        if (tid < cluster) st_cluster(mapa(smem_u32(&sh.even[turn][rank]), tid), make_float2(sa, sb));
-        cluster_sync();
+        const int slot = joins & 1;
+        const uint32_t bar = smem_u32(&sh.even_bar[slot]);
+        if (warp == 0) {
+          if (lane == 0) mbar_expect_tx(bar, 8 * cluster);
+          const float2 mine = sh.part_even[lane & (kWarps - 1)];
+          sa = mine.x;
+          sb = mine.y;
+#pragma unroll
+          for (int o = kWarps / 2; o > 0; o >>= 1) {
+            sa += __shfl_xor_sync(0xffffffffu, sa, o);
+            sb += __shfl_xor_sync(0xffffffffu, sb, o);
+          }
+          if (lane < cluster) st_async(mapa(smem_u32(&sh.even[slot][rank]), lane), mapa(bar, lane), make_float2(sa, sb));
+        }
+        lost = !mbar_poll(bar, joins >> 1 & 1);
         sa = sb = 0.f;
 #pragma unroll
         for (int r = 0; r < kMaxCluster; ++r) {
           if (r < cluster) {
-            sa += sh.even[turn][r].x;
-            sb += sh.even[turn][r].y;
+            sa += sh.even[slot][r].x;
+            sb += sh.even[slot][r].y;
           }
         }
-        turn ^= 1;
+        ++joins;
+      } else {
+        sa = sb = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          sa += sh.part_even[w].x;
+          sb += sh.part_even[w].y;
+        }
       }
       a.s = sa;
       b.s = both ? sb : 1.f;
     }
-    if (__builtin_expect(!(a.s > 1.f / kLarge && a.s < kLarge && b.s > 1.f / kLarge && b.s < kLarge), 0)) {
+    if (__builtin_expect(!lost && !(a.s > 1.f / kLarge && a.s < kLarge && b.s > 1.f / kLarge && b.s < kLarge), 0)) {
       a = b = nothing();
       c_rest = dc_rest = 1e-37f;         // nothing: references move, the same c everywhere
       cp_async_wait<0>();
@@ -733,11 +769,10 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       }
       if (!both) b = Sum{0.f, 0.f, 1.f};
     }
-    const bool valid = a.s > 0.f && a.s < CUDART_INF_F && b.s > 0.f && b.s < CUDART_INF_F;
+    const bool valid = !lost && a.s > 0.f && a.s < CUDART_INF_F && b.s > 0.f && b.s < CUDART_INF_F;
     int chosen = -1, out = -1;
     if (valid) {
-      // strips as short as there is room for, but a few for every warp at most: their sums cost a strip as much as a tile does
-      const int per = max(1, max((to - from + kStrips - 1) / kStrips, min(2, (to - from) / (4 * kWarps)))), n = (to - from + per - 1) / per;
+      int n = 0;                         // strips
       bool precise = false;              // sh.e holds sums of 64 bits
       int rejected = 0;
       float rest = 1.f;                  // no draft: what the rejected tokens leave
@@ -749,6 +784,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         ready = true;
         if (asked >= 0) cp_async_wait<0>();          // the passes use the same slots
         asked = -1;
+        // strips as short as there is room for, but a few for every warp at most: their sums cost a strip as much as a tile does
+        const int per = max(1, max((to - from + kStrips - 1) / kStrips, min(2, (to - from) / (4 * kWarps))));
+        n = (to - from + per - 1) / per;
         if (tid == 0) {
           sh.row = Row{row, drow, vocab, shift, from, to, dvec, per, n};
           // the sums are of 2^(x c - top): what rounding ref c has changed them by is known
@@ -930,8 +968,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       sh.ref[emitted] = a.ref;
       sh.top[emitted] = a.top;
       sh.sum[emitted] = a.s;
-      sh.c[emitted] = c;
-      sh.c_rest[emitted] = c_rest;
+      sh.rest_used[emitted] = c_rest;
     }
     ++emitted;
     if (chosen < 0) break;
@@ -947,7 +984,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       float lp = at >= 0 ? CUDART_NAN_F : 0.f;
       if (out >= 0) {                    // the exponent as it went into the sum: of a token that has nearly all, their roundings cancel
         const Sum a = {sh.ref[tid], sh.top[tid], sh.sum[tid]};
-        lp = (float)(exponent(value(place_of(at).row + out), a, sh.c[tid], sh.c_rest[tid]) * 0.6931471805599453 - log((double)a.s));
+        lp = (float)(exponent(value(place_of(at).row + out), a, sh.c[at], sh.rest_used[tid]) * 0.6931471805599453 - log((double)a.s));
       }
       p.logprob[first + tid] = lp;
     }

@@ -8,7 +8,7 @@
 //
 // A request is a cluster's of up to eight thread blocks, which share every row in contiguous parts and take all decisions alike, each for
 // itself, from sums exchanged through distributed shared memory. A row is read when the walk gets there: the rows of drafts that are not
-// reached are never read.
+// reached are never read. Exchanges are stores that a barrier in the other block counts: a cluster barrier waits for the copies under way too, 2000 cycles.
 //
 // Decisions are those of 64 bits. The sums that a test of a first child needs are taken in fp32, to 2e-6; where u q and r are nearer to each
 // other than that could tell, and for what comes behind a rejection (differences of p and q that are nearly alike), the row is summed
@@ -17,10 +17,10 @@
 // the strip that holds the place.
 // Sums are added up in a fixed order: equal calls give equal results.
 //
-// A launch lasts as long as its longest request. A level of a walk (131072 bf16 logits and the draft's, 64 requests) takes 9 us: some 5 that the row's
+// A launch lasts as long as its longest request. A level of a walk (131072 bf16 logits and the draft's, 64 requests) takes 8 us: some 5 that the row's
 // exponentials take an SM's four blocks, the rest joins; a rejection's pass in 64 bits 33, a draw without one 22, finding the token in its strip 2 to 5.
-// Measured: 64 chains of 6 nodes 97 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 150 to 165 (267),
-// 256 trees of 8 given tokens 111 (300), one chain of 4 over 32000 23.
+// Measured: 64 chains of 6 nodes 92 to 98 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 140 to 150
+// (267), 256 trees of 8 given tokens 111 (300), one chain of 4 over 32000 20.5.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -80,7 +80,8 @@ __shared__ struct {
   float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (reference, sum of the model; of the draft), by turns
   float4 part32[kMostWarps];
   float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference; by turns of their own
-  uint64_t even_bar[2];                  // a phase for each of these turns: eight bytes from every block
+  uint64_t even_bar[2], box_bar[2];      // barriers of these turns and of box's: a phase each time, of the bytes that all blocks send
+  int32_t lost;                          // a block of the cluster has not answered: never, and if it does, the request ends
   int32_t found;
   float c[kNodes], c_rest[kNodes], dc[kNodes], dc_rest[kNodes];
   float ref[kNodes], top[kNodes], sum[kNodes], rest_used[kNodes];      // of the rows walked: the sums (see Sum), the c_rest they were taken with
@@ -91,9 +92,6 @@ __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
-}
-__device__ __forceinline__ void st_cluster(uint32_t addr, double v) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;\n" ::"r"(addr), "d"(v) : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
@@ -107,6 +105,9 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, int32_t v) {
 // Eight bytes into another block's shared memory, counted by a barrier there: neither side needs a fence for what else is under way.
 __device__ __forceinline__ void st_async(uint32_t addr, uint32_t bar, float2 v) {
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];\n" ::"r"(addr), "f"(v.x), "f"(v.y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void st_async(uint32_t addr, uint32_t bar, double v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f64 [%0], %1, [%2];\n" ::"r"(addr), "d"(v), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;\n" ::: "memory");
@@ -224,15 +225,27 @@ __device__ __forceinline__ double warp_sum(double v) {
   for (int sh_ = 16; sh_ > 0; sh_ >>= 1) v += __shfl_xor_sync(0xffffffffu, v, sh_);
   return v;
 }
-// The block's values (part[0][0 .. n - 1], by warp 0's lanes) go to every block of the cluster.
+// Warp 0's n values go to every block of the cluster, as exchange number `turn`; arrived: they all are there.
 __device__ __forceinline__ void publish(int n, double (&v)[kValues], int rank, int cluster, int turn, int lane) {
-  if (lane < cluster) {
-    const uint32_t to = smem_u32(&sh.box[turn][rank][0]);
-    const uint32_t there = cluster > 1 ? mapa(to, lane) : to;
+  double* const to = sh.box[turn & 1][rank];
+  if (cluster > 1) {
+    const uint32_t bar = smem_u32(&sh.box_bar[turn & 1]);
+    if (lane == 0) mbar_expect_tx(bar, 8 * n * cluster);
+    if (lane < cluster) {
+      const uint32_t there = mapa(smem_u32(to), lane), there_bar = mapa(bar, lane);
+#pragma unroll
+      for (int i = 0; i < kValues; ++i)
+        if (i < n) st_async(there + 8 * i, there_bar, v[i]);
+    }
+  } else if (lane == 0) {
 #pragma unroll
     for (int i = 0; i < kValues; ++i)
-      if (i < n) st_cluster(there + 8 * i, v[i]);
+      if (i < n) to[i] = v[i];
   }
+}
+__device__ __forceinline__ void arrived(int cluster, int turn) {
+  if (cluster > 1 && threadIdx.x < 32 && !mbar_poll(smem_u32(&sh.box_bar[turn & 1]), turn >> 1 & 1)) sh.lost = 1;
+  __syncthreads();
 }
 
 // ---- sums in fp32
@@ -305,7 +318,7 @@ __device__ __forceinline__ double weight64(float x, double scale, double top) { 
 // The sum over the blocks of value i.
 __device__ __forceinline__ double total(int i, int cluster, int turn) {
   double v = 0.0;
-  for (int r = 0; r < cluster; ++r) v += sh.box[turn][r][i];
+  for (int r = 0; r < cluster; ++r) v += sh.box[turn & 1][r][i];
   return v;
 }
 // What is left of the probability of a token whose logits are x (the model's) and y (the draft's) behind the rejections so far.
@@ -562,7 +575,7 @@ __device__ __noinline__ void pass(int rejected, int to, int rank, int cluster, i
     }
     publish(n, v, rank, cluster, turn, lane);
   }
-  sync_all(cluster);
+  arrived(cluster, turn);
 }
 
 // THREADS: 512 where there are few requests, so that what runs of them has the threads of an SM each; else 128, four blocks of which an SM runs (128
@@ -594,7 +607,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
     split(sh.dscale[tid], sh.dc[tid], sh.dc_rest[tid]);
   }
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.even_bar[i]), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.even_bar[i]), 1);
+      mbar_init(smem_u32(&sh.box_bar[i]), 1);
+    }
+    sh.lost = 0;
     mbar_init_fence();
   }
   __syncthreads();
@@ -638,7 +655,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
 #pragma unroll 1
     for (; k < Ring<T>::kRing; ++k) cp_async_commit();
   };
-  int cur = 0, emitted = 0, turn = 0, joins = 0, asked = -1;    // asked: the node whose first tiles are on their way
+  int cur = 0, emitted = 0, turn = 0, joins = 0, moves = 0, asked = -1;    // asked: the node whose first tiles are on their way
   float ref = 0.f, dref = 0.f;           // logits of likely tokens: the last accepted one's, where it was accepted
   for (;;) {
     const float scale = sh.scale[cur], dscale = sh.dscale[cur];
@@ -671,7 +688,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       ask_first(place_of(child));
       asked = child;
     };
-    bool lost = false;                   // a block of the cluster has not answered: never, and if it does, the request ends
+    bool lost = false;
     {
       const Ring<T> ring = ring_of(here);
       float s[2] = {0.f, 0.f}, d[2] = {0.f, 0.f};
@@ -712,7 +729,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           }
           if (lane < cluster) st_async(mapa(smem_u32(&sh.even[slot][rank]), lane), mapa(bar, lane), make_float2(sa, sb));
         }
-        lost = !mbar_poll(bar, joins >> 1 & 1);
+        if (warp == 0 && !mbar_poll(bar, joins >> 1 & 1)) sh.lost = 1;
+        __syncthreads();                 // one warp looks, the others leave it the issue slots
+        lost = sh.lost;
         sa = sb = 0.f;
 #pragma unroll
         for (int r = 0; r < kMaxCluster; ++r) {
@@ -761,11 +780,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       __syncthreads();
       join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
       if (cluster > 1) {
-        if (tid < cluster) st_cluster(mapa(smem_u32(&sh.sums[turn][rank]), tid), make_float4(a.ref, a.s, b.ref, b.s));
+        if (tid < cluster) st_cluster(mapa(smem_u32(&sh.sums[moves][rank]), tid), make_float4(a.ref, a.s, b.ref, b.s));
         cluster_sync();
-        join(lane % kMaxCluster < cluster ? sh.sums[turn][lane % kMaxCluster] : make_float4(-CUDART_INF_F, 0.f, -CUDART_INF_F, 0.f),
+        join(lane % kMaxCluster < cluster ? sh.sums[moves][lane % kMaxCluster] : make_float4(-CUDART_INF_F, 0.f, -CUDART_INF_F, 0.f),
              std::integral_constant<int, kMaxCluster / 2>{});
-        turn ^= 1;
+        moves ^= 1;
       }
       if (!both) b = Sum{0.f, 0.f, 1.f};
     }
@@ -803,13 +822,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           if (DRAFT) sh.e.dinv = 1.0 / total(1, cluster, turn);
         }
         __syncthreads();
-        turn ^= 1;
+        ++turn;
         precise = true;
       };
       auto reject = [&]() {              // Z of the pending rejection
         if constexpr (DRAFT) pass<T, DRAFT, kWarps, REST>(rejected, n, rank, cluster, turn);
         const double z = total(0, cluster, turn);
-        turn ^= 1;
+        ++turn;
         if (tid == 0) sh.norm[rejected] = z > kNothing ? 1.0 / z : 0.0;
         __syncthreads();
         ++rejected;
@@ -875,12 +894,12 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           // One rejection and none before: the sums of 64 bits and what it leaves in one pass. The latter is linear in the sums' reciprocals as long
           // as the corrections change no sign.
           sum64(std::integral_constant<int, FIRST>{});
-          turn ^= 1;                     // its values are read here
+          --turn;                        // its values are read here
           fix_p = sh.e.inv - inv;
           fix_q = sh.e.dinv - dinv;
           const double off = fmax(fabs(fix_p) * a.s, fabs(fix_q) * b.s);
           done = off < 0x1p-19 && off * total(2, cluster, turn) <= 1e-12 * total(3, cluster, turn);
-          if (!done) turn ^= 1;
+          if (!done) ++turn;
         } else if (pending && !precise) {
           sum64(std::integral_constant<int, SUMS>{});
         }
@@ -891,7 +910,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           if (!done) pass<T, DRAFT, kWarps, STRIPS>(gone, n, rank, cluster, turn);
           // the blocks' sums; the last block with anything, the one that holds the place
           auto sum_of = [&](int k) {
-            const double* v = sh.box[turn][k];
+            const double* v = sh.box[turn & 1][k];
             return done ? fmax(0.0, v[3] + fix_p * v[4] - fix_q * v[5]) : v[0];
           };
           double all = 0.0, front = 0.0, cum = 0.0;
@@ -907,7 +926,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
             }
             cum += v;
           }
-          turn ^= 1;
+          ++turn;
           const bool fixed = done;
           done = false;
           if (!(all > kNothing) || !(all < CUDART_INF)) continue;
@@ -962,6 +981,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         }
       }
     }
+    if (sh.lost) chosen = out = -1;
     if (rank == 0 && tid == 0) {
       sh.out[emitted] = out;
       sh.walked[emitted] = cur;

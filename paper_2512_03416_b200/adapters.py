@@ -26,8 +26,9 @@ def _matrix(t: torch.Tensor, shape: tuple, device, what: str) -> int:
 
 class Adapters:
     """The adapters of one projection [N, K]: a [adapters, rank, K], b [adapters, N, rank] bf16, scale float32 [adapters] (None: 1). a and
-    scale are kept, not copied; b is laid out anew here, so that an adapter that changes needs new Adapters. rows: which projection of a layer (see
-    ts_adapter_pack): "qkv", "gate_up" (b's rows in its packed order), or "plain" for others and for adapted_project. status: int32, TS_DEV_TIMEOUT where a bounded wait of a projection ran out."""
+    scale are kept, not copied; b, which has to be finite, is laid out anew here, so that an adapter whose b changes needs new Adapters. rows: which
+    projection of a layer (see ts_adapter_pack): "qkv", "gate_up" (b's rows in its packed order), or "plain" for others and for adapted_project.
+    status: int32, TS_DEV_TIMEOUT where a bounded wait of a projection ran out."""
 
     def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None, rows: str = "plain"):
         if rows not in ROWS:

@@ -8,10 +8,10 @@
 // user), so that the launch is bound by the bytes of the adapters in use; in a prompt's chunk x and A come from L2, each A once per 64 tokens.
 // The launch runs next to the product behind it, whose main loop does not need u: a block is small enough (128 threads, 56 KB) to share an SM
 // with one of the product's, and there is one per SM where that is enough. Blocks of 256 threads with 64 to 96 KB of copies under way take less
-// by themselves, but the product waited for them: both together 29.5 and 70.5 us where these take 27 and 62.4 (below).
+// by themselves, but the product waited for them: both together 29.5 and 70.5 us where these took 27 and 62.4.
 //
-// Measured, this launch alone / the product without adapters / both together, us: 64 tokens, 64 adapters of rank 16, K = 4096, N = 6144: 7.6 / 15.8 / 27;
-// 192 tokens, 48 adapters of rank 32, K = N = 8192: 12.2 / 41.4 / 62.4; 2112 tokens, 16 adapters of rank 64, K = 4096, N = 28672: 22.8 / 321 / 363;
+// Measured, this launch alone / the product without adapters / both together, us: 64 tokens, 64 adapters of rank 16, K = 4096, N = 6144: 7.6 / 15.8 / 23.3;
+// 192 tokens, 48 adapters of rank 32, K = N = 8192: 12.2 / 41.4 / 58.4; 2112 tokens, 16 adapters of rank 64, K = 4096, N = 28672: 22.8 / 321 / 363;
 // 2319 tokens, 5 adapters of rank 24, K = 14336, N = 4096: 34.2 / 213 / 236.
 // The partial sums are added up in a fixed order (warps, then blocks): equal calls give equal bits.
 #include <cuda_bf16.h>

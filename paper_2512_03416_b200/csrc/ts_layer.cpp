@@ -273,12 +273,12 @@ int ts_layer_destroy(ts_layer* l) {
 }
 
 size_t ts_layer_adapters_workspace_bytes(const ts_config* cfg, const ts_layer_adapters* ad) {
-  if (!cfg || !ad || cfg->chunk_size <= 0 || cfg->chunk_size > kMaxAdapterTokens || cfg->max_requests <= 0) return 0;
+  if (!cfg || !ad || cfg->chunk_size <= 0 || cfg->max_requests <= 0) return 0;
   size_t total = 0;
   for (const ts_adapters* a : {ad->qkv, ad->o, ad->gate_up, ad->down}) {
     if (!a) continue;
     if (a->rank <= 0 || a->rank > kMaxRank || a->rank % 8 || a->n_adapters <= 0 || a->n_adapters > kMaxAdapters) return 0;
-    total = std::max(total, adapter_bytes(cfg->chunk_size, std::min(cfg->max_requests, kMaxAdapterRows), a->n_adapters, a->rank));
+    total = std::max(total, adapter_bytes(std::min(cfg->chunk_size, kMaxAdapterTokens), std::min(cfg->max_requests, kMaxAdapterRows), a->n_adapters, a->rank));
   }
   return total;
 }
@@ -303,7 +303,7 @@ int ts_layer_attach_adapters(ts_layer* l, const ts_layer_adapters* ad) {
     if (total == 0) return TS_ERR_UNSUPPORTED;
     if (!ad->workspace || ((uintptr_t)ad->workspace & (kAlign - 1))) return TS_ERR_INVALID;
     if (ad->workspace_bytes < total) return TS_ERR_WORKSPACE;
-    plan = adapter_plan_bytes(l->max_tokens, std::min(c->max_requests, kMaxAdapterRows));
+    plan = adapter_plan_bytes(std::min(c->chunk_size, kMaxAdapterTokens), std::min(c->max_requests, kMaxAdapterRows));
     const char* u = (const char*)ad->workspace + plan;
     const int64_t qd = (int64_t)c->n_q_heads * c->head_dim, kvd = (int64_t)c->n_kv_heads * c->head_dim;
     const int64_t out[4] = {qd + 2 * kvd, l->cfg.hidden, 2 * (int64_t)l->cfg.intermediate, l->cfg.hidden};

@@ -79,7 +79,9 @@ __shared__ struct {
   float chance[kNodes], scale[kNodes], dscale[kNodes];
   float4 sums[2][kMaxCluster];           // the blocks' sums in fp32 (reference, sum of the model; of the draft), by turns
   float4 part32[kMostWarps];
-  float2 even[2][kMaxCluster], part_even[kMostWarps];      // the same where all threads have one reference; by turns of their own
+  // The same where all threads have one reference; by turns of their own. Also the warps' parts: where a request has one block, a level has one barrier, and
+  // a warp that is through with it may write the next level's while another one still reads.
+  float2 even[2][kMaxCluster], part_even[2][kMostWarps];
   uint64_t even_bar[2], box_bar[2];      // barriers of these turns and of box's: a phase each time, of the bytes that all blocks send
   int32_t lost;                          // a block of the cluster has not answered: never, and if it does, the request ends
   int32_t found;
@@ -709,14 +711,14 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         sa += __shfl_xor_sync(0xffffffffu, sa, o);
         sb += __shfl_xor_sync(0xffffffffu, sb, o);
       }
-      if (lane == 0) sh.part_even[warp] = make_float2(sa, sb);
+      const int slot = joins & 1;
+      if (lane == 0) sh.part_even[slot][warp] = make_float2(sa, sb);
       __syncthreads();
       if (cluster > 1) {
-        const int slot = joins & 1;
         const uint32_t bar = smem_u32(&sh.even_bar[slot]);
         if (warp == 0) {
           if (lane == 0) mbar_expect_tx(bar, 8 * cluster);
-          const float2 mine = sh.part_even[lane & (kWarps - 1)];
+          const float2 mine = sh.part_even[slot][lane & (kWarps - 1)];
           sa = mine.x;
           sb = mine.y;
 #pragma unroll
@@ -737,15 +739,15 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
             sb += sh.even[slot][r].y;
           }
         }
-        ++joins;
       } else {
         sa = sb = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          sa += sh.part_even[w].x;
-          sb += sh.part_even[w].y;
+          sa += sh.part_even[slot][w].x;
+          sb += sh.part_even[slot][w].y;
         }
       }
+      ++joins;
       a.s = sa;
       b.s = both ? sb : 1.f;
     }

@@ -10,7 +10,7 @@
 // itself, from sums exchanged through distributed shared memory. A row is read when the walk gets there: the rows of drafts that are not
 // reached are never read. Exchanges are stores that a barrier in the other block counts: a cluster barrier waits for the copies under way too, 2000 cycles.
 //
-// Decisions are those of 64 bits. The sums that a test of a first child needs are taken in fp32, to 2e-6; where u q and r are nearer to each
+// Decisions are those of 64 bits. The sums that a test of a first child needs are taken in fp32, to 8.6e-6 at worst (kMargin); where u q and r are nearer to each
 // other than that could tell, and for what comes behind a rejection (differences of p and q that are nearly alike), the row is summed
 // again in 64 bits. The final draw always is: with 100000 tokens, borders of the cumulative sum lie so near to each other that an error of 1e-7
 // would draw a neighbour of the token once in a hundred times. Its cumulative sums are kept per strip of the row; one warp then goes through
@@ -248,13 +248,21 @@ __device__ __forceinline__ void arrived(int cluster, int turn) {
 }
 
 // ---- sums in fp32
+__device__ __forceinline__ float sum8(const float (&v)[8]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 // Weights 2^(x c - top), top = ref c rounded, the same for all: it is as if ref were another number nearby. Where it would not be (kHuge), top is a
 // NaN, and weights are 2^((x - ref) c).
 struct Sum {
   float ref, top, s;
 };
 constexpr float kLarge = 0x1p60f, kHuge = 0x1p20f;
-__device__ __forceinline__ Sum nothing() { return Sum{-CUDART_INF_F, CUDART_NAN_F, 0.f}; }
+// A thread adds up a tile's eight terms by pairs, up to kChain tiles one by one, and these sums in 64 bits, so that what is rounded does not grow with the row. A sum of n
+// terms one by one may be off by n 2^-24 of itself, and terms of one size are off in one direction (4096 of them, a thread's share of 2^20 logits: 5.7e-5).
+constexpr int kChain = 64;
+// How near u q and r (times the sums), relative to both, may be for a test in fp32. One reference for all (2^-24 = 6e-8, ex2 2^-22): a sum's tile, chain, lanes, warps
+// and blocks 96 x 6e-8, its exponents up to 64, rounded twice, 2.6e-6, ex2 0.2e-6: 8.6e-6. A single weight, exponents to 126: 5.5e-6. Three products: 0.2e-6. In all
+// 1.43e-5. Given tokens: r's own sum of rejected weights adds as much again, which (1 + rejected) covers. Moving references: c is short by up to 2^-23 and differences of
+// huge logits are rounded too, exponents to 126 2.4e-5; of a sum, 30 such terms 1.0e-5, moves and joins 1.0e-5, adding 5.6e-6: 5.1e-5 in all.
+constexpr float kMargin = 1.5e-5f, kMarginMoving = 6e-5f;
 __device__ __forceinline__ float top_of(float ref, float c) {
   const float top = __fmul_rn(ref, c);
   return fabsf(top) < kHuge ? top : CUDART_NAN_F;
@@ -268,16 +276,27 @@ __device__ __forceinline__ float moved(const Sum& a, float ref, float top, float
   if (a.ref == -CUDART_INF_F || a.ref == ref) return a.s;                    // nothing, or a NaN
   return a.s * ex2(a.top == a.top && top == top ? a.top - top : (a.ref - ref) * c);
 }
-__device__ __noinline__ Sum add(Sum a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float c) {
+// Where references move, they do so only for a logit whose weight would be more than 2^kAbove: the factor by which a sum then shrinks is rounded, and of
+// two or three moves before all that is left of the sum, and of its error, is nothing. (A reference that follows the largest logit at once may move by a
+// little with every tile, and the roundings of all these moves would add up.)
+constexpr float kAbove = 20.f;
+struct Moving {
+  float ref, top;
+  double s;
+};
+__device__ __noinline__ Moving add(Moving a, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float c) {
   const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
-  float m = a.ref;
+  float m = x[0], w[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i]);
-  const float top = top_of(m, c);
-  Sum b = {m, top, moved(a, m, top, c)};
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, x[i]);
+  if (a.ref == -CUDART_INF_F ? m > a.ref : (m - a.ref) * c > kAbove) {
+    const float top = top_of(m, c);
+    a = Moving{m, top, a.s * moved(Sum{a.ref, a.top, 1.f}, m, top, c)};
+  }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) b.s += m != -CUDART_INF_F ? weight(x[i], b, c, 1e-37f) : x[i] != x[i] ? x[i] : 0.f;
-  return b;
+  for (int i = 0; i < 8; ++i) w[i] = a.ref != -CUDART_INF_F ? weight(x[i], Sum{a.ref, a.top, 0.f}, c, 1e-37f) : x[i] != x[i] ? x[i] : 0.f;
+  a.s += sum8(w);
+  return a;
 }
 // Over groups of 2 * WIDEST lanes.
 template <int WIDEST>
@@ -687,25 +706,37 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       ask_first(place_of(child));
       asked = child;
     };
-    bool lost = false;
+    bool lost = false, moving = false;
     {
       const Ring<T> ring = ring_of(here);
-      float s[2] = {0.f, 0.f}, d[2] = {0.f, 0.f};
+      float s = 0.f, d = 0.f;
+      double whole = 0.0, dwhole = 0.0;
+      int tile = from + warp;
 #pragma unroll 1
-      for (int k = 0, tile = from + warp; tile < to; ++k, tile += kWarps) {
-        float x[8], y[8];
-        ring.get(k, x, y);
-        const int next = tile + Ring<T>::kRing * kWarps;
-        ring.ask(k, next * kTile + base, next < to);
+      for (int k = 0;;) {
+        const int stop = min(to, tile + kChain * kWarps);
+#pragma unroll 1
+        for (; tile < stop; ++k, tile += kWarps) {
+          float x[8], y[8];
+          ring.get(k, x, y);
+          const int next = tile + Ring<T>::kRing * kWarps;
+          ring.ask(k, next * kTile + base, next < to);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i & 1] += ex2(fmaf(x[i], c_rest, fmaf(x[i], c, -a.top)));
-        if (both) {
+          for (int i = 0; i < 8; ++i) x[i] = ex2(fmaf(x[i], c_rest, fmaf(x[i], c, -a.top)));
+          s += sum8(x);
+          if (both) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[i & 1] += ex2(fmaf(y[i], dc_rest, fmaf(y[i], dc, -b.top)));
+            for (int i = 0; i < 8; ++i) y[i] = ex2(fmaf(y[i], dc_rest, fmaf(y[i], dc, -b.top)));
+            d += sum8(y);
+          }
         }
+        if (tile >= to) break;
+        whole += s;
+        dwhole += d;
+        s = d = 0.f;
       }
       ask_child();
-      float sa = s[0] + s[1], sb = d[0] + d[1];
+      float sa = (float)(whole + s), sb = (float)(dwhole + d);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         sa += __shfl_xor_sync(0xffffffffu, sa, o);
@@ -752,7 +783,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
       b.s = both ? sb : 1.f;
     }
     if (__builtin_expect(!lost && !(a.s > 1.f / kLarge && a.s < kLarge && b.s > 1.f / kLarge && b.s < kLarge), 0)) {
-      a = b = nothing();
+      moving = true;
+      Moving ma = {-CUDART_INF_F, CUDART_NAN_F, 0.0}, mb = ma;
       c_rest = dc_rest = 1e-37f;         // nothing: references move, the same c everywhere
       cp_async_wait<0>();
       __syncthreads();
@@ -765,8 +797,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         ring.get(k, x, y);
         const int next = tile + Ring<T>::kRing * kWarps;
         ring.ask(k, next * kTile + base, next < to);
-        a = add(a, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], c);
-        if (both) b = add(b, y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7], dc);
+        ma = add(ma, x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], c);
+        if (both) mb = add(mb, y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7], dc);
       }
       auto join = [&](const float4& v, auto widest) {
         a = Sum{v.x, top_of(v.x, c), v.y};
@@ -774,7 +806,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         lanes_sum<widest.value>(a, c);
         if (both) lanes_sum<widest.value>(b, dc);
       };
-      join(make_float4(a.ref, a.s, b.ref, b.s), std::integral_constant<int, 16>{});
+      join(make_float4(ma.ref, (float)ma.s, mb.ref, (float)mb.s), std::integral_constant<int, 16>{});
       if (lane == 0) sh.part32[warp] = make_float4(a.ref, a.s, b.ref, b.s);
       __syncthreads();
       join(sh.part32[lane & (kWarps - 1)], std::integral_constant<int, kWarps / 2>{});
@@ -846,7 +878,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
           const float have = DRAFT ? weight(x, a, c, c_rest) * b.s : weight(x, a, c, c_rest);
           const float need = DRAFT ? u * weight(y, b, dc, dc_rest) * a.s : u * rest * a.s;
           accept = need < have;
-          close = fabsf(need - have) <= (DRAFT ? 1e-5f * (need + have) : 1e-5f * (1 + rejected) * a.s);
+          const float margin = moving ? kMarginMoving : kMargin;
+          close = fabsf(need - have) <= margin * (DRAFT ? need + have : (1 + rejected) * a.s);
         }
         if (close) {
           if (!precise) {

@@ -89,6 +89,8 @@ size_t adapter_bytes(int64_t M, int64_t n_rows, int64_t n_adapters, int rank) {
 }
 // Rows of a tile as the adapters' part has them: all that a kernel's tile holds, or of a single tile what its tokens need.
 int entry_rows(const ts::GemmPlan& plan, int M) { return plan.pair_tokens > 0 ? plan.pair_tokens : std::min(128, (M + 15) / 16 * 16); }
+// Tokens of a tile
+int entry_tile(const ts::GemmPlan& plan, int M) { return plan.pair_tokens > 0 ? entry_rows(plan, M) : 128; }
 void fill_tiles(const ts::AdapterPlan& plan, int rank, int rows, int64_t N, const int32_t* words, ts::AdapterTiles* out) {
   const int width = granule_width(rank), n = plan.n_tiles + 1 + plan.n_entries;
   out->plan = words;
@@ -353,6 +355,31 @@ int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_ada
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   const ts_config* c = l->view.cfg;
   TSL_CUDA(l, cudaSetDevice(c->device));
+  const int N = (int)n, hidden = l->cfg.hidden, inter = l->cfg.intermediate;
+  const int qd = c->n_q_heads * c->head_dim, kvd = c->n_kv_heads * c->head_dim;
+  // How the projections with adapters are laid out, and for which tiles of tokens: all of it in front of the first launch too.
+  ts::GemmPlan planned[4] = {};
+  ts::AdapterPlan tile_plans[4];
+  int tile_of[4], which_plan[4] = {}, n_tile_plans = 0;
+  for (int i = 0; adapted && i < 4; ++i) {
+    const ts_adapters& ad = l->adapters[i].a;
+    if (!ad.n_adapters) continue;
+    const int out_of[4] = {qd + 2 * kvd, hidden, 2 * inter, hidden}, in_of[4] = {hidden, qd, hidden, inter};
+    const int epi_of[4] = {ts::GEMM_EPI_ROPE, ts::GEMM_EPI_STORE, ts::GEMM_EPI_SILU_MUL, ts::GEMM_EPI_STORE};
+    ts::GemmArgs g;
+    std::memset(&g, 0, sizeof g);
+    g.M = N; g.N = out_of[i]; g.K = in_of[i]; g.epi = epi_of[i];
+    planned[i] = adapter_gemm_plan(g, l->view.n_sms, ad.rank, st->n_rows, row_adapter, l->n_adapters);
+    const int tile = entry_tile(planned[i], N);
+    int& k = which_plan[i];
+    while (k < n_tile_plans && tile_of[k] != tile) ++k;
+    if (k == n_tile_plans) {
+      if (!ts::plan_adapters(N, tile, st->n_rows, st->q_len, row_adapter, l->n_adapters, &tile_plans[k])) return TS_ERR_UNSUPPORTED;
+      tile_of[n_tile_plans++] = tile;
+    }
+    const size_t u_bytes = (size_t)tile_plans[k].n_entries * entry_rows(planned[i], N) * padded_rank(ad.rank) * 2;
+    if (l->adapter_plan + u_bytes > l->adapter_total) return TS_ERR_WORKSPACE;             // never: adapter_bytes is enough
+  }
   char* ws = (char*)l->cfg.workspace;
   // positions of the new tokens (row r's token i sits at ctx_len[r] + i): written by the first RMSNorm
   // launch from row arrays in its parameters, or, for more rows than those hold, uploaded
@@ -385,8 +412,6 @@ int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_ada
     l->pos_busy[slot] = true;
   }
 
-  const int N = (int)n, hidden = l->cfg.hidden, inter = l->cfg.intermediate;
-  const int qd = c->n_q_heads * c->head_dim, kvd = c->n_kv_heads * c->head_dim;
   uint16_t* h = (uint16_t*)(ws + l->L.off_h);
   uint16_t* q = (uint16_t*)(ws + l->L.off_q);
   uint16_t* k = (uint16_t*)(ws + l->L.off_k);
@@ -399,24 +424,20 @@ int ts_layer_step_adapted(ts_layer* l, const ts_step* st, const int32_t* row_ada
   g.status = l->view.status;
   g.wait_cycles = l->view.wait_cycles;
   g.M = N;
-  ts::AdapterPlan tiles;
-  int tile_rows = 0;                                       // of the plan in `tiles`
   ts::AdapterTiles at;
   auto project = [&](const Activations& x, const CUtensorMap& w, const CUtensorMap& w_pair, int which, const uint16_t* in) {
     const LayerAdapters& ad = l->adapters[which];
     ts::GemmPlan plan = {};
     ts::GemmMaps maps = {&x.full, nullptr, &w, &w_pair, nullptr, nullptr, nullptr};
     if (adapted && ad.a.n_adapters) {
-      plan = adapter_gemm_plan(g, l->view.n_sms, ad.a.rank, st->n_rows, row_adapter, l->n_adapters);
-      const int rows = entry_rows(plan, N), tile = plan.pair_tokens > 0 ? rows : 128;
-      if (tile != tile_rows && !ts::plan_adapters(N, tile, st->n_rows, st->q_len, row_adapter, l->n_adapters, &tiles)) return cudaErrorInvalidValue;
-      tile_rows = tile;
+      plan = planned[which];
+      const ts::AdapterPlan& tiles = tile_plans[which_plan[which]];
+      const int rows = entry_rows(plan, N);
       int32_t* words = (int32_t*)l->adapter_ws;
       fill_tiles(tiles, ad.a.rank, rows, g.N, words, &at);
       const ts::AdapterDown down = {in, (const uint16_t*)ad.a.a, ad.a.scale, (uint16_t*)(l->adapter_ws + l->adapter_plan), at.n_inline ? nullptr : words,
                                     g.K, ad.a.rank, rows};
-      if ((size_t)tiles.n_entries * rows * padded_rank(ad.a.rank) * 2 > l->adapter_total - l->adapter_plan) return cudaErrorInvalidValue;   // never
-      const cudaError_t e = ts::launch_adapter_down(down, tiles, tile, at.width, l->view.n_sms, stream);
+      const cudaError_t e = ts::launch_adapter_down(down, tiles, entry_tile(plan, N), at.width, l->view.n_sms, stream);
       if (e != cudaSuccess) return e;
       maps.adapters = &at;
       maps.b = plan.pair_tokens > 0 ? &ad.b_pair : &ad.b;
@@ -526,7 +547,7 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
   const bool pair = plan.pair_tokens > 0;
   const int rows = entry_rows(plan, M);
   ts::AdapterPlan tiles;
-  if (!ts::plan_adapters(M, pair ? rows : 128, n_rows, row_tokens, row_adapter, ad->n_adapters, &tiles)) return TS_ERR_UNSUPPORTED;
+  if (!ts::plan_adapters(M, entry_tile(plan, M), n_rows, row_tokens, row_adapter, ad->n_adapters, &tiles)) return TS_ERR_UNSUPPORTED;
   const size_t plan_bytes = adapter_plan_bytes(M, n_rows);
   int32_t* words = (int32_t*)workspace;
   uint16_t* u = (uint16_t*)((char*)workspace + plan_bytes);
@@ -540,7 +561,7 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
     return TS_ERR_CUDA;
   const ts::AdapterDown down = {(const uint16_t*)x, (const uint16_t*)ad->a, ad->scale, u, at.n_inline ? nullptr : words, K, ad->rank, rows};
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (ts::launch_adapter_down(down, tiles, pair ? rows : 128, at.width, n_sms, stream) != cudaSuccess) return TS_ERR_CUDA;
+  if (ts::launch_adapter_down(down, tiles, entry_tile(plan, M), at.width, n_sms, stream) != cudaSuccess) return TS_ERR_CUDA;
   const ts::GemmMaps maps = {&mx, &mx, &mw, &mw, &mu, &mb, &at};
   return ts::launch_gemm(g, maps, plan, n_sms, stream) == cudaSuccess ? TS_OK : TS_ERR_CUDA;
 }

@@ -644,6 +644,13 @@ int ts_adapter_pack(const void* b, int32_t n_adapters, int32_t N, int32_t rank, 
  * ts_adapter_workspace_bytes: enough for any such call; 0 for arguments outside the limits.
  */
 size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank);
+/*
+ * ts_adapter_plan: how the tokens of such a call are divided, for measurements and tests; host only. tile_tokens: of a tile (128, or a pair's, a multiple of 16 up to
+ * 256). *n_entries: pairs of a tile and an adapter used there; *n_groups: parts of up to *group_tokens (16 or 64) tokens of an adapter; *n_words: 32-bit words that
+ * the launch takes as parameters. TS_ERR_UNSUPPORTED beyond the limits above.
+ */
+int ts_adapter_plan(int32_t M, int32_t tile_tokens, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int32_t n_adapters,
+                    int32_t* n_entries, int32_t* n_groups, int32_t* group_tokens, int32_t* n_words);
 int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const void* x, const void* W, const void* R, void* C,
                        const ts_adapters* adapters, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, void* workspace,
                        size_t workspace_bytes, int32_t tile_m, int32_t* device_status, void* cuda_stream);

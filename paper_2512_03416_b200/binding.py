@@ -121,7 +121,7 @@ EXPORTS = ["ts_pool_bytes", "ts_workspace_bytes", "ts_create", "ts_destroy", "ts
            "ts_layer_workspace_bytes", "ts_pack_gate_up", "ts_layer_create", "ts_layer_destroy", "ts_layer_step",
            "ts_layer_last_cuda_error", "ts_gemm_bf16", "ts_gemm_plan", "ts_cache8_value_bytes",
            "ts_cache8_scale_bytes", "ts_cache8_attach", "ts_tree_attention", "ts_tree_masks", "ts_cache_append",
-           "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_project", "ts_adapter_packed_bytes", "ts_adapter_pack",
+           "ts_cache_read", "ts_token_logprobs", "ts_adapter_workspace_bytes", "ts_adapter_plan", "ts_adapter_project", "ts_adapter_packed_bytes", "ts_adapter_pack",
            "ts_layer_adapters_workspace_bytes", "ts_layer_attach_adapters", "ts_layer_step_adapted",
            "ts_verify_tokens", "ts_request_fork", "ts_requests_free", "ts_copy_pages", "ts_compact_pages", "ts_block_tables"]
 
@@ -212,6 +212,7 @@ def lib() -> ctypes.CDLL:
         adp, i32 = ctypes.POINTER(ts_adapters), ctypes.c_int32
         L.ts_adapter_workspace_bytes.restype = L.ts_adapter_packed_bytes.restype = L.ts_layer_adapters_workspace_bytes.restype = ctypes.c_size_t
         L.ts_adapter_workspace_bytes.argtypes = [i32] * 4
+        L.ts_adapter_plan.argtypes = [i32] * 3 + [vp, vp, i32] + [_i32p] * 4
         L.ts_adapter_packed_bytes.argtypes = [i32] * 3
         L.ts_adapter_pack.argtypes = [vp, i32, i32, i32, i32, vp, vp]
         L.ts_adapter_project.argtypes = [i32] * 4 + [vp] * 4 + [adp, i32, vp, vp, vp, ctypes.c_size_t, i32, vp, vp]
@@ -542,6 +543,16 @@ def int32_array(numbers) -> array.array:
 
 def ts_adapter_workspace_bytes(n_tokens: int, n_rows: int, n_adapters: int, rank: int) -> int:
     return lib().ts_adapter_workspace_bytes(n_tokens, n_rows, n_adapters, rank)
+
+
+def ts_adapter_plan(M: int, tile_tokens: int, row_tokens, row_adapter, n_adapters: int):
+    """Returns (code, (entries, groups, tokens of a group, words))."""
+    tokens, which = int32_array(row_tokens), int32_array(row_adapter)
+    out = [ctypes.c_int32(0) for _ in range(4)]
+    if len(tokens) != len(which):
+        return TS_ERR_INVALID, (0,) * 4
+    rc = lib().ts_adapter_plan(M, tile_tokens, len(tokens), tokens.buffer_info()[0], which.buffer_info()[0], n_adapters, *[ctypes.byref(x) for x in out])
+    return rc, tuple(x.value for x in out)
 
 
 def ts_adapter_packed_bytes(n_adapters: int, N: int, rank: int) -> int:

@@ -37,6 +37,7 @@ struct DownParams {
   AdapterDown d;
   int32_t words[W];
 };
+static_assert(sizeof(DownParams<kAdapterWords>) + sizeof(int) <= 32764, "what a launch's parameters may take");
 
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t r;
@@ -333,26 +334,33 @@ bool plan_adapters(int M, int rows, int n_rows, const int32_t* row_tokens, const
     all += parts[i].len;
     used += i == 0 || parts[i].adapter != parts[i - 1].adapter;
   }
-  // Blocks of 64 tokens where an adapter has more than 16 on average: each A is then read once per 64, but no warps share a stage's K.
-  out->group = all > 16 * (int64_t)used ? kGroup : 16;
   std::vector<int32_t> items, run;
-  int room = 0;                                 // left in the last item
-  for (size_t i = 0; i < parts.size(); ++i) {
-    if (i > 0 && parts[i].adapter != parts[i - 1].adapter) room = 0;
-    for (int skip = 0; skip < parts[i].len;) {
-      if (room == 0) {
-        items.push_back(parts[i].adapter);
-        items.push_back((int32_t)i | skip << 16);
-        room = out->group;
+  auto lay_out = [&](int group) {
+    items.clear();
+    run.clear();
+    int room = 0;                               // left in the last item
+    for (size_t i = 0; i < parts.size(); ++i) {
+      if (i > 0 && parts[i].adapter != parts[i - 1].adapter) room = 0;
+      for (int skip = 0; skip < parts[i].len;) {
+        if (room == 0) {
+          items.push_back(parts[i].adapter);
+          items.push_back((int32_t)i | skip << 16);
+          room = group;
+        }
+        const int take = std::min(room, parts[i].len - skip);
+        items[items.size() - 2] += take << 16;
+        skip += take;
+        room -= take;
       }
-      const int take = std::min(room, parts[i].len - skip);
-      items[items.size() - 2] += take << 16;
-      skip += take;
-      room -= take;
+      run.push_back(parts[i].token | parts[i].len << 16);
+      run.push_back(parts[i].entry);
     }
-    run.push_back(parts[i].token | parts[i].len << 16);
-    run.push_back(parts[i].entry);
-  }
+    out->group = group;
+    return tile_first.size() + adapter.size() + seg_first.size() + segs.size() + items.size() + run.size();
+  };
+  // Blocks of 64 tokens where an adapter has more than 16 on average: each A is then read once per 64, but no warps share a stage's K. Also where the words run out:
+  // an adapter's last block may have one token, and of 16 tokens there are up to four times as many before it.
+  if (all > 16 * (int64_t)used || lay_out(16) > (size_t)kAdapterWords) lay_out(kGroup);
   out->n_tiles = (int)tile_first.size() - 1;
   out->n_entries = (int)adapter.size();
   out->n_groups = (int)items.size() / 2;

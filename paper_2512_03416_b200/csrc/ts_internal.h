@@ -238,7 +238,7 @@ cudaError_t launch_gemm(const GemmArgs& g, const GemmMaps& maps, GemmPlan plan, 
 //   items [groups][2]                                       `group` tokens of an adapter, whatever tiles they are in: adapter | tokens << 16, first run |
 //                                                           its tokens that come before << 16
 //   runs [segments][2]                                      by adapter: first token | tokens << 16, entry
-constexpr int kAdapterWords = 7680;
+constexpr int kAdapterWords = 7936;
 struct AdapterPlan {
   int n_tiles, n_entries, n_groups, group;
   uint32_t o_adapter, o_seg_first, o_seg, o_item, o_run;

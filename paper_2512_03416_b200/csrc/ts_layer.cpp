@@ -58,7 +58,9 @@ bool make_activation_maps(void* encode_fn, const void* ptr, int64_t rows, int64_
 // ---- low-rank adapters
 constexpr int kMaxRank = 256, kMaxAdapters = 65536;
 constexpr int kMaxAdapterRows = 1024, kMaxAdapterTokens = 32768, kManyAdapterRows = 512, kManyAdapterTokens = 8192;
-// their plan fits kAdapterWords: 5 words for each of up to (rows + tiles) segments, 2 for each of (segments, or segments + tokens / 64) groups, 1 per tile
+// Their plan fits kAdapterWords: of r rows in T tiles (of 128 tokens or, with more tokens each, a pair's) there are at most r + T - 1 segments with 5 words each, T + 2
+// words for the tiles, and 2 words for each group, of which there are, in groups of 64, at most one per adapter and one per 64 tokens that are not an
+// adapter's first. 1024 rows of 8192 tokens: 66 + 5 * 1087 + 2 * (1024 + 112) = 7773; 512 rows of 32768: 258 + 5 * 767 + 2 * (512 + 504) = 6125.
 bool adapter_size_ok(int64_t tokens, int64_t rows) {
   return rows <= kMaxAdapterRows && tokens <= kMaxAdapterTokens && (rows <= kManyAdapterRows || tokens <= kManyAdapterTokens);
 }
@@ -579,6 +581,21 @@ int ts_adapter_pack(const void* b, int32_t n_adapters, int32_t N, int32_t rank, 
   if (bytes / 16 / 256 > 0x7fffffffu) return TS_ERR_UNSUPPORTED;
   return ts::launch_adapter_pack((const uint16_t*)b, (uint16_t*)packed, n_adapters, N, rank, granule_width(rank), apart, (cudaStream_t)cuda_stream) == cudaSuccess
              ? TS_OK : TS_ERR_CUDA;
+}
+
+int ts_adapter_plan(int32_t M, int32_t tile_tokens, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int32_t n_adapters,
+                    int32_t* n_entries, int32_t* n_groups, int32_t* group_tokens, int32_t* n_words) {
+  if (M <= 0 || n_rows <= 0 || !row_tokens || !row_adapter || n_adapters <= 0 || n_adapters > kMaxAdapters || !n_entries || !n_groups || !group_tokens || !n_words)
+    return TS_ERR_INVALID;
+  if (tile_tokens < 16 || tile_tokens > 256 || tile_tokens % 16 || !adapter_rows_ok(n_rows, row_tokens, row_adapter, n_adapters, M)) return TS_ERR_INVALID;
+  if (!adapter_size_ok(M, n_rows)) return TS_ERR_UNSUPPORTED;
+  ts::AdapterPlan plan;
+  if (!ts::plan_adapters(M, tile_tokens, n_rows, row_tokens, row_adapter, n_adapters, &plan)) return TS_ERR_UNSUPPORTED;
+  *n_entries = plan.n_entries;
+  *n_groups = plan.n_groups;
+  *group_tokens = plan.group;
+  *n_words = (int32_t)plan.words.size();
+  return TS_OK;
 }
 
 int ts_gemm_plan(int32_t device, int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* tile_m, int32_t* split,

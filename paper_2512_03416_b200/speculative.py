@@ -15,7 +15,9 @@ prompt (ts_request_fork shares its pages), and requests may have low-rank adapte
 from __future__ import annotations
 
 import argparse
+import functools
 import json
+import operator
 from typing import Dict, List, NamedTuple, Optional
 
 import numpy as np
@@ -23,7 +25,7 @@ import torch
 
 from . import binding as B
 from .adapters import Adapters, adapted_project
-from .decoder import Decoder, _check, _raw_stream
+from .decoder import Decoder, TsError, _check, _raw_stream
 from .logprobs import token_logprobs
 from .verify import verify_tokens
 
@@ -235,7 +237,14 @@ class SpeculativeDecoder:
         while min(len(d) for d in done) < n_tokens:
             for d, new in zip(done, self.step()):
                 d += new
+        if self.projection_status():
+            raise TsError(B.TS_ERR_DEVICE_TIMEOUT, "a projection")
         return done
+
+    def projection_status(self) -> int:
+        """TS_DEV_TIMEOUT where a bounded wait of a projection ran out, of one with adapters too (whose status other users of these adapters share).
+        Waits for the steps."""
+        return functools.reduce(operator.or_, (int(s.item()) for s in [self.gemm_status] + [a.status for a in self.adapters.values()]))
 
     def close(self) -> None:
         self.dec.close()
@@ -281,7 +290,7 @@ def main(argv=None) -> int:
     print(json.dumps({"requests": a.requests, "prompt": a.prompt, "cache": a.cache, "nodes_per_tree": sd.nodes, "steps": steps,
                       "tokens": tokens, "tokens_per_request_and_step": round(tokens / steps / a.requests, 3),
                       "ms_per_step": round(ms / steps, 4), "tokens_per_s": round(tokens / ms * 1e3, 1),
-                      "gemm_status": int(sd.gemm_status.item()), "data": "synthetic, random weights"}))
+                      "gemm_status": sd.projection_status(), "data": "synthetic, random weights"}))
     sd.close()
     return 0
 

@@ -66,12 +66,18 @@ class DecoderLayer:
     def pack_gate_up_adapters(self, b_gate, b_up) -> torch.Tensor:
         """b of gate_up [adapters, 2 intermediate, rank] from those of gate and up [adapters, intermediate, rank] of one rank (their rows
         in the order of the packed weights)."""
+        for t, what in ((b_gate, "b_gate"), (b_up, "b_up")):
+            if t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.int16, torch.uint16) or t.device != self.dec.device:
+                raise ValueError(f"{what} must be a bf16 (or int16, uint16) tensor [adapters, intermediate, rank] on {self.dec.device}")
+        if b_gate.shape != b_up.shape or b_gate.dtype != b_up.dtype:
+            raise ValueError(f"b_gate and b_up must be of one shape and type, not {list(b_gate.shape)} {b_gate.dtype} and {list(b_up.shape)} {b_up.dtype}")
         n, inter, rank = b_gate.shape
         b_gate, b_up = b_gate.contiguous(), b_up.contiguous()
         out = torch.empty((n, 2 * inter, rank), dtype=b_gate.dtype, device=self.dec.device)
-        for i in range(n):
-            _check(B.ts_pack_gate_up(b_gate[i].data_ptr(), b_up[i].data_ptr(), out[i].data_ptr(), inter, rank, self.dec._stream()),
-                   "ts_pack_gate_up")
+        with torch.cuda.device(self.dec.device):
+            for i in range(n):
+                _check(B.ts_pack_gate_up(b_gate[i].data_ptr(), b_up[i].data_ptr(), out[i].data_ptr(), inter, rank, self.dec._stream()),
+                       "ts_pack_gate_up")
         return out
 
     def close(self) -> None:

@@ -43,13 +43,14 @@ class Adapters:
             raise ValueError(f"scale must be a contiguous float32 tensor of {n} values on {a.device}")
         self.device, self.rank, self.count = a.device, rank, n
         self.rows, pa, pb = rows, _matrix(a, (n, rank, self.k), a.device, "a"), _matrix(b, (n, self.n, rank), a.device, "b")
-        if b.numel() and not all(math.isfinite(v) for v in torch.aminmax(b.view(torch.bfloat16))):
-            raise ValueError("b must be finite: tokens of other adapters take zeros times it")
         self.tensors = [a, scale]
         with torch.cuda.device(a.device):
             packed = [self._pack(pb, order) for order in ([B.TS_ROWS_PLAIN] if rows == "plain" else [B.TS_ROWS_PLAIN, ROWS[rows]])]
         self.args = B.ts_adapters(n, rank, pa, packed[0], packed[-1], None if scale is None else scale.data_ptr())
         self.status = torch.zeros(1, dtype=torch.int32, device=a.device)
+        # behind the packing: these numbers' way to the host waits for it, and the adapters can be used on any stream
+        if b.numel() and not all(math.isfinite(v) for v in torch.aminmax(b.view(torch.bfloat16))):
+            raise ValueError("b must be finite: tokens of other adapters take zeros times it")
 
     def _pack(self, b: int, order: int) -> int:
         nbytes = B.ts_adapter_packed_bytes(self.count, self.n, self.rank)

@@ -1055,14 +1055,11 @@ int copy_page_pairs(ts_ctx* c, void* cuda_stream) {
     r.base[r.n] = (char*)base;
     r.bytes[r.n++] = bytes;
   };
-  if (c->cfg.kv_pool || !c->cache8.values) {
-    const int rc = ensure_cuda(c, stream, TS_CACHE_BF16);
-    if (rc != TS_OK) return rc;
-    add(c->cfg.kv_pool, 2 * page8);
-  }
+  // Nothing of what a step's first call sets up (ensure_cuda) is needed: a context's first copy is as fast as the others.
+  if (!c->cfg.kv_pool && !c->cache8.values) return cuda_fail(c, cudaErrorInvalidDevicePointer);
+  TS_CUDA(c, cudaSetDevice(c->cfg.device));
+  if (c->cfg.kv_pool) add(c->cfg.kv_pool, 2 * page8);
   if (c->cache8.values) {
-    const int rc = ensure_cuda(c, stream, TS_CACHE_E4M3);
-    if (rc != TS_OK) return rc;
     add(c->cache8.values, page8);
     add(c->cache8.scales, page8 / c->cfg.head_dim);
   }

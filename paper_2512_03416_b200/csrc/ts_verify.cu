@@ -254,7 +254,7 @@ __device__ __forceinline__ float sum8(const float (&v)[8]) { return ((v[0] + v[1
 struct Sum {
   float ref, top, s;
 };
-constexpr float kLarge = 0x1p60f, kHuge = 0x1p20f;
+constexpr float kLarge = 0x1p60f, kHuge = 0x1p20f, kSmall = 0x1p-60f;
 // A thread adds up a tile's eight terms by pairs, up to kChain tiles one by one, and these sums in 64 bits, so that what is rounded does not grow with the row. A sum of n
 // terms one by one may be off by n 2^-24 of itself, and terms of one size are off in one direction (4096 of them, a thread's share of 2^20 logits: 5.7e-5).
 constexpr int kChain = 64;
@@ -874,12 +874,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) verify_kernel(const __
         if (again) continue;
         bool accept = false, close = precise || pending;
         if (!close) {
-          // p and u q, or p and u times what is left, both times the sums: no divisions. (What underflows is close.)
+          // p and u q, or p and u times what is left, both times the sums: no divisions. Below kSmall a weight of 2^-126 or less, which counts as 0, may have been one of theirs
+          // (its product with a sum, below kLarge, is less than that): where both are, 64 bits decide.
           const float have = DRAFT ? weight(x, a, c, c_rest) * b.s : weight(x, a, c, c_rest);
           const float need = DRAFT ? u * weight(y, b, dc, dc_rest) * a.s : u * rest * a.s;
           accept = need < have;
           const float margin = moving ? kMarginMoving : kMargin;
-          close = fabsf(need - have) <= margin * (DRAFT ? need + have : (1 + rejected) * a.s);
+          close = fabsf(need - have) <= margin * (DRAFT ? need + have : (1 + rejected) * a.s) || (DRAFT && fmaxf(need, have) < kSmall);
         }
         if (close) {
           if (!precise) {

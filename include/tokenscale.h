@@ -628,9 +628,10 @@ typedef struct {
 } ts_adapters;
 
 /*
- * ts_adapter_pack: B (DEVICE bf16 [n_adapters][N][rank], row-major, finite: tokens of other adapters take zeros times it) as the kernels read it, to ts_adapter_packed_bytes() bytes (128-byte aligned; 0 for
- * arguments outside the limits): ranks padded to 16, 32 or a multiple of 64 and rows to a multiple of 128 with zeros. order: which rows lie together.
- * TS_ROWS_QKV needs N a multiple of 128, TS_ROWS_GATE_UP (B's rows in the order of ts_pack_gate_up) of 256. Asynchronous on cuda_stream, on the current device.
+ * ts_adapter_pack: B (DEVICE bf16 [n_adapters][N][rank], row-major, finite: tokens of other adapters take zeros times it) as the kernels
+ * read it, to ts_adapter_packed_bytes() bytes (128-byte aligned; 0 for arguments outside the limits): ranks padded to 16, 32 or a multiple of
+ * 64 and rows to a multiple of 128 with zeros. order: which rows lie together. TS_ROWS_QKV needs N a multiple of 128, TS_ROWS_GATE_UP (B's
+ * rows in the order of ts_pack_gate_up) of 256. Asynchronous on cuda_stream, on the current device.
  */
 enum { TS_ROWS_PLAIN = 0, TS_ROWS_QKV = 1, TS_ROWS_GATE_UP = 2 };
 size_t ts_adapter_packed_bytes(int32_t n_adapters, int32_t N, int32_t rank);
@@ -639,15 +640,16 @@ int ts_adapter_pack(const void* b, int32_t n_adapters, int32_t N, int32_t rank, 
 /*
  * ts_adapter_project: C = (R ? R : 0) + x . W^T + the adapters' part, as ts_gemm_bf16 (arguments and limits there). Row r (a request) has the
  * next row_tokens[r] >= 1 rows of x, M in all, and uses adapter row_adapter[r], -1 = none; both HOST arrays. C must not overlap x, R
- * may be C. workspace: DEVICE, 256-byte aligned, ts_adapter_workspace_bytes() bytes, in use until the work enqueued here is done. Up to 1024 rows and 8192
- * tokens, or 512 rows and 32768 tokens, else TS_ERR_UNSUPPORTED. Asynchronous on cuda_stream; two launches, one where no row has an adapter.
+ * may be C. workspace: DEVICE, 256-byte aligned, ts_adapter_workspace_bytes() bytes, in use until the work enqueued here is done. Up to 1024
+ * rows and 8192 tokens, or 512 rows and 32768 tokens, else TS_ERR_UNSUPPORTED. Asynchronous on cuda_stream; two launches, one where no row
+ * has an adapter.
  * ts_adapter_workspace_bytes: enough for any such call; 0 for arguments outside the limits.
  */
 size_t ts_adapter_workspace_bytes(int32_t n_tokens, int32_t n_rows, int32_t n_adapters, int32_t rank);
 /*
- * ts_adapter_plan: how the tokens of such a call are divided, for measurements and tests; host only. tile_tokens: of a tile (128, or a pair's, a multiple of 16 up to
- * 256). *n_entries: pairs of a tile and an adapter used there; *n_groups: parts of up to *group_tokens (16 or 64) tokens of an adapter; *n_words: 32-bit words that
- * the launch takes as parameters. TS_ERR_UNSUPPORTED beyond the limits above.
+ * ts_adapter_plan: how the tokens of such a call are divided, for measurements and tests; host only. tile_tokens: of a tile (128, or a
+ * pair's, a multiple of 16 up to 256). *n_entries: pairs of a tile and an adapter used there; *n_groups: parts of up to *group_tokens (16 or
+ * 64) tokens of an adapter; *n_words: 32-bit words that the launch takes as parameters. TS_ERR_UNSUPPORTED beyond the limits above.
  */
 int ts_adapter_plan(int32_t M, int32_t tile_tokens, int32_t n_rows, const int32_t* row_tokens, const int32_t* row_adapter, int32_t n_adapters,
                     int32_t* n_entries, int32_t* n_groups, int32_t* group_tokens, int32_t* n_words);
@@ -659,8 +661,8 @@ int ts_adapter_project(int32_t device, int32_t M, int32_t N, int32_t K, const vo
  * ts_layer_attach_adapters: gives a layer's projections adapters (each NULL or with the same n_adapters; weights and workspace are the
  * caller's and stay in use; all NULL takes them off again). Wait for the layer's steps before changing them.
  * ts_layer_step_adapted: ts_layer_step in which row r of the step uses adapter row_adapter[r] (HOST, -1 = none) in every projection that has
- * adapters; row_adapter NULL = no adapters. Limits as for ts_adapter_project where one is used. ts_layer_adapters_workspace_bytes: 0 where no projection has
- * adapters or on a bad shape.
+ * adapters; row_adapter NULL = no adapters. Limits as for ts_adapter_project where one is used; a step that is not served has launched and
+ * changed nothing. ts_layer_adapters_workspace_bytes: 0 where no projection has adapters or on a bad shape.
  */
 typedef struct {
   const ts_adapters *qkv, *o, *gate_up, *down;
@@ -679,12 +681,13 @@ int ts_layer_step_adapted(ts_layer* layer, const ts_step* step, const int32_t* r
  *   r = p; the children of the node, in order: with token t accepted where u_accept[child] * q(t) < r(t) (given: u_accept[child] < r(t)): on to it;
  *   otherwise r = max(r - q, 0) (given: r without t), normalised (as it was where nothing is left);
  *   no child left: the token drawn is the first whose cumulative sum of r exceeds u_sample[r], and the request is done.
- * Decided as in 64 bits. count[r] = tokens emitted (1 to the depth of the tree + 1); the request's places of emitted hold them, those of logprob their
- * log p (natural), those of path the rows of the nodes walked (absolute; node 0 first), which ts_cache_append takes as `source`: count[r]
- * of them are the last emitted token and the accepted ones. Behind them -1, 0 and -1.
- * u_accept, u_sample: from [0, 1). Nodes whose parent or token does not exist are passed over, and so is a given token that comes twice below a node. A row that is no
- * distribution (a NaN, +inf, or nothing but -inf in it; in the draft's row of a node with children) ends its request with token -1, log probability NaN.
- * A node with no children makes this a sampler: n_nodes 1. No workspace; asynchronous on cuda_stream; calls on different streams are independent.
+ * Decided as in 64 bits. count[r] = tokens emitted (1 to the depth of the tree + 1); the request's places of emitted hold them, those of
+ * logprob their log p (natural), those of path the rows of the nodes walked (absolute; node 0 first), which ts_cache_append takes as
+ * `source`: count[r] of them are the last emitted token and the accepted ones. Behind them -1, 0 and -1.
+ * u_accept, u_sample: from [0, 1). Nodes whose parent or token does not exist are passed over, and so is a given token that comes twice below
+ * a node. A row that is no distribution (a NaN, +inf, or nothing but -inf in it; in the draft's row of a node with children) ends its request
+ * with token -1, log probability NaN. A node with no children makes this a sampler: n_nodes 1. No workspace; asynchronous on cuda_stream;
+ * calls on different streams are independent.
  */
 typedef struct {
   int32_t device;
@@ -713,13 +716,13 @@ int ts_verify_tokens(const ts_verify* args, void* cuda_stream);
  * (a step, ts_kv_append, ts_cache_append: positions from the cached length on) is refused with TS_ERR_SHARED_PAGE and nothing changes. The calls
  * copy in every cache that the context has (the bf16 pool, an attached 8-bit cache); copies are enqueued on cuda_stream, in whose order
  * the steps around them have to be.
- * ts_request_fork: for each i < n a new request (slots_out[i], id req_ids[i]) of the first n_tokens[i] cached tokens of request slots[i] (n_tokens NULL:
- *   all of them). It shares the pages that these fill and gets a copy of its own of the last one where they fill it partly, so that both
+ * ts_request_fork: for each i < n a new request (slots_out[i], id req_ids[i]) of the first n_tokens[i] cached tokens of request slots[i]
+ *   (n_tokens NULL: all of them). It shares the pages that these fill and gets a copy of its own of the last one where they fill it partly, so that both
  *   may go on. A request may come several times. TS_ERR_NO_SLOT, TS_ERR_NO_PAGES (reserved pages are left): nothing has changed.
  *   To go back to a length inside a shared page, fork the request at that length and free the old one.
  * ts_requests_free: ts_request_free of n requests, each listed once. A page is free when no table holds it. (Released tokens count per request.)
- * ts_copy_pages: page dst[i] becomes what page src[i] holds, for callers that lay tables out themselves (ts_block_table_set). Any pages of the pool;
- *   each dst once, none a src too, none in two tables (TS_ERR_SHARED_PAGE).
+ * ts_copy_pages: page dst[i] becomes what page src[i] holds, for callers that lay tables out themselves (ts_block_table_set). Any pages of
+ *   the pool; each dst once, none a src too, none in two tables (TS_ERR_SHARED_PAGE). No copy here needs the context's workspace.
  * ts_compact_pages: moves up to max_moves pages in use from the end of the pool to free ones at its front and changes the tables. moves_out (may be
  *   NULL, room for 2 * max_moves) gets (from, to) of each; *n_moves_out, *n_used_out (may be NULL): moves made, and one past the last page in use.
  * ts_block_tables: the tables of n requests, rows of `width` entries, -1 behind a table's end (TS_ERR_TABLE_SHORT if one is longer).

@@ -19,8 +19,8 @@
 //
 // A launch lasts as long as its longest request. A level of a walk (131072 bf16 logits and the draft's, 64 requests) takes 8 us: some 5 that the row's
 // exponentials take an SM's four blocks, the rest joins; a rejection's pass in 64 bits 33, a draw without one 22, finding the token in its strip 2 to 5.
-// Measured: 64 chains of 6 nodes 92 to 98 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 140 to 150
-// (267), 256 trees of 8 given tokens 111 (300), one chain of 4 over 32000 20.5.
+// Measured: 64 chains of 6 nodes 87 to 99 us (library exponentials, one tile at a time: 238), 48 trees of up to 25 nodes over 100003 fp32 logits 135 to 158
+// (267), 256 trees of 8 given tokens 110 to 116 (300), one chain of 4 over 32000 20.5, a token each of 64 rows of 131072 28 to 36.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 

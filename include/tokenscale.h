@@ -717,8 +717,8 @@ int ts_verify_tokens(const ts_verify* args, void* cuda_stream);
  * copy in every cache that the context has (the bf16 pool, an attached 8-bit cache); copies are enqueued on cuda_stream, in whose order
  * the steps around them have to be.
  * ts_request_fork: for each i < n a new request (slots_out[i], id req_ids[i]) of the first n_tokens[i] cached tokens of request slots[i]
- *   (n_tokens NULL: all of them). It shares the pages that these fill and gets a copy of its own of the last one where they fill it partly, so that both
- *   may go on. A request may come several times. TS_ERR_NO_SLOT, TS_ERR_NO_PAGES (reserved pages are left): nothing has changed.
+ *   (n_tokens NULL: all of them). It shares the pages that these fill and gets a copy of its own of the last one where they fill it partly,
+ *   so that both may go on. A request may come several times. TS_ERR_NO_SLOT, TS_ERR_NO_PAGES (reserved pages are left): nothing has changed.
  *   To go back to a length inside a shared page, fork the request at that length and free the old one.
  * ts_requests_free: ts_request_free of n requests, each listed once. A page is free when no table holds it. (Released tokens count per request.)
  * ts_copy_pages: page dst[i] becomes what page src[i] holds, for callers that lay tables out themselves (ts_block_table_set). Any pages of
